@@ -9,6 +9,10 @@
  *   dasc_refresh  device replay of the gated delta rule (Eq. 1; suffix-refresh policy, Section 4.2)
  *   dasc_pack_int8 / dasc_restore_int8
  *                 device the same copies with the INT8 checkpoint codec fused in (Appendix D, Eq. 10)
+ *   dasc_decay_attn / dasc_decay_step
+ *                 device linear attention with a decay per head (no delta correction) over the same states: prompts, single tokens
+ *   dasc_verify_draft
+ *                 device how many drafted tokens of each request stand, and its next token
  *
  * Conventions
  *   - No exception crosses this boundary; every call returns a dasc_status_t.
@@ -58,7 +62,7 @@ typedef enum {
   DASC_ERR_ALLOC = 4,       /* host or device allocation failed (dasc_plan only) */
   DASC_ERR_CUDA = 5,        /* a CUDA runtime call or launch failed */
   DASC_ERR_WORKSPACE = 6,   /* workspace missing, misaligned or too small */
-  DASC_ERR_TIMEOUT = 7,     /* a bounded device-side wait ran out (reported by dasc_refresh_status) */
+  DASC_ERR_TIMEOUT = 7,     /* a bounded device-side wait ran out (reported by dasc_refresh_status, dasc_decay_status) */
   DASC_ERR_DOMAIN = 8       /* log-decay outside the chunked kernel's range (reported by dasc_refresh_status) */
 } dasc_status_t;
 
@@ -526,6 +530,98 @@ dasc_status_t dasc_refresh_static(const dasc_plan_t *plan, float *state_base, in
                                   int32_t n_req, int64_t total_tokens, int32_t max_seqlen, int32_t layer_begin,
                                   int32_t layer_end, float q_scale, void *o, int32_t o_dtype, int32_t mode,
                                   void **scratch_out, void *cuda_stream);
+
+/*
+ * Linear attention with one decay per value head and token, for layers without the delta correction of Eq. 1 (the paper has
+ * no counterpart; the states, their plan of kind GDN with its per-head decay parameters, Store and Load are those above):
+ *     S_t = exp(g_t) S_{t-1} + k_t v_t^T        o_t = q_scale * S_t^T q_t
+ * dasc_decay_attn runs each request's token range (a prompt, a part of one, drafted tokens), dasc_decay_step one token per
+ * request.  Layout of states and streams as for dasc_refresh, with Lc = layer_end - layer_begin and T = total_tokens:
+ *   q, k   [Lc][T][n_k_heads][d_k]   bf16 or fp32 (io_dtype); q may be NULL when o is
+ *   v      [Lc][T][n_v_heads][d_v]   same dtype
+ *   g      fp32 log-decay, any g <= 0 (-infinity: everything before the token is forgotten)
+ *          decay DASC_DECAY_PER_TOKEN: [Lc][T][n_v_heads];  DASC_DECAY_PER_HEAD: [Lc][n_v_heads], the same for every token
+ *   o      [Lc][T][n_v_heads][d_v]   o_dtype; NULL = outputs not wanted
+ *   cu_seqlens DEVICE int32[n_req+1], ascending from 0, as for dasc_refresh
+ *   seq_used   DEVICE int32[n_req] or NULL: of request r's tokens only the first min(seq_used[r], all of them) are run (a
+ *          negative number counts as 0); rows of o behind them are left as they were.  dasc_verify_draft's n_kept fits here.
+ *   from_zero  DEVICE int32[n_req] or NULL: where != 0 the request starts from a zero state (S_0 = 0; the stored
+ *          state is not read, so it may hold anything)
+ *   req_idx    DEVICE int32[n_req]: which dense state each request owns (distinct).  A negative entry is padding: the
+ *          request's state and its rows of o are left as they were.
+ *   max_seqlen an upper bound on any request's token count; it chooses kernels and the split of long requests and limits
+ *          nothing
+ * mode:
+ *   DASC_DECAY_CONTINUE             S_0 as stored (or zero), every state is written back
+ *   DASC_DECAY_SCRATCH_MERGE_LOCAL  S_0 = 0, only the heads the plan OMITS are written back (as for dasc_refresh)
+ *   DASC_DECAY_SCORE                S_0 as stored (or zero), no state is written: outputs of drafted tokens.  A recurrent state
+ *                                   cannot be rewound the way a KV cache can, so drafts are scored first and the state is
+ *                                   advanced over those that stand by a second call (CONTINUE, seq_used, o = NULL).
+ * A request without tokens still has its S_0 written where the mode writes a state that does not start as stored.
+ *
+ * algo SEQUENTIAL: token by token in fp32; d_k of 32, 64 or 128 and any d_v that is a multiple of 32.
+ * algo CHUNKED: chunks of 64 tokens on the tensor cores, for d_k = d_v = 128 and bf16 q, k, v (DASC_ERR_SHAPE
+ *   otherwise).  Operands that are not exact in bf16 (weights inside a chunk, decayed keys, the state) are pairs of bf16,
+ *   16 mantissa bits, and sums are fp32.  A token with a NaN or an infinity in v makes its column of the state and of
+ *   all later outputs NaN (where exact arithmetic may keep an infinity); earlier outputs are not touched by it.
+ * algo AUTO: CHUNKED where shape and type allow it and the requests are long enough to gain, else SEQUENTIAL.
+ *
+ * workspace: DEVICE scratch of at least dasc_decay_workspace_bytes() for these sizes, 256-byte aligned, private to the call until
+ *   it completes; needs no initialisation; NULL where that size is 0.  Two calls that may overlap (two streams, two
+ *   captured graphs replayed together) each need their own.
+ * dasc_decay_status: after the stream has been synchronised, DASC_OK or DASC_ERR_TIMEOUT if a bounded device-side wait of
+ *   the last call with this workspace gave up (the states of the requests concerned are not written).  Copies device -> host.
+ * Errors: as for dasc_refresh, before any launch.  The plan must be of kind GDN (DASC_ERR_UNSUPPORTED otherwise).
+ * Sums run in a fixed order: equal calls give equal bits.
+ */
+typedef enum { DASC_DECAY_PER_TOKEN = 0, DASC_DECAY_PER_HEAD = 1 } dasc_decay_kind_t;
+typedef enum {
+  DASC_DECAY_CONTINUE = 0,
+  DASC_DECAY_SCRATCH_MERGE_LOCAL = 1,
+  DASC_DECAY_SCORE = 2
+} dasc_decay_mode_t;
+dasc_status_t dasc_decay_workspace_bytes(const dasc_plan_t *plan, int32_t n_req, int32_t n_layers_in_call, int64_t total_tokens,
+                                         int32_t max_seqlen, int32_t algo, size_t *out);
+dasc_status_t dasc_decay_attn(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride,
+                              const int32_t *req_idx, const void *q, const void *k, const void *v, int32_t io_dtype,
+                              const float *g, int32_t decay, const int32_t *cu_seqlens, const int32_t *seq_used,
+                              const int32_t *from_zero, int32_t n_req, int64_t total_tokens, int32_t max_seqlen,
+                              int32_t layer_begin, int32_t layer_end, float q_scale, void *o, int32_t o_dtype, int32_t mode,
+                              int32_t algo, void *workspace, size_t workspace_bytes, void *cuda_stream);
+dasc_status_t dasc_decay_status(const void *workspace, size_t workspace_bytes);
+/* One token per request: token r of the streams ([Lc][n_req][heads][d]) belongs to request r; every state is read,
+ * advanced and written back, and o is required.  Shapes as for SEQUENTIAL. */
+dasc_status_t dasc_decay_step(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride,
+                              const int32_t *req_idx, const void *q, const void *k, const void *v, int32_t io_dtype,
+                              const float *g, int32_t decay, int32_t n_req, int32_t layer_begin, int32_t layer_end,
+                              float q_scale, void *o, int32_t o_dtype, void *cuda_stream);
+
+/*
+ * Verification of drafted tokens against the target's probabilities, from given random numbers, so that what is
+ * sampled follows the target's distribution (speculative sampling).  Request r drafted n_r = cu_drafts[r+1] - cu_drafts[r]
+ * tokens x_0 .. and the target scored n_r + 1 positions; n_r may be 0.
+ *   target  DEVICE [cu_drafts[n_req] + n_req][vocab]: request r's rows start at cu_drafts[r] + r; probabilities, `dtype`
+ *   draft   DEVICE [cu_drafts[n_req]][vocab]: what the drafter drew each token from, same dtype; NULL = a deterministic
+ *           drafter, probability 1 at its token
+ *   target_stride, draft_stride  elements between rows, >= vocab
+ *   tokens  DEVICE int32[cu_drafts[n_req]];  cu_drafts DEVICE int32[n_req+1], ascending from 0
+ *   u_accept DEVICE fp32[cu_drafts[n_req]], u_next DEVICE fp32[n_req]: uniform numbers in [0, 1)
+ *   (tokens and u_accept may both be NULL where nobody drafted)
+ * In 64-bit arithmetic: token j stands if all before it do and u_j * draft_j(x_j) < target_j(x_j); a token outside
+ * [0, vocab) does not stand.  The next token is drawn, at the first token i that does not stand, from the weights
+ * max(target_i - draft_i, 0), or, where these are all zero, from target_i; where all stand, from target_{n_r}: the smallest
+ * index whose running sum of weights exceeds u_next * (sum of weights).  A NaN, an infinity or a negative number has weight 0; where
+ * no weight is left the next token is -1.
+ *   out     DEVICE int32[n_req][out_stride]: the tokens that stand, the next token, then -1 up to entry max_drafts;
+ *           out_stride >= max_drafts + 1.  A request with more than max_drafts tokens is cut to max_drafts.
+ *   n_kept  DEVICE int32[n_req]: 1 + how many stand, the scored positions over which a recurrent state may be advanced
+ *           (seq_used of dasc_decay_attn)
+ * The current device must be the one that holds the buffers (DASC_ERR_INVALID_ARG otherwise).
+ */
+dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const void *draft, int64_t draft_stride,
+                                int32_t dtype, int32_t vocab, const int32_t *tokens, const int32_t *cu_drafts,
+                                const float *u_accept, const float *u_next, int32_t n_req, int32_t max_drafts, int32_t *out,
+                                int64_t out_stride, int32_t *n_kept, void *cuda_stream);
 
 const char *dasc_status_string(dasc_status_t status);
 /* "major.minor.patch" of this library. */

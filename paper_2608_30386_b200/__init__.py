@@ -13,4 +13,6 @@ from .binding import (  # noqa: F401
     dasc_restore_padded, dasc_slot_budget, dasc_tp_balance, dasc_pack_tp, dasc_restore_tp, dasc_tp_head_permutation,
     dasc_conv_store, dasc_conv_load, dasc_plan_save, dasc_plan_load, dasc_refresh_counters, dasc_debug_set_refresh_poll_limit,
     dasc_debug_refresh_form,
+    DECAY_CONTINUE, DECAY_PER_HEAD, DECAY_PER_TOKEN, DECAY_SCORE, DECAY_SCRATCH_MERGE_LOCAL, dasc_decay_attn, dasc_decay_status,
+    dasc_decay_step, dasc_decay_workspace_bytes, dasc_verify_draft,
 )

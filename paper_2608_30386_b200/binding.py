@@ -25,6 +25,8 @@ SCOPE_HEAD, SCOPE_LAYER, SCOPE_MODEL = 0, 1, 2
 IO_BF16, IO_FP32 = 0, 1
 REFRESH_CONTINUE, REFRESH_SCRATCH_MERGE_LOCAL = 0, 1
 ALGO_AUTO, ALGO_SEQUENTIAL, ALGO_CHUNKED = 0, 1, 2
+DECAY_PER_TOKEN, DECAY_PER_HEAD = 0, 1
+DECAY_CONTINUE, DECAY_SCRATCH_MERGE_LOCAL, DECAY_SCORE = 0, 1, 2
 
 OK, ERR_INVALID_ARG, ERR_SHAPE, ERR_UNSUPPORTED, ERR_ALLOC, ERR_CUDA, ERR_WORKSPACE, ERR_TIMEOUT, ERR_DOMAIN = range(9)
 
@@ -38,6 +40,7 @@ EXPORTS = (
     "dasc_tp_balance", "dasc_pack_tp", "dasc_restore_tp", "dasc_tp_head_permutation", "dasc_conv_store", "dasc_conv_load",
     "dasc_refresh_counters", "dasc_debug_set_refresh_poll_limit", "dasc_debug_refresh_form",
     "dasc_refresh_workspace_bytes", "dasc_refresh", "dasc_refresh_status", "dasc_refresh_window", "dasc_refresh_static",
+    "dasc_decay_workspace_bytes", "dasc_decay_attn", "dasc_decay_status", "dasc_decay_step", "dasc_verify_draft",
     "dasc_status_string", "dasc_version",
 )
 
@@ -136,6 +139,19 @@ def lib() -> C.CDLL:
                                           C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
                                           C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_void_p,
                                           C.c_int32, C.c_int32, C.POINTER(C.c_void_p), C.c_void_p]
+        L.dasc_decay_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int32,
+                                                 C.POINTER(C.c_size_t)]
+        L.dasc_decay_attn.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_void_p,
+                                      C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.dasc_decay_status.argtypes = [C.c_void_p, C.c_size_t]
+        L.dasc_decay_step.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                      C.c_float, C.c_void_p, C.c_int32, C.c_void_p]
+        L.dasc_verify_draft.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p,
+                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64,
+                                        C.c_void_p, C.c_void_p]
         L.dasc_status_string.restype = C.c_char_p
         L.dasc_status_string.argtypes = [C.c_int]
         L.dasc_version.restype = C.c_char_p
@@ -167,7 +183,7 @@ def _call():
         spec = importlib.util.spec_from_file_location("_dasccall", CALL_PATH)
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)
-        mod.init(*_stream_lookup(), torch.bfloat16, lambda x: _ptr(x).value or 0)
+        mod.init(*_stream_lookup(), torch.bfloat16, lambda x: _ptr(x).value or 0, torch.float32, torch.int32)
         _native = mod
     return _native
 
@@ -517,3 +533,64 @@ def dasc_refresh_static(plan: Plan, state: torch.Tensor, layer_stride: int, req_
                                      layer_end, float(q_scale), _ptr(o), o_io, mode, C.byref(scratch),
                                      _stream_ptr(stream)), "dasc_refresh_static")
     return int(scratch.value or 0)
+
+
+def dasc_decay_workspace_bytes(plan: Plan, n_req: int, n_layers_in_call: int, total_tokens: int, max_seqlen: int,
+                               algo: int = ALGO_AUTO) -> int:
+    """Bytes of workspace of ``dasc_decay_attn`` for these sizes (0: none)."""
+    out = C.c_size_t()
+    _check(lib().dasc_decay_workspace_bytes(plan.handle, n_req, n_layers_in_call, total_tokens, max_seqlen, algo, C.byref(out)),
+           "dasc_decay_workspace_bytes")
+    return int(out.value)
+
+
+def dasc_decay_attn(plan: Plan, state: torch.Tensor, layer_stride: int, req_stride: int, req_idx: torch.Tensor,
+                    q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, cu_seqlens: torch.Tensor,
+                    total_tokens: int, max_seqlen: int, *, seq_used: torch.Tensor | None = None,
+                    from_zero: torch.Tensor | None = None, decay: int = DECAY_PER_TOKEN, layer_begin: int = 0,
+                    layer_end: int | None = None, q_scale: float = 1.0, o: torch.Tensor | None = None,
+                    mode: int = DECAY_CONTINUE, algo: int = ALGO_AUTO, workspace: torch.Tensor | None = None, stream=None):
+    """Linear attention with a decay per value head over each request's tokens: outputs into ``o``, states advanced in place
+    (``DECAY_SCORE``: outputs only).  ``seq_used`` (int32 [n_req], device): run only that many tokens of each request, for
+    instance ``dasc_verify_draft``'s ``n_kept``; ``from_zero`` (int32 [n_req], device): requests that start from a zero state.
+    A negative ``req_idx`` is padding.  ``q`` may be None when ``o`` is."""
+    _check((_native or _call()).decay_attn(
+        plan.handle, state, layer_stride, req_stride, req_idx, q, k, v, g, decay, layer_begin,
+        plan.info.n_layers if layer_end is None else layer_end, q_scale, o, cu_seqlens, total_tokens, max_seqlen, seq_used, from_zero,
+        mode, algo, workspace, stream), "dasc_decay_attn")
+
+
+def dasc_decay_status(workspace) -> int:
+    """Status of the last ``dasc_decay_attn`` with ``workspace``; call after synchronising the stream."""
+    if workspace is None:
+        return OK
+    return int(lib().dasc_decay_status(_ptr(workspace), int(workspace.numel() * workspace.element_size())))
+
+
+def dasc_decay_step(plan: Plan, state: torch.Tensor, layer_stride: int, req_stride: int, req_idx: torch.Tensor, q: torch.Tensor,
+                    k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, o: torch.Tensor, *, decay: int = DECAY_PER_TOKEN,
+                    layer_begin: int = 0, layer_end: int | None = None, q_scale: float = 1.0, stream=None):
+    """``dasc_decay_attn`` for one token per request: streams [layers in the call][n_req][heads][d], states in place."""
+    _check((_native or _call()).decay_step(
+        plan.handle, state, layer_stride, req_stride, req_idx, q, k, v, g, decay, layer_begin,
+        plan.info.n_layers if layer_end is None else layer_end, q_scale, o, stream), "dasc_decay_step")
+
+
+def dasc_verify_draft(target: torch.Tensor, draft: torch.Tensor | None, tokens: torch.Tensor, cu_drafts: torch.Tensor,
+                      u_accept: torch.Tensor, u_next: torch.Tensor, out: torch.Tensor, n_kept: torch.Tensor, stream=None):
+    """How many of each request's drafted tokens stand, and its next token.  ``target`` [drafts + n_req, vocab] (request r's rows
+    from ``cu_drafts[r] + r`` on) and ``draft`` [drafts, vocab] (None: a deterministic drafter) are probabilities, bf16 or fp32,
+    with rows that may be strided; ``out`` int32 [n_req, most drafts + 1] and ``n_kept`` int32 [n_req] are written."""
+    (rows, vocab), (ts, t1) = target.shape, target.stride()
+    (n_out, width), (os_, o1) = out.shape, out.stride()
+    n_drafts, n_req = tokens.numel(), cu_drafts.numel() - 1
+    if n_out < n_req or rows < n_drafts + n_req or (t1 != 1 and vocab > 1) or (o1 != 1 and width > 1) or width < 1:
+        raise ValueError("target needs a row per drafted token and request, out one per request, both dense in their last dimension")
+    ds = vocab
+    if draft is not None:
+        ds, d1 = draft.stride()
+        if draft.shape[0] < n_drafts or draft.shape[1] != vocab or (d1 != 1 and vocab > 1):
+            raise ValueError("draft needs a row of the vocabulary per drafted token, dense in its last dimension")
+        ds = vocab if n_drafts <= 1 else ds  # (a stride that nothing is reached by says nothing)
+    _check((_native or _call()).verify_draft(target, vocab if rows <= 1 else ts, draft, ds, vocab, tokens, cu_drafts, u_accept, u_next,
+                                             width - 1, out, width if n_out <= 1 else os_, n_kept, stream), "dasc_verify_draft")

@@ -769,6 +769,155 @@ dasc_status_t dasc_refresh_counters(const void *workspace, size_t workspace_byte
 
 void dasc_debug_set_refresh_poll_limit(uint32_t polls) { __atomic_store_n(&g_dasc_debug_poll_limit, polls, __ATOMIC_RELAXED); }
 
+// ---- linear attention with a decay per head ------------------------------------------------------------------------------------
+
+namespace {
+
+bool decay_shape_ok(const dasc_plan_t *plan) {
+  const int32_t k = plan->info.d_k;
+  return (k == 32 || k == 64 || k == 128) && plan->info.d_v % 32 == 0;
+}
+
+// Every argument check of dasc_decay_attn (cu_seqlens given) and dasc_decay_step, before anything is launched.
+dasc_status_t decay_validate(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride, const int32_t *req_idx,
+                             const void *q, const void *k, const void *v, int32_t io_dtype, const float *g, int32_t decay, int32_t n_req,
+                             int64_t total_tokens, int32_t layer_begin, int32_t layer_end, float q_scale, void *o, int32_t o_dtype,
+                             int32_t mode, DascDecayArgs *a) {
+  if (!plan || plan->info.device < 0) return DASC_ERR_INVALID_ARG;
+  if (n_req < 0 || total_tokens < 0) return DASC_ERR_INVALID_ARG;
+  if (layer_begin < 0 || layer_end < layer_begin || layer_end > plan->info.n_layers) return DASC_ERR_INVALID_ARG;
+  if (io_dtype != DASC_IO_BF16 && io_dtype != DASC_IO_FP32) return DASC_ERR_INVALID_ARG;
+  if (o && o_dtype != DASC_IO_BF16 && o_dtype != DASC_IO_FP32) return DASC_ERR_INVALID_ARG;
+  if (decay != DASC_DECAY_PER_TOKEN && decay != DASC_DECAY_PER_HEAD) return DASC_ERR_INVALID_ARG;
+  if (mode != DASC_DECAY_CONTINUE && mode != DASC_DECAY_SCRATCH_MERGE_LOCAL && mode != DASC_DECAY_SCORE) return DASC_ERR_INVALID_ARG;
+  if (plan->info.kind != DASC_GDN) return DASC_ERR_UNSUPPORTED;  // a decay per key channel is not this recurrence
+  if (!decay_shape_ok(plan)) return DASC_ERR_SHAPE;
+  const int32_t layers = layer_end - layer_begin;
+  if (total_tokens > INT32_MAX || static_cast<double>(n_req) * layers * plan->info.n_v_heads * (plan->info.d_v / 32) > INT32_MAX)
+    return DASC_ERR_SHAPE;
+  if (n_req == 0 || layers == 0) return DASC_OK;
+  if (!state_base || !req_idx || !aligned16(state_base)) return DASC_ERR_INVALID_ARG;
+  if (total_tokens > 0 && (!k || !v || !g || (o && !q))) return DASC_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || (reinterpret_cast<uintptr_t>(g) & 3u)) return DASC_ERR_INVALID_ARG;
+  if (layer_stride < 0 || req_stride < 0 || layer_stride % 4 || req_stride % 4) return DASC_ERR_INVALID_ARG;
+  if (layers > 1 && layer_stride < plan->info.dense_floats_per_layer && req_stride < plan->info.dense_floats_per_layer)
+    return DASC_ERR_INVALID_ARG;  // layers of one request would overlap
+  if (const dasc_status_t ds = check_device(plan); ds != DASC_OK) return ds;
+  a->H_v = plan->info.n_v_heads;
+  a->H_k = plan->info.n_k_heads;
+  a->d_k = plan->info.d_k;
+  a->d_v = plan->info.d_v;
+  a->state = state_base;
+  a->layer_stride = layer_stride;
+  a->req_stride = req_stride;
+  a->req_idx = req_idx;
+  a->q = q;
+  a->k = k;
+  a->v = v;
+  a->io_bf16 = io_dtype == DASC_IO_BF16;
+  a->g = g;
+  a->g_per_head = decay == DASC_DECAY_PER_HEAD;
+  a->n_req = n_req;
+  a->total_tokens = total_tokens;
+  a->layer_begin = layer_begin;
+  a->n_layers_in_call = layers;
+  a->q_scale = q_scale;
+  a->o = o;
+  a->o_bf16 = o_dtype == DASC_IO_BF16;
+  a->mode = mode;
+  a->row_keep = plan->d_row_keep;
+  a->rows_per_layer = plan->rows_per_layer;
+  return DASC_OK;
+}
+
+}  // namespace
+
+dasc_status_t dasc_decay_workspace_bytes(const dasc_plan_t *plan, int32_t n_req, int32_t n_layers_in_call, int64_t total_tokens,
+                                         int32_t max_seqlen, int32_t algo, size_t *out) {
+  if (!plan || !out || n_req < 0 || n_layers_in_call < 0 || total_tokens < 0) return DASC_ERR_INVALID_ARG;
+  if (algo != DASC_ALGO_AUTO && algo != DASC_ALGO_SEQUENTIAL && algo != DASC_ALGO_CHUNKED) return DASC_ERR_INVALID_ARG;
+  *out = 0;
+  return DASC_OK;
+}
+
+dasc_status_t dasc_decay_attn(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride,
+                              const int32_t *req_idx, const void *q, const void *k, const void *v, int32_t io_dtype,
+                              const float *g, int32_t decay, const int32_t *cu_seqlens, const int32_t *seq_used,
+                              const int32_t *from_zero, int32_t n_req, int64_t total_tokens, int32_t max_seqlen,
+                              int32_t layer_begin, int32_t layer_end, float q_scale, void *o, int32_t o_dtype, int32_t mode,
+                              int32_t algo, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+  TraceRange trace("dasc_decay_attn");
+  DascDecayArgs a{};
+  if (algo != DASC_ALGO_AUTO && algo != DASC_ALGO_SEQUENTIAL && algo != DASC_ALGO_CHUNKED) return DASC_ERR_INVALID_ARG;
+  if (max_seqlen < 0 || (mode == DASC_DECAY_SCORE && !o)) return DASC_ERR_INVALID_ARG;
+  const dasc_status_t st = decay_validate(plan, state_base, layer_stride, req_stride, req_idx, q, k, v, io_dtype, g, decay, n_req, total_tokens,
+                                          layer_begin, layer_end, q_scale, o, o_dtype, mode, &a);
+  if (st != DASC_OK || n_req == 0 || layer_end == layer_begin) return st;
+  if (!cu_seqlens) return DASC_ERR_INVALID_ARG;
+  a.cu_seqlens = cu_seqlens;
+  a.seq_used = seq_used;
+  a.from_zero = from_zero;
+  a.max_seqlen = max_seqlen;
+  if (algo == DASC_ALGO_CHUNKED) return DASC_ERR_UNSUPPORTED;
+  return dasc_launch_decay_seq(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
+}
+
+dasc_status_t dasc_decay_step(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride,
+                              const int32_t *req_idx, const void *q, const void *k, const void *v, int32_t io_dtype,
+                              const float *g, int32_t decay, int32_t n_req, int32_t layer_begin, int32_t layer_end,
+                              float q_scale, void *o, int32_t o_dtype, void *cuda_stream) {
+  TraceRange trace("dasc_decay_step");
+  DascDecayArgs a{};
+  const dasc_status_t st = decay_validate(plan, state_base, layer_stride, req_stride, req_idx, q, k, v, io_dtype, g, decay, n_req, n_req,
+                                          layer_begin, layer_end, q_scale, o, o_dtype, DASC_DECAY_CONTINUE, &a);
+  if (st != DASC_OK || n_req == 0 || layer_end == layer_begin) return st;
+  if (!o) return DASC_ERR_INVALID_ARG;
+  return dasc_launch_decay_seq(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
+}
+
+dasc_status_t dasc_decay_status(const void *workspace, size_t workspace_bytes) {
+  return DASC_OK;
+}
+
+dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const void *draft, int64_t draft_stride,
+                                int32_t dtype, int32_t vocab, const int32_t *tokens, const int32_t *cu_drafts,
+                                const float *u_accept, const float *u_next, int32_t n_req, int32_t max_drafts, int32_t *out,
+                                int64_t out_stride, int32_t *n_kept, void *cuda_stream) {
+  TraceRange trace("dasc_verify_draft");
+  if (n_req < 0 || max_drafts < 0 || vocab <= 0) return DASC_ERR_INVALID_ARG;
+  if (dtype != DASC_IO_BF16 && dtype != DASC_IO_FP32) return DASC_ERR_INVALID_ARG;
+  if (n_req > INT32_MAX / 16 || vocab > INT32_MAX / 2 || max_drafts > INT32_MAX / 2) return DASC_ERR_SHAPE;
+  if (n_req == 0) return DASC_OK;
+  if (!target || !cu_drafts || !u_next || !out || !n_kept || !tokens != !u_accept) return DASC_ERR_INVALID_ARG;
+  const uintptr_t esz = dtype == DASC_IO_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(target) % esz || reinterpret_cast<uintptr_t>(draft) % esz) return DASC_ERR_INVALID_ARG;
+  if (target_stride < vocab || (draft && draft_stride < vocab) || out_stride < static_cast<int64_t>(max_drafts) + 1)
+    return DASC_ERR_INVALID_ARG;
+  // there is no plan to say which device the buffers are on
+  int dev = -1;
+  cudaPointerAttributes at{};
+  if (cudaGetDevice(&dev) != cudaSuccess) return DASC_ERR_CUDA;
+  if (cudaPointerGetAttributes(&at, target) != cudaSuccess) return DASC_ERR_CUDA;
+  if (at.type == cudaMemoryTypeUnregistered || (at.type == cudaMemoryTypeDevice && at.device != dev)) return DASC_ERR_INVALID_ARG;
+  DascVerifyArgs a{};
+  a.target = target;
+  a.target_stride = target_stride;
+  a.draft = draft;
+  a.draft_stride = draft_stride;
+  a.bf16 = dtype == DASC_IO_BF16;
+  a.vocab = vocab;
+  a.tokens = tokens;
+  a.cu_drafts = cu_drafts;
+  a.u_accept = u_accept;
+  a.u_next = u_next;
+  a.n_req = n_req;
+  a.max_drafts = max_drafts;
+  a.out = out;
+  a.out_stride = out_stride;
+  a.n_kept = n_kept;
+  return dasc_launch_verify_draft(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
+}
+
 const char *dasc_status_string(dasc_status_t s) {
   switch (s) {
     case DASC_OK: return "ok";

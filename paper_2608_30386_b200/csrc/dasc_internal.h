@@ -124,3 +124,48 @@ int dasc_launch_refresh_chunked(const DascRefreshArgs &a, void *stream);
 size_t dasc_refresh_chunked_workspace_bytes(int32_t n_req, int32_t n_layers_in_call, int32_t H_v);
 // Test hook (see dasc_debug_set_refresh_poll_limit in dasc.h).
 extern uint32_t g_dasc_debug_poll_limit;
+
+// Linear attention with a decay per head (decay_seq.cu, decay_chunked.cu).
+struct DascDecayArgs {
+  int32_t H_v, H_k, d_k, d_v;
+  float *state;
+  int64_t layer_stride, req_stride;
+  const int32_t *req_idx;
+  const void *q, *k, *v;
+  int32_t io_bf16;
+  const float *g;
+  int32_t g_per_head;         // 1: g is [Lc][H_v], else [Lc][T][H_v]
+  const int32_t *cu_seqlens;  // null: one token per request, token r is request r's (total_tokens = n_req)
+  const int32_t *seq_used;    // device, [n_req], or null: tokens of each request that are run
+  const int32_t *from_zero;   // device, [n_req], or null: != 0 starts from a zero state
+  int32_t n_req;
+  int64_t total_tokens;
+  int32_t max_seqlen;
+  int32_t layer_begin, n_layers_in_call;
+  float q_scale;
+  void *o;
+  int32_t o_bf16;
+  int32_t mode;               // dasc_decay_mode_t
+  const uint8_t *row_keep;    // device, [L][rows_per_layer]
+  int64_t rows_per_layer;
+  void *workspace;            // chunked kernel only
+};
+// Both return a cudaError_t as int, or -1 if the shape has no kernel.
+int dasc_launch_decay_seq(const DascDecayArgs &a, void *stream);
+int dasc_launch_decay_chunked(const DascDecayArgs &a, void *stream);
+// Bytes of workspace of the chunked kernel: status words, and the states of the segments where it splits requests.
+size_t dasc_decay_chunked_workspace_bytes(int32_t n_req, int32_t n_layers_in_call, int32_t H_v, int64_t total_tokens, int32_t max_seqlen);
+
+// verify_draft.cu
+struct DascVerifyArgs {
+  const void *target, *draft;
+  int64_t target_stride, draft_stride;
+  int32_t bf16, vocab;
+  const int32_t *tokens, *cu_drafts;
+  const float *u_accept, *u_next;
+  int32_t n_req, max_drafts;
+  int32_t *out;
+  int64_t out_stride;
+  int32_t *n_kept;
+};
+int dasc_launch_verify_draft(const DascVerifyArgs &a, void *stream);

@@ -1,0 +1,244 @@
+// Verification of drafted tokens: which of them stand, and the next token by inverse transform sampling, from given random
+// numbers.  All comparisons and sums are in 64 bits: a running sum over a vocabulary in 32 bits would move the border between
+// two tokens by more than many of them weigh.
+//
+// Split: a request is one cluster of CL thread blocks, each of which owns a contiguous part of the row, and in it each warp a
+// contiguous run of tiles.  One pass sums the weights per warp; the sums meet through distributed shared memory in a fixed
+// order, every block finds the one warp whose part holds the threshold, and that warp goes over its own few tiles again (they
+// are in L2).  One launch, no workspace, nothing depends on the order of arrival.
+// Bound: one pass over a row of the target, and one of the drafter where a token does not stand.
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+
+#include "decay_common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace {
+
+constexpr int NT = 512, NW = NT / 32;
+constexpr int TILE = 128;  // entries of a row that a warp takes at once: four per lane
+
+template <typename T>
+__device__ __forceinline__ float prob(T x) {
+  if constexpr (sizeof(T) == 2)
+    return __bfloat162float(x);
+  else
+    return x;
+}
+// A probability that is none counts as nothing.
+__device__ __forceinline__ double clean(float x) { return x > 0.f && x < __int_as_float(0x7f800000) ? static_cast<double>(x) : 0.0; }
+
+// four entries of a row, from entry i on; 0 behind the end
+template <typename T, bool VEC>
+__device__ __forceinline__ void load4(const T *row, int i, int vocab, float (&x)[4]) {
+  if (VEC && i + 4 <= vocab) {
+    if constexpr (sizeof(T) == 4) {
+      const float4 v = *reinterpret_cast<const float4 *>(row + i);
+      x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+    } else {
+      const uint2 v = *reinterpret_cast<const uint2 *>(row + i);
+      x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+      x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = i + j < vocab ? prob<T>(row[i + j]) : 0.f;
+  }
+}
+
+template <typename T, bool VEC, int CL>
+__global__ void __launch_bounds__(NT) verify_draft_kernel(const __grid_constant__ DascVerifyArgs a) {
+  __shared__ double warp_sum[NW], s_before, s_threshold;
+  __shared__ int s_count, s_winner;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int r = blockIdx.x / CL, rank = blockIdx.x % CL;
+  stream_order_begin();
+
+  const int64_t d0 = a.cu_drafts[r];
+  const int n = a.tokens ? min(max(static_cast<int>(a.cu_drafts[r + 1] - d0), 0), a.max_drafts) : 0;
+  const T *const target = static_cast<const T *>(a.target) + (d0 + r) * a.target_stride;
+  const T *const draft = a.draft ? static_cast<const T *>(a.draft) + d0 * a.draft_stride : nullptr;
+  // every block of the cluster looks for itself which tokens stand: two probabilities each
+  if (warp == 0) {
+    int count = 0;
+    for (int j0 = 0; j0 < n; j0 += 32) {
+      const int j = j0 + lane;
+      bool stands = false;
+      if (j < n) {
+        const int x = a.tokens[d0 + j];
+        if (x >= 0 && x < a.vocab) {
+          const double p = prob<T>(target[j * a.target_stride + x]), q = draft ? prob<T>(draft[j * a.draft_stride + x]) : 1.f;
+          stands = static_cast<double>(a.u_accept[d0 + j]) * q < p;
+        }
+      }
+      const uint32_t no = ~__ballot_sync(0xffffffffu, stands);
+      count = j0 + (no ? __ffs(no) - 1 : 32);
+      if (no) break;
+    }
+    if (lane == 0) s_count = min(count, n);
+  }
+  __syncthreads();
+  const int count = s_count;
+  const bool all = count == n;
+  const T *const prow = target + count * a.target_stride;
+  const T *qrow = !all && draft ? draft + count * a.draft_stride : nullptr;
+  int taken = !all && !draft ? a.tokens[d0 + count] : -1;  // a deterministic drafter's token: its probability is 1
+
+  if (rank == 0) {
+    int32_t *const out = a.out + r * a.out_stride;
+    for (int j = tid; j <= a.max_drafts; j += NT)
+      if (j != count) out[j] = j < count ? a.tokens[d0 + j] : -1;
+    if (tid == 0) a.n_kept[r] = count + 1;
+  }
+
+  const int tiles = (a.vocab + TILE - 1) / TILE, per_warp = (tiles + CL * NW - 1) / (CL * NW);
+  const int gw = rank * NW + warp;
+  const int first = min(gw * per_warp, tiles), last = min(first + per_warp, tiles);
+  auto weights = [&](int tile, double (&w)[4]) {
+    const int i = tile * TILE + lane * 4;
+    float p[4], q[4] = {0.f, 0.f, 0.f, 0.f};
+    load4<T, VEC>(prow, i, a.vocab, p);
+    if (qrow) load4<T, VEC>(qrow, i, a.vocab, q);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const double d = clean(p[j]) - (i + j == taken ? 1.0 : clean(q[j]));
+      w[j] = d > 0.0 ? d : 0.0;
+    }
+  };
+
+  cg::cluster_group cluster = cg::this_cluster();
+  constexpr int PER = (CL * NW + 31) / 32;
+  for (int attempt = 0; attempt < 2; ++attempt) {
+    double sum = 0.0;
+#pragma unroll 4
+    for (int t = first; t < last; ++t) {
+      double w[4];
+      weights(t, w);
+      sum += (w[0] + w[1]) + (w[2] + w[3]);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (lane == 0) warp_sum[warp] = sum;
+    cluster.sync();
+    double x[PER];  // lane l of the first warp: the sums of warps PER l ... of the cluster
+#pragma unroll
+    for (int j = 0; j < PER; ++j) x[j] = 0.0;
+    if (warp == 0) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const int i = lane * PER + j;
+        if (i < CL * NW) x[j] = cluster.map_shared_rank(warp_sum, i / NW)[i % NW];
+      }
+    }
+    cluster.sync();  // (no block changes its sums, or ends, while another still reads them)
+    if (warp == 0) {
+      double incl = 0.0;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) incl += x[j];
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const double y = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += y;
+      }
+      const double total = __shfl_sync(0xffffffffu, incl, 31);
+      double run = __shfl_up_sync(0xffffffffu, incl, 1);
+      if (lane == 0) run = 0.0;
+      // the first warp whose part of the row takes the running sum over the threshold (the last one with any weight, should
+      // a random number not be below 1)
+      const double threshold = fmax(static_cast<double>(a.u_next[r]) * total, 0.0);
+      int here = -1, some = -1;
+      double before = 0.0, before_some = 0.0;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const double next = run + x[j];
+        if (x[j] > 0.0) {
+          some = lane * PER + j;
+          before_some = run;
+          if (here < 0 && next > threshold) {
+            here = some;
+            before = run;
+          }
+        }
+        run = next;
+      }
+      uint32_t m = __ballot_sync(0xffffffffu, here >= 0);
+      int l = m ? __ffs(m) - 1 : 0;
+      if (!m) {
+        m = __ballot_sync(0xffffffffu, some >= 0);
+        l = m ? 31 - __clz(m) : 0;
+        here = some;
+        before = before_some;
+      }
+      if (lane == l) {
+        s_winner = total > 0.0 ? here : -1;
+        s_before = before;
+        s_threshold = threshold;
+      }
+    }
+    __syncthreads();
+    if (s_winner >= 0 || (!qrow && taken < 0)) break;
+    qrow = nullptr;  // the drafter leaves nothing: the target's own row
+    taken = -1;
+    __syncthreads();
+  }
+  const int winner = s_winner;
+  if (winner < 0) {
+    if (rank == 0 && tid == 0) a.out[r * a.out_stride + count] = -1;
+    return;
+  }
+  if (gw != winner) return;
+  double before = s_before;
+  const double threshold = s_threshold;
+  int token = -1, last_some = -1;
+  for (int t = first; t < last && token < 0; ++t) {
+    double w[4];
+    weights(t, w);
+    double incl = (w[0] + w[1]) + (w[2] + w[3]);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const double y = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += y;
+    }
+    const double excl = __shfl_up_sync(0xffffffffu, incl, 1);
+    double x = before + (lane > 0 ? excl : 0.0);
+    int here = -1, any = -1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x += w[j];
+      if (w[j] > 0.0) {
+        any = j;
+        if (here < 0 && x > threshold) here = j;
+      }
+    }
+    const uint32_t hit = __ballot_sync(0xffffffffu, here >= 0), some_here = __ballot_sync(0xffffffffu, any >= 0);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      token = t * TILE + l * 4 + __shfl_sync(0xffffffffu, here, l);
+    } else if (some_here) {
+      const int l = 31 - __clz(some_here);
+      last_some = t * TILE + l * 4 + __shfl_sync(0xffffffffu, any, l);
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (lane == 0) a.out[r * a.out_stride + count] = token >= 0 ? token : last_some;
+}
+
+template <typename T, bool VEC, int CL>
+int launch(const DascVerifyArgs &a, void *stream) {
+  return static_cast<int>(launch_clusters(verify_draft_kernel<T, VEC, CL>, dim3(static_cast<unsigned>(a.n_req) * CL), dim3(NT), CL, 0, stream, a));
+}
+
+template <typename T>
+int launch_type(const DascVerifyArgs &a, void *stream) {
+  // four entries per load where every row starts on their boundary
+  auto even = [](const void *p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0 && stride % 4 == 0; };
+  const bool vec = even(a.target, a.target_stride) && (!a.draft || even(a.draft, a.draft_stride));
+  return vec ? launch<T, true, 8>(a, stream) : launch<T, false, 8>(a, stream);
+}
+
+}  // namespace
+
+int dasc_launch_verify_draft(const DascVerifyArgs &a, void *stream) {
+  return a.bf16 ? launch_type<__nv_bfloat16>(a, stream) : launch_type<float>(a, stream);
+}
