@@ -440,7 +440,7 @@ dasc_status_t dasc_refresh(const dasc_plan_t *plan, float *state_base, int64_t l
 dasc_status_t dasc_refresh_status(const void *workspace, size_t workspace_bytes);
 dasc_status_t dasc_refresh_counters(const void *workspace, size_t workspace_bytes, int32_t *handed_over,
                                     int32_t *replayed_exactly);
-/* Test hook, not for production use: when `polls` != 0 the chunked kernel's
+/* Test hook, not for production use: when `polls` != 0 the chunked kernels' (dasc_refresh, dasc_decay_attn)
  * issuing warp begins every CTA with a wait of only that many polls, for tiles
  * that cannot be there yet, so that a test can watch a bounded wait run out
  * (DASC_ERR_TIMEOUT, its units left unwritten, the context still usable).

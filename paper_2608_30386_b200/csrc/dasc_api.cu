@@ -778,6 +778,12 @@ bool decay_shape_ok(const dasc_plan_t *plan) {
   return (k == 32 || k == 64 || k == 128) && plan->info.d_v % 32 == 0;
 }
 
+// Requests of at most this many tokens (by the caller's bound) run token by token under AUTO.
+constexpr int kDecayShort = 16;
+bool decay_chunked_shape(const dasc_plan_t *plan, int32_t layers, int64_t total_tokens) {
+  return chunked_shape_ok(plan) && total_tokens > 0 && static_cast<double>(layers) * total_tokens <= INT32_MAX;  // (32-bit token coordinates)
+}
+
 // Every argument check of dasc_decay_attn (cu_seqlens given) and dasc_decay_step, before anything is launched.
 dasc_status_t decay_validate(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride, const int32_t *req_idx,
                              const void *q, const void *k, const void *v, int32_t io_dtype, const float *g, int32_t decay, int32_t n_req,
@@ -836,7 +842,9 @@ dasc_status_t dasc_decay_workspace_bytes(const dasc_plan_t *plan, int32_t n_req,
                                          int32_t max_seqlen, int32_t algo, size_t *out) {
   if (!plan || !out || n_req < 0 || n_layers_in_call < 0 || total_tokens < 0) return DASC_ERR_INVALID_ARG;
   if (algo != DASC_ALGO_AUTO && algo != DASC_ALGO_SEQUENTIAL && algo != DASC_ALGO_CHUNKED) return DASC_ERR_INVALID_ARG;
-  *out = 0;
+  const bool chunked = algo != DASC_ALGO_SEQUENTIAL && decay_chunked_shape(plan, n_layers_in_call, total_tokens) &&
+                       (algo == DASC_ALGO_CHUNKED || max_seqlen > kDecayShort);
+  *out = chunked ? dasc_decay_chunked_workspace_bytes(n_req, n_layers_in_call, plan->info.n_v_heads, total_tokens, max_seqlen) : 0;
   return DASC_OK;
 }
 
@@ -858,7 +866,17 @@ dasc_status_t dasc_decay_attn(const dasc_plan_t *plan, float *state_base, int64_
   a.seq_used = seq_used;
   a.from_zero = from_zero;
   a.max_seqlen = max_seqlen;
-  if (algo == DASC_ALGO_CHUNKED) return DASC_ERR_UNSUPPORTED;
+  const bool shape_ok = chunked_shape_ok(plan) && a.io_bf16;
+  if (algo == DASC_ALGO_CHUNKED && !shape_ok) return DASC_ERR_SHAPE;
+  const bool fits = shape_ok && decay_chunked_shape(plan, a.n_layers_in_call, total_tokens);
+  if (algo == DASC_ALGO_CHUNKED && !fits && total_tokens > 0) return DASC_ERR_SHAPE;
+  const bool usable = workspace && !(reinterpret_cast<uintptr_t>(workspace) & 255u) && workspace_bytes >= kDecayStatusWords * sizeof(uint32_t);
+  a.workspace = usable ? workspace : nullptr;
+  if (fits && (algo == DASC_ALGO_CHUNKED || (algo == DASC_ALGO_AUTO && max_seqlen > kDecayShort))) {
+    if (!usable || workspace_bytes < dasc_decay_chunked_workspace_bytes(n_req, a.n_layers_in_call, a.H_v, total_tokens, max_seqlen))
+      return DASC_ERR_WORKSPACE;
+    return dasc_launch_decay_chunked(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
+  }
   return dasc_launch_decay_seq(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
 }
 
@@ -876,6 +894,11 @@ dasc_status_t dasc_decay_step(const dasc_plan_t *plan, float *state_base, int64_
 }
 
 dasc_status_t dasc_decay_status(const void *workspace, size_t workspace_bytes) {
+  uint32_t flag[kDecayStatusWords];
+  if (!workspace || workspace_bytes < sizeof flag) return DASC_OK;  // nothing was recorded
+  if (cudaMemcpy(flag, workspace, sizeof flag, cudaMemcpyDeviceToHost) != cudaSuccess) return DASC_ERR_CUDA;
+  for (uint32_t f : flag)
+    if (f != 0) return DASC_ERR_TIMEOUT;
   return DASC_OK;
 }
 

@@ -148,8 +148,11 @@ struct DascDecayArgs {
   int32_t mode;               // dasc_decay_mode_t
   const uint8_t *row_keep;    // device, [L][rows_per_layer]
   int64_t rows_per_layer;
-  void *workspace;            // chunked kernel only
+  void *workspace;            // status words first; the token-by-token kernel clears them where there are any
+  uint32_t poll_limit_first_wait;  // test hook: poll limit of the issuing warp's very first wait (0 = the normal limit)
 };
+// Workspace: a status word per thread block of each of the chunked kernel's two launches (1: a wait ran out), then the segments.
+constexpr int kDecayStatusWords = 512;
 // Both return a cudaError_t as int, or -1 if the shape has no kernel.
 int dasc_launch_decay_seq(const DascDecayArgs &a, void *stream);
 int dasc_launch_decay_chunked(const DascDecayArgs &a, void *stream);

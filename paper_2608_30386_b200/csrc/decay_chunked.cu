@@ -1,0 +1,874 @@
+// Linear attention with a decay per head, chunked form on the tensor cores, for d_k = d_v = 128 and bf16 streams.
+//
+// With G_t the sum of the log-decays of a chunk up to its token t (log2 units here), S_0 the state at its start:
+//   O   = q_scale (diag(e^G) Q S_0 + P V),   P_ti = e^{G_t - G_i} q_t . k_i for i <= t, else 0
+//   S_C = e^{G_C} S_0 + Kw^T V,               Kw_i = e^{G_C - G_i} k_i
+// Products, C = 64 tokens, everything transposed so that d_v is the M index (the accumulators' 128 lanes):
+//   QK   Q K^T               -> P before its weights    smem x smem, M = 64
+//   QS   S_0^T Q^T           -> outputs from the state   tmem x smem   (S_0 as a bf16 pair)
+//   PV   V^T P^T             -> outputs inside the chunk  smem x smem   (P as a pair; only the rows a slice of i can reach)
+//   KV   V^T Kw              -> what the chunk adds        smem x smem   (Kw as a pair)
+// V, K and Q are exact in bf16 and are used as they land; V and Kw are read with their token index as K, which for 16-bit
+// operands is the same tile.  A pair of bf16 (x rounded, and the rest rounded) holds 16 bits of the mantissa: an operand rounded
+// to bf16 once would cost the fp32 state its last 16 bits and as much of the outputs as their own rounding does.
+//
+// One thread block per SM walks over (request, layer, head) units, or over segments of long ones; roles of its warps:
+//   0       TMA: tiles of K, Q, V, three chunks ahead
+//   1       issues the products
+//   2       sums of log-decays (in 64 bits), weights of a chunk
+//   3 - 6   P: out of tensor memory, weighted, into its operand tiles; the outputs of the chunk before
+//   7 - 10  Kw; looks at V for values that are none
+//   11 - 18 the state, in fp32 registers: a thread has 64 key channels of one column
+// The only chain from chunk to chunk is S <- e^{G_C} S + (KV), 64 packed multiply-adds per thread, and its bf16 pair on the way
+// to QS; KV itself does not depend on the state.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "decay_common.cuh"
+#include "tcgen05_util.cuh"
+
+namespace {
+
+using namespace tc5;
+
+constexpr int C = 64, D = 128;
+constexpr int kSms = 148;
+constexpr int NS = 3;    // stages of K, Q, V
+constexpr int RING = 4;  // chunks whose weights are kept
+constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_K = 7, WARP_S = 11, NWARP = 19;  // (P: from 3 on)
+constexpr int NT = NWARP * 32;
+constexpr int kMaxSorted = 512;  // entries (requests x segments) that are taken longest first
+constexpr uint32_t kMaxPolls = 1u << 22;
+constexpr uint32_t kStatusWords = kDecayStatusWords / 2;  // per launch: one word per thread block
+
+constexpr uint32_t TILE = C * D * 2;  // 64 tokens x 128 channels: two blocks of [64 rows][128 bytes]
+constexpr uint32_t BLOCK = TILE / 2;
+constexpr uint32_t OFF_K = 0, OFF_Q = OFF_K + NS * TILE, OFF_V = OFF_Q + NS * TILE;
+constexpr uint32_t OFF_KH = OFF_V + NS * TILE, OFF_KL = OFF_KH + TILE;
+constexpr uint32_t OFF_PH = OFF_KL + TILE, OFF_PL = OFF_PH + C * C * 2;
+constexpr uint32_t OFF_O = OFF_PL + C * C * 2;  // [4 warps][64 tokens][32 columns] bf16 on their way out
+constexpr uint32_t OFF_MISC = OFF_O + TILE;
+
+constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 320, COL_OT = 448;
+
+struct Weights {  // of one chunk
+  float ghi[C], glo[C];  // G_t = ghi + glo, ghi a multiple of 2^-6: differences of ghi are exact
+  float w[C];            // e^{G_C - G_i}; 0 behind the last token
+  float eg[C];           // e^{G_t}
+  float all;             // e^{G_C}
+  int32_t has_bad;       // V holds values that are none:
+  int32_t bad[D];        // the first token with one, per column (C: no such token)
+};
+struct Misc {
+  uint64_t full_k[NS], full_q[NS], full_v[NS], empty_k[NS], empty_q[NS], empty_v[NS];
+  uint64_t dec_full[RING], dec_empty[RING];
+  uint64_t bar_p, bar_s, bar_o, bar_d;           // tensor core: QK, QS, PV, KV of a chunk have completed
+  uint64_t p_ready, k_ready, s_ready;            // operands of PV, KV, QS are in place
+  uint64_t o_free, d_free;                       // their accumulators have been read
+  uint64_t drain;
+  uint32_t tmem_base;
+  volatile uint32_t abort_flag;
+  Weights wt[RING];
+  uint16_t order[kMaxSorted];
+};
+constexpr uint32_t SMEM_BYTES = OFF_MISC + sizeof(Misc);
+static_assert(SMEM_BYTES <= 227 * 1024);
+static_assert(kMaxSorted * 4 <= TILE);
+
+struct Split {
+  int32_t nseg, seg_chunks;  // segments of a request, chunks of a segment (the last one takes what is left)
+  int32_t phase;             // 0: requests are not split; 1: states of all segments but the last, from zero; 2: everything, from the joined states
+  float *seg_state;          // [unit][nseg][D][D]
+  float *seg_decay;          // [unit][nseg]
+  uint32_t *status;          // [kStatusWords] of this launch
+};
+
+// The states and tokens of one unit, or of one segment of it.
+struct Item {
+  int64_t state;   // offset of its state in floats; < 0: nothing to write
+  int64_t tok0;    // its first token in the streams of the call
+  int64_t unit;
+  int32_t n, head, k_head, seg, lc;
+  bool zero, joined;
+};
+
+__device__ __forceinline__ float ex2f(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t *bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void arrive_warp(uint64_t *bar, int lane) {
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
+}
+// Bounded wait; once one has run out, no wait of this thread block lasts longer than one poll.
+__device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, Misc *m) {
+  for (uint32_t i = 0; !mbar_try_wait(bar, parity); ++i) {
+    if (m->abort_flag) return;
+    if (i == kMaxPolls) {
+      m->abort_flag = 1;
+      return;
+    }
+  }
+}
+__device__ __forceinline__ int uni(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+// Barrier of `n` threads: does the predicate hold for any of them?
+template <int ID, int N>
+__device__ __forceinline__ bool any_of(bool p) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred.aligned q, %2, %3, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"(static_cast<uint32_t>(p)), "n"(ID), "n"(N)
+      : "memory");
+  return any != 0;
+}
+
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+// (x, y) as a pair of bf16 pairs: hi = rounded, lo = the rest, rounded
+__device__ __forceinline__ void split2(uint64_t xy, uint32_t &hi, uint32_t &lo) {
+  const float2 v = dunpack2(xy);
+  hi = bf16x2(v.x, v.y);
+  const float2 r = dunpack2(dadd2(xy, dpack2(-bf_lo(hi), -bf_hi(hi))));
+  lo = bf16x2(r.x, r.y);
+}
+__device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
+}
+
+__device__ __forceinline__ int chunks_of(int n) { return (n + C - 1) / C; }
+// Segments that a request of `chunks` chunks really has.
+__device__ __forceinline__ int segments_of(const Split &sp, int chunks) {
+  return sp.nseg == 1 ? 1 : min(sp.nseg, max((chunks + sp.seg_chunks - 1) / sp.seg_chunks, 1));
+}
+// Chunks of entry `e` = (request, segment) that this launch runs.
+__device__ __forceinline__ int entry_chunks(const DascDecayArgs &a, const Split &sp, int e) {
+  const int r = e / sp.nseg, s = e - r * sp.nseg;
+  if (a.req_idx[r] < 0) return 0;
+  const int chunks = chunks_of(decay_range(a, r).n), segs = segments_of(sp, chunks);
+  if (s >= segs || (sp.phase == 1 && s == segs - 1)) return 0;
+  return s == segs - 1 ? chunks - s * sp.seg_chunks : sp.seg_chunks;
+}
+
+// This thread block's items, one after the other: every gridDim.x-th, there and back, so that each block gets long and short ones.
+struct Walk {
+  int64_t k = 0;
+  template <bool WITH_O>
+  __device__ __forceinline__ bool next(const DascDecayArgs &a, const Split &sp, const Misc *m, bool sorted, Item &x) {
+    const int64_t per_entry = static_cast<int64_t>(a.n_layers_in_call) * a.H_v, total = per_entry * a.n_req * sp.nseg;
+    for (;; ++k) {
+      const int64_t idx = k * gridDim.x + ((k & 1) ? gridDim.x - 1u - blockIdx.x : blockIdx.x);
+      if (idx >= total) {
+        // (on the way back a block's turn can be behind the end although the next one is not: there is no next one then)
+        return false;
+      }
+      int e = static_cast<int>(idx / per_entry);
+      const int rest = static_cast<int>(idx - e * per_entry);
+      if (sorted) e = m->order[e];
+      const int r = e / sp.nseg, s = e - r * sp.nseg;
+      const int req = a.req_idx[r];
+      if (req < 0) continue;
+      const DecayRange range = decay_range(a, r);
+      const int chunks = chunks_of(range.n), segs = segments_of(sp, chunks);
+      const bool last = s == segs - 1;
+      if (s >= segs || (sp.phase == 1 && last)) continue;
+      x.lc = rest / a.H_v;
+      x.head = rest - x.lc * a.H_v;
+      x.k_head = x.head / (a.H_v / a.H_k);
+      const int layer = a.layer_begin + x.lc;
+      const bool merge = a.mode == DASC_DECAY_SCRATCH_MERGE_LOCAL;
+      const bool write = a.mode != DASC_DECAY_SCORE && !(merge && a.row_keep[layer * a.rows_per_layer + x.head * D]);
+      if (!write && !a.o) continue;
+      x.zero = merge || (a.from_zero && a.from_zero[r] != 0);
+      x.joined = sp.phase == 2 && segs > 1;
+      if (sp.phase == 1) x.zero = true;
+      if (chunks == 0 && !(write && x.zero)) continue;
+      x.seg = s;
+      x.unit = (static_cast<int64_t>(r) * a.n_layers_in_call + x.lc) * a.H_v + x.head;
+      x.tok0 = static_cast<int64_t>(x.lc) * a.total_tokens + range.begin + static_cast<int64_t>(s) * sp.seg_chunks * C;
+      x.n = last ? range.n - s * sp.seg_chunks * C : sp.seg_chunks * C;
+      x.state = req * a.req_stride + layer * a.layer_stride + static_cast<int64_t>(x.head) * (D * D);
+      if (!(last && write)) x.state = -1 - x.state;  // (read, not written)
+      ++k;
+      return true;
+    }
+  }
+};
+
+template <bool WITH_O, typename OT>
+__global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_constant__ DascDecayArgs a, const __grid_constant__ Split sp,
+                                                             const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
+                                                             const __grid_constant__ CUtensorMap tmap_v) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const uint32_t sbase = smem_u32(smem);
+  Misc *const m = reinterpret_cast<Misc *>(smem + OFF_MISC);
+  const int tid = threadIdx.x, warp = uni(tid >> 5), lane = tid & 31;
+
+  if (tid == 0) {
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(&m->full_k[i], 1);
+      mbar_init(&m->full_q[i], 1);
+      mbar_init(&m->full_v[i], 1);
+      mbar_init(&m->empty_k[i], WITH_O ? 5 : 4);  // Kw's warps; QK
+      mbar_init(&m->empty_q[i], 1);
+      mbar_init(&m->empty_v[i], 1);
+    }
+    for (int i = 0; i < RING; ++i) {
+      mbar_init(&m->dec_full[i], 1);
+      mbar_init(&m->dec_empty[i], WITH_O ? 16 : 12);
+    }
+    mbar_init(&m->bar_p, 1);
+    mbar_init(&m->bar_s, 1);
+    mbar_init(&m->bar_o, 1);
+    mbar_init(&m->bar_d, 1);
+    mbar_init(&m->p_ready, 4);
+    mbar_init(&m->k_ready, 4);
+    mbar_init(&m->s_ready, 8);
+    mbar_init(&m->o_free, 4);
+    mbar_init(&m->d_free, 8);
+    mbar_init(&m->drain, 1);
+    m->abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == WARP_MMA) {
+    tmem_alloc(&m->tmem_base, 512);
+    tmem_relinquish();
+  }
+  stream_order_wait();
+  const int entries = a.n_req * sp.nseg;
+  const bool sorted = entries > 1 && entries <= kMaxSorted;
+  if (sorted) {  // longest first, ties in their order
+    int32_t *const key = reinterpret_cast<int32_t *>(smem);
+    for (int e = tid; e < (entries + 3) / 4 * 4; e += NT) key[e] = e < entries ? entry_chunks(a, sp, e) : -1;
+    __syncthreads();
+    for (int e = tid; e < entries; e += NT) {
+      const int own = key[e];
+      int rank = 0;
+      for (int j = 0; j < entries; j += 4) {
+        const int4 o = *reinterpret_cast<const int4 *>(key + j);
+        rank += (o.x > own || (o.x == own && j < e)) + (o.y > own || (o.y == own && j + 1 < e)) + (o.z > own || (o.z == own && j + 2 < e)) +
+                (o.w > own || (o.w == own && j + 3 < e));
+      }
+      m->order[rank] = static_cast<uint16_t>(e);
+    }
+    fence_smem_to_async();  // (tiles land where the keys were)
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tm = static_cast<uint32_t>(uni(static_cast<int>(m->tmem_base)));
+
+  Walk walk;
+  Item x;
+  int n = 0;  // chunks so far: buffers and barrier phases go by it
+  const auto stage = [](int i) { return static_cast<uint32_t>(i) % NS; };
+  const auto stage_phase = [](int i) { return static_cast<uint32_t>(i) / NS & 1u; };
+  const auto slot = [](int i) { return static_cast<uint32_t>(i) % RING; };
+  const auto slot_phase = [](int i) { return static_cast<uint32_t>(i) / RING & 1u; };
+
+  if (warp == WARP_TMA) {
+    if (lane == 0) {
+      int nk = 0, nq = 0, nv = 0;  // tiles asked for
+      bool stop = false;
+      while (!stop && walk.next<WITH_O>(a, sp, m, sorted, x)) {
+        for (int c = 0; c < chunks_of(x.n) && !stop; ++c, ++n) {
+          const uint32_t st = stage(n), ph = stage_phase(n) ^ 1u;
+          const int32_t z = static_cast<int32_t>(x.tok0 + c * C);
+          const auto load = [&](uint64_t *empty, uint64_t *full, uint32_t off, const CUtensorMap *map, int head, int &count) {
+            if (n >= NS) wait_bar(&empty[st], ph, m);
+            stop |= m->abort_flag != 0;
+            if (stop) return;
+            mbar_expect_tx(&full[st], TILE);
+            tma_load_3d(sbase + off + st * TILE, map, 0, head, z, &full[st]);
+            tma_load_3d(sbase + off + st * TILE + BLOCK, map, 64, head, z, &full[st]);
+            ++count;
+          };
+          load(m->empty_k, m->full_k, OFF_K, &tmap_k, x.k_head, nk);
+          if (WITH_O) load(m->empty_q, m->full_q, OFF_Q, &tmap_q, x.k_head, nq);
+          load(m->empty_v, m->full_v, OFF_V, &tmap_v, x.head, nv);
+        }
+      }
+      // Copies in flight land before the block ends, whoever has given up waiting for them.
+      const auto land = [&](uint64_t *full, int count) {
+        for (int i = max(count - NS, 0); i < count; ++i)
+          for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(&full[stage(i)], stage_phase(i)); ++p) {
+          }
+      };
+      land(m->full_k, nk);
+      land(m->full_q, nq);
+      land(m->full_v, nv);
+    }
+  } else if (warp == WARP_MMA) {
+    constexpr uint32_t ID_QK = idesc_bf16(64, 64), ID_QS = idesc_bf16(128, 64), ID_KV = idesc_bf16(128, 128, true, true);
+    const auto gave_up = [&]() { return uni(m->abort_flag) != 0; };  // (one answer for the whole warp)
+    const auto qk = [&](int i) {
+      const uint32_t st = stage(i);
+      wait_bar(&m->full_k[st], stage_phase(i), m);
+      wait_bar(&m->full_q[st], stage_phase(i), m);
+      tc_fence_after_sync();
+      if (gave_up()) return;
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+          const uint32_t o = st * TILE + (kk >> 2) * BLOCK + (kk & 3) * 32;
+          mma_ss_bf16(tm + COL_P, desc_kmajor(sbase + OFF_Q + o), desc_kmajor(sbase + OFF_K + o), ID_QK, kk != 0);
+        }
+        mma_commit(&m->bar_p);
+        mma_commit(&m->empty_k[st]);
+      }
+      __syncwarp();
+    };
+    int all = 0;  // chunks of all items: which chunk is the last is known one item ahead
+    bool more = walk.next<WITH_O>(a, sp, m, sorted, x);
+    while (more && chunks_of(x.n) == 0) more = walk.next<WITH_O>(a, sp, m, sorted, x);
+    all = more ? chunks_of(x.n) : 0;
+    // Test hook: a first, short wait for operands that cannot be there yet.
+    if (a.poll_limit_first_wait && all > 0) {
+      bool done = false;
+      for (uint32_t i = 0; i < a.poll_limit_first_wait && !done; ++i) done = mbar_test_wait(&m->k_ready, 0);
+      if (!done) m->abort_flag = 1;
+    }
+    if (WITH_O && all > 0) qk(0);
+    for (; n < all && !gave_up(); ++n) {
+      if (n + 1 == all) {
+        more = walk.next<WITH_O>(a, sp, m, sorted, x);
+        while (more && chunks_of(x.n) == 0) more = walk.next<WITH_O>(a, sp, m, sorted, x);
+        if (more) all += chunks_of(x.n);
+      }
+      const uint32_t st = stage(n), par = n & 1u;
+      const uint32_t vb = sbase + OFF_V + st * TILE;
+      // KV
+      wait_bar(&m->k_ready, par, m);
+      wait_bar(&m->full_v[st], stage_phase(n), m);
+      if (n > 0) wait_bar(&m->d_free, par ^ 1u, m);
+      tc_fence_after_sync();
+      if (gave_up()) break;
+      if (elect_one()) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t s = (i & 3) * 2048;
+          mma_ss_bf16(tm + COL_D, desc_mn_bf16(vb + s, BLOCK), desc_mn_bf16(sbase + (i < 4 ? OFF_KH : OFF_KL) + s, BLOCK), ID_KV, i != 0);
+        }
+        mma_commit(&m->bar_d);
+        if (!WITH_O) mma_commit(&m->empty_v[st]);
+      }
+      __syncwarp();
+      if (WITH_O) {
+        // QS
+        wait_bar(&m->s_ready, par, m);
+        tc_fence_after_sync();
+        if (gave_up()) break;
+        if (elect_one()) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int kk = i & 7;
+            mma_ts_bf16(tm + COL_OI + par * 64, tm + (i < 8 ? COL_SH : COL_SL) + kk * 8,
+                        desc_kmajor(sbase + OFF_Q + st * TILE + (kk >> 2) * BLOCK + (kk & 3) * 32), ID_QS, i != 0);
+          }
+          mma_commit(&m->bar_s);
+          mma_commit(&m->empty_q[st]);
+        }
+        __syncwarp();
+        // PV: tokens 16 s ... 16 s + 15 reach the rows from 16 s on
+        wait_bar(&m->p_ready, par, m);
+        if (n > 0) wait_bar(&m->o_free, par ^ 1u, m);
+        tc_fence_after_sync();
+        if (gave_up()) break;
+        if (elect_one()) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t s = i & 3;
+            mma_ss_bf16(tm + COL_OT + 16 * s, desc_mn_bf16(vb + s * 2048, BLOCK),
+                        desc_kmajor(sbase + (i < 4 ? OFF_PH : OFF_PL) + s * 2048 + s * 32), idesc_bf16(128, 64 - 16 * s, true, false), i != 0);
+          }
+          mma_commit(&m->bar_o);
+          mma_commit(&m->empty_v[st]);
+        }
+        __syncwarp();
+        if (n + 1 < all) qk(n + 1);
+      }
+    }
+    // products in flight end before their memory is given back, whoever has given up waiting for them
+    if (elect_one()) mma_commit(&m->drain);
+    __syncwarp();
+    for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(&m->drain, 0); ++p) {
+    }
+  } else if (warp == WARP_DECAY) {
+    while (walk.next<WITH_O>(a, sp, m, sorted, x)) {
+      const float *const g = a.g_per_head ? a.g + x.lc * a.H_v + x.head : a.g + x.tok0 * a.H_v + x.head;
+      const int64_t stride = a.g_per_head ? 0 : a.H_v;
+      const auto fetch = [&](int c, float (&y)[2]) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int t = c * C + 2 * lane + j;
+          y[j] = t < x.n ? g[t * stride] : 0.f;
+        }
+      };
+      float cur[2], nxt[2];
+      fetch(0, cur);
+      for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
+        fetch(c + 1, nxt);
+        if (n >= RING) wait_bar(&m->dec_empty[slot(n)], slot_phase(n) ^ 1u, m);
+        Weights &w = m->wt[slot(n)];
+        // log-decays below -10^4 forget everything; clamped, so that their sums stay where 64 bits are exact enough and none is infinite
+        double G[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) G[j] = static_cast<double>(cur[j] < -1e4f ? -1e4f : cur[j]) * 1.4426950408889634;
+        double incl = G[0] + G[1];
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const double y = __shfl_up_sync(0xffffffffu, incl, d);
+          if (lane >= d) incl += y;
+        }
+        const double total = __shfl_sync(0xffffffffu, incl, 31);
+        double run = __shfl_up_sync(0xffffffffu, incl, 1);
+        if (lane == 0) run = 0.0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          run += G[j];
+          const int t = 2 * lane + j;
+          const float hi = static_cast<float>(rint(run * 64.0) * (1.0 / 64.0));
+          w.ghi[t] = hi;
+          w.glo[t] = static_cast<float>(run - static_cast<double>(hi));
+          w.w[t] = c * C + t < x.n ? ex2f(static_cast<float>(total - run)) : 0.f;
+          w.eg[t] = ex2f(static_cast<float>(run));
+        }
+        if (lane == 0) w.all = ex2f(static_cast<float>(total));
+        arrive_warp(&m->dec_full[slot(n)], lane);
+        cur[0] = nxt[0];
+        cur[1] = nxt[1];
+      }
+    }
+  } else if (warp < WARP_K) {
+    // ---- P, and the outputs of the chunk before ----
+    if constexpr (WITH_O) {
+      const int quad = warp & 3, g = lane >> 2, tig = lane & 3;
+      const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
+      const int64_t v_stride = static_cast<int64_t>(a.H_v) * D;
+      unsigned char *const ost = smem + OFF_O + quad * 4096;
+      OT *prev_o = nullptr;  // the chunk before: where its outputs go, and how many tokens it has
+      int prev_n = 0;
+      const auto outputs = [&](int i) {
+        const Weights &w = m->wt[slot(i)];
+        const bool has_bad = w.has_bad != 0;
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          uint32_t oi[32], ot[32];
+          const uint32_t at = tl + (static_cast<uint32_t>(half * 16) << 16);
+          tmem_ld_16x256b(at + COL_OI + (i & 1) * 64, oi);
+          tmem_ld_16x256b(at + COL_OT, ot);
+          tmem_ld_wait();
+          if (half == 1) {
+            tc_fence_before_sync();
+            arrive_warp(&m->o_free, lane);
+          }
+          const int v0 = quad * 32 + half * 16 + g;
+          const int bad0 = has_bad ? w.bad[v0] : C, bad1 = has_bad ? w.bad[v0 + 8] : C;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int t = 8 * j + 2 * tig;
+            const float2 e = *reinterpret_cast<const float2 *>(&w.eg[t]);
+            float y[4];
+            y[0] = a.q_scale * fmaf(e.x, __uint_as_float(oi[4 * j]), __uint_as_float(ot[4 * j]));
+            y[1] = a.q_scale * fmaf(e.y, __uint_as_float(oi[4 * j + 1]), __uint_as_float(ot[4 * j + 1]));
+            y[2] = a.q_scale * fmaf(e.x, __uint_as_float(oi[4 * j + 2]), __uint_as_float(ot[4 * j + 2]));
+            y[3] = a.q_scale * fmaf(e.y, __uint_as_float(oi[4 * j + 3]), __uint_as_float(ot[4 * j + 3]));
+            if (has_bad) {
+              const float nan = __int_as_float(0x7fffffff);
+              if (t >= bad0) y[0] = nan;
+              if (t + 1 >= bad0) y[1] = nan;
+              if (t >= bad1) y[2] = nan;
+              if (t + 1 >= bad1) y[3] = nan;
+            }
+            if constexpr (sizeof(OT) == 2) {
+              ot[2 * j] = bf16x2(y[0], y[1]);
+              ot[2 * j + 1] = bf16x2(y[2], y[3]);
+            } else {
+              OT *const o = prev_o + v0;
+              if (t < prev_n) {
+                o[t * v_stride] = y[0];
+                o[t * v_stride + 8] = y[2];
+              }
+              if (t + 1 < prev_n) {
+                o[(t + 1) * v_stride] = y[1];
+                o[(t + 1) * v_stride + 8] = y[3];
+              }
+            }
+          }
+          if constexpr (sizeof(OT) == 2) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+              const int t = 8 * (j + (lane >> 4)) + (lane & 7), ch = half * 2 + (lane >> 3 & 1);
+              stmatrix_x4_trans(smem_u32(ost) + t * 64 + ((ch ^ (t >> 1 & 3)) << 4), ot[2 * j], ot[2 * j + 1], ot[2 * j + 2], ot[2 * j + 3]);
+            }
+          }
+        }
+        if constexpr (sizeof(OT) == 2) {
+          __syncwarp();
+#pragma unroll
+          for (int i8 = 0; i8 < 8; ++i8) {
+            const int t = i8 * 8 + (lane >> 2), ch = lane & 3;
+            const uint4 y = *reinterpret_cast<const uint4 *>(ost + t * 64 + ((ch ^ (t >> 1 & 3)) << 4));
+            if (t < prev_n) *reinterpret_cast<uint4 *>(prev_o + t * v_stride + quad * 32 + ch * 8) = y;
+          }
+          __syncwarp();
+        }
+        arrive_warp(&m->dec_empty[slot(i)], lane);
+      };
+      while (walk.next<WITH_O>(a, sp, m, sorted, x)) {
+        OT *const o = static_cast<OT *>(a.o) + (x.tok0 * a.H_v + x.head) * D;
+        for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
+          const Weights &w = m->wt[slot(n)];
+          wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
+          const int t0 = quad * 16 + g, t1 = t0 + 8;
+          const float h0 = w.ghi[t0], l0 = w.glo[t0], h1 = w.ghi[t1], l1 = w.glo[t1];
+          wait_bar(&m->bar_p, n & 1u, m);
+          tc_fence_after_sync();
+          uint32_t p[32], ph[16], pl[16];
+          tmem_ld_16x256b(tl + COL_P, p);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            if (j < 2 * (quad + 1)) {
+              const int i = 8 * j + 2 * tig;
+              const float2 hi = *reinterpret_cast<const float2 *>(&w.ghi[i]), lo = *reinterpret_cast<const float2 *>(&w.glo[i]);
+              const float y0 = i <= t0 ? __uint_as_float(p[4 * j]) * ex2f((h0 - hi.x) + (l0 - lo.x)) : 0.f;
+              const float y1 = i + 1 <= t0 ? __uint_as_float(p[4 * j + 1]) * ex2f((h0 - hi.y) + (l0 - lo.y)) : 0.f;
+              const float y2 = i <= t1 ? __uint_as_float(p[4 * j + 2]) * ex2f((h1 - hi.x) + (l1 - lo.x)) : 0.f;
+              const float y3 = i + 1 <= t1 ? __uint_as_float(p[4 * j + 3]) * ex2f((h1 - hi.y) + (l1 - lo.y)) : 0.f;
+              split2(dpack2(y0, y1), ph[2 * j], pl[2 * j]);
+              split2(dpack2(y2, y3), ph[2 * j + 1], pl[2 * j + 1]);
+            }
+          }
+          if (n > 0) wait_bar(&m->bar_o, (n - 1) & 1u, m);  // PV of the chunk before has read its P
+          tc_fence_after_sync();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            if (j < 2 * (quad + 1)) {
+              const uint32_t o0 = t0 * 128 + ((j ^ (t0 & 7)) << 4) + tig * 4, o1 = o0 + 8 * 128;
+              *reinterpret_cast<uint32_t *>(smem + OFF_PH + o0) = ph[2 * j];
+              *reinterpret_cast<uint32_t *>(smem + OFF_PH + o1) = ph[2 * j + 1];
+              *reinterpret_cast<uint32_t *>(smem + OFF_PL + o0) = pl[2 * j];
+              *reinterpret_cast<uint32_t *>(smem + OFF_PL + o1) = pl[2 * j + 1];
+            }
+          }
+          fence_smem_to_async();
+          tc_fence_before_sync();
+          arrive_warp(&m->p_ready, lane);
+          if (n > 0) outputs(n - 1);
+          prev_o = o + c * C * v_stride;
+          prev_n = x.n - c * C;
+        }
+      }
+      if (n > 0) {
+        wait_bar(&m->bar_o, (n - 1) & 1u, m);
+        tc_fence_after_sync();
+        if (!m->abort_flag) outputs(n - 1);
+      }
+    }
+  } else if (warp < WARP_S) {
+    // ---- Kw ----
+    const int kt = tid - WARP_K * 32;
+    while (walk.next<WITH_O>(a, sp, m, sorted, x)) {
+      for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
+        const uint32_t st = stage(n);
+        const int rows = min(x.n - c * C, C);
+        Weights &w = m->wt[slot(n)];
+        wait_bar(&m->full_v[st], stage_phase(n), m);
+        // V: a value that is none would reach every row of its column through products with weights that are zero.  0 * x + sum is
+        // NaN from the first of them on.
+        unsigned char *const vt = smem + OFF_V + st * TILE + kt * 16;
+        __nv_bfloat162 probe = __floats2bfloat162_rn(0.f, 0.f);
+        const __nv_bfloat162 zero2 = probe;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint4 y = *reinterpret_cast<const uint4 *>(vt + i * 2048);
+          if (rows < C && (kt >> 3) + (i & 3) * 16 >= rows) {  // behind the last token
+            y = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4 *>(vt + i * 2048) = y;
+          }
+          const __nv_bfloat162 *const e = reinterpret_cast<const __nv_bfloat162 *>(&y);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) probe = __hfma2(e[j], zero2, probe);
+        }
+        wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
+        const bool none = __isnan(__low2float(probe)) || __isnan(__high2float(probe));
+        if (any_of<1, 128>(none)) {
+          w.bad[kt] = C;
+          asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i) {
+            const int row = (kt >> 3) + (i & 3) * 16, col = (i >> 2) * 64 + (((kt & 7) ^ (row & 7)) << 3);
+            uint16_t *const e = reinterpret_cast<uint16_t *>(vt + i * 2048);
+            for (int j = 0; j < 8; ++j)
+              if ((e[j] & 0x7F80u) == 0x7F80u) {
+                e[j] = 0;
+                atomicMin(&w.bad[col + j], row);
+              }
+          }
+          if (kt == 0) w.has_bad = 1;
+        } else if (kt == 0) {
+          w.has_bad = 0;
+        }
+        wait_bar(&m->full_k[st], stage_phase(n), m);
+        if (n > 0) wait_bar(&m->bar_d, (n - 1) & 1u, m);  // KV of the chunk before has read its Kw
+        const unsigned char *const kr = smem + OFF_K + st * TILE + kt * 16;
+        unsigned char *const kh = smem + OFF_KH + kt * 16, *const kl = smem + OFF_KL + kt * 16;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int row = (kt >> 3) + (i & 3) * 16;
+          const float f = w.w[row];
+          const uint64_t ff = dpack2(f, f);
+          uint4 y = *reinterpret_cast<const uint4 *>(kr + i * 2048);
+          if (row >= rows) y = make_uint4(0u, 0u, 0u, 0u);
+          uint4 hi, lo;
+          split2(dmul2(dpack2(bf_lo(y.x), bf_hi(y.x)), ff), hi.x, lo.x);
+          split2(dmul2(dpack2(bf_lo(y.y), bf_hi(y.y)), ff), hi.y, lo.y);
+          split2(dmul2(dpack2(bf_lo(y.z), bf_hi(y.z)), ff), hi.z, lo.z);
+          split2(dmul2(dpack2(bf_lo(y.w), bf_hi(y.w)), ff), hi.w, lo.w);
+          *reinterpret_cast<uint4 *>(kh + i * 2048) = hi;
+          *reinterpret_cast<uint4 *>(kl + i * 2048) = lo;
+        }
+        fence_smem_to_async();
+        arrive_warp(&m->k_ready, lane);
+        if (lane == 0) {
+          mbar_arrive(&m->empty_k[st]);
+          mbar_arrive(&m->dec_empty[slot(n)]);
+        }
+      }
+    }
+  } else {
+    // ---- the state ----
+    const int quad = warp & 3, half = (warp - WARP_S) >> 2;
+    const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
+    const int v = quad * 32 + lane, k0 = half * 64;
+    while (walk.next<WITH_O>(a, sp, m, sorted, x)) {
+      uint64_t S[32];
+      const int64_t state = x.state < 0 ? -1 - x.state : x.state;
+      const float *const src = (x.joined ? sp.seg_state + (x.unit * sp.nseg + x.seg) * (D * D) : a.state + state) + k0 * D + v;
+      if (x.joined || !x.zero) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) S[j] = dpack2(src[2 * j * D], src[(2 * j + 1) * D]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) S[j] = 0;
+      }
+      float decay = 1.f;
+      for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
+        const Weights &w = m->wt[slot(n)];
+        if constexpr (WITH_O) {
+          if (n > 0) wait_bar(&m->bar_s, (n - 1) & 1u, m);  // QS of the chunk before has read its state
+          tc_fence_after_sync();
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            uint32_t hi[16], lo[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) split2(S[b * 16 + j], hi[j], lo[j]);
+            tmem_st16(tl + COL_SH + half * 32 + b * 16, hi);
+            tmem_st16(tl + COL_SL + half * 32 + b * 16, lo);
+          }
+          tmem_st_wait();
+          tc_fence_before_sync();
+          arrive_warp(&m->s_ready, lane);
+        }
+        wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
+        const float f = w.all;
+        const uint64_t ff = dpack2(f, f);
+        decay *= f;
+        wait_bar(&m->bar_d, n & 1u, m);
+        tc_fence_after_sync();
+        const bool bad = w.has_bad != 0 && w.bad[v] < C;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          uint32_t d[16];
+          tmem_ld16(tl + COL_D + k0 + b * 16, d);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            S[b * 8 + j] = dfma2(S[b * 8 + j], ff, dpack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
+        }
+        tc_fence_before_sync();
+        arrive_warp(&m->d_free, lane);
+        if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
+        if (bad) {
+          const float nan = __int_as_float(0x7fffffff);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) S[j] = dpack2(nan, nan);
+        }
+      }
+      // a unit is written as a whole or, after a time-out, not at all
+      if (any_of<2, 256>(m->abort_flag != 0)) break;
+      float *dst = nullptr;
+      if (sp.phase == 1) {
+        dst = sp.seg_state + (x.unit * sp.nseg + x.seg + 1) * (D * D);
+        if (warp == WARP_S && lane == 0) sp.seg_decay[x.unit * sp.nseg + x.seg] = decay;
+      } else if (x.state >= 0) {
+        dst = a.state + state;
+      }
+      if (dst) {
+        dst += k0 * D + v;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float2 y = dunpack2(S[j]);
+          dst[2 * j * D] = y.x;
+          dst[(2 * j + 1) * D] = y.y;
+        }
+      }
+    }
+  }
+  stream_order_release();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == WARP_MMA) tmem_dealloc(tm, 512);
+  // every block says how it ended, the first one also for the blocks there are not: nobody has to clear the words beforehand
+  if (tid == 0) sp.status[blockIdx.x] = m->abort_flag;
+  if (blockIdx.x == 0) {
+    for (uint32_t i = gridDim.x + tid; i < kStatusWords; i += NT) sp.status[i] = 0;
+    if (sp.phase == 0)
+      for (uint32_t i = tid; i < kStatusWords; i += NT) sp.status[kStatusWords + i] = 0;
+  }
+}
+
+// States at the starts of a unit's segments: seg_state[unit][0] = its own, [s] = e^{G of segment s-1} [s-1] + what segment s-1 adds
+// (which [s] held).  One thread per four values.
+__global__ void __launch_bounds__(256) decay_join_kernel(const __grid_constant__ DascDecayArgs a, const __grid_constant__ Split sp) {
+  const int64_t unit = blockIdx.x / (D * D / 1024);
+  const int at = (blockIdx.x % (D * D / 1024)) * 1024 + threadIdx.x * 4;
+  const int h = static_cast<int>(unit % a.H_v), lc = static_cast<int>(unit / a.H_v % a.n_layers_in_call);
+  const int r = static_cast<int>(unit / a.H_v / a.n_layers_in_call);
+  stream_order_begin();
+  const int req = a.req_idx[r];
+  if (req < 0) return;
+  const int segs = segments_of(sp, chunks_of(decay_range(a, r).n));
+  if (segs <= 1) return;
+  const bool merge = a.mode == DASC_DECAY_SCRATCH_MERGE_LOCAL;
+  const int layer = a.layer_begin + lc;
+  if (!a.o && (a.mode == DASC_DECAY_SCORE || (merge && a.row_keep[layer * a.rows_per_layer + h * D]))) return;
+  float4 run = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (!merge && !(a.from_zero && a.from_zero[r] != 0))
+    run = *reinterpret_cast<const float4 *>(a.state + req * a.req_stride + layer * a.layer_stride + static_cast<int64_t>(h) * (D * D) + at);
+  float *const seg = sp.seg_state + unit * sp.nseg * (D * D) + at;
+  *reinterpret_cast<float4 *>(seg) = run;
+  for (int s = 1; s < segs; ++s) {
+    const float f = sp.seg_decay[unit * sp.nseg + s - 1];
+    const float4 y = *reinterpret_cast<const float4 *>(seg + static_cast<int64_t>(s) * (D * D));
+    run = make_float4(fmaf(f, run.x, y.x), fmaf(f, run.y, y.y), fmaf(f, run.z, y.z), fmaf(f, run.w, y.w));
+    *reinterpret_cast<float4 *>(seg + static_cast<int64_t>(s) * (D * D)) = run;
+  }
+}
+
+// cuTensorMapEncodeTiled is a driver entry point, looked up through the runtime at first use (no link-time dependency on libcuda).
+using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                   const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn() {
+  static EncodeTiledFn fn = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) p = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+
+// How long requests are split: into as many segments as make the longest chain of chunks on one SM shortest, by the caller's bound on
+// the length.  All but the last segment are then run twice (their states first, without outputs).
+struct SplitSizes {
+  int32_t nseg, seg_chunks;
+};
+SplitSizes split_sizes(int32_t n_req, int32_t layers, int32_t H_v, int64_t total_tokens, int32_t max_seqlen) {
+  const int64_t units = static_cast<int64_t>(n_req) * layers * H_v;
+  const int64_t longest = (std::max<int64_t>(std::min<int64_t>(max_seqlen, total_tokens), 1) + C - 1) / C;
+  SplitSizes best{1, static_cast<int32_t>(longest)};
+  if (units == 0 || units > 2 * kSms || longest < 16) return best;
+  const double even = static_cast<double>(std::min<int64_t>(total_tokens / C + n_req, longest * n_req)) * layers * H_v / longest;  // units as long as the longest
+  double cost = 0;
+  for (int nseg = 1; nseg <= 16 && units * nseg <= 1024 && n_req * nseg <= kMaxSorted; ++nseg) {
+    const int64_t chunks = (longest + nseg - 1) / nseg;
+    if (nseg > 1 && chunks < 4) break;
+    const double rounds = std::max(1.0, static_cast<double>(static_cast<int64_t>((even * nseg + kSms - 1) / kSms)));
+    const double t = rounds * chunks * (nseg > 1 ? 1.6 : 1.0) + (nseg > 1 ? 10.0 : 0.0);
+    if (nseg == 1 || t < cost) {
+      cost = t;
+      best = {nseg, static_cast<int32_t>(chunks)};
+    }
+  }
+  return best;
+}
+
+template <bool WITH_O, typename OT>
+cudaError_t launch(const DascDecayArgs &a, const Split &sp, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, void *stream) {
+  auto kern = decay_chunked_kernel<WITH_O, OT>;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(SMEM_BYTES));
+  if (e != cudaSuccess) return e;
+  const int64_t items = static_cast<int64_t>(a.n_req) * a.n_layers_in_call * a.H_v * sp.nseg;
+  return launch_blocks(kern, dim3(static_cast<unsigned>(std::min<int64_t>(items, kSms))), dim3(NT), SMEM_BYTES, stream, a, sp, q, k, v);
+}
+
+}  // namespace
+
+size_t dasc_decay_chunked_workspace_bytes(int32_t n_req, int32_t n_layers_in_call, int32_t H_v, int64_t total_tokens, int32_t max_seqlen) {
+  const SplitSizes s = split_sizes(n_req, n_layers_in_call, H_v, total_tokens, max_seqlen);
+  size_t bytes = kDecayStatusWords * sizeof(uint32_t);
+  if (s.nseg > 1) {
+    const size_t segs = static_cast<size_t>(n_req) * n_layers_in_call * H_v * s.nseg;
+    bytes += (segs * sizeof(float) + 255) / 256 * 256 + segs * D * D * sizeof(float);
+  }
+  return bytes;
+}
+
+int dasc_launch_decay_chunked(const DascDecayArgs &args, void *stream) {
+  if (args.d_k != D || args.d_v != D || !args.io_bf16) return -1;
+  DascDecayArgs a = args;
+  a.poll_limit_first_wait = __atomic_load_n(&g_dasc_debug_poll_limit, __ATOMIC_RELAXED);
+  CUtensorMap tmap_q{}, tmap_k{}, tmap_v{};
+  const EncodeTiledFn encode = encode_tiled_fn();
+  if (!encode) return static_cast<int>(cudaErrorNotSupported);
+  // the streams [Lc*T tokens][heads][128]: boxes of 64 tokens x one head x 64 channels, 128 bytes, swizzled as the operand tiles are
+  const auto make_map = [&](CUtensorMap *map, const void *base, int heads) {
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(heads),
+                                static_cast<cuuint64_t>(a.n_layers_in_call) * static_cast<cuuint64_t>(a.total_tokens)};
+    const cuuint64_t strides[2] = {D * 2, static_cast<cuuint64_t>(heads) * D * 2};
+    const cuuint32_t box[3] = {64, 1, static_cast<cuuint32_t>(C)}, ones[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  if (!make_map(&tmap_k, a.k, a.H_k) || !make_map(&tmap_v, a.v, a.H_v) || (a.o && !make_map(&tmap_q, a.q, a.H_k)))
+    return static_cast<int>(cudaErrorInvalidValue);
+  const SplitSizes sizes = split_sizes(a.n_req, a.n_layers_in_call, a.H_v, a.total_tokens, a.max_seqlen);
+  uint32_t *const ws = static_cast<uint32_t *>(a.workspace);
+  Split sp{sizes.nseg, sizes.seg_chunks, 0, nullptr, nullptr, ws};
+  cudaError_t e = cudaSuccess;
+  if (sp.nseg > 1) {
+    const int64_t units = static_cast<int64_t>(a.n_req) * a.n_layers_in_call * a.H_v;
+    unsigned char *const p = static_cast<unsigned char *>(a.workspace) + kDecayStatusWords * sizeof(uint32_t);
+    sp.seg_decay = reinterpret_cast<float *>(p);
+    sp.seg_state = reinterpret_cast<float *>(p + (units * sp.nseg * sizeof(float) + 255) / 256 * 256);
+    sp.phase = 1;
+    sp.status = ws + kStatusWords;
+    e = launch<false, __nv_bfloat16>(a, sp, tmap_q, tmap_k, tmap_v, stream);
+    if (e == cudaSuccess)
+      e = launch_blocks(decay_join_kernel, dim3(static_cast<unsigned>(units * (D * D / 1024))), dim3(256), 0, stream, a, sp);
+    sp.phase = 2;
+    sp.status = ws;
+  }
+  if (e != cudaSuccess) return static_cast<int>(e);
+  if (!a.o) return static_cast<int>(launch<false, __nv_bfloat16>(a, sp, tmap_q, tmap_k, tmap_v, stream));
+  return static_cast<int>(a.o_bf16 ? launch<true, __nv_bfloat16>(a, sp, tmap_q, tmap_k, tmap_v, stream)
+                                   : launch<true, float>(a, sp, tmap_q, tmap_k, tmap_v, stream));
+}

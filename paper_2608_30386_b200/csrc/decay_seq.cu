@@ -67,6 +67,8 @@ __global__ void __launch_bounds__(NT, 3) decay_seq_kernel(const __grid_constant_
   else
     stream_order_wait();
 
+  if (!STEP && a.workspace && blockIdx.x == 0)  // nothing here can time out
+    for (int i = tid; i < kDecayStatusWords; i += NT) static_cast<uint32_t *>(a.workspace)[i] = 0;
   const int req = a.req_idx[r];
   if (req < 0) return;
   const DecayRange range = decay_range(a, r);

@@ -257,6 +257,26 @@ __device__ __forceinline__ void mma_ss_bf16(uint32_t d_tmem, uint64_t a_desc, ui
       : "memory");
 }
 
+// The same with a 16-bit operand's M or N index, not K, contiguous in shared memory.
+__host__ __device__ constexpr uint32_t idesc_bf16(uint32_t M, uint32_t N, bool a_mn_major, bool b_mn_major) {
+  return idesc_bf16(M, N) | (uint32_t(a_mn_major) << 15) | (uint32_t(b_mn_major) << 16);
+}
+// MN-major 16-bit operand tiles with the 128-byte swizzle: rows = K index, blocks of 64 elements along M/N, [R rows][128 bytes] each and
+// `block_bytes` apart (LBO); groups of 8 K rows are 1024 bytes apart (SBO).  This is the layout of the K-major tile of the transposed
+// matrix, so one tile serves in both orientations.  `smem_addr` points at the first K row of the slice (a multiple of 8).
+__device__ __forceinline__ uint64_t desc_mn_bf16(uint32_t smem_addr, uint32_t block_bytes) {
+  return kDescSw128 | (uint64_t{(smem_addr & 0x3FFFFu) >> 4}) | (uint64_t{block_bytes >> 4} << 16) | (uint64_t{1024 >> 4} << 32);
+}
+// D[tmem] (+)= A[tmem] * B[smem], bf16; A is M lanes x 8 columns (16 values, two per column) at a_tmem.
+__device__ __forceinline__ void mma_ts_bf16(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(uint32_t(accumulate))
+      : "memory");
+}
+
 // D[tmem] (+)= A[smem] * B[smem]; one K = 8 slice.  Issued by a single thread.
 __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, bool accumulate) {
   asm volatile(
