@@ -19,6 +19,7 @@
 //   3 - 6   P: out of tensor memory, weighted, into its operand tiles; the outputs of the chunk before
 //   7 - 10  Kw; looks at V for values that are none
 //   11 - 18 the state, in fp32 registers: a thread has 64 key channels of one column
+//   19      looks up the units ahead of all others
 // The only chain from chunk to chunk is S <- e^{G_C} S + (KV), 64 packed multiply-adds per thread, and its bf16 pair on the way
 // to QS; KV itself does not depend on the state.
 #include <cuda.h>
@@ -37,8 +38,8 @@ using namespace tc5;
 constexpr int C = 64, D = 128;
 constexpr int kSms = 148;
 constexpr int NS = 3;    // stages of K, Q, V
-constexpr int RING = 4;  // chunks whose weights are kept
-constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_K = 7, WARP_S = 11, NWARP = 19;  // (P: from 3 on)
+constexpr int RING = 4;  // chunks whose weights are kept, and units that are looked up ahead
+constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_K = 7, WARP_S = 11, WARP_ITEM = 19, NWARP = 20;  // (P: from 3 on)
 constexpr int NT = NWARP * 32;
 constexpr int kMaxSorted = 512;  // entries (requests x segments) that are taken longest first
 constexpr uint32_t kMaxPolls = 1u << 22;
@@ -62,9 +63,21 @@ struct Weights {  // of one chunk
   int32_t has_bad;       // V holds values that are none:
   int32_t bad[D];        // the first token with one, per column (C: no such token)
 };
+// The states and tokens of one unit, or of one segment of it.
+struct Item {
+  int64_t state;   // offset of its state in floats
+  int64_t tok0;    // its first token in the streams of the call
+  int32_t unit, seg;
+  int32_t n;       // tokens; negative: there are no more items
+  int32_t head, k_head, lc;
+  int32_t from;    // 0: starts from zero, 1: from its state, 2: from the joined state of its segment
+  int32_t write;   // its state is written back
+};
+
 struct Misc {
+  Item items[RING];
   uint64_t full_k[NS], full_q[NS], full_v[NS], empty_k[NS], empty_q[NS], empty_v[NS];
-  uint64_t dec_full[RING], dec_empty[RING];
+  uint64_t dec_full[RING], dec_empty[RING], item_full[RING], item_empty[RING];
   uint64_t bar_p, bar_s, bar_o, bar_d;           // tensor core: QK, QS, PV, KV of a chunk have completed
   uint64_t p_ready, k_ready, s_ready;            // operands of PV, KV, QS are in place
   uint64_t o_free, d_free;                       // their accumulators have been read
@@ -84,15 +97,6 @@ struct Split {
   float *seg_state;          // [unit][nseg][D][D]
   float *seg_decay;          // [unit][nseg]
   uint32_t *status;          // [kStatusWords] of this launch
-};
-
-// The states and tokens of one unit, or of one segment of it.
-struct Item {
-  int64_t state;   // offset of its state in floats; < 0: nothing to write
-  int64_t tok0;    // its first token in the streams of the call
-  int64_t unit;
-  int32_t n, head, k_head, seg, lc;
-  bool zero, joined;
 };
 
 __device__ __forceinline__ float ex2f(float x) {
@@ -144,7 +148,7 @@ __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 
 __device__ __forceinline__ void split2(uint64_t xy, uint32_t &hi, uint32_t &lo) {
   const float2 v = dunpack2(xy);
   hi = bf16x2(v.x, v.y);
-  const float2 r = dunpack2(dadd2(xy, dpack2(-bf_lo(hi), -bf_hi(hi))));
+  const float2 r = dunpack2(dsub2(xy, dpack2(bf_lo(hi), bf_hi(hi))));
   lo = bf16x2(r.x, r.y);
 }
 __device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
@@ -165,50 +169,41 @@ __device__ __forceinline__ int entry_chunks(const DascDecayArgs &a, const Split 
   return s == segs - 1 ? chunks - s * sp.seg_chunks : sp.seg_chunks;
 }
 
-// This thread block's items, one after the other: every gridDim.x-th, there and back, so that each block gets long and short ones.
-struct Walk {
-  int64_t k = 0;
-  template <bool WITH_O>
-  __device__ __forceinline__ bool next(const DascDecayArgs &a, const Split &sp, const Misc *m, bool sorted, Item &x) {
-    const int64_t per_entry = static_cast<int64_t>(a.n_layers_in_call) * a.H_v, total = per_entry * a.n_req * sp.nseg;
-    for (;; ++k) {
-      const int64_t idx = k * gridDim.x + ((k & 1) ? gridDim.x - 1u - blockIdx.x : blockIdx.x);
-      if (idx >= total) {
-        // (on the way back a block's turn can be behind the end although the next one is not: there is no next one then)
-        return false;
-      }
-      int e = static_cast<int>(idx / per_entry);
-      const int rest = static_cast<int>(idx - e * per_entry);
-      if (sorted) e = m->order[e];
-      const int r = e / sp.nseg, s = e - r * sp.nseg;
-      const int req = a.req_idx[r];
-      if (req < 0) continue;
-      const DecayRange range = decay_range(a, r);
-      const int chunks = chunks_of(range.n), segs = segments_of(sp, chunks);
-      const bool last = s == segs - 1;
-      if (s >= segs || (sp.phase == 1 && last)) continue;
-      x.lc = rest / a.H_v;
-      x.head = rest - x.lc * a.H_v;
-      x.k_head = x.head / (a.H_v / a.H_k);
-      const int layer = a.layer_begin + x.lc;
-      const bool merge = a.mode == DASC_DECAY_SCRATCH_MERGE_LOCAL;
-      const bool write = a.mode != DASC_DECAY_SCORE && !(merge && a.row_keep[layer * a.rows_per_layer + x.head * D]);
-      if (!write && !a.o) continue;
-      x.zero = merge || (a.from_zero && a.from_zero[r] != 0);
-      x.joined = sp.phase == 2 && segs > 1;
-      if (sp.phase == 1) x.zero = true;
-      if (chunks == 0 && !(write && x.zero)) continue;
-      x.seg = s;
-      x.unit = (static_cast<int64_t>(r) * a.n_layers_in_call + x.lc) * a.H_v + x.head;
-      x.tok0 = static_cast<int64_t>(x.lc) * a.total_tokens + range.begin + static_cast<int64_t>(s) * sp.seg_chunks * C;
-      x.n = last ? range.n - s * sp.seg_chunks * C : sp.seg_chunks * C;
-      x.state = req * a.req_stride + layer * a.layer_stride + static_cast<int64_t>(x.head) * (D * D);
-      if (!(last && write)) x.state = -1 - x.state;  // (read, not written)
-      ++k;
-      return true;
-    }
-  }
-};
+// This thread block's k-th item: every gridDim.x-th, there and back, so that each block gets long and short ones.  False: nothing to do
+// there; x.n < 0: there is no such item.
+__device__ __forceinline__ bool item_at(const DascDecayArgs &a, const Split &sp, const Misc *m, bool sorted, uint32_t k, Item &x) {
+  const uint32_t per_entry = static_cast<uint32_t>(a.n_layers_in_call) * a.H_v, total = per_entry * a.n_req * sp.nseg;
+  const uint64_t idx64 = static_cast<uint64_t>(k) * gridDim.x + ((k & 1) ? gridDim.x - 1u - blockIdx.x : blockIdx.x);
+  x.n = -1;
+  if (idx64 >= total) return true;
+  const uint32_t idx = static_cast<uint32_t>(idx64);
+  int e = static_cast<int>(idx / per_entry);
+  const int rest = static_cast<int>(idx - e * per_entry);
+  if (sorted) e = m->order[e];
+  const int r = e / sp.nseg, s = e - r * sp.nseg;
+  const int req = a.req_idx[r];
+  if (req < 0) return false;
+  const DecayRange range = decay_range(a, r);
+  const int chunks = chunks_of(range.n), segs = segments_of(sp, chunks);
+  const bool last = s == segs - 1;
+  if (s >= segs || (sp.phase == 1 && last)) return false;
+  x.lc = rest / a.H_v;
+  x.head = rest - x.lc * a.H_v;
+  x.k_head = x.head / (a.H_v / a.H_k);
+  const int layer = a.layer_begin + x.lc;
+  const bool merge = a.mode == DASC_DECAY_SCRATCH_MERGE_LOCAL;
+  const bool write = a.mode != DASC_DECAY_SCORE && !(merge && a.row_keep[layer * a.rows_per_layer + x.head * D]);
+  const bool zero = merge || (a.from_zero && a.from_zero[r] != 0);
+  if ((!write && !a.o) || (chunks == 0 && !(write && zero))) return false;
+  x.from = sp.phase == 1 ? 0 : sp.phase == 2 && segs > 1 ? 2 : zero ? 0 : 1;
+  x.write = last && write;
+  x.seg = s;
+  x.unit = (r * a.n_layers_in_call + x.lc) * a.H_v + x.head;
+  x.tok0 = static_cast<int64_t>(x.lc) * a.total_tokens + range.begin + static_cast<int64_t>(s) * sp.seg_chunks * C;
+  x.n = last ? range.n - s * sp.seg_chunks * C : sp.seg_chunks * C;
+  x.state = req * a.req_stride + layer * a.layer_stride + static_cast<int64_t>(x.head) * (D * D);
+  return true;
+}
 
 template <bool WITH_O, typename OT>
 __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_constant__ DascDecayArgs a, const __grid_constant__ Split sp,
@@ -231,6 +226,8 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     for (int i = 0; i < RING; ++i) {
       mbar_init(&m->dec_full[i], 1);
       mbar_init(&m->dec_empty[i], WITH_O ? 16 : 12);
+      mbar_init(&m->item_full[i], 1);
+      mbar_init(&m->item_empty[i], WITH_O ? 19 : 15);
     }
     mbar_init(&m->bar_p, 1);
     mbar_init(&m->bar_s, 1);
@@ -273,9 +270,13 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
   tc_fence_after_sync();
   const uint32_t tm = static_cast<uint32_t>(uni(static_cast<int>(m->tmem_base)));
 
-  Walk walk;
-  Item x;
   int n = 0;  // chunks so far: buffers and barrier phases go by it
+  // Item `it` of this block, once it has been looked up; false: there are no more, or a wait has run out.
+  const auto take = [&](int it) {
+    wait_bar(&m->item_full[it % RING], static_cast<uint32_t>(it) / RING & 1u, m);
+    return m->abort_flag == 0 && m->items[it % RING].n >= 0;
+  };
+  const auto release = [&](int it) { arrive_warp(&m->item_empty[it % RING], lane); };
   const auto stage = [](int i) { return static_cast<uint32_t>(i) % NS; };
   const auto stage_phase = [](int i) { return static_cast<uint32_t>(i) / NS & 1u; };
   const auto slot = [](int i) { return static_cast<uint32_t>(i) % RING; };
@@ -285,7 +286,9 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     if (lane == 0) {
       int nk = 0, nq = 0, nv = 0;  // tiles asked for
       bool stop = false;
-      while (!stop && walk.next<WITH_O>(a, sp, m, sorted, x)) {
+      for (int it = 0; !stop && take(it); ++it) {
+        const Item x = m->items[it % RING];
+        mbar_arrive(&m->item_empty[it % RING]);
         for (int c = 0; c < chunks_of(x.n) && !stop; ++c, ++n) {
           const uint32_t st = stage(n), ph = stage_phase(n) ^ 1u;
           const int32_t z = static_cast<int32_t>(x.tok0 + c * C);
@@ -323,20 +326,27 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       tc_fence_after_sync();
       if (gave_up()) return;
       if (elect_one()) {
+        const uint64_t q = desc_kmajor(sbase + OFF_Q + st * TILE), k = desc_kmajor(sbase + OFF_K + st * TILE);
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) {
-          const uint32_t o = st * TILE + (kk >> 2) * BLOCK + (kk & 3) * 32;
-          mma_ss_bf16(tm + COL_P, desc_kmajor(sbase + OFF_Q + o), desc_kmajor(sbase + OFF_K + o), ID_QK, kk != 0);
+          const uint32_t o = (kk >> 2) * BLOCK + (kk & 3) * 32;
+          mma_ss_bf16(tm + COL_P, q + (o >> 4), k + (o >> 4), ID_QK, kk != 0);
         }
         mma_commit(&m->bar_p);
         mma_commit(&m->empty_k[st]);
       }
       __syncwarp();
     };
-    int all = 0;  // chunks of all items: which chunk is the last is known one item ahead
-    bool more = walk.next<WITH_O>(a, sp, m, sorted, x);
-    while (more && chunks_of(x.n) == 0) more = walk.next<WITH_O>(a, sp, m, sorted, x);
-    all = more ? chunks_of(x.n) : 0;
+    int it = 0, all = 0;  // chunks of all items that have been looked up
+    const auto look = [&]() {  // the next item with tokens, if there is one
+      int chunks = 0;
+      while (chunks == 0 && uni(take(it))) {
+        chunks = chunks_of(m->items[it % RING].n);
+        release(it++);
+      }
+      all += chunks;
+    };
+    look();
     // Test hook: a first, short wait for operands that cannot be there yet.
     if (a.poll_limit_first_wait && all > 0) {
       bool done = false;
@@ -345,13 +355,9 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     }
     if (WITH_O && all > 0) qk(0);
     for (; n < all && !gave_up(); ++n) {
-      if (n + 1 == all) {
-        more = walk.next<WITH_O>(a, sp, m, sorted, x);
-        while (more && chunks_of(x.n) == 0) more = walk.next<WITH_O>(a, sp, m, sorted, x);
-        if (more) all += chunks_of(x.n);
-      }
+      if (n + 1 == all) look();
       const uint32_t st = stage(n), par = n & 1u;
-      const uint32_t vb = sbase + OFF_V + st * TILE;
+      const uint64_t vd = desc_mn_bf16(sbase + OFF_V + st * TILE, BLOCK);
       // KV
       wait_bar(&m->k_ready, par, m);
       wait_bar(&m->full_v[st], stage_phase(n), m);
@@ -359,10 +365,11 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       tc_fence_after_sync();
       if (gave_up()) break;
       if (elect_one()) {
+        const uint64_t kw = desc_mn_bf16(sbase + OFF_KH, BLOCK);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const uint32_t s = (i & 3) * 2048;
-          mma_ss_bf16(tm + COL_D, desc_mn_bf16(vb + s, BLOCK), desc_mn_bf16(sbase + (i < 4 ? OFF_KH : OFF_KL) + s, BLOCK), ID_KV, i != 0);
+          mma_ss_bf16(tm + COL_D, vd + (s >> 4), kw + (((i < 4 ? 0 : OFF_KL - OFF_KH) + s) >> 4), ID_KV, i != 0);
         }
         mma_commit(&m->bar_d);
         if (!WITH_O) mma_commit(&m->empty_v[st]);
@@ -374,11 +381,11 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         tc_fence_after_sync();
         if (gave_up()) break;
         if (elect_one()) {
+          const uint64_t q = desc_kmajor(sbase + OFF_Q + st * TILE);
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int kk = i & 7;
-            mma_ts_bf16(tm + COL_OI + par * 64, tm + (i < 8 ? COL_SH : COL_SL) + kk * 8,
-                        desc_kmajor(sbase + OFF_Q + st * TILE + (kk >> 2) * BLOCK + (kk & 3) * 32), ID_QS, i != 0);
+            mma_ts_bf16(tm + COL_OI + par * 64, tm + (i < 8 ? COL_SH : COL_SL) + kk * 8, q + (((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4), ID_QS, i != 0);
           }
           mma_commit(&m->bar_s);
           mma_commit(&m->empty_q[st]);
@@ -390,11 +397,12 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         tc_fence_after_sync();
         if (gave_up()) break;
         if (elect_one()) {
+          const uint64_t p = desc_kmajor(sbase + OFF_PH);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const uint32_t s = i & 3;
-            mma_ss_bf16(tm + COL_OT + 16 * s, desc_mn_bf16(vb + s * 2048, BLOCK),
-                        desc_kmajor(sbase + (i < 4 ? OFF_PH : OFF_PL) + s * 2048 + s * 32), idesc_bf16(128, 64 - 16 * s, true, false), i != 0);
+            mma_ss_bf16(tm + COL_OT + 16 * s, vd + (s * 2048 >> 4), p + (((i < 4 ? 0 : OFF_PL - OFF_PH) + s * 2048 + s * 32) >> 4),
+                        idesc_bf16(128, 64 - 16 * s, true, false), i != 0);
           }
           mma_commit(&m->bar_o);
           mma_commit(&m->empty_v[st]);
@@ -409,7 +417,9 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(&m->drain, 0); ++p) {
     }
   } else if (warp == WARP_DECAY) {
-    while (walk.next<WITH_O>(a, sp, m, sorted, x)) {
+    for (int it = 0; uni(take(it)); ++it) {
+      const Item x = m->items[it % RING];
+      release(it);
       const float *const g = a.g_per_head ? a.g + x.lc * a.H_v + x.head : a.g + x.tok0 * a.H_v + x.head;
       const int64_t stride = a.g_per_head ? 0 : a.H_v;
       const auto fetch = [&](int c, float (&y)[2]) {
@@ -530,16 +540,26 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         }
         arrive_warp(&m->dec_empty[slot(i)], lane);
       };
-      while (walk.next<WITH_O>(a, sp, m, sorted, x)) {
-        OT *const o = static_cast<OT *>(a.o) + (x.tok0 * a.H_v + x.head) * D;
-        for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
+      OT *o = nullptr;
+      int it = 0, left = 0;  // tokens left of the item
+      for (;; ++n) {
+        bool more = left > 0;
+        while (!more && uni(take(it))) {
+          const Item &x = m->items[it % RING];
+          o = static_cast<OT *>(a.o) + (x.tok0 * a.H_v + x.head) * D;
+          left = x.n;
+          more = left > 0;
+          release(it++);
+        }
+        uint32_t ph[16], pl[16];
+        const int t0 = quad * 16 + g, t1 = t0 + 8;
+        if (more) {
           const Weights &w = m->wt[slot(n)];
           wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-          const int t0 = quad * 16 + g, t1 = t0 + 8;
           const float h0 = w.ghi[t0], l0 = w.glo[t0], h1 = w.ghi[t1], l1 = w.glo[t1];
           wait_bar(&m->bar_p, n & 1u, m);
           tc_fence_after_sync();
-          uint32_t p[32], ph[16], pl[16];
+          uint32_t p[32];
           tmem_ld_16x256b(tl + COL_P, p);
           tmem_ld_wait();
 #pragma unroll
@@ -555,8 +575,10 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
               split2(dpack2(y2, y3), ph[2 * j + 1], pl[2 * j + 1]);
             }
           }
-          if (n > 0) wait_bar(&m->bar_o, (n - 1) & 1u, m);  // PV of the chunk before has read its P
-          tc_fence_after_sync();
+        }
+        if (n > 0) wait_bar(&m->bar_o, (n - 1) & 1u, m);  // PV of the chunk before has read its P
+        tc_fence_after_sync();
+        if (more) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             if (j < 2 * (quad + 1)) {
@@ -570,24 +592,25 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           fence_smem_to_async();
           tc_fence_before_sync();
           arrive_warp(&m->p_ready, lane);
-          if (n > 0) outputs(n - 1);
-          prev_o = o + c * C * v_stride;
-          prev_n = x.n - c * C;
         }
-      }
-      if (n > 0) {
-        wait_bar(&m->bar_o, (n - 1) & 1u, m);
-        tc_fence_after_sync();
-        if (!m->abort_flag) outputs(n - 1);
+        if (n > 0 && !uni(m->abort_flag)) outputs(n - 1);
+        if (!more) break;
+        prev_o = o;
+        prev_n = left;
+        o += C * v_stride;
+        left -= C;
       }
     }
   } else if (warp < WARP_S) {
     // ---- Kw ----
     const int kt = tid - WARP_K * 32;
-    while (walk.next<WITH_O>(a, sp, m, sorted, x)) {
-      for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
+    for (int it = 0;; ++it) {
+      if (any_of<1, 128>(!take(it))) break;  // (one answer for all four warps)
+      const int tokens = m->items[it % RING].n;
+      release(it);
+      for (int c = 0; c < chunks_of(tokens); ++c, ++n) {
         const uint32_t st = stage(n);
-        const int rows = min(x.n - c * C, C);
+        const int rows = min(tokens - c * C, C);
         Weights &w = m->wt[slot(n)];
         wait_bar(&m->full_v[st], stage_phase(n), m);
         // V: a value that is none would reach every row of its column through products with weights that are zero.  0 * x + sum is
@@ -615,6 +638,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           for (int i = 0; i < 8; ++i) {
             const int row = (kt >> 3) + (i & 3) * 16, col = (i >> 2) * 64 + (((kt & 7) ^ (row & 7)) << 3);
             uint16_t *const e = reinterpret_cast<uint16_t *>(vt + i * 2048);
+#pragma unroll 1
             for (int j = 0; j < 8; ++j)
               if ((e[j] & 0x7F80u) == 0x7F80u) {
                 e[j] = 0;
@@ -629,7 +653,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         if (n > 0) wait_bar(&m->bar_d, (n - 1) & 1u, m);  // KV of the chunk before has read its Kw
         const unsigned char *const kr = smem + OFF_K + st * TILE + kt * 16;
         unsigned char *const kh = smem + OFF_KH + kt * 16, *const kl = smem + OFF_KL + kt * 16;
-#pragma unroll
+#pragma unroll 2
         for (int i = 0; i < 8; ++i) {
           const int row = (kt >> 3) + (i & 3) * 16;
           const float f = w.w[row];
@@ -652,16 +676,19 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         }
       }
     }
-  } else {
+  } else if (warp < WARP_ITEM) {
     // ---- the state ----
     const int quad = warp & 3, half = (warp - WARP_S) >> 2;
     const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
     const int v = quad * 32 + lane, k0 = half * 64;
-    while (walk.next<WITH_O>(a, sp, m, sorted, x)) {
+    for (int it = 0;; ++it) {
+      if (any_of<2, 256>(!take(it))) break;  // (one answer for all eight warps)
+      const Item x = m->items[it % RING];
+      release(it);
       uint64_t S[32];
-      const int64_t state = x.state < 0 ? -1 - x.state : x.state;
-      const float *const src = (x.joined ? sp.seg_state + (x.unit * sp.nseg + x.seg) * (D * D) : a.state + state) + k0 * D + v;
-      if (x.joined || !x.zero) {
+      const int64_t seg_at = (static_cast<int64_t>(x.unit) * sp.nseg + x.seg) * (D * D);
+      const float *const src = (x.from == 2 ? sp.seg_state + seg_at : a.state + x.state) + k0 * D + v;
+      if (x.from != 0) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) S[j] = dpack2(src[2 * j * D], src[(2 * j + 1) * D]);
       } else {
@@ -675,12 +702,12 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           if (n > 0) wait_bar(&m->bar_s, (n - 1) & 1u, m);  // QS of the chunk before has read its state
           tc_fence_after_sync();
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            uint32_t hi[16], lo[16];
+          for (int b = 0; b < 4; ++b) {
+            uint32_t hi[8], lo[8];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) split2(S[b * 16 + j], hi[j], lo[j]);
-            tmem_st16(tl + COL_SH + half * 32 + b * 16, hi);
-            tmem_st16(tl + COL_SL + half * 32 + b * 16, lo);
+            for (int j = 0; j < 8; ++j) split2(S[b * 8 + j], hi[j], lo[j]);
+            tmem_st8(tl + COL_SH + half * 32 + b * 8, hi);
+            tmem_st8(tl + COL_SL + half * 32 + b * 8, lo);
           }
           tmem_st_wait();
           tc_fence_before_sync();
@@ -715,10 +742,10 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       if (any_of<2, 256>(m->abort_flag != 0)) break;
       float *dst = nullptr;
       if (sp.phase == 1) {
-        dst = sp.seg_state + (x.unit * sp.nseg + x.seg + 1) * (D * D);
-        if (warp == WARP_S && lane == 0) sp.seg_decay[x.unit * sp.nseg + x.seg] = decay;
-      } else if (x.state >= 0) {
-        dst = a.state + state;
+        dst = sp.seg_state + seg_at + D * D;
+        if (warp == WARP_S && lane == 0) sp.seg_decay[static_cast<int64_t>(x.unit) * sp.nseg + x.seg] = decay;
+      } else if (x.write) {
+        dst = a.state + x.state;
       }
       if (dst) {
         dst += k0 * D + v;
@@ -729,6 +756,18 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           dst[(2 * j + 1) * D] = y.y;
         }
       }
+    }
+  }
+  if (warp == WARP_ITEM) {
+    int it = 0;
+    for (uint32_t k = 0; m->abort_flag == 0; ++k) {
+      Item x;
+      if (!item_at(a, sp, m, sorted, k, x)) continue;
+      if (it >= RING) wait_bar(&m->item_empty[it % RING], (static_cast<uint32_t>(it) / RING & 1u) ^ 1u, m);
+      if (lane == 0) m->items[it % RING] = x;
+      arrive_warp(&m->item_full[it % RING], lane);
+      ++it;
+      if (x.n < 0) break;
     }
   }
   stream_order_release();
