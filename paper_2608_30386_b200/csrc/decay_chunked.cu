@@ -16,10 +16,11 @@
 //   0       TMA: tiles of K, Q, V, three chunks ahead
 //   1       issues the products
 //   2       sums of log-decays (in 64 bits), weights of a chunk
-//   3 - 6   P: out of tensor memory, weighted, into its operand tiles; the outputs of the chunk before
-//   7 - 10  Kw; looks at V for values that are none
-//   11 - 18 the state, in fp32 registers: a thread has 64 key channels of one column
-//   19      looks up the units ahead of all others
+//   3       looks up the units ahead of all others
+//   4 - 7   P: out of tensor memory, weighted, into its operand tiles
+//   8 - 11  outputs
+//   12 - 15 Kw; looks at V for values that are none
+//   16 - 23 the state, in fp32 registers: a thread has 64 key channels of one column
 // The only chain from chunk to chunk is S <- e^{G_C} S + (KV), 64 packed multiply-adds per thread, and its bf16 pair on the way
 // to QS; KV itself does not depend on the state.
 #include <cuda.h>
@@ -39,7 +40,11 @@ constexpr int C = 64, D = 128;
 constexpr int kSms = 148;
 constexpr int NS = 3;    // stages of K, Q, V
 constexpr int RING = 4;  // chunks whose weights are kept, and units that are looked up ahead
-constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_K = 7, WARP_S = 11, WARP_ITEM = 19, NWARP = 20;  // (P: from 3 on)
+constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_P = 4, WARP_O = 8, WARP_K = 12, WARP_S = 16, NWARP = 24;
+// Registers of a thread, by groups of four warps: what the launch gives each (65,536 over all threads, in steps of 8), and how the roles
+// share it out.
+constexpr int REGS = 80, REGS_0 = 40, REGS_P = 80, REGS_O = 80, REGS_K = 72, REGS_S = 104;
+static_assert(NWARP * 32 * REGS <= 65536 && REGS_0 + REGS_P + REGS_O + REGS_K + 2 * REGS_S <= NWARP / 4 * REGS);
 constexpr int NT = NWARP * 32;
 constexpr int kMaxSorted = 512;  // entries (requests x segments) that are taken longest first
 constexpr uint32_t kMaxPolls = 1u << 22;
@@ -58,7 +63,11 @@ constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 
 struct Weights {  // of one chunk
   float ghi[C], glo[C];  // G_t = ghi + glo, ghi a multiple of 2^-6: differences of ghi are exact
   float w[C];            // e^{G_C - G_i}; 0 behind the last token
-  float eg[C];           // e^{G_t}
+  float eg[C];           // q_scale e^{G_t}
+  // P's weights outside its diagonal blocks of 16 x 16 are products: with B the last token before t's block, e^{G_t - G_B} times
+  // e^{G_B - G_i}, neither above 1
+  float row[C];          // q_scale e^{G_t - G_B}
+  float col[3][3 * 16];  // e^{G_B - G_i}, B = 15, 31, 47
   float all;             // e^{G_C}
   int32_t has_bad;       // V holds values that are none:
   int32_t bad[D];        // the first token with one, per column (C: no such token)
@@ -111,15 +120,24 @@ __device__ __forceinline__ void arrive_warp(uint64_t *bar, int lane) {
   __syncwarp();
   if (lane == 0) mbar_arrive(bar);
 }
-// Bounded wait; once one has run out, no wait of this thread block lasts longer than one poll.
+// Bounded wait; once one has run out, no wait of this thread block lasts longer than one poll.  Written as the smallest loop there is: it is
+// inlined at some thirty places, and the roles' code together has to stay within reach of the instruction caches.
 __device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, Misc *m) {
-  for (uint32_t i = 0; !mbar_try_wait(bar, parity); ++i) {
-    if (m->abort_flag) return;
-    if (i == kMaxPolls) {
-      m->abort_flag = 1;
-      return;
-    }
-  }
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b32 n, f;\n\t"
+      "mov.b32 n, 0;\n"
+      "POLL:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%0], %1;\n\t"
+      "@p bra DONE;\n\t"
+      "ld.volatile.shared.b32 f, [%2];\n\t"
+      "add.u32 n, n, 1;\n\t"
+      "setp.ne.b32 q, n, %3;\n\t"
+      "setp.eq.and.b32 p, f, 0, q;\n\t"
+      "@p bra POLL;\n\t"
+      "st.volatile.shared.b32 [%2], 1;\n"
+      "DONE:\n\t}" ::"r"(smem_u32(bar)),
+      "r"(parity), "r"(smem_u32(const_cast<uint32_t *>(&m->abort_flag))), "n"(kMaxPolls)
+      : "memory");
 }
 __device__ __forceinline__ int uni(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 // Barrier of `n` threads: does the predicate hold for any of them?
@@ -154,6 +172,11 @@ __device__ __forceinline__ void split2(uint64_t xy, uint32_t &hi, uint32_t &lo) 
 __device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
 }
+
+template <int N>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 __device__ __forceinline__ int chunks_of(int n) { return (n + C - 1) / C; }
 // Segments that a request of `chunks` chunks really has.
@@ -225,9 +248,9 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     }
     for (int i = 0; i < RING; ++i) {
       mbar_init(&m->dec_full[i], 1);
-      mbar_init(&m->dec_empty[i], WITH_O ? 16 : 12);
+      mbar_init(&m->dec_empty[i], WITH_O ? 20 : 12);
       mbar_init(&m->item_full[i], 1);
-      mbar_init(&m->item_empty[i], WITH_O ? 19 : 15);
+      mbar_init(&m->item_empty[i], WITH_O ? 23 : 15);
     }
     mbar_init(&m->bar_p, 1);
     mbar_init(&m->bar_s, 1);
@@ -256,6 +279,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     for (int e = tid; e < entries; e += NT) {
       const int own = key[e];
       int rank = 0;
+#pragma unroll 1
       for (int j = 0; j < entries; j += 4) {
         const int4 o = *reinterpret_cast<const int4 *>(key + j);
         rank += (o.x > own || (o.x == own && j < e)) + (o.y > own || (o.y == own && j + 1 < e)) + (o.z > own || (o.z == own && j + 2 < e)) +
@@ -282,13 +306,17 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
   const auto slot = [](int i) { return static_cast<uint32_t>(i) % RING; };
   const auto slot_phase = [](int i) { return static_cast<uint32_t>(i) / RING & 1u; };
 
+  if (warp < WARP_P) {
+    regs_down<REGS_0>();
   if (warp == WARP_TMA) {
     if (lane == 0) {
       int nk = 0, nq = 0, nv = 0;  // tiles asked for
       bool stop = false;
+#pragma unroll 1
       for (int it = 0; !stop && take(it); ++it) {
         const Item x = m->items[it % RING];
         mbar_arrive(&m->item_empty[it % RING]);
+#pragma unroll 1
         for (int c = 0; c < chunks_of(x.n) && !stop; ++c, ++n) {
           const uint32_t st = stage(n), ph = stage_phase(n) ^ 1u;
           const int32_t z = static_cast<int32_t>(x.tok0 + c * C);
@@ -309,6 +337,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       // Copies in flight land before the block ends, whoever has given up waiting for them.
       const auto land = [&](uint64_t *full, int count) {
         for (int i = max(count - NS, 0); i < count; ++i)
+#pragma unroll 1
           for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(&full[stage(i)], stage_phase(i)); ++p) {
           }
       };
@@ -354,6 +383,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       if (!done) m->abort_flag = 1;
     }
     if (WITH_O && all > 0) qk(0);
+#pragma unroll 1
     for (; n < all && !gave_up(); ++n) {
       if (n + 1 == all) look();
       const uint32_t st = stage(n), par = n & 1u;
@@ -393,6 +423,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         __syncwarp();
         // PV: tokens 16 s ... 16 s + 15 reach the rows from 16 s on
         wait_bar(&m->p_ready, par, m);
+        if (n + 1 < all) qk(n + 1);  // (its accumulator has been read; the next P is waited for longest)
         if (n > 0) wait_bar(&m->o_free, par ^ 1u, m);
         tc_fence_after_sync();
         if (gave_up()) break;
@@ -408,15 +439,16 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           mma_commit(&m->empty_v[st]);
         }
         __syncwarp();
-        if (n + 1 < all) qk(n + 1);
       }
     }
     // products in flight end before their memory is given back, whoever has given up waiting for them
     if (elect_one()) mma_commit(&m->drain);
     __syncwarp();
+#pragma unroll 1
     for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(&m->drain, 0); ++p) {
     }
   } else if (warp == WARP_DECAY) {
+#pragma unroll 1
     for (int it = 0; uni(take(it)); ++it) {
       const Item x = m->items[it % RING];
       release(it);
@@ -431,6 +463,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       };
       float cur[2], nxt[2];
       fetch(0, cur);
+#pragma unroll 1
       for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
         fetch(c + 1, nxt);
         if (n >= RING) wait_bar(&m->dec_empty[slot(n)], slot_phase(n) ^ 1u, m);
@@ -448,15 +481,27 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         const double total = __shfl_sync(0xffffffffu, incl, 31);
         double run = __shfl_up_sync(0xffffffffu, incl, 1);
         if (lane == 0) run = 0.0;
+        // sums up to tokens 15, 31, 47
+        double B[3];
+#pragma unroll
+        for (int b = 0; b < 3; ++b) B[b] = __shfl_sync(0xffffffffu, incl, 8 * b + 7);
+        const int block = lane >> 3;
+        const double before = block == 0 ? 0.0 : block == 1 ? B[0] : block == 2 ? B[1] : B[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           run += G[j];
           const int t = 2 * lane + j;
           const float hi = static_cast<float>(rint(run * 64.0) * (1.0 / 64.0));
-          w.ghi[t] = hi;
-          w.glo[t] = static_cast<float>(run - static_cast<double>(hi));
           w.w[t] = c * C + t < x.n ? ex2f(static_cast<float>(total - run)) : 0.f;
-          w.eg[t] = ex2f(static_cast<float>(run));
+          if (WITH_O) {
+            w.ghi[t] = hi;
+            w.glo[t] = static_cast<float>(run - static_cast<double>(hi));
+            w.eg[t] = a.q_scale * ex2f(static_cast<float>(run));
+            w.row[t] = a.q_scale * ex2f(static_cast<float>(run - before));
+#pragma unroll
+            for (int b = 0; b < 3; ++b)
+              if (block <= b) w.col[b][t] = ex2f(static_cast<float>(B[b] - run));
+          }
         }
         if (lane == 0) w.all = ex2f(static_cast<float>(total));
         arrive_warp(&m->dec_full[slot(n)], lane);
@@ -464,150 +509,178 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         cur[1] = nxt[1];
       }
     }
-  } else if (warp < WARP_K) {
-    // ---- P, and the outputs of the chunk before ----
+  } else {
+    int it = 0;
+#pragma unroll 1
+    for (uint32_t k = 0; m->abort_flag == 0; ++k) {
+      Item x;
+      if (!item_at(a, sp, m, sorted, k, x)) continue;
+      if (it >= RING) wait_bar(&m->item_empty[it % RING], (static_cast<uint32_t>(it) / RING & 1u) ^ 1u, m);
+      if (lane == 0) m->items[it % RING] = x;
+      arrive_warp(&m->item_full[it % RING], lane);
+      ++it;
+      if (x.n < 0) break;
+    }
+  }
+  } else if (warp < WARP_O) {
+    // ---- P ----
     if constexpr (WITH_O) {
       const int quad = warp & 3, g = lane >> 2, tig = lane & 3;
-      const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
-      const int64_t v_stride = static_cast<int64_t>(a.H_v) * D;
-      unsigned char *const ost = smem + OFF_O + quad * 4096;
-      OT *prev_o = nullptr;  // the chunk before: where its outputs go, and how many tokens it has
-      int prev_n = 0;
-      const auto outputs = [&](int i) {
-        const Weights &w = m->wt[slot(i)];
-        const bool has_bad = w.has_bad != 0;
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          uint32_t oi[32], ot[32];
-          const uint32_t at = tl + (static_cast<uint32_t>(half * 16) << 16);
-          tmem_ld_16x256b(at + COL_OI + (i & 1) * 64, oi);
-          tmem_ld_16x256b(at + COL_OT, ot);
-          tmem_ld_wait();
-          if (half == 1) {
-            tc_fence_before_sync();
-            arrive_warp(&m->o_free, lane);
-          }
-          const int v0 = quad * 32 + half * 16 + g;
-          const int bad0 = has_bad ? w.bad[v0] : C, bad1 = has_bad ? w.bad[v0 + 8] : C;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int t = 8 * j + 2 * tig;
-            const float2 e = *reinterpret_cast<const float2 *>(&w.eg[t]);
-            float y[4];
-            y[0] = a.q_scale * fmaf(e.x, __uint_as_float(oi[4 * j]), __uint_as_float(ot[4 * j]));
-            y[1] = a.q_scale * fmaf(e.y, __uint_as_float(oi[4 * j + 1]), __uint_as_float(ot[4 * j + 1]));
-            y[2] = a.q_scale * fmaf(e.x, __uint_as_float(oi[4 * j + 2]), __uint_as_float(ot[4 * j + 2]));
-            y[3] = a.q_scale * fmaf(e.y, __uint_as_float(oi[4 * j + 3]), __uint_as_float(ot[4 * j + 3]));
-            if (has_bad) {
-              const float nan = __int_as_float(0x7fffffff);
-              if (t >= bad0) y[0] = nan;
-              if (t + 1 >= bad0) y[1] = nan;
-              if (t >= bad1) y[2] = nan;
-              if (t + 1 >= bad1) y[3] = nan;
-            }
-            if constexpr (sizeof(OT) == 2) {
-              ot[2 * j] = bf16x2(y[0], y[1]);
-              ot[2 * j + 1] = bf16x2(y[2], y[3]);
-            } else {
-              OT *const o = prev_o + v0;
-              if (t < prev_n) {
-                o[t * v_stride] = y[0];
-                o[t * v_stride + 8] = y[2];
-              }
-              if (t + 1 < prev_n) {
-                o[(t + 1) * v_stride] = y[1];
-                o[(t + 1) * v_stride + 8] = y[3];
-              }
-            }
-          }
-          if constexpr (sizeof(OT) == 2) {
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-              const int t = 8 * (j + (lane >> 4)) + (lane & 7), ch = half * 2 + (lane >> 3 & 1);
-              stmatrix_x4_trans(smem_u32(ost) + t * 64 + ((ch ^ (t >> 1 & 3)) << 4), ot[2 * j], ot[2 * j + 1], ot[2 * j + 2], ot[2 * j + 3]);
-            }
-          }
-        }
-        if constexpr (sizeof(OT) == 2) {
-          __syncwarp();
-#pragma unroll
-          for (int i8 = 0; i8 < 8; ++i8) {
-            const int t = i8 * 8 + (lane >> 2), ch = lane & 3;
-            const uint4 y = *reinterpret_cast<const uint4 *>(ost + t * 64 + ((ch ^ (t >> 1 & 3)) << 4));
-            if (t < prev_n) *reinterpret_cast<uint4 *>(prev_o + t * v_stride + quad * 32 + ch * 8) = y;
-          }
-          __syncwarp();
-        }
-        arrive_warp(&m->dec_empty[slot(i)], lane);
+      const uint32_t tp = tm + (static_cast<uint32_t>(quad * 32) << 16) + COL_P;
+      const int t0 = quad * 16 + g, t1 = t0 + 8;  // this thread's rows; columns 16 s + 2 tig, + 1, + 8, + 9
+      unsigned char *const ps = smem + OFF_PH + t0 * 128 + tig * 4;
+      const auto put = [&](int j, uint64_t y0, uint64_t y1) {  // columns 8 j + 2 tig, + 1
+        uint32_t hi, lo;
+        unsigned char *const p = ps + ((j ^ (t0 & 7)) << 4);
+        split2(y0, hi, lo);
+        *reinterpret_cast<uint32_t *>(p) = hi;
+        *reinterpret_cast<uint32_t *>(p + (OFF_PL - OFF_PH)) = lo;
+        split2(y1, hi, lo);
+        *reinterpret_cast<uint32_t *>(p + 8 * 128) = hi;
+        *reinterpret_cast<uint32_t *>(p + 8 * 128 + (OFF_PL - OFF_PH)) = lo;
       };
-      OT *o = nullptr;
-      int it = 0, left = 0;  // tokens left of the item
-      for (;; ++n) {
-        bool more = left > 0;
-        while (!more && uni(take(it))) {
-          const Item &x = m->items[it % RING];
-          o = static_cast<OT *>(a.o) + (x.tok0 * a.H_v + x.head) * D;
-          left = x.n;
-          more = left > 0;
-          release(it++);
-        }
-        uint32_t ph[16], pl[16];
-        const int t0 = quad * 16 + g, t1 = t0 + 8;
-        if (more) {
+      const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
+#pragma unroll 1
+      for (int it = 0; uni(take(it)); ++it) {
+        const int tokens = m->items[it % RING].n;
+        release(it);
+#pragma unroll 1
+        for (int c = 0; c < chunks_of(tokens); ++c, ++n) {
           const Weights &w = m->wt[slot(n)];
           wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-          const float h0 = w.ghi[t0], l0 = w.glo[t0], h1 = w.ghi[t1], l1 = w.glo[t1];
           wait_bar(&m->bar_p, n & 1u, m);
+          if (n > 0) wait_bar(&m->bar_o, (n - 1) & 1u, m);  // PV of the chunk before has read its P
           tc_fence_after_sync();
-          uint32_t p[32];
-          tmem_ld_16x256b(tl + COL_P, p);
-          tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            if (j < 2 * (quad + 1)) {
-              const int i = 8 * j + 2 * tig;
-              const float2 hi = *reinterpret_cast<const float2 *>(&w.ghi[i]), lo = *reinterpret_cast<const float2 *>(&w.glo[i]);
-              const float y0 = i <= t0 ? __uint_as_float(p[4 * j]) * ex2f((h0 - hi.x) + (l0 - lo.x)) : 0.f;
-              const float y1 = i + 1 <= t0 ? __uint_as_float(p[4 * j + 1]) * ex2f((h0 - hi.y) + (l0 - lo.y)) : 0.f;
-              const float y2 = i <= t1 ? __uint_as_float(p[4 * j + 2]) * ex2f((h1 - hi.x) + (l1 - lo.x)) : 0.f;
-              const float y3 = i + 1 <= t1 ? __uint_as_float(p[4 * j + 3]) * ex2f((h1 - hi.y) + (l1 - lo.y)) : 0.f;
-              split2(dpack2(y0, y1), ph[2 * j], pl[2 * j]);
-              split2(dpack2(y2, y3), ph[2 * j + 1], pl[2 * j + 1]);
-            }
+          const float r0 = w.row[t0], r1 = w.row[t1];
+          const uint64_t rr0 = dpack2(r0, r0), rr1 = dpack2(r1, r1);
+          const float *const col = w.col[quad > 0 ? quad - 1 : 0] + 2 * tig;
+#pragma unroll 1
+          for (int s = 0; s < quad; ++s) {
+            uint32_t p[8];
+            tmem_ld_16x256b(tp + 16 * s, p);
+            const uint64_t c0 = *reinterpret_cast<const uint64_t *>(col + 16 * s), c1 = *reinterpret_cast<const uint64_t *>(col + 16 * s + 8);
+            tmem_ld_wait();
+            put(2 * s, dmul2(pair(p[0], p[1]), dmul2(rr0, c0)), dmul2(pair(p[2], p[3]), dmul2(rr1, c0)));
+            put(2 * s + 1, dmul2(pair(p[4], p[5]), dmul2(rr0, c1)), dmul2(pair(p[6], p[7]), dmul2(rr1, c1)));
           }
-        }
-        if (n > 0) wait_bar(&m->bar_o, (n - 1) & 1u, m);  // PV of the chunk before has read its P
-        tc_fence_after_sync();
-        if (more) {
+          {
+            uint32_t p[8];
+            tmem_ld_16x256b(tp + 16 * quad, p);
+            const float h0 = w.ghi[t0], l0 = w.glo[t0], h1 = w.ghi[t1], l1 = w.glo[t1];
+            tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            if (j < 2 * (quad + 1)) {
-              const uint32_t o0 = t0 * 128 + ((j ^ (t0 & 7)) << 4) + tig * 4, o1 = o0 + 8 * 128;
-              *reinterpret_cast<uint32_t *>(smem + OFF_PH + o0) = ph[2 * j];
-              *reinterpret_cast<uint32_t *>(smem + OFF_PH + o1) = ph[2 * j + 1];
-              *reinterpret_cast<uint32_t *>(smem + OFF_PL + o0) = pl[2 * j];
-              *reinterpret_cast<uint32_t *>(smem + OFF_PL + o1) = pl[2 * j + 1];
+            for (int b = 0; b < 2; ++b) {
+              const int i = 16 * quad + 8 * b + 2 * tig;
+              const float2 hi = *reinterpret_cast<const float2 *>(&w.ghi[i]), lo = *reinterpret_cast<const float2 *>(&w.glo[i]);
+              const auto at = [&](int e, int t, int col, float ht, float lt, float hi_i, float lo_i) {
+                return col <= t ? __uint_as_float(p[4 * b + e]) * (a.q_scale * ex2f((ht - hi_i) + (lt - lo_i))) : 0.f;
+              };
+              put(2 * quad + b, dpack2(at(0, t0, i, h0, l0, hi.x, lo.x), at(1, t0, i + 1, h0, l0, hi.y, lo.y)),
+                  dpack2(at(2, t1, i, h1, l1, hi.x, lo.x), at(3, t1, i + 1, h1, l1, hi.y, lo.y)));
             }
           }
           fence_smem_to_async();
           tc_fence_before_sync();
           arrive_warp(&m->p_ready, lane);
+          if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
         }
-        if (n > 0 && !uni(m->abort_flag)) outputs(n - 1);
-        if (!more) break;
-        prev_o = o;
-        prev_n = left;
-        o += C * v_stride;
-        left -= C;
+      }
+    }
+  } else if (warp < WARP_K) {
+    // ---- outputs ----
+    if constexpr (WITH_O) {
+      const int quad = warp & 3, g = lane >> 2, tig = lane & 3;
+      const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
+      const int64_t v_stride = static_cast<int64_t>(a.H_v) * D;
+      unsigned char *const ost = smem + OFF_O + quad * 4096;
+#pragma unroll 1
+      for (int it = 0; uni(take(it)); ++it) {
+        const int tokens = m->items[it % RING].n;
+        OT *o = static_cast<OT *>(a.o) + (m->items[it % RING].tok0 * a.H_v + m->items[it % RING].head) * D + quad * 32;
+        release(it);
+#pragma unroll 1
+        for (int c = 0; c < chunks_of(tokens); ++c, ++n, o += C * v_stride) {
+          const Weights &w = m->wt[slot(n)];
+          const int rows = tokens - c * C;
+          wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
+          wait_bar(&m->bar_o, n & 1u, m);
+          tc_fence_after_sync();
+          const bool has_bad = w.has_bad != 0;
+#pragma unroll 1
+          for (int part = 0; part < 4; ++part) {  // 16 columns of d_v (part & 1), 32 tokens (part >> 1)
+            const int half = part & 1, tb = part >> 1;
+            uint32_t oi[16], ot[16];
+            const uint32_t at = tl + (static_cast<uint32_t>(half * 16) << 16) + tb * 32;
+            tmem_ld_16x256b(at + COL_OI + (n & 1) * 64, oi);
+            tmem_ld_16x256b(at + COL_OT, ot);
+            tmem_ld_wait();
+            if (part == 3) {
+              tc_fence_before_sync();
+              arrive_warp(&m->o_free, lane);
+            }
+            const int v0 = half * 16 + g;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int t = tb * 32 + 8 * j + 2 * tig;
+              const uint64_t e = *reinterpret_cast<const uint64_t *>(&w.eg[t]);
+              const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
+              float2 y0 = dunpack2(dfma2(e, pair(oi[4 * j], oi[4 * j + 1]), pair(ot[4 * j], ot[4 * j + 1])));
+              float2 y1 = dunpack2(dfma2(e, pair(oi[4 * j + 2], oi[4 * j + 3]), pair(ot[4 * j + 2], ot[4 * j + 3])));
+              if (has_bad) {
+                const float nan = __int_as_float(0x7fffffff);
+                const int bad0 = w.bad[quad * 32 + v0], bad1 = w.bad[quad * 32 + v0 + 8];
+                if (t >= bad0) y0.x = nan;
+                if (t + 1 >= bad0) y0.y = nan;
+                if (t >= bad1) y1.x = nan;
+                if (t + 1 >= bad1) y1.y = nan;
+              }
+              if constexpr (sizeof(OT) == 2) {
+                ot[2 * j] = bf16x2(y0.x, y0.y);
+                ot[2 * j + 1] = bf16x2(y1.x, y1.y);
+              } else {
+                OT *const p = o + t * v_stride + v0;
+                if (t < rows) {
+                  p[0] = y0.x;
+                  p[8] = y1.x;
+                }
+                if (t + 1 < rows) {
+                  p[v_stride] = y0.y;
+                  p[v_stride + 8] = y1.y;
+                }
+              }
+            }
+            if constexpr (sizeof(OT) == 2) {
+#pragma unroll
+              for (int j = 0; j < 4; j += 2) {
+                const int t = tb * 32 + 8 * (j + (lane >> 4)) + (lane & 7), ch = half * 2 + (lane >> 3 & 1);
+                stmatrix_x4_trans(smem_u32(ost) + t * 64 + ((ch ^ (t >> 1 & 3)) << 4), ot[2 * j], ot[2 * j + 1], ot[2 * j + 2], ot[2 * j + 3]);
+              }
+            }
+          }
+          if constexpr (sizeof(OT) == 2) {
+            __syncwarp();
+#pragma unroll
+            for (int i8 = 0; i8 < 8; ++i8) {
+              const int t = i8 * 8 + (lane >> 2), ch = lane & 3;
+              const uint4 y = *reinterpret_cast<const uint4 *>(ost + t * 64 + ((ch ^ (t >> 1 & 3)) << 4));
+              if (t < rows) *reinterpret_cast<uint4 *>(o + t * v_stride + ch * 8) = y;
+            }
+            __syncwarp();
+          }
+          arrive_warp(&m->dec_empty[slot(n)], lane);
+        }
       }
     }
   } else if (warp < WARP_S) {
     // ---- Kw ----
+    regs_down<REGS_K>();
     const int kt = tid - WARP_K * 32;
+#pragma unroll 1
     for (int it = 0;; ++it) {
       if (any_of<1, 128>(!take(it))) break;  // (one answer for all four warps)
       const int tokens = m->items[it % RING].n;
       release(it);
+#pragma unroll 1
       for (int c = 0; c < chunks_of(tokens); ++c, ++n) {
         const uint32_t st = stage(n);
         const int rows = min(tokens - c * C, C);
@@ -676,11 +749,13 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         }
       }
     }
-  } else if (warp < WARP_ITEM) {
+  } else {
     // ---- the state ----
+    regs_up<REGS_S>();
     const int quad = warp & 3, half = (warp - WARP_S) >> 2;
     const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
     const int v = quad * 32 + lane, k0 = half * 64;
+#pragma unroll 1
     for (int it = 0;; ++it) {
       if (any_of<2, 256>(!take(it))) break;  // (one answer for all eight warps)
       const Item x = m->items[it % RING];
@@ -696,6 +771,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         for (int j = 0; j < 32; ++j) S[j] = 0;
       }
       float decay = 1.f;
+#pragma unroll 1
       for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
         const Weights &w = m->wt[slot(n)];
         if constexpr (WITH_O) {
@@ -756,18 +832,6 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           dst[(2 * j + 1) * D] = y.y;
         }
       }
-    }
-  }
-  if (warp == WARP_ITEM) {
-    int it = 0;
-    for (uint32_t k = 0; m->abort_flag == 0; ++k) {
-      Item x;
-      if (!item_at(a, sp, m, sorted, k, x)) continue;
-      if (it >= RING) wait_bar(&m->item_empty[it % RING], (static_cast<uint32_t>(it) / RING & 1u) ^ 1u, m);
-      if (lane == 0) m->items[it % RING] = x;
-      arrive_warp(&m->item_full[it % RING], lane);
-      ++it;
-      if (x.n < 0) break;
     }
   }
   stream_order_release();
