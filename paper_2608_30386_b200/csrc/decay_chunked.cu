@@ -13,10 +13,9 @@
 // to bf16 once would cost the fp32 state its last 16 bits and as much of the outputs as their own rounding does.
 //
 // One thread block per SM walks over (request, layer, head) units, or over segments of long ones; roles of its warps:
-//   0       TMA: tiles of K, Q, V, three chunks ahead
-//   1       issues the products
-//   2       sums of log-decays (in 64 bits), weights of a chunk
-//   3       looks up the units ahead of all others
+//   0       looks up the units; TMA: tiles of K, Q, V, three chunks ahead
+//   1, 3    issue the products: KV; QK, QS and PV (issue alone, at 60 to 100 cycles a product, filled one warp's time)
+//   2       sums of log-decays (as pairs of fp32), weights of a chunk
 //   4 - 7   P: out of tensor memory, weighted, into its operand tiles
 //   8 - 11  outputs
 //   12 - 15 Kw; looks at V for values that are none
@@ -40,10 +39,10 @@ constexpr int C = 64, D = 128;
 constexpr int kSms = 148;
 constexpr int NS = 3;    // stages of K, Q, V
 constexpr int RING = 4;  // chunks whose weights are kept, and units that are looked up ahead
-constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_P = 4, WARP_O = 8, WARP_K = 12, WARP_S = 16, NWARP = 24;
+constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_MMA_O = 3, WARP_P = 4, WARP_O = 8, WARP_K = 12, WARP_S = 16, NWARP = 24;
 // Registers of a thread, by groups of four warps: what the launch gives each (65,536 over all threads, in steps of 8), and how the roles
 // share it out.
-constexpr int REGS = 80, REGS_0 = 40, REGS_P = 80, REGS_O = 80, REGS_K = 72, REGS_S = 104;
+constexpr int REGS = 80, REGS_0 = 56, REGS_P = 72, REGS_O = 72, REGS_K = 72, REGS_S = 104;
 static_assert(NWARP * 32 * REGS <= 65536 && REGS_0 + REGS_P + REGS_O + REGS_K + 2 * REGS_S <= NWARP / 4 * REGS);
 constexpr int NT = NWARP * 32;
 constexpr int kMaxSorted = 512;  // entries (requests x segments) that are taken longest first
@@ -85,12 +84,12 @@ struct Item {
 
 struct Misc {
   Item items[RING];
-  uint64_t full_k[NS], full_q[NS], full_v[NS], empty_k[NS], empty_q[NS], empty_v[NS];
+  uint64_t full_k[NS], full_q[NS], full_v[NS], empty_k[NS], empty_q[NS], empty_v[NS], v_ready[NS];
   uint64_t dec_full[RING], dec_empty[RING], item_full[RING], item_empty[RING];
   uint64_t bar_p, bar_s, bar_o, bar_d;           // tensor core: QK, QS, PV, KV of a chunk have completed
   uint64_t p_ready, k_ready, s_ready;            // operands of PV, KV, QS are in place
   uint64_t o_free, d_free;                       // their accumulators have been read
-  uint64_t drain;
+  uint64_t drain[2];
   uint32_t tmem_base;
   volatile uint32_t abort_flag;
   Weights wt[RING];
@@ -242,15 +241,16 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       mbar_init(&m->full_k[i], 1);
       mbar_init(&m->full_q[i], 1);
       mbar_init(&m->full_v[i], 1);
+      mbar_init(&m->v_ready[i], 4);
       mbar_init(&m->empty_k[i], WITH_O ? 5 : 4);  // Kw's warps; QK
       mbar_init(&m->empty_q[i], 1);
-      mbar_init(&m->empty_v[i], 1);
+      mbar_init(&m->empty_v[i], WITH_O ? 2 : 1);  // KV; PV
     }
     for (int i = 0; i < RING; ++i) {
       mbar_init(&m->dec_full[i], 1);
       mbar_init(&m->dec_empty[i], WITH_O ? 20 : 12);
       mbar_init(&m->item_full[i], 1);
-      mbar_init(&m->item_empty[i], WITH_O ? 23 : 15);
+      mbar_init(&m->item_empty[i], WITH_O ? 23 : 14);
     }
     mbar_init(&m->bar_p, 1);
     mbar_init(&m->bar_s, 1);
@@ -261,7 +261,8 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     mbar_init(&m->s_ready, 8);
     mbar_init(&m->o_free, 4);
     mbar_init(&m->d_free, 8);
-    mbar_init(&m->drain, 1);
+    mbar_init(&m->drain[0], 1);
+    mbar_init(&m->drain[1], 1);
     m->abort_flag = 0;
     fence_mbar_init();
   }
@@ -308,31 +309,60 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
 
   if (warp < WARP_P) {
     regs_down<REGS_0>();
-  if (warp == WARP_TMA) {
-    if (lane == 0) {
+    if (warp == WARP_TMA) {
+      // The next item is looked up, and its state brought into L2, behind the first loads of this one.
       int nk = 0, nq = 0, nv = 0;  // tiles asked for
       bool stop = false;
+      uint32_t k = 0;
+      int it = 0;
+      const auto publish = [&]() {
+        Item x;
+        while (!item_at(a, sp, m, sorted, k++, x)) {
+        }
+        if (it >= RING) wait_bar(&m->item_empty[it % RING], (static_cast<uint32_t>(it) / RING & 1u) ^ 1u, m);
+        if (lane == 0) m->items[it % RING] = x;
+        if (x.n >= 0 && x.from != 0 && lane < 4) {
+          const float *const src = x.from == 2 ? sp.seg_state + (static_cast<int64_t>(x.unit) * sp.nseg + x.seg) * (D * D) : a.state + x.state;
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + lane * (D * D / 4)), "n"(D * D) : "memory");
+        }
+        arrive_warp(&m->item_full[it % RING], lane);
+        ++it;
+        return x;
+      };
+      Item x, next;
+      bool ask = true;
+      int c = 0, chunks = 0;
 #pragma unroll 1
-      for (int it = 0; !stop && take(it); ++it) {
-        const Item x = m->items[it % RING];
-        mbar_arrive(&m->item_empty[it % RING]);
-#pragma unroll 1
-        for (int c = 0; c < chunks_of(x.n) && !stop; ++c, ++n) {
-          const uint32_t st = stage(n), ph = stage_phase(n) ^ 1u;
-          const int32_t z = static_cast<int32_t>(x.tok0 + c * C);
-          const auto load = [&](uint64_t *empty, uint64_t *full, uint32_t off, const CUtensorMap *map, int head, int &count) {
-            if (n >= NS) wait_bar(&empty[st], ph, m);
-            stop |= m->abort_flag != 0;
-            if (stop) return;
+      for (;;) {
+        if (ask) next = publish();
+        ask = false;
+        if (c == chunks) {
+          x = next;
+          if (x.n < 0) break;
+          chunks = chunks_of(x.n);
+          c = 0;
+          ask = true;
+          if (chunks == 0) continue;
+        }
+        const uint32_t st = stage(n), ph = stage_phase(n) ^ 1u;
+        const int32_t z = static_cast<int32_t>(x.tok0 + c * C);
+        const auto load = [&](uint64_t *empty, uint64_t *full, uint32_t off, const CUtensorMap *map, int head, int &count) {
+          if (n >= NS) wait_bar(&empty[st], ph, m);
+          stop |= uni(m->abort_flag) != 0;
+          if (stop) return;
+          if (lane == 0) {
             mbar_expect_tx(&full[st], TILE);
             tma_load_3d(sbase + off + st * TILE, map, 0, head, z, &full[st]);
             tma_load_3d(sbase + off + st * TILE + BLOCK, map, 64, head, z, &full[st]);
-            ++count;
-          };
-          load(m->empty_k, m->full_k, OFF_K, &tmap_k, x.k_head, nk);
-          if (WITH_O) load(m->empty_q, m->full_q, OFF_Q, &tmap_q, x.k_head, nq);
-          load(m->empty_v, m->full_v, OFF_V, &tmap_v, x.head, nv);
-        }
+          }
+          ++count;
+        };
+        load(m->empty_k, m->full_k, OFF_K, &tmap_k, x.k_head, nk);
+        if (WITH_O) load(m->empty_q, m->full_q, OFF_Q, &tmap_q, x.k_head, nq);
+        load(m->empty_v, m->full_v, OFF_V, &tmap_v, x.head, nv);
+        if (stop) break;
+        ++c;
+        ++n;
       }
       // Copies in flight land before the block ends, whoever has given up waiting for them.
       const auto land = [&](uint64_t *full, int count) {
@@ -344,109 +374,129 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       land(m->full_k, nk);
       land(m->full_q, nq);
       land(m->full_v, nv);
-    }
-  } else if (warp == WARP_MMA) {
-    constexpr uint32_t ID_QK = idesc_bf16(64, 64), ID_QS = idesc_bf16(128, 64), ID_KV = idesc_bf16(128, 128, true, true);
-    const auto gave_up = [&]() { return uni(m->abort_flag) != 0; };  // (one answer for the whole warp)
-    const auto qk = [&](int i) {
-      const uint32_t st = stage(i);
-      wait_bar(&m->full_k[st], stage_phase(i), m);
-      wait_bar(&m->full_q[st], stage_phase(i), m);
-      tc_fence_after_sync();
-      if (gave_up()) return;
-      if (elect_one()) {
-        const uint64_t q = desc_kmajor(sbase + OFF_Q + st * TILE), k = desc_kmajor(sbase + OFF_K + st * TILE);
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-          const uint32_t o = (kk >> 2) * BLOCK + (kk & 3) * 32;
-          mma_ss_bf16(tm + COL_P, q + (o >> 4), k + (o >> 4), ID_QK, kk != 0);
+    } else if (warp == WARP_MMA || warp == WARP_MMA_O) {
+      const auto gave_up = [&]() { return uni(m->abort_flag) != 0; };  // (one answer for the whole warp)
+      int it = 0, all = 0;  // chunks of all items that have been looked up
+      const auto look = [&]() {  // the next item with tokens, if there is one
+        int chunks = 0;
+        while (chunks == 0 && uni(take(it))) {
+          chunks = chunks_of(m->items[it % RING].n);
+          release(it++);
         }
-        mma_commit(&m->bar_p);
-        mma_commit(&m->empty_k[st]);
-      }
-      __syncwarp();
-    };
-    int it = 0, all = 0;  // chunks of all items that have been looked up
-    const auto look = [&]() {  // the next item with tokens, if there is one
-      int chunks = 0;
-      while (chunks == 0 && uni(take(it))) {
-        chunks = chunks_of(m->items[it % RING].n);
-        release(it++);
-      }
-      all += chunks;
-    };
-    look();
-    // Test hook: a first, short wait for operands that cannot be there yet.
-    if (a.poll_limit_first_wait && all > 0) {
-      bool done = false;
-      for (uint32_t i = 0; i < a.poll_limit_first_wait && !done; ++i) done = mbar_test_wait(&m->k_ready, 0);
-      if (!done) m->abort_flag = 1;
-    }
-    if (WITH_O && all > 0) qk(0);
+        all += chunks;
+      };
+      if (warp == WARP_MMA) {
+        constexpr uint32_t ID_KV = idesc_bf16(128, 128, true, true);
+        look();
+        // Test hook: a first, short wait for operands that cannot be there yet.
+        if (a.poll_limit_first_wait && all > 0) {
+          bool done = false;
+          for (uint32_t i = 0; i < a.poll_limit_first_wait && !done; ++i) done = mbar_test_wait(&m->k_ready, 0);
+          if (!done) m->abort_flag = 1;
+        }
 #pragma unroll 1
-    for (; n < all && !gave_up(); ++n) {
-      if (n + 1 == all) look();
-      const uint32_t st = stage(n), par = n & 1u;
-      const uint64_t vd = desc_mn_bf16(sbase + OFF_V + st * TILE, BLOCK);
-      // KV
-      wait_bar(&m->k_ready, par, m);
-      wait_bar(&m->full_v[st], stage_phase(n), m);
-      if (n > 0) wait_bar(&m->d_free, par ^ 1u, m);
-      tc_fence_after_sync();
-      if (gave_up()) break;
-      if (elect_one()) {
-        const uint64_t kw = desc_mn_bf16(sbase + OFF_KH, BLOCK);
+        for (; n < all && !gave_up(); ++n) {
+          if (n + 1 == all) look();
+          const uint32_t st = stage(n), par = n & 1u;
+          wait_bar(&m->k_ready, par, m);
+          wait_bar(&m->full_v[st], stage_phase(n), m);
+          if (n > 0) wait_bar(&m->d_free, par ^ 1u, m);
+          tc_fence_after_sync();
+          if (gave_up()) break;
+          if (elect_one()) {
+            const uint32_t v = desc_lo_mn(sbase + OFF_V, BLOCK) + st * (TILE >> 4), kw = desc_lo_mn(sbase + OFF_KH, BLOCK);
+            mma16_ss<false>(tm + COL_D, v, kw, ID_KV);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t s = (i & 3) * 2048;
-          mma_ss_bf16(tm + COL_D, vd + (s >> 4), kw + (((i < 4 ? 0 : OFF_KL - OFF_KH) + s) >> 4), ID_KV, i != 0);
-        }
-        mma_commit(&m->bar_d);
-        if (!WITH_O) mma_commit(&m->empty_v[st]);
-      }
-      __syncwarp();
-      if (WITH_O) {
-        // QS
-        wait_bar(&m->s_ready, par, m);
-        tc_fence_after_sync();
-        if (gave_up()) break;
-        if (elect_one()) {
-          const uint64_t q = desc_kmajor(sbase + OFF_Q + st * TILE);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int kk = i & 7;
-            mma_ts_bf16(tm + COL_OI + par * 64, tm + (i < 8 ? COL_SH : COL_SL) + kk * 8, q + (((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4), ID_QS, i != 0);
+            for (int i = 1; i < 8; ++i) {
+              const uint32_t s = (i & 3) * 2048;
+              mma16_ss<true>(tm + COL_D, v + (s >> 4), kw + (((i < 4 ? 0 : OFF_KL - OFF_KH) + s) >> 4), ID_KV);
+            }
+            mma_commit(&m->bar_d);
+            mma_commit(&m->empty_v[st]);
           }
-          mma_commit(&m->bar_s);
-          mma_commit(&m->empty_q[st]);
+          __syncwarp();
         }
-        __syncwarp();
-        // PV: tokens 16 s ... 16 s + 15 reach the rows from 16 s on
-        wait_bar(&m->p_ready, par, m);
-        if (n + 1 < all) qk(n + 1);  // (its accumulator has been read; the next P is waited for longest)
-        if (n > 0) wait_bar(&m->o_free, par ^ 1u, m);
-        tc_fence_after_sync();
-        if (gave_up()) break;
-        if (elect_one()) {
-          const uint64_t p = desc_kmajor(sbase + OFF_PH);
+      } else if constexpr (WITH_O) {
+        constexpr uint32_t ID_QK = idesc_bf16(64, 64), ID_QS = idesc_bf16(128, 64);
+        const auto qk = [&](int i) {
+          const uint32_t st = stage(i);
+          wait_bar(&m->full_k[st], stage_phase(i), m);
+          wait_bar(&m->full_q[st], stage_phase(i), m);
+          tc_fence_after_sync();
+          if (gave_up()) return;
+          if (elect_one()) {
+            const uint32_t q = desc_lo_k(sbase + OFF_Q) + st * (TILE >> 4), k = desc_lo_k(sbase + OFF_K) + st * (TILE >> 4);
+            mma16_ss<false>(tm + COL_P, q, k, ID_QK);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t s = i & 3;
-            mma_ss_bf16(tm + COL_OT + 16 * s, vd + (s * 2048 >> 4), p + (((i < 4 ? 0 : OFF_PL - OFF_PH) + s * 2048 + s * 32) >> 4),
-                        idesc_bf16(128, 64 - 16 * s, true, false), i != 0);
+            for (int kk = 1; kk < 8; ++kk) {
+              const uint32_t o = ((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4;
+              mma16_ss<true>(tm + COL_P, q + o, k + o, ID_QK);
+            }
+            mma_commit(&m->bar_p);
+            mma_commit(&m->empty_k[st]);
           }
-          mma_commit(&m->bar_o);
-          mma_commit(&m->empty_v[st]);
-        }
-        __syncwarp();
-      }
-    }
-    // products in flight end before their memory is given back, whoever has given up waiting for them
-    if (elect_one()) mma_commit(&m->drain);
-    __syncwarp();
+          __syncwarp();
+        };
+        look();
+        bool first = true;
 #pragma unroll 1
-    for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(&m->drain, 0); ++p) {
-    }
+        for (n = -1; n < all && !gave_up(); ++n) {
+          if (n + 1 == all) look();
+          const uint32_t st = stage(n), par = n & 1u;
+          if (!first) {
+            // QS
+            wait_bar(&m->s_ready, par, m);
+            wait_bar(&m->full_q[st], stage_phase(n), m);
+            tc_fence_after_sync();
+            if (gave_up()) break;
+            if (elect_one()) {
+              const uint32_t q = desc_lo_k(sbase + OFF_Q) + st * (TILE >> 4);
+              const uint32_t d = tm + COL_OI + par * 64;
+              mma16_ts<false>(d, tm + COL_SH, q, ID_QS);
+#pragma unroll
+              for (int i = 1; i < 16; ++i) {
+                const int kk = i & 7;
+                mma16_ts<true>(d, tm + (i < 8 ? COL_SH : COL_SL) + kk * 8, q + (((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4), ID_QS);
+              }
+              mma_commit(&m->bar_s);
+              mma_commit(&m->empty_q[st]);
+            }
+            __syncwarp();
+            wait_bar(&m->p_ready, par, m);
+          }
+          // the next chunk's QK ahead of this one's PV: its accumulator has been read, and the next P is waited for longest
+          if (n + 1 < all) qk(n + 1);
+          if (!first) {
+            // PV: tokens 16 s ... 16 s + 15 reach the rows from 16 s on
+            wait_bar(&m->full_v[st], stage_phase(n), m);
+            wait_bar(&m->v_ready[st], stage_phase(n), m);
+            if (n > 0) wait_bar(&m->o_free, par ^ 1u, m);
+            tc_fence_after_sync();
+            if (gave_up()) break;
+            if (elect_one()) {
+              const uint32_t v = desc_lo_mn(sbase + OFF_V, BLOCK) + st * (TILE >> 4), p = desc_lo_k(sbase + OFF_PH);
+              mma16_ss<false>(tm + COL_OT, v, p, idesc_bf16(128, 64, true, false));
+#pragma unroll
+              for (int i = 1; i < 8; ++i) {
+                const uint32_t s = i & 3;
+                mma16_ss<true>(tm + COL_OT + 16 * s, v + (s * 2048 >> 4), p + (((i < 4 ? 0 : OFF_PL - OFF_PH) + s * 2048 + s * 32) >> 4),
+                               idesc_bf16(128, 64 - 16 * s, true, false));
+              }
+              mma_commit(&m->bar_o);
+              mma_commit(&m->empty_v[st]);
+            }
+            __syncwarp();
+          }
+          first = false;
+        }
+      }
+      // products in flight end before their memory is given back, whoever has given up waiting for them
+      uint64_t *const drain = &m->drain[warp == WARP_MMA ? 0 : 1];
+      if (elect_one()) mma_commit(drain);
+      __syncwarp();
+#pragma unroll 1
+      for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(drain, 0); ++p) {
+      }
   } else if (warp == WARP_DECAY) {
 #pragma unroll 1
     for (int it = 0; uni(take(it)); ++it) {
@@ -468,62 +518,62 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         fetch(c + 1, nxt);
         if (n >= RING) wait_bar(&m->dec_empty[slot(n)], slot_phase(n) ^ 1u, m);
         Weights &w = m->wt[slot(n)];
-        // log-decays below -10^4 forget everything; clamped, so that their sums stay where 64 bits are exact enough and none is infinite
-        double G[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) G[j] = static_cast<double>(cur[j] < -1e4f ? -1e4f : cur[j]) * 1.4426950408889634;
-        double incl = G[0] + G[1];
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const double y = __shfl_up_sync(0xffffffffu, incl, d);
-          if (lane >= d) incl += y;
-        }
-        const double total = __shfl_sync(0xffffffffu, incl, 31);
-        double run = __shfl_up_sync(0xffffffffu, incl, 1);
-        if (lane == 0) run = 0.0;
-        // sums up to tokens 15, 31, 47
-        double B[3];
-#pragma unroll
-        for (int b = 0; b < 3; ++b) B[b] = __shfl_sync(0xffffffffu, incl, 8 * b + 7);
-        const int block = lane >> 3;
-        const double before = block == 0 ? 0.0 : block == 1 ? B[0] : block == 2 ? B[1] : B[2];
+        // Log-decays in log2 units as pairs: hi a multiple of 2^-6, so that sums of 64 and their differences are exact (below -2048 a
+        // token forgets everything, and is clamped there), lo the rest, at most 2^-7 each.
+        float hi[2], lo[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          run += G[j];
-          const int t = 2 * lane + j;
-          const float hi = static_cast<float>(rint(run * 64.0) * (1.0 / 64.0));
-          w.w[t] = c * C + t < x.n ? ex2f(static_cast<float>(total - run)) : 0.f;
-          if (WITH_O) {
-            w.ghi[t] = hi;
-            w.glo[t] = static_cast<float>(run - static_cast<double>(hi));
-            w.eg[t] = a.q_scale * ex2f(static_cast<float>(run));
-            w.row[t] = a.q_scale * ex2f(static_cast<float>(run - before));
+          constexpr float L = 1.4426950408889634f, L_LO = static_cast<float>(1.4426950408889634 - static_cast<double>(L));
+          const float x = cur[j] < -1400.f ? -1400.f : cur[j];
+          const float p = x * L;
+          hi[j] = rintf(p * 64.f) * (1.f / 64.f);
+          lo[j] = (p - hi[j]) + fmaf(x, L, -p) + x * L_LO;
+        }
+        float sum_hi = hi[0] + hi[1], sum_lo = lo[0] + lo[1];
 #pragma unroll
-            for (int b = 0; b < 3; ++b)
-              if (block <= b) w.col[b][t] = ex2f(static_cast<float>(B[b] - run));
+        for (int d = 1; d < 32; d <<= 1) {
+          const float y = __shfl_up_sync(0xffffffffu, sum_hi, d), z = __shfl_up_sync(0xffffffffu, sum_lo, d);
+          if (lane >= d) {
+            sum_hi += y;
+            sum_lo += z;
           }
         }
-        if (lane == 0) w.all = ex2f(static_cast<float>(total));
+        const auto sum_at = [&](int l, float &h, float &l_) {  // up to lane l's second token
+          h = __shfl_sync(0xffffffffu, sum_hi, l);
+          l_ = __shfl_sync(0xffffffffu, sum_lo, l);
+        };
+        float all_hi, all_lo;
+        sum_at(31, all_hi, all_lo);
+        // this lane's tokens: sums up to the first and up to the second
+        const float gh[2] = {sum_hi - hi[1], sum_hi}, gl[2] = {sum_lo - lo[1], sum_lo};
+        const bool in[2] = {c * C + 2 * lane < x.n, c * C + 2 * lane + 1 < x.n};
+        const auto two = [](float *at, float x, float y) { *reinterpret_cast<float2 *>(at) = make_float2(x, y); };
+        two(&w.w[2 * lane], in[0] ? ex2f((all_hi - gh[0]) + (all_lo - gl[0])) : 0.f, in[1] ? ex2f((all_hi - gh[1]) + (all_lo - gl[1])) : 0.f);
+        if (WITH_O) {
+          two(&w.ghi[2 * lane], gh[0], gh[1]);
+          two(&w.glo[2 * lane], gl[0], gl[1]);
+          two(&w.eg[2 * lane], a.q_scale * ex2f(gh[0] + gl[0]), a.q_scale * ex2f(gh[1] + gl[1]));
+          const int block = lane >> 3;
+          float bh = 0.f, bl = 0.f;
+#pragma unroll
+          for (int b = 0; b < 3; ++b) {
+            float h, l;
+            sum_at(8 * b + 7, h, l);
+            if (block == b + 1) bh = h, bl = l;
+            if (block <= b) two(&w.col[b][2 * lane], ex2f((h - gh[0]) + (l - gl[0])), ex2f((h - gh[1]) + (l - gl[1])));
+          }
+          two(&w.row[2 * lane], a.q_scale * ex2f((gh[0] - bh) + (gl[0] - bl)), a.q_scale * ex2f((gh[1] - bh) + (gl[1] - bl)));
+        }
+        if (lane == 0) w.all = ex2f(all_hi + all_lo);
         arrive_warp(&m->dec_full[slot(n)], lane);
         cur[0] = nxt[0];
         cur[1] = nxt[1];
       }
     }
-  } else {
-    int it = 0;
-#pragma unroll 1
-    for (uint32_t k = 0; m->abort_flag == 0; ++k) {
-      Item x;
-      if (!item_at(a, sp, m, sorted, k, x)) continue;
-      if (it >= RING) wait_bar(&m->item_empty[it % RING], (static_cast<uint32_t>(it) / RING & 1u) ^ 1u, m);
-      if (lane == 0) m->items[it % RING] = x;
-      arrive_warp(&m->item_full[it % RING], lane);
-      ++it;
-      if (x.n < 0) break;
-    }
   }
   } else if (warp < WARP_O) {
     // ---- P ----
+    regs_down<REGS_P>();
     if constexpr (WITH_O) {
       const int quad = warp & 3, g = lane >> 2, tig = lane & 3;
       const uint32_t tp = tm + (static_cast<uint32_t>(quad * 32) << 16) + COL_P;
@@ -588,6 +638,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     }
   } else if (warp < WARP_K) {
     // ---- outputs ----
+    regs_down<REGS_O>();
     if constexpr (WITH_O) {
       const int quad = warp & 3, g = lane >> 2, tig = lane & 3;
       const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
@@ -626,14 +677,6 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
               const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
               float2 y0 = dunpack2(dfma2(e, pair(oi[4 * j], oi[4 * j + 1]), pair(ot[4 * j], ot[4 * j + 1])));
               float2 y1 = dunpack2(dfma2(e, pair(oi[4 * j + 2], oi[4 * j + 3]), pair(ot[4 * j + 2], ot[4 * j + 3])));
-              if (has_bad) {
-                const float nan = __int_as_float(0x7fffffff);
-                const int bad0 = w.bad[quad * 32 + v0], bad1 = w.bad[quad * 32 + v0 + 8];
-                if (t >= bad0) y0.x = nan;
-                if (t + 1 >= bad0) y0.y = nan;
-                if (t >= bad1) y1.x = nan;
-                if (t + 1 >= bad1) y1.y = nan;
-              }
               if constexpr (sizeof(OT) == 2) {
                 ot[2 * j] = bf16x2(y0.x, y0.y);
                 ot[2 * j + 1] = bf16x2(y1.x, y1.y);
@@ -657,9 +700,20 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
               }
             }
           }
-          if constexpr (sizeof(OT) == 2) {
+          __syncwarp();
+          if (has_bad) {  // a lane per column
+            const OT nan = static_cast<OT>(__int_as_float(0x7fffffff));
+#pragma unroll 1
+            for (int t = w.bad[quad * 32 + lane]; t < rows && t < C; ++t) {
+              if constexpr (sizeof(OT) == 2)
+                *reinterpret_cast<OT *>(ost + t * 64 + ((lane >> 3 ^ (t >> 1 & 3)) << 4) + (lane & 7) * 2) = nan;
+              else
+                o[t * v_stride + lane] = nan;
+            }
             __syncwarp();
-#pragma unroll
+          }
+          if constexpr (sizeof(OT) == 2) {
+#pragma unroll 2
             for (int i8 = 0; i8 < 8; ++i8) {
               const int t = i8 * 8 + (lane >> 2), ch = lane & 3;
               const uint4 y = *reinterpret_cast<const uint4 *>(ost + t * 64 + ((ch ^ (t >> 1 & 3)) << 4));
@@ -722,6 +776,8 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         } else if (kt == 0) {
           w.has_bad = 0;
         }
+        fence_smem_to_async();
+        arrive_warp(&m->v_ready[st], lane);
         wait_bar(&m->full_k[st], stage_phase(n), m);
         if (n > 0) wait_bar(&m->bar_d, (n - 1) & 1u, m);  // KV of the chunk before has read its Kw
         const unsigned char *const kr = smem + OFF_K + st * TILE + kt * 16;
@@ -790,12 +846,12 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           arrive_warp(&m->s_ready, lane);
         }
         wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-        const float f = w.all;
-        const uint64_t ff = dpack2(f, f);
+        float f = w.all;
         decay *= f;
         wait_bar(&m->bar_d, n & 1u, m);
         tc_fence_after_sync();
-        const bool bad = w.has_bad != 0 && w.bad[v] < C;
+        if (w.has_bad != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
+        const uint64_t ff = dpack2(f, f);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           uint32_t d[16];
@@ -808,11 +864,6 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         tc_fence_before_sync();
         arrive_warp(&m->d_free, lane);
         if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
-        if (bad) {
-          const float nan = __int_as_float(0x7fffffff);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) S[j] = dpack2(nan, nan);
-        }
       }
       // a unit is written as a whole or, after a time-out, not at all
       if (any_of<2, 256>(m->abort_flag != 0)) break;

@@ -267,19 +267,37 @@ __device__ __forceinline__ void mma_ss_bf16(uint32_t d_tmem, uint64_t a_desc, ui
 __host__ __device__ constexpr uint32_t idesc_bf16(uint32_t M, uint32_t N, bool a_mn_major, bool b_mn_major) {
   return idesc_bf16(M, N) | (uint32_t(a_mn_major) << 15) | (uint32_t(b_mn_major) << 16);
 }
-// MN-major 16-bit operand tiles with the 128-byte swizzle: rows = K index, blocks of 64 elements along M/N, [R rows][128 bytes] each and
-// `block_bytes` apart (LBO); groups of 8 K rows are 1024 bytes apart (SBO).  This is the layout of the K-major tile of the transposed
-// matrix, so one tile serves in both orientations.  `smem_addr` points at the first K row of the slice (a multiple of 8).
-__device__ __forceinline__ uint64_t desc_mn_bf16(uint32_t smem_addr, uint32_t block_bytes) {
-  return kDescSw128 | (uint64_t{(smem_addr & 0x3FFFFu) >> 4}) | (uint64_t{block_bytes >> 4} << 16) | (uint64_t{1024 >> 4} << 32);
+// 16-bit operand tiles with the 128-byte swizzle, their descriptors in halves: the upper one is the same for every tile of an orientation, the
+// lower one holds the address and can be stepped by adding bytes / 16 (shared-memory addresses stay far below its 14 bits).
+// K-major: rows = M or N index; MN-major: rows = K index, blocks of 64 elements along M/N, [R rows][128 bytes] each and `block_bytes`
+// apart (LBO); groups of 8 rows are 1024 bytes apart (SBO).  MN-major is the layout of the K-major tile of the transposed
+// matrix, so one tile serves in both orientations.  A slice of an MN-major tile starts at its first K row (a multiple of 8).
+constexpr uint32_t kDescHi16 = static_cast<uint32_t>((kDescSw128 | (uint64_t{1024 >> 4} << 32)) >> 32);
+__device__ __forceinline__ uint32_t desc_lo_k(uint32_t smem_addr) { return ((smem_addr & 0x3FFFFu) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_lo_mn(uint32_t smem_addr, uint32_t block_bytes) {
+  return ((smem_addr & 0x3FFFFu) >> 4) | ((block_bytes >> 4) << 16);
 }
-// D[tmem] (+)= A[tmem] * B[smem], bf16; A is M lanes x 8 columns (16 values, two per column) at a_tmem.
-__device__ __forceinline__ void mma_ts_bf16(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, bool accumulate) {
+// D[tmem] (+)= A * B, bf16, one K = 16 slice; ACC is a compile-time constant.
+template <bool ACC>
+__device__ __forceinline__ void mma16_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(uint32_t(accumulate))
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 a, {%1, %4};\n\t"
+      "mov.b64 b, {%2, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kDescHi16), "n"(ACC ? 1 : 0)
+      : "memory");
+}
+// A is M lanes x 8 columns (16 values, two per column) at a_tmem.
+template <bool ACC>
+__device__ __forceinline__ void mma16_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 b, {%2, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_lo), "r"(idesc), "n"(kDescHi16), "n"(ACC ? 1 : 0)
       : "memory");
 }
 
