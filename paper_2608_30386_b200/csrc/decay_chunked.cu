@@ -6,11 +6,13 @@
 // Products, C = 64 tokens, everything transposed so that d_v is the M index (the accumulators' 128 lanes):
 //   QK   Q K^T               -> P before its weights    smem x smem, M = 64
 //   QS   S_0^T Q^T           -> outputs from the state   tmem x smem   (S_0 as a bf16 pair)
-//   PV   V^T P^T             -> outputs inside the chunk  smem x smem   (P as a pair; only the rows a slice of i can reach)
-//   KV   V^T Kw              -> what the chunk adds        smem x smem   (Kw as a pair)
-// V, K and Q are exact in bf16 and are used as they land; V and Kw are read with their token index as K, which for 16-bit
-// operands is the same tile.  A pair of bf16 (x rounded, and the rest rounded) holds 16 bits of the mantissa: an operand rounded
-// to bf16 once would cost the fp32 state its last 16 bits and as much of the outputs as their own rounding does.
+//   PV   V^T P^T             -> outputs inside the chunk  tmem x smem   (P as a pair; only the rows a slice of i can reach)
+//   KV   V^T Kw              -> what the chunk adds        tmem x smem   (Kw in three parts)
+// V, K and Q are exact in bf16: Q and K are used as they land, V^T goes to tensor memory (the tensor core's reads of shared memory are
+// what bounds the products: a product of 128 x 128 x 16 takes 65 cycles, 64 of which it reads both operands from there).
+// A value in n parts of bf16 (x rounded, the rest rounded, ...) is good to 2^-8n: rounded once, an operand would cost the outputs
+// as much as their own rounding does, and the fp32 state its last 16 bits; in pairs the state is good to 2.4e-6, in three parts it is
+// as good as fp32.
 //
 // One thread block per SM walks over (request, layer, head) units, or over segments of long ones; roles of its warps:
 //   0       looks up the units; TMA: tiles of K, Q, V, three chunks ahead
@@ -37,7 +39,8 @@ using namespace tc5;
 
 constexpr int C = 64, D = 128;
 constexpr int kSms = 148;
-constexpr int NS = 3;    // stages of K, Q, V
+constexpr int NS = 3, NS_V = 2;  // stages of K and Q; of V
+constexpr int KSPLIT = 3;        // parts of Kw
 constexpr int RING = 4;  // chunks whose weights are kept, and units that are looked up ahead
 constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_MMA_O = 3, WARP_P = 4, WARP_O = 8, WARP_K = 12, WARP_S = 16, NWARP = 24;
 // Registers of a thread, by groups of four warps: what the launch gives each (65,536 over all threads, in steps of 8), and how the roles
@@ -52,14 +55,14 @@ constexpr uint32_t kStatusWords = kDecayStatusWords / 2;  // per launch: one wor
 constexpr uint32_t TILE = C * D * 2;  // 64 tokens x 128 channels: two blocks of [64 rows][128 bytes]
 constexpr uint32_t BLOCK = TILE / 2;
 constexpr uint32_t OFF_K = 0, OFF_Q = OFF_K + NS * TILE, OFF_V = OFF_Q + NS * TILE;
-constexpr uint32_t OFF_KH = OFF_V + NS * TILE, OFF_KL = OFF_KH + TILE;
-constexpr uint32_t OFF_PH = OFF_KL + TILE, OFF_PL = OFF_PH + C * C * 2;
+constexpr uint32_t OFF_KW = OFF_V + NS_V * TILE;  // [KSPLIT]
+constexpr uint32_t OFF_PH = OFF_KW + KSPLIT * TILE, OFF_PL = OFF_PH + C * C * 2;
 constexpr uint32_t OFF_O = OFF_PL + C * C * 2;  // [4 warps][64 tokens][32 columns] bf16 on their way out
 constexpr uint32_t OFF_MISC = OFF_O + TILE;
 
-constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 320, COL_OT = 448;
+constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 320, COL_OT = 384, COL_V = 448;  // (V^T twice, by chunk parity)
 
-struct Weights {  // of one chunk
+struct alignas(16) Weights {  // of one chunk (read in pairs)
   float ghi[C], glo[C];  // G_t = ghi + glo, ghi a multiple of 2^-6: differences of ghi are exact
   float w[C];            // e^{G_C - G_i}; 0 behind the last token
   float eg[C];           // q_scale e^{G_t}
@@ -68,7 +71,7 @@ struct Weights {  // of one chunk
   float row[C];          // q_scale e^{G_t - G_B}
   float col[3][3 * 16];  // e^{G_B - G_i}, B = 15, 31, 47
   float all;             // e^{G_C}
-  int32_t has_bad;       // V holds values that are none:
+  int32_t has_bad[4];    // V's columns of 32 hold values that are none:
   int32_t bad[D];        // the first token with one, per column (C: no such token)
 };
 // The states and tokens of one unit, or of one segment of it.
@@ -84,11 +87,12 @@ struct Item {
 
 struct Misc {
   Item items[RING];
-  uint64_t full_k[NS], full_q[NS], full_v[NS], empty_k[NS], empty_q[NS], empty_v[NS], v_ready[NS];
+  uint64_t full_k[NS], full_q[NS], full_v[NS_V], empty_k[NS], empty_q[NS], empty_v[NS_V];
   uint64_t dec_full[RING], dec_empty[RING], item_full[RING], item_empty[RING];
-  uint64_t bar_p, bar_s, bar_o, bar_d;           // tensor core: QK, QS, PV, KV of a chunk have completed
-  uint64_t p_ready, k_ready, s_ready;            // operands of PV, KV, QS are in place
-  uint64_t o_free, d_free;                       // their accumulators have been read
+  uint64_t bar_p, bar_s, bar_o[2], bar_d;        // tensor core: QK, QS, PV (by chunk parity), KV of a chunk have completed
+  uint64_t bar_kw;                               // and the first half of KV
+  uint64_t v_ready[2], k_ready[2], p_ready, s_ready;  // V^T (by chunk parity), the halves of Kw, P, the state are in place
+  uint64_t o_free, d_free;                       // accumulators have been read
   uint64_t drain[2];
   uint32_t tmem_base;
   volatile uint32_t abort_flag;
@@ -161,12 +165,19 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
 }
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-// (x, y) as a pair of bf16 pairs: hi = rounded, lo = the rest, rounded
-__device__ __forceinline__ void split2(uint64_t xy, uint32_t &hi, uint32_t &lo) {
+// (x, y) rounded to bf16; what is left of them stays in xy
+__device__ __forceinline__ uint32_t take_bf16x2(uint64_t &xy) {
   const float2 v = dunpack2(xy);
-  hi = bf16x2(v.x, v.y);
-  const float2 r = dunpack2(dsub2(xy, dpack2(bf_lo(hi), bf_hi(hi))));
-  lo = bf16x2(r.x, r.y);
+  const uint32_t b = bf16x2(v.x, v.y);
+  xy = dsub2(xy, dpack2(bf_lo(b), bf_hi(b)));
+  return b;
+}
+__device__ __forceinline__ void split2(uint64_t xy, uint32_t &hi, uint32_t &lo) {
+  hi = take_bf16x2(xy);
+  lo = take_bf16x2(xy);
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t &r0, uint32_t &r1, uint32_t &r2, uint32_t &r3, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
@@ -240,12 +251,19 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     for (int i = 0; i < NS; ++i) {
       mbar_init(&m->full_k[i], 1);
       mbar_init(&m->full_q[i], 1);
-      mbar_init(&m->full_v[i], 1);
-      mbar_init(&m->v_ready[i], 4);
       mbar_init(&m->empty_k[i], WITH_O ? 5 : 4);  // Kw's warps; QK
       mbar_init(&m->empty_q[i], 1);
-      mbar_init(&m->empty_v[i], WITH_O ? 2 : 1);  // KV; PV
     }
+    for (int i = 0; i < NS_V; ++i) {
+      mbar_init(&m->full_v[i], 1);
+      mbar_init(&m->empty_v[i], 4);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&m->bar_o[i], 1);
+      mbar_init(&m->v_ready[i], 4);
+      mbar_init(&m->k_ready[i], 4);
+    }
+    mbar_init(&m->bar_kw, 1);
     for (int i = 0; i < RING; ++i) {
       mbar_init(&m->dec_full[i], 1);
       mbar_init(&m->dec_empty[i], WITH_O ? 20 : 12);
@@ -254,10 +272,8 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     }
     mbar_init(&m->bar_p, 1);
     mbar_init(&m->bar_s, 1);
-    mbar_init(&m->bar_o, 1);
     mbar_init(&m->bar_d, 1);
     mbar_init(&m->p_ready, 4);
-    mbar_init(&m->k_ready, 4);
     mbar_init(&m->s_ready, 8);
     mbar_init(&m->o_free, 4);
     mbar_init(&m->d_free, 8);
@@ -304,6 +320,9 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
   const auto release = [&](int it) { arrive_warp(&m->item_empty[it % RING], lane); };
   const auto stage = [](int i) { return static_cast<uint32_t>(i) % NS; };
   const auto stage_phase = [](int i) { return static_cast<uint32_t>(i) / NS & 1u; };
+  const auto stage_v = [](int i) { return static_cast<uint32_t>(i) % NS_V; };
+  const auto stage_v_phase = [](int i) { return static_cast<uint32_t>(i) / NS_V & 1u; };
+  const auto phase2 = [](int i) { return static_cast<uint32_t>(i) >> 1 & 1u; };  // of what there are two of, by chunk parity
   const auto slot = [](int i) { return static_cast<uint32_t>(i) % RING; };
   const auto slot_phase = [](int i) { return static_cast<uint32_t>(i) / RING & 1u; };
 
@@ -344,10 +363,10 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           ask = true;
           if (chunks == 0) continue;
         }
-        const uint32_t st = stage(n), ph = stage_phase(n) ^ 1u;
         const int32_t z = static_cast<int32_t>(x.tok0 + c * C);
-        const auto load = [&](uint64_t *empty, uint64_t *full, uint32_t off, const CUtensorMap *map, int head, int &count) {
-          if (n >= NS) wait_bar(&empty[st], ph, m);
+        const auto load = [&](uint64_t *empty, uint64_t *full, uint32_t st, uint32_t ph, int stages, uint32_t off, const CUtensorMap *map, int head,
+                              int &count) {
+          if (n >= stages) wait_bar(&empty[st], ph ^ 1u, m);
           stop |= uni(m->abort_flag) != 0;
           if (stop) return;
           if (lane == 0) {
@@ -357,64 +376,69 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           }
           ++count;
         };
-        load(m->empty_k, m->full_k, OFF_K, &tmap_k, x.k_head, nk);
-        if (WITH_O) load(m->empty_q, m->full_q, OFF_Q, &tmap_q, x.k_head, nq);
-        load(m->empty_v, m->full_v, OFF_V, &tmap_v, x.head, nv);
+        load(m->empty_v, m->full_v, stage_v(n), stage_v_phase(n), NS_V, OFF_V, &tmap_v, x.head, nv);
+        load(m->empty_k, m->full_k, stage(n), stage_phase(n), NS, OFF_K, &tmap_k, x.k_head, nk);
+        if (WITH_O) load(m->empty_q, m->full_q, stage(n), stage_phase(n), NS, OFF_Q, &tmap_q, x.k_head, nq);
         if (stop) break;
         ++c;
         ++n;
       }
       // Copies in flight land before the block ends, whoever has given up waiting for them.
-      const auto land = [&](uint64_t *full, int count) {
-        for (int i = max(count - NS, 0); i < count; ++i)
+      const auto land = [&](uint64_t *bar, uint32_t phase) {
 #pragma unroll 1
-          for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(&full[stage(i)], stage_phase(i)); ++p) {
-          }
+        for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(bar, phase); ++p) {
+        }
       };
-      land(m->full_k, nk);
-      land(m->full_q, nq);
-      land(m->full_v, nv);
+#pragma unroll 1
+      for (int i = max(n - NS, 0); i <= n; ++i) {
+        if (i < nv && i >= nv - NS_V) land(&m->full_v[stage_v(i)], stage_v_phase(i));
+        if (i < nk && i >= nk - NS) land(&m->full_k[stage(i)], stage_phase(i));
+        if (i < nq && i >= nq - NS) land(&m->full_q[stage(i)], stage_phase(i));
+      }
     } else if (warp == WARP_MMA || warp == WARP_MMA_O) {
       const auto gave_up = [&]() { return uni(m->abort_flag) != 0; };  // (one answer for the whole warp)
       int it = 0, all = 0;  // chunks of all items that have been looked up
       const auto look = [&]() {  // the next item with tokens, if there is one
         int chunks = 0;
         while (chunks == 0 && uni(take(it))) {
-          chunks = chunks_of(m->items[it % RING].n);
+          chunks = uni(chunks_of(m->items[it % RING].n));
           release(it++);
         }
         all += chunks;
       };
       if (warp == WARP_MMA) {
-        constexpr uint32_t ID_KV = idesc_bf16(128, 128, true, true);
+        constexpr uint32_t ID_KV = idesc_bf16(128, 128, false, true);
         look();
         // Test hook: a first, short wait for operands that cannot be there yet.
         if (a.poll_limit_first_wait && all > 0) {
           bool done = false;
-          for (uint32_t i = 0; i < a.poll_limit_first_wait && !done; ++i) done = mbar_test_wait(&m->k_ready, 0);
+          for (uint32_t i = 0; i < a.poll_limit_first_wait && !done; ++i) done = mbar_test_wait(&m->k_ready[0], 0);
           if (!done) m->abort_flag = 1;
         }
 #pragma unroll 1
         for (; n < all && !gave_up(); ++n) {
           if (n + 1 == all) look();
-          const uint32_t st = stage(n), par = n & 1u;
-          wait_bar(&m->k_ready, par, m);
-          wait_bar(&m->full_v[st], stage_phase(n), m);
+          const uint32_t par = n & 1u;
+          wait_bar(&m->v_ready[par], phase2(n), m);
           if (n > 0) wait_bar(&m->d_free, par ^ 1u, m);
-          tc_fence_after_sync();
-          if (gave_up()) break;
-          if (elect_one()) {
-            const uint32_t v = desc_lo_mn(sbase + OFF_V, BLOCK) + st * (TILE >> 4), kw = desc_lo_mn(sbase + OFF_KH, BLOCK);
-            mma16_ss<false>(tm + COL_D, v, kw, ID_KV);
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {  // 32 tokens each, so that the next Kw can follow behind
+            wait_bar(&m->k_ready[half], par, m);
+            tc_fence_after_sync();
+            if (gave_up()) break;
+            if (elect_one()) {
+              const uint32_t v = tm + COL_V + par * 32 + half * 16, kw = desc_lo_mn(sbase + OFF_KW, BLOCK) + half * (2 * 2048 >> 4);
+              if (half == 0)
+                mma16_ts<false>(tm + COL_D, v, kw, ID_KV);
+              else
+                mma16_ts<true>(tm + COL_D, v, kw, ID_KV);
 #pragma unroll
-            for (int i = 1; i < 8; ++i) {
-              const uint32_t s = (i & 3) * 2048;
-              mma16_ss<true>(tm + COL_D, v + (s >> 4), kw + (((i < 4 ? 0 : OFF_KL - OFF_KH) + s) >> 4), ID_KV);
+              for (int i = 1; i < 2 * KSPLIT; ++i)
+                mma16_ts<true>(tm + COL_D, v + (i & 1) * 8, kw + (((i >> 1) * TILE + (i & 1) * 2048) >> 4), ID_KV);
+              mma_commit(half == 0 ? &m->bar_kw : &m->bar_d);
             }
-            mma_commit(&m->bar_d);
-            mma_commit(&m->empty_v[st]);
+            __syncwarp();
           }
-          __syncwarp();
         }
       } else if constexpr (WITH_O) {
         constexpr uint32_t ID_QK = idesc_bf16(64, 64), ID_QS = idesc_bf16(128, 64);
@@ -446,12 +470,12 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           if (!first) {
             // QS
             wait_bar(&m->s_ready, par, m);
-            wait_bar(&m->full_q[st], stage_phase(n), m);
+            if (n > 0) wait_bar(&m->o_free, par ^ 1u, m);
             tc_fence_after_sync();
             if (gave_up()) break;
             if (elect_one()) {
               const uint32_t q = desc_lo_k(sbase + OFF_Q) + st * (TILE >> 4);
-              const uint32_t d = tm + COL_OI + par * 64;
+              const uint32_t d = tm + COL_OI;
               mma16_ts<false>(d, tm + COL_SH, q, ID_QS);
 #pragma unroll
               for (int i = 1; i < 16; ++i) {
@@ -468,22 +492,18 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           if (n + 1 < all) qk(n + 1);
           if (!first) {
             // PV: tokens 16 s ... 16 s + 15 reach the rows from 16 s on
-            wait_bar(&m->full_v[st], stage_phase(n), m);
-            wait_bar(&m->v_ready[st], stage_phase(n), m);
-            if (n > 0) wait_bar(&m->o_free, par ^ 1u, m);
+            wait_bar(&m->v_ready[par], phase2(n), m);
             tc_fence_after_sync();
             if (gave_up()) break;
             if (elect_one()) {
-              const uint32_t v = desc_lo_mn(sbase + OFF_V, BLOCK) + st * (TILE >> 4), p = desc_lo_k(sbase + OFF_PH);
-              mma16_ss<false>(tm + COL_OT, v, p, idesc_bf16(128, 64, true, false));
+              const uint32_t v = tm + COL_V + par * 32, p = desc_lo_k(sbase + OFF_PH);
+              mma16_ts<false>(tm + COL_OT, v, p, idesc_bf16(128, 64));
 #pragma unroll
               for (int i = 1; i < 8; ++i) {
                 const uint32_t s = i & 3;
-                mma16_ss<true>(tm + COL_OT + 16 * s, v + (s * 2048 >> 4), p + (((i < 4 ? 0 : OFF_PL - OFF_PH) + s * 2048 + s * 32) >> 4),
-                               idesc_bf16(128, 64 - 16 * s, true, false));
+                mma16_ts<true>(tm + COL_OT + 16 * s, v + 8 * s, p + (((i < 4 ? 0 : OFF_PL - OFF_PH) + s * 2048 + s * 32) >> 4), idesc_bf16(128, 64 - 16 * s));
               }
-              mma_commit(&m->bar_o);
-              mma_commit(&m->empty_v[st]);
+              mma_commit(&m->bar_o[par]);
             }
             __syncwarp();
           }
@@ -599,7 +619,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           const Weights &w = m->wt[slot(n)];
           wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
           wait_bar(&m->bar_p, n & 1u, m);
-          if (n > 0) wait_bar(&m->bar_o, (n - 1) & 1u, m);  // PV of the chunk before has read its P
+          if (n > 0) wait_bar(&m->bar_o[(n - 1) & 1], phase2(n - 1), m);  // PV of the chunk before has read its P
           tc_fence_after_sync();
           const float r0 = w.row[t0], r1 = w.row[t1];
           const uint64_t rr0 = dpack2(r0, r0), rr1 = dpack2(r1, r1);
@@ -654,15 +674,15 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           const Weights &w = m->wt[slot(n)];
           const int rows = tokens - c * C;
           wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-          wait_bar(&m->bar_o, n & 1u, m);
+          wait_bar(&m->bar_o[n & 1], phase2(n), m);
           tc_fence_after_sync();
-          const bool has_bad = w.has_bad != 0;
+          const bool has_bad = w.has_bad[quad] != 0;
 #pragma unroll 1
           for (int part = 0; part < 4; ++part) {  // 16 columns of d_v (part & 1), 32 tokens (part >> 1)
             const int half = part & 1, tb = part >> 1;
             uint32_t oi[16], ot[16];
             const uint32_t at = tl + (static_cast<uint32_t>(half * 16) << 16) + tb * 32;
-            tmem_ld_16x256b(at + COL_OI + (n & 1) * 64, oi);
+            tmem_ld_16x256b(at + COL_OI, oi);
             tmem_ld_16x256b(at + COL_OT, ot);
             tmem_ld_wait();
             if (part == 3) {
@@ -728,7 +748,8 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
   } else if (warp < WARP_S) {
     // ---- Kw ----
     regs_down<REGS_K>();
-    const int kt = tid - WARP_K * 32;
+    const int kt = tid - WARP_K * 32, quad = warp & 3;
+    const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
 #pragma unroll 1
     for (int it = 0;; ++it) {
       if (any_of<1, 128>(!take(it))) break;  // (one answer for all four warps)
@@ -736,69 +757,99 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       release(it);
 #pragma unroll 1
       for (int c = 0; c < chunks_of(tokens); ++c, ++n) {
-        const uint32_t st = stage(n);
+        const uint32_t st = stage(n), par = n & 1u;
         const int rows = min(tokens - c * C, C);
         Weights &w = m->wt[slot(n)];
-        wait_bar(&m->full_v[st], stage_phase(n), m);
-        // V: a value that is none would reach every row of its column through products with weights that are zero.  0 * x + sum is
-        // NaN from the first of them on.
-        unsigned char *const vt = smem + OFF_V + st * TILE + kt * 16;
-        __nv_bfloat162 probe = __floats2bfloat162_rn(0.f, 0.f);
-        const __nv_bfloat162 zero2 = probe;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          uint4 y = *reinterpret_cast<const uint4 *>(vt + i * 2048);
-          if (rows < C && (kt >> 3) + (i & 3) * 16 >= rows) {  // behind the last token
-            y = make_uint4(0u, 0u, 0u, 0u);
-            *reinterpret_cast<uint4 *>(vt + i * 2048) = y;
-          }
-          const __nv_bfloat162 *const e = reinterpret_cast<const __nv_bfloat162 *>(&y);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) probe = __hfma2(e[j], zero2, probe);
-        }
+        wait_bar(&m->full_v[stage_v(n)], stage_v_phase(n), m);
         wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-        const bool none = __isnan(__low2float(probe)) || __isnan(__high2float(probe));
-        if (any_of<1, 128>(none)) {
-          w.bad[kt] = C;
-          asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (n > 1) {  // the products of the chunk before the last have read their V^T (their KV has been waited for below)
+          if (WITH_O) wait_bar(&m->bar_o[par], phase2(n - 2), m);
+          tc_fence_after_sync();
+        }
+        // V^T, this warp's 32 columns.  A value that is none would reach every row of its column through products with weights that are
+        // zero, so it is taken out and remembered; 0 * x + sum is NaN from the first of them on.
+        unsigned char *const vt = smem + OFF_V + stage_v(n) * TILE + (quad >> 1) * BLOCK;
+        bool looked = false;
+        uint32_t r[2][16];
 #pragma unroll 1
-          for (int i = 0; i < 8; ++i) {
-            const int row = (kt >> 3) + (i & 3) * 16, col = (i >> 2) * 64 + (((kt & 7) ^ (row & 7)) << 3);
-            uint16_t *const e = reinterpret_cast<uint16_t *>(vt + i * 2048);
-#pragma unroll 1
-            for (int j = 0; j < 8; ++j)
-              if ((e[j] & 0x7F80u) == 0x7F80u) {
-                e[j] = 0;
-                atomicMin(&w.bad[col + j], row);
-              }
+        for (;;) {
+          __nv_bfloat162 probe = __floats2bfloat162_rn(0.f, 0.f);
+          const __nv_bfloat162 zero2 = probe;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+              const int t = 8 * (j + (lane >> 4)) + (lane & 7), ch = (quad & 1) * 4 + h * 2 + (lane >> 3 & 1);
+              ldmatrix_x4_trans(r[h][2 * j], r[h][2 * j + 1], r[h][2 * j + 2], r[h][2 * j + 3], smem_u32(vt) + t * 128 + ((ch ^ (t & 7)) << 4));
+            }
           }
-          if (kt == 0) w.has_bad = 1;
-        } else if (kt == 0) {
-          w.has_bad = 0;
+          if (rows < C) {  // nothing from behind the last token
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const int t = 8 * (j >> 1) + 2 * (lane & 3);
+              const uint32_t keep = t + 1 < rows ? 0xFFFFFFFFu : t < rows ? 0xFFFFu : 0u;
+              r[0][j] &= keep;
+              r[1][j] &= keep;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            probe = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&r[0][j]), zero2, probe);
+            probe = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&r[1][j]), zero2, probe);
+          }
+          const bool none = __isnan(__low2float(probe)) || __isnan(__high2float(probe));
+          if (!__any_sync(0xffffffffu, none) || looked) break;
+          looked = true;
+          int first = C;  // of column `lane`
+#pragma unroll 1
+          for (int t = rows - 1; t >= 0; --t) {
+            uint16_t *const e = reinterpret_cast<uint16_t *>(vt + t * 128 + ((((quad & 1) * 4 + (lane >> 3)) ^ (t & 7)) << 4) + (lane & 7) * 2);
+            if ((*e & 0x7F80u) == 0x7F80u) {
+              *e = 0;
+              first = t;
+            }
+          }
+          w.bad[quad * 32 + lane] = first;
+          fence_smem_to_async();  // (the next tile lands here)
+          __syncwarp();
         }
-        fence_smem_to_async();
-        arrive_warp(&m->v_ready[st], lane);
+        if (lane == 0) w.has_bad[quad] = looked;
+        tmem_st_16x128b(tl + COL_V + par * 32, r[0]);
+        tmem_st_16x128b(tl + COL_V + par * 32 + (16u << 16), r[1]);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        arrive_warp(&m->v_ready[par], lane);
+        if (lane == 0) mbar_arrive(&m->empty_v[stage_v(n)]);
+        // Kw, 32 tokens at a time
         wait_bar(&m->full_k[st], stage_phase(n), m);
-        if (n > 0) wait_bar(&m->bar_d, (n - 1) & 1u, m);  // KV of the chunk before has read its Kw
         const unsigned char *const kr = smem + OFF_K + st * TILE + kt * 16;
-        unsigned char *const kh = smem + OFF_KH + kt * 16, *const kl = smem + OFF_KL + kt * 16;
-#pragma unroll 2
-        for (int i = 0; i < 8; ++i) {
-          const int row = (kt >> 3) + (i & 3) * 16;
-          const float f = w.w[row];
-          const uint64_t ff = dpack2(f, f);
-          uint4 y = *reinterpret_cast<const uint4 *>(kr + i * 2048);
-          if (row >= rows) y = make_uint4(0u, 0u, 0u, 0u);
-          uint4 hi, lo;
-          split2(dmul2(dpack2(bf_lo(y.x), bf_hi(y.x)), ff), hi.x, lo.x);
-          split2(dmul2(dpack2(bf_lo(y.y), bf_hi(y.y)), ff), hi.y, lo.y);
-          split2(dmul2(dpack2(bf_lo(y.z), bf_hi(y.z)), ff), hi.z, lo.z);
-          split2(dmul2(dpack2(bf_lo(y.w), bf_hi(y.w)), ff), hi.w, lo.w);
-          *reinterpret_cast<uint4 *>(kh + i * 2048) = hi;
-          *reinterpret_cast<uint4 *>(kl + i * 2048) = lo;
+        unsigned char *const kw = smem + OFF_KW + kt * 16;
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          if (n > 0) wait_bar(half == 0 ? &m->bar_kw : &m->bar_d, (n - 1) & 1u, m);  // KV of the chunk before has read this half
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int row = (kt >> 3) + (half * 2 + (i & 1)) * 16;
+            const uint32_t at = ((i >> 1) * 4 + half * 2 + (i & 1)) * 2048;
+            const float f = w.w[row];
+            const uint64_t ff = dpack2(f, f);
+            uint4 y = *reinterpret_cast<const uint4 *>(kr + at);
+            if (row >= rows) y = make_uint4(0u, 0u, 0u, 0u);
+            uint64_t rest[4] = {dmul2(dpack2(bf_lo(y.x), bf_hi(y.x)), ff), dmul2(dpack2(bf_lo(y.y), bf_hi(y.y)), ff),
+                                dmul2(dpack2(bf_lo(y.z), bf_hi(y.z)), ff), dmul2(dpack2(bf_lo(y.w), bf_hi(y.w)), ff)};
+#pragma unroll
+            for (int part = 0; part < KSPLIT; ++part) {
+              uint4 b;
+              b.x = take_bf16x2(rest[0]);
+              b.y = take_bf16x2(rest[1]);
+              b.z = take_bf16x2(rest[2]);
+              b.w = take_bf16x2(rest[3]);
+              *reinterpret_cast<uint4 *>(kw + part * TILE + at) = b;
+            }
+          }
+          fence_smem_to_async();
+          arrive_warp(&m->k_ready[half], lane);
         }
-        fence_smem_to_async();
-        arrive_warp(&m->k_ready, lane);
         if (lane == 0) {
           mbar_arrive(&m->empty_k[st]);
           mbar_arrive(&m->dec_empty[slot(n)]);
@@ -850,7 +901,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         decay *= f;
         wait_bar(&m->bar_d, n & 1u, m);
         tc_fence_after_sync();
-        if (w.has_bad != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
+        if (w.has_bad[quad] != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
         const uint64_t ff = dpack2(f, f);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
