@@ -49,7 +49,7 @@ constexpr int REGS = 80, REGS_0 = 56, REGS_P = 72, REGS_O = 72, REGS_K = 72, REG
 static_assert(NWARP * 32 * REGS <= 65536 && REGS_0 + REGS_P + REGS_O + REGS_K + 2 * REGS_S <= NWARP / 4 * REGS);
 constexpr int NT = NWARP * 32;
 constexpr int kMaxSorted = 512;  // entries (requests x segments) that are taken longest first
-constexpr uint32_t kMaxPolls = 1u << 22;
+constexpr uint32_t kMaxPolls = 1u << 22, kPollNs = 1000;  // a poll sleeps for up to that long: the warps that wait leave the issue slots to the others
 constexpr uint32_t kStatusWords = kDecayStatusWords / 2;  // per launch: one word per thread block
 
 constexpr uint32_t TILE = C * D * 2;  // 64 tokens x 128 channels: two blocks of [64 rows][128 bytes]
@@ -130,7 +130,7 @@ __device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, Misc *m
       "{\n\t.reg .pred p, q;\n\t.reg .b32 n, f;\n\t"
       "mov.b32 n, 0;\n"
       "POLL:\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%0], %1;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%0], %1, %4;\n\t"
       "@p bra DONE;\n\t"
       "ld.volatile.shared.b32 f, [%2];\n\t"
       "add.u32 n, n, 1;\n\t"
@@ -139,7 +139,7 @@ __device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, Misc *m
       "@p bra POLL;\n\t"
       "st.volatile.shared.b32 [%2], 1;\n"
       "DONE:\n\t}" ::"r"(smem_u32(bar)),
-      "r"(parity), "r"(smem_u32(const_cast<uint32_t *>(&m->abort_flag))), "n"(kMaxPolls)
+      "r"(parity), "r"(smem_u32(const_cast<uint32_t *>(&m->abort_flag))), "n"(kMaxPolls), "r"(kPollNs)
       : "memory");
 }
 __device__ __forceinline__ int uni(int x) { return __shfl_sync(0xffffffffu, x, 0); }
@@ -769,6 +769,13 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         // V^T, this warp's 32 columns.  A value that is none would reach every row of its column through products with weights that are
         // zero, so it is taken out and remembered; 0 * x + sum is NaN from the first of them on.
         unsigned char *const vt = smem + OFF_V + stage_v(n) * TILE + (quad >> 1) * BLOCK;
+        if (rows < C) {  // nothing from behind the last token
+#pragma unroll 1
+          for (int t = rows + (lane >> 2); t < C; t += 8)
+            *reinterpret_cast<uint4 *>(vt + t * 128 + ((((quad & 1) * 4 + (lane & 3)) ^ (t & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+          fence_smem_to_async();  // (the next tile lands here)
+          __syncwarp();
+        }
         bool looked = false;
         uint32_t r[2][16];
 #pragma unroll 1
@@ -781,15 +788,6 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
             for (int j = 0; j < 8; j += 2) {
               const int t = 8 * (j + (lane >> 4)) + (lane & 7), ch = (quad & 1) * 4 + h * 2 + (lane >> 3 & 1);
               ldmatrix_x4_trans(r[h][2 * j], r[h][2 * j + 1], r[h][2 * j + 2], r[h][2 * j + 3], smem_u32(vt) + t * 128 + ((ch ^ (t & 7)) << 4));
-            }
-          }
-          if (rows < C) {  // nothing from behind the last token
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const int t = 8 * (j >> 1) + 2 * (lane & 3);
-              const uint32_t keep = t + 1 < rows ? 0xFFFFFFFFu : t < rows ? 0xFFFFu : 0u;
-              r[0][j] &= keep;
-              r[1][j] &= keep;
             }
           }
 #pragma unroll
@@ -827,7 +825,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
           if (n > 0) wait_bar(half == 0 ? &m->bar_kw : &m->bar_d, (n - 1) & 1u, m);  // KV of the chunk before has read this half
-#pragma unroll
+#pragma unroll 2
           for (int i = 0; i < 4; ++i) {
             const int row = (kt >> 3) + (half * 2 + (i & 1)) * 16;
             const uint32_t at = ((i >> 1) * 4 + half * 2 + (i & 1)) * 2048;
