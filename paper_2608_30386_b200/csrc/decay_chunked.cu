@@ -6,14 +6,14 @@
 // Products, C = 64 tokens, everything transposed so that d_v is the M index (the accumulators' 128 lanes):
 //   QK   Q K^T               -> P before its weights    smem x smem, M = 64
 //   QS   S_0^T Q^T           -> outputs from the state   tmem x smem   (S_0 as a bf16 pair)
-//   PV   V^T P^T             -> outputs inside the chunk  tmem x smem   (P as a pair; only the rows a slice of i can reach)
-//   KV   Vw^T K              -> what the chunk adds        tmem x smem   (Vw in three parts; 64 key channels at a time)
+//   PV   V^T P^T             -> outputs inside the chunk  smem x smem   (P as a pair; only the rows a slice of i can reach)
+//   KV   Vw^T K              -> what the chunk adds        tmem x smem   (Vw in three parts)
 // V, K and Q are exact in bf16 and are used as they land; V and K are read with their token index as K, which for 16-bit operands is
 // the same tile.  A value in n parts of bf16 (x rounded, the rest rounded, ...) is good to 2^-8n: rounded once, an operand would cost
 // the outputs as much as their own rounding does, and the fp32 state its last 16 bits; in pairs the state was good to 2.4e-6, in three
 // parts it is as good as fp32.
 // What the products read of shared memory counts: one of 128 x 128 x 16 with both operands there takes 65 cycles, 64 of which it reads,
-// and the warps' own accesses go through the same pipe.  So the operands that are made here (V^T, Vw, the state) go to tensor memory; with
+// and the warps' own accesses go through the same pipe.  So the operands that are made here (Vw, the state) go to tensor memory; with
 // weights on K instead, written to shared memory, a chunk took 15 % longer.
 //
 // One thread block per SM walks over (request, layer, head) units, or over segments of long ones; roles of its warps:
@@ -23,7 +23,9 @@
 //   4 - 7   P: out of tensor memory, weighted, into its operand tiles
 //   8 - 11  outputs
 //   12 - 15 Vw; looks at V for values that are none
-//   16 - 23 the state, in fp32 registers: a thread has 64 key channels of one column
+//   16 - 23 the state, in fp32 registers: a thread has 64 key channels of one column.  Between two units they exchange the last state with
+//           the next one's, which has landed in shared memory by then, and it leaves from there: stored from registers, 64 KB
+//           took 3.5 k cycles, which the products waited for
 // The only chain from chunk to chunk is S <- e^{G_C} S + (KV), 64 packed multiply-adds per thread, and its bf16 pair on the way
 // to QS; KV itself does not depend on the state.
 #include <cuda.h>
@@ -41,7 +43,7 @@ using namespace tc5;
 
 constexpr int C = 64, D = 128;
 constexpr int kSms = 148;
-constexpr int NS_K = 3, NS_Q = 2, NS_V = 2;  // stages of K, Q, V
+constexpr int NS_K = 3, NS_Q = 2, NS_V = 3;  // stages of K, Q, V
 constexpr int VSPLIT = 3;                    // parts of Vw
 constexpr int RING = 4;  // chunks whose weights are kept, and units that are looked up ahead
 constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_MMA_O = 3, WARP_P = 4, WARP_O = 8, WARP_V = 12, WARP_S = 16, NWARP = 24;
@@ -59,11 +61,12 @@ constexpr uint32_t BLOCK = TILE / 2;
 constexpr uint32_t OFF_K = 0, OFF_Q = OFF_K + NS_K * TILE, OFF_V = OFF_Q + NS_Q * TILE;
 constexpr uint32_t OFF_S = OFF_V + NS_V * TILE;  // the next unit's state
 constexpr uint32_t OFF_PH = OFF_S + D * D * 4, OFF_PL = OFF_PH + C * C * 2;
-constexpr uint32_t OFF_O = OFF_PL + C * C * 2;  // [4 warps][64 tokens][32 columns] bf16 on their way out
-constexpr uint32_t OFF_MISC = OFF_O + TILE;
+constexpr uint32_t OFF_O = OFF_PL + C * C * 2;  // [4 warps][32 tokens][32 columns] bf16 on their way out
+constexpr uint32_t OFF_MISC = OFF_O + TILE / 2;
 
-constexpr uint32_t COL_D = 0, COL_SH = 64, COL_SL = 128, COL_P = 192, COL_OI = 256, COL_OT = 320, COL_VW = 384, COL_V = 480;
-static_assert(COL_VW + 32 * VSPLIT <= COL_V);
+// Tensor memory.  P has M = 64 and takes 16 lanes of each quadrant, so its columns from 32 on lie in the other 16.
+constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 288, COL_OT = 352, COL_VW = 416;
+static_assert(COL_VW + 32 * VSPLIT <= 512);
 
 struct alignas(16) Weights {  // of one chunk (read in pairs)
   float ghi[C], glo[C];  // G_t = ghi + glo, ghi a multiple of 2^-6: differences of ghi are exact
@@ -72,7 +75,7 @@ struct alignas(16) Weights {  // of one chunk (read in pairs)
   // P's weights outside its diagonal blocks of 16 x 16 are products: with B the last token before t's block, e^{G_t - G_B} times
   // e^{G_B - G_i}, neither above 1
   float row[C];          // q_scale e^{G_t - G_B}
-  float col[3][3 * 16];  // e^{G_B - G_i}, B = 15, 31, 47
+  float col[6 * 16];     // e^{G_B - G_i}, B = 15, 31, 47: 16, 32, 48 of them
   float all;             // e^{G_C}
   int32_t has_bad[4];    // V's columns of 32 hold values that are none:
   int32_t bad[D];        // the first token with one, per column (C: no such token)
@@ -91,11 +94,12 @@ struct Item {
 struct Misc {
   Item items[RING];
   uint64_t full_k[NS_K], full_q[NS_Q], full_v[NS_V], empty_k[NS_K], empty_q[NS_Q], empty_v[NS_V];
-  uint64_t s_full, s_empty;                      // the next unit's state has landed, has been taken
+  uint64_t v_ok[NS_V];                           // V has been looked at
+  uint64_t s_full, s_empty;                      // the next unit's state has landed; its place is free again
   uint64_t dec_full[RING], dec_empty[RING], item_full[RING], item_empty[RING];
-  uint64_t bar_p, bar_s, bar_o[2], bar_d[2];     // tensor core: QK, QS, PV (by chunk parity), the halves of KV have completed
-  uint64_t w_ready, v_ready, p_ready, s_ready;   // Vw, V^T, P, the state are in place
-  uint64_t o_free, d_free[2];                    // accumulators have been read (KV's by each half of the state's warps)
+  uint64_t bar_p, bar_s, bar_o[2], bar_d[2];     // tensor core: QK, QS, PV (by chunk parity), KV of 32 tokens and of the others have completed
+  uint64_t w_ready[2], p_ready, s_ready;         // Vw of 32 tokens and of the others, P, the state are in place
+  uint64_t o_free, d_free;                       // accumulators have been read
   uint64_t drain[2];
   uint32_t tmem_base;
   volatile uint32_t abort_flag;
@@ -261,17 +265,17 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     }
     for (int i = 0; i < NS_V; ++i) {
       mbar_init(&m->full_v[i], 1);
-      mbar_init(&m->empty_v[i], 4);
+      mbar_init(&m->empty_v[i], WITH_O ? 5 : 4);  // Vw's warps; PV
+      mbar_init(&m->v_ok[i], 4);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&m->bar_o[i], 1);
       mbar_init(&m->bar_d[i], 1);
-      mbar_init(&m->d_free[i], 4);
+      mbar_init(&m->w_ready[i], 4);
     }
+    mbar_init(&m->d_free, 8);
     mbar_init(&m->s_full, 1);
-    mbar_init(&m->s_empty, 8);
-    mbar_init(&m->w_ready, 4);
-    mbar_init(&m->v_ready, 4);
+    mbar_init(&m->s_empty, 1);
     for (int i = 0; i < RING; ++i) {
       mbar_init(&m->dec_full[i], 1);
       mbar_init(&m->dec_empty[i], WITH_O ? 20 : 12);
@@ -337,28 +341,30 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
   if (warp < WARP_P) {
     regs_down<REGS_0>();
     if (warp == WARP_TMA) {
-      // The next item is looked up behind the first loads of this one, and its state is asked for as soon as the last one has been taken.
+      // The next item is looked up behind the first loads of this one, and its state is asked for as soon as there is room.
       int nk = 0, nq = 0, nv = 0, ns = 0;  // tiles and states asked for
       bool stop = false, pending = false;
-      const float *src = nullptr;
       uint32_t k = 0;
       int it = 0;
+      Item x, next{};
       const auto load_state = [&](bool wait) {
-        if (ns > 0) {
+        if (it > 1) {  // the place is free once per item: when the one before this has begun
           if (wait)
-            wait_bar(&m->s_empty, (ns - 1) & 1u, m);
-          else if (!uni(mbar_test_wait(&m->s_empty, (ns - 1) & 1u)))
+            wait_bar(&m->s_empty, it & 1u, m);
+          else if (!uni(mbar_test_wait(&m->s_empty, it & 1u)))
             return;
         }
         pending = false;
         if (uni(m->abort_flag)) return;
+        if (next.from == 0) return;
+        const float *const src =
+            next.from == 2 ? sp.seg_state + (static_cast<int64_t>(next.unit) * sp.nseg + next.seg) * (D * D) : a.state + next.state;
         if (lane == 0) {
           mbar_expect_tx(&m->s_full, D * D * 4);
           for (int i = 0; i < 4; ++i) bulk_load(sbase + OFF_S + i * (D * D), src + i * (D * D / 4), D * D, &m->s_full);
         }
         ++ns;
       };
-      Item x, next;
       bool ask = true;
       int c = 0, chunks = 0;
 #pragma unroll 1
@@ -371,8 +377,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           if (lane == 0) m->items[it % RING] = next;
           arrive_warp(&m->item_full[it % RING], lane);
           ++it;
-          pending = next.n >= 0 && next.from != 0;
-          src = next.from == 2 ? sp.seg_state + (static_cast<int64_t>(next.unit) * sp.nseg + next.seg) * (D * D) : a.state + next.state;
+          pending = next.n >= 0;
           ask = false;
         }
         if (c == chunks) {
@@ -428,12 +433,12 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         all += chunks;
       };
       if (warp == WARP_MMA) {
-        constexpr uint32_t ID_KV = idesc_bf16(128, 64, false, true);
+        constexpr uint32_t ID_KV = idesc_bf16(128, 128, false, true);
         look();
         // Test hook: a first, short wait for operands that cannot be there yet.
         if (a.poll_limit_first_wait && all > 0) {
           bool done = false;
-          for (uint32_t i = 0; i < a.poll_limit_first_wait && !done; ++i) done = mbar_test_wait(&m->w_ready, 0);
+          for (uint32_t i = 0; i < a.poll_limit_first_wait && !done; ++i) done = mbar_test_wait(&m->w_ready[0], 0);
           if (!done) m->abort_flag = 1;
         }
 #pragma unroll 1
@@ -441,17 +446,20 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           if (n + 1 == all) look();
           const uint32_t par = n & 1u, st = stage_k(n);
           wait_bar(&m->full_k[st], phase_k(n), m);
-          wait_bar(&m->w_ready, par, m);
+          if (n > 0) wait_bar(&m->d_free, par ^ 1u, m);
 #pragma unroll 1
-          for (int half = 0; half < 2; ++half) {  // 64 key channels each, in one accumulator: there is no room for two
-            if (n + half > 0) wait_bar(&m->d_free[half ^ 1], par ^ half ^ 1u, m);
+          for (int half = 0; half < 2; ++half) {  // 32 tokens each, so that the next Vw can follow behind
+            wait_bar(&m->w_ready[half], par, m);
             tc_fence_after_sync();
             if (gave_up()) break;
             if (elect_one()) {
-              const uint32_t v = tm + COL_VW, k = desc_lo_mn(sbase + OFF_K, BLOCK) + (st * TILE + half * BLOCK >> 4);
-              mma16_ts<false>(tm + COL_D, v, k, ID_KV);
+              const uint32_t v = tm + COL_VW + half * 16, k = desc_lo_mn(sbase + OFF_K, BLOCK) + (st * TILE + half * (2 * 2048) >> 4);
+              if (half == 0)
+                mma16_ts<false>(tm + COL_D, v, k, ID_KV);
+              else
+                mma16_ts<true>(tm + COL_D, v, k, ID_KV);
 #pragma unroll
-              for (int i = 1; i < 4 * VSPLIT; ++i) mma16_ts<true>(tm + COL_D, v + (i >> 2) * 32 + (i & 3) * 8, k + ((i & 3) * 2048 >> 4), ID_KV);
+              for (int i = 1; i < 2 * VSPLIT; ++i) mma16_ts<true>(tm + COL_D, v + (i >> 1) * 32 + (i & 1) * 8, k + ((i & 1) * 2048 >> 4), ID_KV);
               mma_commit(&m->bar_d[half]);
               if (half == 1) mma_commit(&m->empty_k[st]);
             }
@@ -459,7 +467,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           }
         }
       } else if constexpr (WITH_O) {
-        constexpr uint32_t ID_QK = idesc_bf16(64, 64), ID_QS = idesc_bf16(128, 64);
+        constexpr uint32_t ID_QK = idesc_bf16(64, 32), ID_QS = idesc_bf16(128, 64);
         const auto qk = [&](int i) {
           wait_bar(&m->full_k[stage_k(i)], phase_k(i), m);
           wait_bar(&m->full_q[stage_q(i)], phase_q(i), m);
@@ -467,11 +475,15 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           if (gave_up()) return;
           if (elect_one()) {
             const uint32_t q = desc_lo_k(sbase + OFF_Q) + stage_q(i) * (TILE >> 4), k = desc_lo_k(sbase + OFF_K) + stage_k(i) * (TILE >> 4);
-            mma16_ss<false>(tm + COL_P, q, k, ID_QK);
 #pragma unroll
-            for (int kk = 1; kk < 8; ++kk) {
-              const uint32_t o = ((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4;
-              mma16_ss<true>(tm + COL_P, q + o, k + o, ID_QK);
+            for (int half = 0; half < 2; ++half) {  // 32 keys each
+              const uint32_t d = tm + COL_P + (static_cast<uint32_t>(half * 16) << 16), kh = k + (half * 32 * 128 >> 4);
+              mma16_ss<false>(d, q, kh, ID_QK);
+#pragma unroll
+              for (int kk = 1; kk < 8; ++kk) {
+                const uint32_t o = ((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4;
+                mma16_ss<true>(d, q + o, kh + o, ID_QK);
+              }
             }
             mma_commit(&m->bar_p);
             mma_commit(&m->empty_k[stage_k(i)]);
@@ -509,18 +521,21 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           if (n + 1 < all) qk(n + 1);
           if (!first) {
             // PV: tokens 16 s ... 16 s + 15 reach the rows from 16 s on
-            wait_bar(&m->v_ready, par, m);
+            wait_bar(&m->full_v[stage_v(n)], phase_v(n), m);
+            wait_bar(&m->v_ok[stage_v(n)], phase_v(n), m);
             tc_fence_after_sync();
             if (gave_up()) break;
             if (elect_one()) {
-              const uint32_t v = tm + COL_V, p = desc_lo_k(sbase + OFF_PH);
-              mma16_ts<false>(tm + COL_OT, v, p, idesc_bf16(128, 64));
+              const uint32_t v = desc_lo_mn(sbase + OFF_V, BLOCK) + stage_v(n) * (TILE >> 4), p = desc_lo_k(sbase + OFF_PH);
+              mma16_ss<false>(tm + COL_OT, v, p, idesc_bf16(128, 64, true, false));
 #pragma unroll
               for (int i = 1; i < 8; ++i) {
                 const uint32_t s = i & 3;
-                mma16_ts<true>(tm + COL_OT + 16 * s, v + 8 * s, p + (((i < 4 ? 0 : OFF_PL - OFF_PH) + s * 2048 + s * 32) >> 4), idesc_bf16(128, 64 - 16 * s));
+                mma16_ss<true>(tm + COL_OT + 16 * s, v + (s * 2048 >> 4), p + (((i < 4 ? 0 : OFF_PL - OFF_PH) + s * 2048 + s * 32) >> 4),
+                               idesc_bf16(128, 64 - 16 * s, true, false));
               }
               mma_commit(&m->bar_o[par]);
+              mma_commit(&m->empty_v[stage_v(n)]);
             }
             __syncwarp();
           }
@@ -597,7 +612,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
             float h, l;
             sum_at(8 * b + 7, h, l);
             if (block == b + 1) bh = h, bl = l;
-            if (block <= b) two(&w.col[b][2 * lane], ex2f((h - gh[0]) + (l - gl[0])), ex2f((h - gh[1]) + (l - gl[1])));
+            if (block <= b) two(&w.col[b * (b + 1) * 8 + 2 * lane], ex2f((h - gh[0]) + (l - gl[0])), ex2f((h - gh[1]) + (l - gl[1])));
           }
           two(&w.row[2 * lane], a.q_scale * ex2f((gh[0] - bh) + (gl[0] - bl)), a.q_scale * ex2f((gh[1] - bh) + (gl[1] - bl)));
         }
@@ -627,6 +642,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         *reinterpret_cast<uint32_t *>(p + 8 * 128 + (OFF_PL - OFF_PH)) = lo;
       };
       const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
+      const auto place = [](int s) { return static_cast<uint32_t>(s & 1) * 16u + (static_cast<uint32_t>(s >> 1) << 20); };  // of 16 columns of P
 #pragma unroll 1
       for (int it = 0; uni(take(it)); ++it) {
         const int tokens = m->items[it % RING].n;
@@ -640,11 +656,11 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           tc_fence_after_sync();
           const float r0 = w.row[t0], r1 = w.row[t1];
           const uint64_t rr0 = dpack2(r0, r0), rr1 = dpack2(r1, r1);
-          const float *const col = w.col[quad > 0 ? quad - 1 : 0] + 2 * tig;
+          const float *const col = w.col + quad * (quad - 1) * 8 + 2 * tig;
 #pragma unroll 1
           for (int s = 0; s < quad; ++s) {
             uint32_t p[8];
-            tmem_ld_16x256b(tp + 16 * s, p);
+            tmem_ld_16x256b(tp + place(s), p);
             const uint64_t c0 = *reinterpret_cast<const uint64_t *>(col + 16 * s), c1 = *reinterpret_cast<const uint64_t *>(col + 16 * s + 8);
             tmem_ld_wait();
             put(2 * s, dmul2(pair(p[0], p[1]), dmul2(rr0, c0)), dmul2(pair(p[2], p[3]), dmul2(rr1, c0)));
@@ -652,7 +668,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           }
           {
             uint32_t p[8];
-            tmem_ld_16x256b(tp + 16 * quad, p);
+            tmem_ld_16x256b(tp + place(quad), p);
             const float h0 = w.ghi[t0], l0 = w.glo[t0], h1 = w.ghi[t1], l1 = w.glo[t1];
             tmem_ld_wait();
 #pragma unroll
@@ -680,7 +696,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       const int quad = warp & 3, g = lane >> 2, tig = lane & 3;
       const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
       const int64_t v_stride = static_cast<int64_t>(a.H_v) * D;
-      unsigned char *const ost = smem + OFF_O + quad * 4096;
+      unsigned char *const ost = smem + OFF_O + quad * 2048;
 #pragma unroll 1
       for (int it = 0; uni(take(it)); ++it) {
         const int tokens = m->items[it % RING].n;
@@ -694,29 +710,26 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           wait_bar(&m->bar_o[n & 1], phase2(n), m);
           tc_fence_after_sync();
           const bool has_bad = w.has_bad[quad] != 0;
-#pragma unroll 1
-          for (int part = 0; part < 4; ++part) {  // 16 columns of d_v (part & 1), 32 tokens (part >> 1)
+          const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
+          uint32_t y[4][8];  // bf16 pairs along the tokens: 16 columns (part & 1), 32 tokens (part >> 1)
+#pragma unroll
+          for (int part = 0; part < 4; ++part) {
             const int half = part & 1, tb = part >> 1;
             uint32_t oi[16], ot[16];
             const uint32_t at = tl + (static_cast<uint32_t>(half * 16) << 16) + tb * 32;
             tmem_ld_16x256b(at + COL_OI, oi);
             tmem_ld_16x256b(at + COL_OT, ot);
             tmem_ld_wait();
-            if (part == 3) {
-              tc_fence_before_sync();
-              arrive_warp(&m->o_free, lane);
-            }
             const int v0 = half * 16 + g;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const int t = tb * 32 + 8 * j + 2 * tig;
               const uint64_t e = *reinterpret_cast<const uint64_t *>(&w.eg[t]);
-              const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
-              float2 y0 = dunpack2(dfma2(e, pair(oi[4 * j], oi[4 * j + 1]), pair(ot[4 * j], ot[4 * j + 1])));
-              float2 y1 = dunpack2(dfma2(e, pair(oi[4 * j + 2], oi[4 * j + 3]), pair(ot[4 * j + 2], ot[4 * j + 3])));
+              const float2 y0 = dunpack2(dfma2(e, pair(oi[4 * j], oi[4 * j + 1]), pair(ot[4 * j], ot[4 * j + 1])));
+              const float2 y1 = dunpack2(dfma2(e, pair(oi[4 * j + 2], oi[4 * j + 3]), pair(ot[4 * j + 2], ot[4 * j + 3])));
               if constexpr (sizeof(OT) == 2) {
-                ot[2 * j] = bf16x2(y0.x, y0.y);
-                ot[2 * j + 1] = bf16x2(y1.x, y1.y);
+                y[part][2 * j] = bf16x2(y0.x, y0.y);
+                y[part][2 * j + 1] = bf16x2(y1.x, y1.y);
               } else {
                 OT *const p = o + t * v_stride + v0;
                 if (t < rows) {
@@ -729,34 +742,36 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
                 }
               }
             }
-            if constexpr (sizeof(OT) == 2) {
+          }
+          tc_fence_before_sync();
+          arrive_warp(&m->o_free, lane);
+          if constexpr (sizeof(OT) == 2) {
 #pragma unroll
-              for (int j = 0; j < 4; j += 2) {
-                const int t = tb * 32 + 8 * (j + (lane >> 4)) + (lane & 7), ch = half * 2 + (lane >> 3 & 1);
-                stmatrix_x4_trans(smem_u32(ost) + t * 64 + ((ch ^ (t >> 1 & 3)) << 4), ot[2 * j], ot[2 * j + 1], ot[2 * j + 2], ot[2 * j + 3]);
+            for (int tb = 0; tb < 2; ++tb) {
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                for (int j = 0; j < 4; j += 2) {
+                  const uint32_t *const r = &y[2 * tb + half][2 * j];
+                  const int t = 8 * (j + (lane >> 4)) + (lane & 7), ch = half * 2 + (lane >> 3 & 1);
+                  stmatrix_x4_trans(smem_u32(ost) + t * 64 + ((ch ^ (t >> 1 & 3)) << 4), r[0], r[1], r[2], r[3]);
+                }
               }
+              __syncwarp();
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int t = i * 8 + (lane >> 2), ch = lane & 3;
+                const uint4 z = *reinterpret_cast<const uint4 *>(ost + t * 64 + ((ch ^ (t >> 1 & 3)) << 4));
+                if (32 * tb + t < rows) *reinterpret_cast<uint4 *>(o + (32 * tb + t) * v_stride + ch * 8) = z;
+              }
+              __syncwarp();
             }
           }
-          __syncwarp();
-          if (has_bad) {  // a lane per column
+          if (has_bad) {  // a lane per column, over what the warp has just stored
+            __syncwarp();
             const OT nan = static_cast<OT>(__int_as_float(0x7fffffff));
 #pragma unroll 1
-            for (int t = w.bad[quad * 32 + lane]; t < rows && t < C; ++t) {
-              if constexpr (sizeof(OT) == 2)
-                *reinterpret_cast<OT *>(ost + t * 64 + ((lane >> 3 ^ (t >> 1 & 3)) << 4) + (lane & 7) * 2) = nan;
-              else
-                o[t * v_stride + lane] = nan;
-            }
-            __syncwarp();
-          }
-          if constexpr (sizeof(OT) == 2) {
-#pragma unroll 2
-            for (int i8 = 0; i8 < 8; ++i8) {
-              const int t = i8 * 8 + (lane >> 2), ch = lane & 3;
-              const uint4 y = *reinterpret_cast<const uint4 *>(ost + t * 64 + ((ch ^ (t >> 1 & 3)) << 4));
-              if (t < rows) *reinterpret_cast<uint4 *>(o + t * v_stride + ch * 8) = y;
-            }
-            __syncwarp();
+            for (int t = w.bad[quad * 32 + lane]; t < rows && t < C; ++t) o[t * v_stride + lane] = nan;
           }
           arrive_warp(&m->dec_empty[slot(n)], lane);
         }
@@ -791,72 +806,66 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           __syncwarp();
         }
         wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-        if (n > 0) wait_bar(&m->bar_d[1], (n - 1) & 1u, m);  // KV of the chunk before has read its Vw
-        tc_fence_after_sync();
-        // A value that is none would reach every row of its column through products with weights that are zero, so it is taken out and
-        // remembered; 0 * x + sum is NaN from the first of them on.
         const auto load = [&](int s, int h, uint32_t (&r)[4]) {  // tokens 16 s ..., columns 16 h ... of this warp's: (column g (+ 8), tokens 2 tig, + 1 (+ 8))
           const int t = 16 * s + 8 * (lane >> 4) + (lane & 7), ch = (quad & 1) * 4 + h * 2 + (lane >> 3 & 1);
           ldmatrix_x4_trans(r[0], r[1], r[2], r[3], smem_u32(tile) + t * 128 + ((ch ^ (t & 7)) << 4));
         };
-        bool looked = false;
+        int first = C;  // of column `lane`: the first token with a value that is none
+        bool some = false;
 #pragma unroll 1
-        for (;;) {
-          __nv_bfloat162 probe = __floats2bfloat162_rn(0.f, 0.f);
-          const __nv_bfloat162 zero2 = probe;
-#pragma unroll 2
-          for (int i = 0; i < 8; ++i) {  // 16 columns of V (i & 1), 16 tokens (i >> 1)
-            const int s = i >> 1, h = i & 1;
-            uint32_t r[4];
-            load(s, h, r);
-            const uint64_t w0 = *reinterpret_cast<const uint64_t *>(&w.w[16 * s + 2 * tig]), w1 = *reinterpret_cast<const uint64_t *>(&w.w[16 * s + 8 + 2 * tig]);
-            uint64_t rest[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              probe = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&r[j]), zero2, probe);
-              rest[j] = dmul2(dpack2(bf_lo(r[j]), bf_hi(r[j])), j < 2 ? w0 : w1);
-            }
-#pragma unroll
-            for (int part = 0; part < VSPLIT; ++part) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) r[j] = take_bf16x2(rest[j]);
-              tmem_st_16x128b(tl + COL_VW + part * 32 + s * 8 + (static_cast<uint32_t>(h * 16) << 16), r);
-            }
-          }
-          const bool none = __isnan(__low2float(probe)) || __isnan(__high2float(probe));
-          if (!__any_sync(0xffffffffu, none) || looked) break;
-          looked = true;
-          int first = C;  // of column `lane`
-#pragma unroll 1
-          for (int t = rows - 1; t >= 0; --t) {
-            uint16_t *const e = reinterpret_cast<uint16_t *>(tile + t * 128 + ((((quad & 1) * 4 + (lane >> 3)) ^ (t & 7)) << 4) + (lane & 7) * 2);
-            if ((*e & 0x7F80u) == 0x7F80u) {
-              *e = 0;
-              first = t;
-            }
-          }
-          w.bad[quad * 32 + lane] = first;
-          fence_smem_to_async();
-          __syncwarp();
-        }
-        if (lane == 0) w.has_bad[quad] = looked;
-        tmem_st_wait();
-        tc_fence_before_sync();
-        arrive_warp(&m->w_ready, lane);
-        if (WITH_O) {
-          if (n > 0) wait_bar(&m->bar_o[(n - 1) & 1], phase2(n - 1), m);  // PV of the chunk before has read its V^T
+        for (int half = 0; half < 2; ++half) {  // 32 tokens each
+          if (n > 0) wait_bar(&m->bar_d[half], (n - 1) & 1u, m);  // KV of the chunk before has read this Vw
           tc_fence_after_sync();
-#pragma unroll 4
-          for (int i = 0; i < 8; ++i) {
-            uint32_t r[4];
-            load(i >> 1, i & 1, r);
-            tmem_st_16x128b(tl + COL_V + (i >> 1) * 8 + (static_cast<uint32_t>((i & 1) * 16) << 16), r);
+          // A value that is none would reach every row of its column through products with weights that are zero, so it is taken out and
+          // remembered; 0 * x + sum is NaN from the first of them on.
+          bool looked = false;
+#pragma unroll 1
+          for (;;) {
+            __nv_bfloat162 probe = __floats2bfloat162_rn(0.f, 0.f);
+            const __nv_bfloat162 zero2 = probe;
+#pragma unroll 2
+            for (int i = 0; i < 4; ++i) {  // 16 columns of V (i & 1), 16 tokens (i >> 1)
+              const int s = half * 2 + (i >> 1), h = i & 1;
+              uint32_t r[4];
+              load(s, h, r);
+              const uint64_t w0 = *reinterpret_cast<const uint64_t *>(&w.w[16 * s + 2 * tig]), w1 = *reinterpret_cast<const uint64_t *>(&w.w[16 * s + 8 + 2 * tig]);
+              uint64_t rest[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                probe = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&r[j]), zero2, probe);
+                rest[j] = dmul2(dpack2(bf_lo(r[j]), bf_hi(r[j])), j < 2 ? w0 : w1);
+              }
+#pragma unroll
+              for (int part = 0; part < VSPLIT; ++part) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = take_bf16x2(rest[j]);
+                tmem_st_16x128b(tl + COL_VW + part * 32 + s * 8 + (static_cast<uint32_t>(h * 16) << 16), r);
+              }
+            }
+            const bool none = __isnan(__low2float(probe)) || __isnan(__high2float(probe));
+            if (!__any_sync(0xffffffffu, none) || looked) break;
+            looked = some = true;
+#pragma unroll 1
+            for (int t = min(rows, half * 32 + 32) - 1; t >= half * 32; --t) {
+              uint16_t *const e = reinterpret_cast<uint16_t *>(tile + t * 128 + ((((quad & 1) * 4 + (lane >> 3)) ^ (t & 7)) << 4) + (lane & 7) * 2);
+              if ((*e & 0x7F80u) == 0x7F80u) {
+                *e = 0;
+                if (first == C || first > t) first = t;
+              }
+            }
+            fence_smem_to_async();
+            __syncwarp();
+          }
+          if (half == 1) {
+            if (some) w.bad[quad * 32 + lane] = first;
+            if (lane == 0) w.has_bad[quad] = some;
           }
           tmem_st_wait();
           tc_fence_before_sync();
-          arrive_warp(&m->v_ready, lane);
+          arrive_warp(&m->w_ready[half], lane);
         }
         if (lane == 0) {
+          mbar_arrive(&m->v_ok[stage_v(n)]);
           mbar_arrive(&m->empty_v[stage_v(n)]);
           mbar_arrive(&m->dec_empty[slot(n)]);
         }
@@ -868,25 +877,51 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     const int quad = warp & 3, half = (warp - WARP_S) >> 2;
     const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
     const int v = quad * 32 + lane, k0 = half * 64;
-    int ns = 0;  // states taken
+    float *const mine = reinterpret_cast<float *>(smem + OFF_S) + k0 * D + v;  // this thread's place in the staged state
+    const bool leader = warp == WARP_S && lane == 0;
+    uint64_t S[32];
+    int ns = 0;               // states taken
+    float *dst = nullptr;     // where the last unit's state goes
+    bool leaving = false;     // the leader: it is on its way
+    const auto left = [&]() {
+      if (leaving) bulk_wait_read();
+      leaving = false;
+      mbar_arrive(&m->s_empty);
+    };
 #pragma unroll 1
     for (int it = 0;; ++it) {
-      if (any_of<2, 256>(!take(it))) break;  // (one answer for all eight warps)
-      const Item x = m->items[it % RING];
-      release(it);
-      uint64_t S[32];
-      const int64_t seg_at = (static_cast<int64_t>(x.unit) * sp.nseg + x.seg) * (D * D);
-      if (x.from != 0) {
-        wait_bar(&m->s_full, ns & 1u, m);
-        const float *const src = reinterpret_cast<const float *>(smem + OFF_S) + k0 * D + v;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) S[j] = dpack2(src[2 * j * D], src[(2 * j + 1) * D]);
-        arrive_warp(&m->s_empty, lane);
-        ++ns;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) S[j] = 0;
+      const bool end = any_of<2, 256>(!take(it));  // (one answer for all eight warps)
+      if (end && any_of<2, 256>(m->abort_flag != 0)) break;  // after a time-out a unit is not written at all
+      Item x;
+      if (!end) {
+        x = m->items[it % RING];
+        release(it);
       }
+      const bool from = !end && x.from != 0;
+      if (from) wait_bar(&m->s_full, ns++ & 1u, m);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        float a0 = 0.f, a1 = 0.f;
+        if (from) {
+          a0 = mine[2 * j * D];
+          a1 = mine[(2 * j + 1) * D];
+        }
+        if (dst) {
+          const float2 y = dunpack2(S[j]);
+          mine[2 * j * D] = y.x;
+          mine[(2 * j + 1) * D] = y.y;
+        }
+        S[j] = dpack2(a0, a1);
+      }
+      fence_smem_to_async();
+      asm volatile("bar.sync 2, 256;" ::: "memory");
+      if (leader && dst) {
+        for (int i = 0; i < 4; ++i) bulk_store(dst + i * (D * D / 4), sbase + OFF_S + i * (D * D), D * D);
+        bulk_commit();
+        leaving = true;
+      }
+      if (end) break;
+      const int64_t seg_at = (static_cast<int64_t>(x.unit) * sp.nseg + x.seg) * (D * D);
       float decay = 1.f;
 #pragma unroll 1
       for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
@@ -909,42 +944,34 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
         float f = w.all;
         decay *= f;
-        wait_bar(&m->bar_d[half], n & 1u, m);
+        wait_bar(&m->bar_d[1], n & 1u, m);
         tc_fence_after_sync();
         if (w.has_bad[quad] != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
         const uint64_t ff = dpack2(f, f);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           uint32_t d[16];
-          tmem_ld16(tl + COL_D + b * 16, d);
+          tmem_ld16(tl + COL_D + k0 + b * 16, d);
           tmem_ld_wait();
 #pragma unroll
           for (int j = 0; j < 8; ++j)
             S[b * 8 + j] = dfma2(S[b * 8 + j], ff, dpack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
         }
         tc_fence_before_sync();
-        arrive_warp(&m->d_free[half], lane);
+        arrive_warp(&m->d_free, lane);
         if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
+        if (leader && c == 0) left();
       }
-      // a unit is written as a whole or, after a time-out, not at all
-      if (any_of<2, 256>(m->abort_flag != 0)) break;
-      float *dst = nullptr;
+      if (leader && chunks_of(x.n) == 0) left();
+      dst = nullptr;
       if (sp.phase == 1) {
         dst = sp.seg_state + seg_at + D * D;
-        if (warp == WARP_S && lane == 0) sp.seg_decay[static_cast<int64_t>(x.unit) * sp.nseg + x.seg] = decay;
+        if (leader) sp.seg_decay[static_cast<int64_t>(x.unit) * sp.nseg + x.seg] = decay;
       } else if (x.write) {
         dst = a.state + x.state;
       }
-      if (dst) {
-        dst += k0 * D + v;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const float2 y = dunpack2(S[j]);
-          dst[2 * j * D] = y.x;
-          dst[(2 * j + 1) * D] = y.y;
-        }
-      }
     }
+    if (leader) bulk_wait();
   }
   stream_order_release();
   tc_fence_before_sync();

@@ -71,6 +71,14 @@ __device__ __forceinline__ void bulk_load(uint32_t dst_smem, const void *src, ui
                : "memory");
 }
 
+// Untiled store, likewise; the issuing thread commits it to a group and waits for that.
+__device__ __forceinline__ void bulk_store(void *dst, uint32_t src_smem, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src_smem), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }  // the sources may be overwritten
+__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 // One lane of a converged warp.  The compiler knows that a branch on this predicate runs with a single active thread, so the
 // tcgen05 instructions below it take their descriptors straight from uniform registers; behind `lane == 0` it has to allow
 // for several active threads with different operands and serialises every one of them in a loop.
