@@ -6,14 +6,14 @@
 // Products, C = 64 tokens, everything transposed so that d_v is the M index (the accumulators' 128 lanes):
 //   QK   Q K^T               -> P before its weights    smem x smem, M = 64
 //   QS   S_0^T Q^T           -> outputs from the state   tmem x smem   (S_0 as a bf16 pair)
-//   PV   V^T P^T             -> outputs inside the chunk  smem x smem   (P as a pair; only the rows a slice of i can reach)
+//   PV   V^T P^T             -> outputs inside the chunk  tmem x smem   (P as a pair; only the rows a slice of i can reach)
 //   KV   Vw^T K              -> what the chunk adds        tmem x smem   (Vw in three parts)
 // V, K and Q are exact in bf16 and are used as they land; V and K are read with their token index as K, which for 16-bit operands is
 // the same tile.  A value in n parts of bf16 (x rounded, the rest rounded, ...) is good to 2^-8n: rounded once, an operand would cost
 // the outputs as much as their own rounding does, and the fp32 state its last 16 bits; in pairs the state was good to 2.4e-6, in three
 // parts it is as good as fp32.
 // What the products read of shared memory counts: one of 128 x 128 x 16 with both operands there takes 65 cycles, 64 of which it reads,
-// and the warps' own accesses go through the same pipe.  So the operands that are made here (Vw, the state) go to tensor memory; with
+// and the warps' own accesses go through the same pipe.  So the operands that are made here (V^T, Vw, the state) go to tensor memory; with
 // weights on K instead, written to shared memory, a chunk took 15 % longer.
 //
 // One thread block per SM walks over (request, layer, head) units, or over segments of long ones; roles of its warps:
@@ -43,8 +43,9 @@ using namespace tc5;
 
 constexpr int C = 64, D = 128;
 constexpr int kSms = 148;
-constexpr int NS_K = 3, NS_Q = 2, NS_V = 3;  // stages of K, Q, V
-constexpr int VSPLIT = 3;                    // parts of Vw
+constexpr int NS_K = 3, NS_Q = 3, NS_V = 2;  // stages of K, Q, V: from the end of a tile's use, the next one takes 3 k cycles to land
+constexpr int VSPLIT = 2;                    // parts of Vw
+constexpr int WBUF = 2;                      // Vw goes through tensor memory 16 tokens at a time, in this many places
 constexpr int RING = 4;  // chunks whose weights are kept, and units that are looked up ahead
 constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_MMA_O = 3, WARP_P = 4, WARP_O = 8, WARP_V = 12, WARP_S = 16, NWARP = 24;
 // Registers of a thread, by groups of four warps: what the launch gives each (65,536 over all threads, in steps of 8), and how the roles
@@ -64,9 +65,8 @@ constexpr uint32_t OFF_PH = OFF_S + D * D * 4, OFF_PL = OFF_PH + C * C * 2;
 constexpr uint32_t OFF_O = OFF_PL + C * C * 2;  // [4 warps][32 tokens][32 columns] bf16 on their way out
 constexpr uint32_t OFF_MISC = OFF_O + TILE / 2;
 
-// Tensor memory.  P has M = 64 and takes 16 lanes of each quadrant, so its columns from 32 on lie in the other 16.
-constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 288, COL_OT = 352, COL_VW = 416;
-static_assert(COL_VW + 32 * VSPLIT <= 512);
+constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 320, COL_OT = 384, COL_V = 448, COL_VW = 480;
+static_assert(COL_VW + 8 * VSPLIT * WBUF <= 512);
 
 struct alignas(16) Weights {  // of one chunk (read in pairs)
   float ghi[C], glo[C];  // G_t = ghi + glo, ghi a multiple of 2^-6: differences of ghi are exact
@@ -97,8 +97,9 @@ struct Misc {
   uint64_t v_ok[NS_V];                           // V has been looked at
   uint64_t s_full, s_empty;                      // the next unit's state has landed; its place is free again
   uint64_t dec_full[RING], dec_empty[RING], item_full[RING], item_empty[RING];
-  uint64_t bar_p, bar_s, bar_o[2], bar_d[2];     // tensor core: QK, QS, PV (by chunk parity), KV of 32 tokens and of the others have completed
-  uint64_t w_ready[2], p_ready, s_ready;         // Vw of 32 tokens and of the others, P, the state are in place
+  uint64_t bar_p, bar_s, bar_o[2], bar_d;        // tensor core: QK, QS, PV (by chunk parity), KV of a chunk have completed
+  uint64_t bar_w[WBUF], w_ready[WBUF];           // KV of 16 tokens has completed; their Vw is in place
+  uint64_t p_ready, s_ready;                     // P and V^T, the state are in place
   uint64_t o_free, d_free;                       // accumulators have been read
   uint64_t drain[2];
   uint32_t tmem_base;
@@ -195,6 +196,13 @@ __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.al
 template <int N>
 __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
+// Where a lane's row of V is for ldmatrix: tokens 16 s ..., columns 32 quad + 16 h ... of a tile; a thread then holds column
+// g (+ 8), tokens 2 tig, + 1 (+ 8).
+__device__ __forceinline__ uint32_t v_place(uint32_t tile, int quad, int s, int h, int lane) {
+  const int t = 16 * s + 8 * (lane >> 4) + (lane & 7), ch = (quad & 1) * 4 + h * 2 + (lane >> 3 & 1);
+  return tile + (quad >> 1) * BLOCK + t * 128 + ((ch ^ (t & 7)) << 4);
+}
+
 __device__ __forceinline__ int chunks_of(int n) { return (n + C - 1) / C; }
 // Segments that a request of `chunks` chunks really has.
 __device__ __forceinline__ int segments_of(const Split &sp, int chunks) {
@@ -265,14 +273,17 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     }
     for (int i = 0; i < NS_V; ++i) {
       mbar_init(&m->full_v[i], 1);
-      mbar_init(&m->empty_v[i], WITH_O ? 5 : 4);  // Vw's warps; PV
+      mbar_init(&m->empty_v[i], WITH_O ? 8 : 4);  // Vw's warps; V^T's
       mbar_init(&m->v_ok[i], 4);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&m->bar_o[i], 1);
-      mbar_init(&m->bar_d[i], 1);
+    }
+    for (int i = 0; i < WBUF; ++i) {
+      mbar_init(&m->bar_w[i], 1);
       mbar_init(&m->w_ready[i], 4);
     }
+    mbar_init(&m->bar_d, 1);
     mbar_init(&m->d_free, 8);
     mbar_init(&m->s_full, 1);
     mbar_init(&m->s_empty, 1);
@@ -334,6 +345,8 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
   const auto phase_q = [](int i) { return static_cast<uint32_t>(i) / NS_Q & 1u; };
   const auto stage_v = [](int i) { return static_cast<uint32_t>(i) % NS_V; };
   const auto phase_v = [](int i) { return static_cast<uint32_t>(i) / NS_V & 1u; };
+  const auto buf_w = [](int i) { return static_cast<uint32_t>(i) % WBUF; };  // of 16 tokens
+  const auto phase_w = [](int i) { return static_cast<uint32_t>(i) / WBUF & 1u; };
   const auto phase2 = [](int i) { return static_cast<uint32_t>(i) >> 1 & 1u; };  // of what there are two of, by chunk parity
   const auto slot = [](int i) { return static_cast<uint32_t>(i) % RING; };
   const auto slot_phase = [](int i) { return static_cast<uint32_t>(i) / RING & 1u; };
@@ -448,26 +461,30 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           wait_bar(&m->full_k[st], phase_k(n), m);
           if (n > 0) wait_bar(&m->d_free, par ^ 1u, m);
 #pragma unroll 1
-          for (int half = 0; half < 2; ++half) {  // 32 tokens each, so that the next Vw can follow behind
-            wait_bar(&m->w_ready[half], par, m);
+          for (int s = 0; s < 4; ++s) {
+            const int i = 4 * n + s;
+            wait_bar(&m->w_ready[buf_w(i)], phase_w(i), m);
             tc_fence_after_sync();
             if (gave_up()) break;
             if (elect_one()) {
-              const uint32_t v = tm + COL_VW + half * 16, k = desc_lo_mn(sbase + OFF_K, BLOCK) + (st * TILE + half * (2 * 2048) >> 4);
-              if (half == 0)
+              const uint32_t v = tm + COL_VW + buf_w(i) * (8 * VSPLIT), k = desc_lo_mn(sbase + OFF_K, BLOCK) + (st * TILE + s * 2048 >> 4);
+              if (s == 0)
                 mma16_ts<false>(tm + COL_D, v, k, ID_KV);
               else
                 mma16_ts<true>(tm + COL_D, v, k, ID_KV);
 #pragma unroll
-              for (int i = 1; i < 2 * VSPLIT; ++i) mma16_ts<true>(tm + COL_D, v + (i >> 1) * 32 + (i & 1) * 8, k + ((i & 1) * 2048 >> 4), ID_KV);
-              mma_commit(&m->bar_d[half]);
-              if (half == 1) mma_commit(&m->empty_k[st]);
+              for (int part = 1; part < VSPLIT; ++part) mma16_ts<true>(tm + COL_D, v + part * 8, k, ID_KV);
+              mma_commit(&m->bar_w[buf_w(i)]);
+              if (s == 3) {
+                mma_commit(&m->bar_d);
+                mma_commit(&m->empty_k[st]);
+              }
             }
             __syncwarp();
           }
         }
       } else if constexpr (WITH_O) {
-        constexpr uint32_t ID_QK = idesc_bf16(64, 32), ID_QS = idesc_bf16(128, 64);
+        constexpr uint32_t ID_QK = idesc_bf16(64, 64), ID_QS = idesc_bf16(128, 64);
         const auto qk = [&](int i) {
           wait_bar(&m->full_k[stage_k(i)], phase_k(i), m);
           wait_bar(&m->full_q[stage_q(i)], phase_q(i), m);
@@ -475,15 +492,11 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           if (gave_up()) return;
           if (elect_one()) {
             const uint32_t q = desc_lo_k(sbase + OFF_Q) + stage_q(i) * (TILE >> 4), k = desc_lo_k(sbase + OFF_K) + stage_k(i) * (TILE >> 4);
+            mma16_ss<false>(tm + COL_P, q, k, ID_QK);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {  // 32 keys each
-              const uint32_t d = tm + COL_P + (static_cast<uint32_t>(half * 16) << 16), kh = k + (half * 32 * 128 >> 4);
-              mma16_ss<false>(d, q, kh, ID_QK);
-#pragma unroll
-              for (int kk = 1; kk < 8; ++kk) {
-                const uint32_t o = ((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4;
-                mma16_ss<true>(d, q + o, kh + o, ID_QK);
-              }
+            for (int kk = 1; kk < 8; ++kk) {
+              const uint32_t o = ((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4;
+              mma16_ss<true>(tm + COL_P, q + o, k + o, ID_QK);
             }
             mma_commit(&m->bar_p);
             mma_commit(&m->empty_k[stage_k(i)]);
@@ -516,26 +529,22 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
             }
             __syncwarp();
             wait_bar(&m->p_ready, par, m);
+            tc_fence_after_sync();
+            if (gave_up()) break;
           }
           // the next chunk's QK ahead of this one's PV: its accumulator has been read, and the next P is waited for longest
           if (n + 1 < all) qk(n + 1);
           if (!first) {
             // PV: tokens 16 s ... 16 s + 15 reach the rows from 16 s on
-            wait_bar(&m->full_v[stage_v(n)], phase_v(n), m);
-            wait_bar(&m->v_ok[stage_v(n)], phase_v(n), m);
-            tc_fence_after_sync();
-            if (gave_up()) break;
             if (elect_one()) {
-              const uint32_t v = desc_lo_mn(sbase + OFF_V, BLOCK) + stage_v(n) * (TILE >> 4), p = desc_lo_k(sbase + OFF_PH);
-              mma16_ss<false>(tm + COL_OT, v, p, idesc_bf16(128, 64, true, false));
+              const uint32_t v = tm + COL_V, p = desc_lo_k(sbase + OFF_PH);
+              mma16_ts<false>(tm + COL_OT, v, p, idesc_bf16(128, 64));
 #pragma unroll
               for (int i = 1; i < 8; ++i) {
                 const uint32_t s = i & 3;
-                mma16_ss<true>(tm + COL_OT + 16 * s, v + (s * 2048 >> 4), p + (((i < 4 ? 0 : OFF_PL - OFF_PH) + s * 2048 + s * 32) >> 4),
-                               idesc_bf16(128, 64 - 16 * s, true, false));
+                mma16_ts<true>(tm + COL_OT + 16 * s, v + 8 * s, p + (((i < 4 ? 0 : OFF_PL - OFF_PH) + s * 2048 + s * 32) >> 4), idesc_bf16(128, 64 - 16 * s));
               }
               mma_commit(&m->bar_o[par]);
-              mma_commit(&m->empty_v[stage_v(n)]);
             }
             __syncwarp();
           }
@@ -642,7 +651,6 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         *reinterpret_cast<uint32_t *>(p + 8 * 128 + (OFF_PL - OFF_PH)) = lo;
       };
       const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
-      const auto place = [](int s) { return static_cast<uint32_t>(s & 1) * 16u + (static_cast<uint32_t>(s >> 1) << 20); };  // of 16 columns of P
 #pragma unroll 1
       for (int it = 0; uni(take(it)); ++it) {
         const int tokens = m->items[it % RING].n;
@@ -660,7 +668,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
 #pragma unroll 1
           for (int s = 0; s < quad; ++s) {
             uint32_t p[8];
-            tmem_ld_16x256b(tp + place(s), p);
+            tmem_ld_16x256b(tp + 16 * s, p);
             const uint64_t c0 = *reinterpret_cast<const uint64_t *>(col + 16 * s), c1 = *reinterpret_cast<const uint64_t *>(col + 16 * s + 8);
             tmem_ld_wait();
             put(2 * s, dmul2(pair(p[0], p[1]), dmul2(rr0, c0)), dmul2(pair(p[2], p[3]), dmul2(rr1, c0)));
@@ -668,7 +676,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           }
           {
             uint32_t p[8];
-            tmem_ld_16x256b(tp + place(quad), p);
+            tmem_ld_16x256b(tp + 16 * quad, p);
             const float h0 = w.ghi[t0], l0 = w.glo[t0], h1 = w.ghi[t1], l1 = w.glo[t1];
             tmem_ld_wait();
 #pragma unroll
@@ -682,9 +690,19 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
                   dpack2(at(2, t1, i, h1, l1, hi.x, lo.x), at(3, t1, i + 1, h1, l1, hi.y, lo.y)));
             }
           }
+          // V^T, 32 columns of V per warp, as it is (once it has been looked at)
+          wait_bar(&m->v_ok[stage_v(n)], phase_v(n), m);
+#pragma unroll 2
+          for (int i = 0; i < 8; ++i) {
+            uint32_t r[4];
+            ldmatrix_x4_trans(r[0], r[1], r[2], r[3], v_place(smem_u32(smem + OFF_V + stage_v(n) * TILE), quad, i >> 1, i & 1, lane));
+            tmem_st_16x128b(tp - COL_P + COL_V + (i >> 1) * 8 + (static_cast<uint32_t>((i & 1) * 16) << 16), r);
+          }
+          tmem_st_wait();
           fence_smem_to_async();
           tc_fence_before_sync();
           arrive_warp(&m->p_ready, lane);
+          if (lane == 0) mbar_arrive(&m->empty_v[stage_v(n)]);
           if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
         }
       }
@@ -806,16 +824,15 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           __syncwarp();
         }
         wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-        const auto load = [&](int s, int h, uint32_t (&r)[4]) {  // tokens 16 s ..., columns 16 h ... of this warp's: (column g (+ 8), tokens 2 tig, + 1 (+ 8))
-          const int t = 16 * s + 8 * (lane >> 4) + (lane & 7), ch = (quad & 1) * 4 + h * 2 + (lane >> 3 & 1);
-          ldmatrix_x4_trans(r[0], r[1], r[2], r[3], smem_u32(tile) + t * 128 + ((ch ^ (t & 7)) << 4));
-        };
         int first = C;  // of column `lane`: the first token with a value that is none
         bool some = false;
 #pragma unroll 1
-        for (int half = 0; half < 2; ++half) {  // 32 tokens each
-          if (n > 0) wait_bar(&m->bar_d[half], (n - 1) & 1u, m);  // KV of the chunk before has read this Vw
+        for (int s = 0; s < 4; ++s) {  // 16 tokens each
+          const int i = 4 * n + s;
+          if (i >= WBUF) wait_bar(&m->bar_w[buf_w(i)], phase_w(i) ^ 1u, m);  // KV has read what was there
           tc_fence_after_sync();
+          const uint64_t w0 = *reinterpret_cast<const uint64_t *>(&w.w[16 * s + 2 * tig]), w1 = *reinterpret_cast<const uint64_t *>(&w.w[16 * s + 8 + 2 * tig]);
+          const uint32_t to = tl + COL_VW + buf_w(i) * (8 * VSPLIT);
           // A value that is none would reach every row of its column through products with weights that are zero, so it is taken out and
           // remembered; 0 * x + sum is NaN from the first of them on.
           bool looked = false;
@@ -823,12 +840,10 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           for (;;) {
             __nv_bfloat162 probe = __floats2bfloat162_rn(0.f, 0.f);
             const __nv_bfloat162 zero2 = probe;
-#pragma unroll 2
-            for (int i = 0; i < 4; ++i) {  // 16 columns of V (i & 1), 16 tokens (i >> 1)
-              const int s = half * 2 + (i >> 1), h = i & 1;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {  // 16 columns of V each
               uint32_t r[4];
-              load(s, h, r);
-              const uint64_t w0 = *reinterpret_cast<const uint64_t *>(&w.w[16 * s + 2 * tig]), w1 = *reinterpret_cast<const uint64_t *>(&w.w[16 * s + 8 + 2 * tig]);
+              ldmatrix_x4_trans(r[0], r[1], r[2], r[3], v_place(smem_u32(smem + OFF_V + stage_v(n) * TILE), quad, s, h, lane));
               uint64_t rest[4];
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
@@ -839,14 +854,14 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
               for (int part = 0; part < VSPLIT; ++part) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) r[j] = take_bf16x2(rest[j]);
-                tmem_st_16x128b(tl + COL_VW + part * 32 + s * 8 + (static_cast<uint32_t>(h * 16) << 16), r);
+                tmem_st_16x128b(to + part * 8 + (static_cast<uint32_t>(h * 16) << 16), r);
               }
             }
             const bool none = __isnan(__low2float(probe)) || __isnan(__high2float(probe));
             if (!__any_sync(0xffffffffu, none) || looked) break;
             looked = some = true;
 #pragma unroll 1
-            for (int t = min(rows, half * 32 + 32) - 1; t >= half * 32; --t) {
+            for (int t = min(rows, 16 * s + 16) - 1; t >= 16 * s; --t) {
               uint16_t *const e = reinterpret_cast<uint16_t *>(tile + t * 128 + ((((quad & 1) * 4 + (lane >> 3)) ^ (t & 7)) << 4) + (lane & 7) * 2);
               if ((*e & 0x7F80u) == 0x7F80u) {
                 *e = 0;
@@ -856,13 +871,13 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
             fence_smem_to_async();
             __syncwarp();
           }
-          if (half == 1) {
+          if (s == 3) {
             if (some) w.bad[quad * 32 + lane] = first;
             if (lane == 0) w.has_bad[quad] = some;
           }
           tmem_st_wait();
           tc_fence_before_sync();
-          arrive_warp(&m->w_ready[half], lane);
+          arrive_warp(&m->w_ready[buf_w(i)], lane);
         }
         if (lane == 0) {
           mbar_arrive(&m->v_ok[stage_v(n)]);
@@ -900,18 +915,24 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       const bool from = !end && x.from != 0;
       if (from) wait_bar(&m->s_full, ns++ & 1u, m);
 #pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        float a0 = 0.f, a1 = 0.f;
+      for (int b = 0; b < 4; ++b) {
+        float next[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) next[j] = 0.f;
         if (from) {
-          a0 = mine[2 * j * D];
-          a1 = mine[(2 * j + 1) * D];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) next[j] = mine[(16 * b + j) * D];
         }
         if (dst) {
-          const float2 y = dunpack2(S[j]);
-          mine[2 * j * D] = y.x;
-          mine[(2 * j + 1) * D] = y.y;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float2 y = dunpack2(S[8 * b + j]);
+            mine[(16 * b + 2 * j) * D] = y.x;
+            mine[(16 * b + 2 * j + 1) * D] = y.y;
+          }
         }
-        S[j] = dpack2(a0, a1);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) S[8 * b + j] = dpack2(next[2 * j], next[2 * j + 1]);
       }
       fence_smem_to_async();
       asm volatile("bar.sync 2, 256;" ::: "memory");
@@ -944,7 +965,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
         float f = w.all;
         decay *= f;
-        wait_bar(&m->bar_d[1], n & 1u, m);
+        wait_bar(&m->bar_d, n & 1u, m);
         tc_fence_after_sync();
         if (w.has_bad[quad] != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
         const uint64_t ff = dpack2(f, f);
