@@ -2,30 +2,27 @@
 //
 // With G_t the sum of the log-decays of a chunk up to its token t (log2 units here), S_0 the state at its start:
 //   O   = q_scale (diag(e^G) Q S_0 + P V),   P_ti = e^{G_t - G_i} q_t . k_i for i <= t, else 0
-//   S_C = e^{G_C} S_0 + K^T Vw,              Vw_i = e^{G_C - G_i} v_i
+//   S_C = e^{G_C} S_0 + Kw^T V,               Kw_i = e^{G_C - G_i} k_i
 // Products, C = 64 tokens, everything transposed so that d_v is the M index (the accumulators' 128 lanes):
 //   QK   Q K^T               -> P before its weights    smem x smem, M = 64
 //   QS   S_0^T Q^T           -> outputs from the state   tmem x smem   (S_0 as a bf16 pair)
 //   PV   V^T P^T             -> outputs inside the chunk  tmem x smem   (P as a pair; only the rows a slice of i can reach)
-//   KV   Vw^T K              -> what the chunk adds        tmem x smem   (Vw in three parts)
-// V, K and Q are exact in bf16 and are used as they land; V and K are read with their token index as K, which for 16-bit operands is
-// the same tile.  A value in n parts of bf16 (x rounded, the rest rounded, ...) is good to 2^-8n: rounded once, an operand would cost
-// the outputs as much as their own rounding does, and the fp32 state its last 16 bits; in pairs the state was good to 2.4e-6, in three
-// parts it is as good as fp32.
-// What the products read of shared memory counts: one of 128 x 128 x 16 with both operands there takes 65 cycles, 64 of which it reads,
-// and the warps' own accesses go through the same pipe.  So the operands that are made here (V^T, Vw, the state) go to tensor memory; with
-// weights on K instead, written to shared memory, a chunk took 15 % longer.
+//   KV   V^T Kw              -> what the chunk adds        tmem x smem   (Kw in three parts)
+// V, K and Q are exact in bf16: Q and K are used as they land, V^T goes to tensor memory (the tensor core's reads of shared memory are
+// what bounds the products: a product of 128 x 128 x 16 takes 65 cycles, 64 of which it reads both operands from there).
+// A value in n parts of bf16 (x rounded, the rest rounded, ...) is good to 2^-8n: rounded once, an operand would cost the outputs
+// as much as their own rounding does, and the fp32 state its last 16 bits; in pairs the state is good to 2.4e-6, in three parts it is
+// as good as fp32.
 //
 // One thread block per SM walks over (request, layer, head) units, or over segments of long ones; roles of its warps:
-//   0       looks up the units; TMA: tiles of K, Q, V, two or three chunks ahead, and the next unit's state
+//   0       looks up the units; TMA: tiles of K, Q, V, three chunks ahead
 //   1, 3    issue the products: KV; QK, QS and PV (issue alone, at 60 to 100 cycles a product, filled one warp's time)
 //   2       sums of log-decays (as pairs of fp32), weights of a chunk
 //   4 - 7   P: out of tensor memory, weighted, into its operand tiles
 //   8 - 11  outputs
-//   12 - 15 Vw; looks at V for values that are none
-//   16 - 23 the state, in fp32 registers: a thread has 64 key channels of one column.  Between two units they exchange the last state with
-//           the next one's, which has landed in shared memory by then, and it leaves from there: stored from registers, 64 KB
-//           took 3.5 k cycles, which the products waited for
+//   12 - 15 Kw
+//   16 - 23 the state, in fp32 registers: a thread has 64 key channels of one column; V^T, which is
+//           looked at there for values that are none
 // The only chain from chunk to chunk is S <- e^{G_C} S + (KV), 64 packed multiply-adds per thread, and its bf16 pair on the way
 // to QS; KV itself does not depend on the state.
 #include <cuda.h>
@@ -43,15 +40,14 @@ using namespace tc5;
 
 constexpr int C = 64, D = 128;
 constexpr int kSms = 148;
-constexpr int NS_K = 3, NS_Q = 3, NS_V = 2;  // stages of K, Q, V: from the end of a tile's use, the next one takes 3 k cycles to land
-constexpr int VSPLIT = 2;                    // parts of Vw
-constexpr int WBUF = 2;                      // Vw goes through tensor memory 16 tokens at a time, in this many places
+constexpr int NS = 3, NS_V = 2;  // stages of K and Q; of V
+constexpr int KSPLIT = 3;        // parts of Kw
 constexpr int RING = 4;  // chunks whose weights are kept, and units that are looked up ahead
-constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_MMA_O = 3, WARP_P = 4, WARP_O = 8, WARP_V = 12, WARP_S = 16, NWARP = 24;
+constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_MMA_O = 3, WARP_P = 4, WARP_O = 8, WARP_K = 12, WARP_S = 16, NWARP = 24;
 // Registers of a thread, by groups of four warps: what the launch gives each (65,536 over all threads, in steps of 8), and how the roles
 // share it out.
-constexpr int REGS = 80, REGS_0 = 56, REGS_P = 72, REGS_O = 72, REGS_V = 72, REGS_S = 104;
-static_assert(NWARP * 32 * REGS <= 65536 && REGS_0 + REGS_P + REGS_O + REGS_V + 2 * REGS_S <= NWARP / 4 * REGS);
+constexpr int REGS = 80, REGS_0 = 56, REGS_P = 72, REGS_O = 72, REGS_K = 72, REGS_S = 104;
+static_assert(NWARP * 32 * REGS <= 65536 && REGS_0 + REGS_P + REGS_O + REGS_K + 2 * REGS_S <= NWARP / 4 * REGS);
 constexpr int NT = NWARP * 32;
 constexpr int kMaxSorted = 512;  // entries (requests x segments) that are taken longest first
 constexpr uint32_t kMaxPolls = 1u << 22, kPollNs = 1000;  // a poll sleeps for up to that long: the warps that wait leave the issue slots to the others
@@ -59,14 +55,13 @@ constexpr uint32_t kStatusWords = kDecayStatusWords / 2;  // per launch: one wor
 
 constexpr uint32_t TILE = C * D * 2;  // 64 tokens x 128 channels: two blocks of [64 rows][128 bytes]
 constexpr uint32_t BLOCK = TILE / 2;
-constexpr uint32_t OFF_K = 0, OFF_Q = OFF_K + NS_K * TILE, OFF_V = OFF_Q + NS_Q * TILE;
-constexpr uint32_t OFF_S = OFF_V + NS_V * TILE;  // the next unit's state
-constexpr uint32_t OFF_PH = OFF_S + D * D * 4, OFF_PL = OFF_PH + C * C * 2;
-constexpr uint32_t OFF_O = OFF_PL + C * C * 2;  // [4 warps][32 tokens][32 columns] bf16 on their way out
-constexpr uint32_t OFF_MISC = OFF_O + TILE / 2;
+constexpr uint32_t OFF_K = 0, OFF_Q = OFF_K + NS * TILE, OFF_V = OFF_Q + NS * TILE;
+constexpr uint32_t OFF_KW = OFF_V + NS_V * TILE;  // [KSPLIT]
+constexpr uint32_t OFF_PH = OFF_KW + KSPLIT * TILE, OFF_PL = OFF_PH + C * C * 2;
+constexpr uint32_t OFF_O = OFF_PL + C * C * 2;  // [4 warps][64 tokens][32 columns] bf16 on their way out
+constexpr uint32_t OFF_MISC = OFF_O + TILE;
 
-constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 320, COL_OT = 384, COL_V = 448, COL_VW = 480;
-static_assert(COL_VW + 8 * VSPLIT * WBUF <= 512);
+constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 320, COL_OT = 384, COL_V = 448;  // (V^T twice, by chunk parity)
 
 struct alignas(16) Weights {  // of one chunk (read in pairs)
   float ghi[C], glo[C];  // G_t = ghi + glo, ghi a multiple of 2^-6: differences of ghi are exact
@@ -75,9 +70,9 @@ struct alignas(16) Weights {  // of one chunk (read in pairs)
   // P's weights outside its diagonal blocks of 16 x 16 are products: with B the last token before t's block, e^{G_t - G_B} times
   // e^{G_B - G_i}, neither above 1
   float row[C];          // q_scale e^{G_t - G_B}
-  float col[6 * 16];     // e^{G_B - G_i}, B = 15, 31, 47: 16, 32, 48 of them
+  float col[3][3 * 16];  // e^{G_B - G_i}, B = 15, 31, 47
   float all;             // e^{G_C}
-  int32_t has_bad[4];    // V's columns of 32 hold values that are none:
+  int32_t has_bad[8];    // V's columns of 16 hold values that are none:
   int32_t bad[D];        // the first token with one, per column (C: no such token)
 };
 // The states and tokens of one unit, or of one segment of it.
@@ -93,13 +88,11 @@ struct Item {
 
 struct Misc {
   Item items[RING];
-  uint64_t full_k[NS_K], full_q[NS_Q], full_v[NS_V], empty_k[NS_K], empty_q[NS_Q], empty_v[NS_V];
-  uint64_t v_ok[NS_V];                           // V has been looked at
-  uint64_t s_full, s_empty;                      // the next unit's state has landed; its place is free again
+  uint64_t full_k[NS], full_q[NS], full_v[NS_V], empty_k[NS], empty_q[NS], empty_v[NS_V];
   uint64_t dec_full[RING], dec_empty[RING], item_full[RING], item_empty[RING];
   uint64_t bar_p, bar_s, bar_o[2], bar_d;        // tensor core: QK, QS, PV (by chunk parity), KV of a chunk have completed
-  uint64_t bar_w[WBUF], w_ready[WBUF];           // KV of 16 tokens has completed; their Vw is in place
-  uint64_t p_ready, s_ready;                     // P and V^T, the state are in place
+  uint64_t bar_kw;                               // and the first half of KV
+  uint64_t v_ready[2], k_ready[2], p_ready, s_ready;  // V^T (by chunk parity), the halves of Kw, P, the state are in place
   uint64_t o_free, d_free;                       // accumulators have been read
   uint64_t drain[2];
   uint32_t tmem_base;
@@ -196,13 +189,6 @@ __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.al
 template <int N>
 __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// Where a lane's row of V is for ldmatrix: tokens 16 s ..., columns 32 quad + 16 h ... of a tile; a thread then holds column
-// g (+ 8), tokens 2 tig, + 1 (+ 8).
-__device__ __forceinline__ uint32_t v_place(uint32_t tile, int quad, int s, int h, int lane) {
-  const int t = 16 * s + 8 * (lane >> 4) + (lane & 7), ch = (quad & 1) * 4 + h * 2 + (lane >> 3 & 1);
-  return tile + (quad >> 1) * BLOCK + t * 128 + ((ch ^ (t & 7)) << 4);
-}
-
 __device__ __forceinline__ int chunks_of(int n) { return (n + C - 1) / C; }
 // Segments that a request of `chunks` chunks really has.
 __device__ __forceinline__ int segments_of(const Split &sp, int chunks) {
@@ -263,30 +249,22 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
   const int tid = threadIdx.x, warp = uni(tid >> 5), lane = tid & 31;
 
   if (tid == 0) {
-    for (int i = 0; i < NS_K; ++i) {
+    for (int i = 0; i < NS; ++i) {
       mbar_init(&m->full_k[i], 1);
-      mbar_init(&m->empty_k[i], WITH_O ? 2 : 1);  // KV; QK
-    }
-    for (int i = 0; i < NS_Q; ++i) {
       mbar_init(&m->full_q[i], 1);
+      mbar_init(&m->empty_k[i], WITH_O ? 5 : 4);  // Kw's warps; QK
       mbar_init(&m->empty_q[i], 1);
     }
     for (int i = 0; i < NS_V; ++i) {
       mbar_init(&m->full_v[i], 1);
-      mbar_init(&m->empty_v[i], WITH_O ? 8 : 4);  // Vw's warps; V^T's
-      mbar_init(&m->v_ok[i], 4);
+      mbar_init(&m->empty_v[i], 8);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&m->bar_o[i], 1);
+      mbar_init(&m->v_ready[i], 8);
+      mbar_init(&m->k_ready[i], 4);
     }
-    for (int i = 0; i < WBUF; ++i) {
-      mbar_init(&m->bar_w[i], 1);
-      mbar_init(&m->w_ready[i], 4);
-    }
-    mbar_init(&m->bar_d, 1);
-    mbar_init(&m->d_free, 8);
-    mbar_init(&m->s_full, 1);
-    mbar_init(&m->s_empty, 1);
+    mbar_init(&m->bar_kw, 1);
     for (int i = 0; i < RING; ++i) {
       mbar_init(&m->dec_full[i], 1);
       mbar_init(&m->dec_empty[i], WITH_O ? 20 : 12);
@@ -295,9 +273,11 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     }
     mbar_init(&m->bar_p, 1);
     mbar_init(&m->bar_s, 1);
+    mbar_init(&m->bar_d, 1);
     mbar_init(&m->p_ready, 4);
     mbar_init(&m->s_ready, 8);
     mbar_init(&m->o_free, 4);
+    mbar_init(&m->d_free, 8);
     mbar_init(&m->drain[0], 1);
     mbar_init(&m->drain[1], 1);
     m->abort_flag = 0;
@@ -339,14 +319,10 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     return m->abort_flag == 0 && m->items[it % RING].n >= 0;
   };
   const auto release = [&](int it) { arrive_warp(&m->item_empty[it % RING], lane); };
-  const auto stage_k = [](int i) { return static_cast<uint32_t>(i) % NS_K; };
-  const auto phase_k = [](int i) { return static_cast<uint32_t>(i) / NS_K & 1u; };
-  const auto stage_q = [](int i) { return static_cast<uint32_t>(i) % NS_Q; };
-  const auto phase_q = [](int i) { return static_cast<uint32_t>(i) / NS_Q & 1u; };
+  const auto stage = [](int i) { return static_cast<uint32_t>(i) % NS; };
+  const auto stage_phase = [](int i) { return static_cast<uint32_t>(i) / NS & 1u; };
   const auto stage_v = [](int i) { return static_cast<uint32_t>(i) % NS_V; };
-  const auto phase_v = [](int i) { return static_cast<uint32_t>(i) / NS_V & 1u; };
-  const auto buf_w = [](int i) { return static_cast<uint32_t>(i) % WBUF; };  // of 16 tokens
-  const auto phase_w = [](int i) { return static_cast<uint32_t>(i) / WBUF & 1u; };
+  const auto stage_v_phase = [](int i) { return static_cast<uint32_t>(i) / NS_V & 1u; };
   const auto phase2 = [](int i) { return static_cast<uint32_t>(i) >> 1 & 1u; };  // of what there are two of, by chunk parity
   const auto slot = [](int i) { return static_cast<uint32_t>(i) % RING; };
   const auto slot_phase = [](int i) { return static_cast<uint32_t>(i) / RING & 1u; };
@@ -354,45 +330,32 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
   if (warp < WARP_P) {
     regs_down<REGS_0>();
     if (warp == WARP_TMA) {
-      // The next item is looked up behind the first loads of this one, and its state is asked for as soon as there is room.
-      int nk = 0, nq = 0, nv = 0, ns = 0;  // tiles and states asked for
-      bool stop = false, pending = false;
+      // The next item is looked up, and its state brought into L2, behind the first loads of this one.
+      int nk = 0, nq = 0, nv = 0;  // tiles asked for
+      bool stop = false;
       uint32_t k = 0;
       int it = 0;
-      Item x, next{};
-      const auto load_state = [&](bool wait) {
-        if (it > 1) {  // the place is free once per item: when the one before this has begun
-          if (wait)
-            wait_bar(&m->s_empty, it & 1u, m);
-          else if (!uni(mbar_test_wait(&m->s_empty, it & 1u)))
-            return;
+      const auto publish = [&]() {
+        Item x;
+        while (!item_at(a, sp, m, sorted, k++, x)) {
         }
-        pending = false;
-        if (uni(m->abort_flag)) return;
-        if (next.from == 0) return;
-        const float *const src =
-            next.from == 2 ? sp.seg_state + (static_cast<int64_t>(next.unit) * sp.nseg + next.seg) * (D * D) : a.state + next.state;
-        if (lane == 0) {
-          mbar_expect_tx(&m->s_full, D * D * 4);
-          for (int i = 0; i < 4; ++i) bulk_load(sbase + OFF_S + i * (D * D), src + i * (D * D / 4), D * D, &m->s_full);
+        if (it >= RING) wait_bar(&m->item_empty[it % RING], (static_cast<uint32_t>(it) / RING & 1u) ^ 1u, m);
+        if (lane == 0) m->items[it % RING] = x;
+        if (x.n >= 0 && x.from != 0 && lane < 4) {
+          const float *const src = x.from == 2 ? sp.seg_state + (static_cast<int64_t>(x.unit) * sp.nseg + x.seg) * (D * D) : a.state + x.state;
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + lane * (D * D / 4)), "n"(D * D) : "memory");
         }
-        ++ns;
+        arrive_warp(&m->item_full[it % RING], lane);
+        ++it;
+        return x;
       };
+      Item x, next;
       bool ask = true;
       int c = 0, chunks = 0;
 #pragma unroll 1
       for (;;) {
-        if (pending) load_state(ask);
-        if (ask) {
-          while (!item_at(a, sp, m, sorted, k++, next)) {
-          }
-          if (it >= RING) wait_bar(&m->item_empty[it % RING], (static_cast<uint32_t>(it) / RING & 1u) ^ 1u, m);
-          if (lane == 0) m->items[it % RING] = next;
-          arrive_warp(&m->item_full[it % RING], lane);
-          ++it;
-          pending = next.n >= 0;
-          ask = false;
-        }
+        if (ask) next = publish();
+        ask = false;
         if (c == chunks) {
           x = next;
           if (x.n < 0) break;
@@ -414,9 +377,9 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           }
           ++count;
         };
-        load(m->empty_v, m->full_v, stage_v(n), phase_v(n), NS_V, OFF_V, &tmap_v, x.head, nv);
-        load(m->empty_k, m->full_k, stage_k(n), phase_k(n), NS_K, OFF_K, &tmap_k, x.k_head, nk);
-        if (WITH_O) load(m->empty_q, m->full_q, stage_q(n), phase_q(n), NS_Q, OFF_Q, &tmap_q, x.k_head, nq);
+        load(m->empty_v, m->full_v, stage_v(n), stage_v_phase(n), NS_V, OFF_V, &tmap_v, x.head, nv);
+        load(m->empty_k, m->full_k, stage(n), stage_phase(n), NS, OFF_K, &tmap_k, x.k_head, nk);
+        if (WITH_O) load(m->empty_q, m->full_q, stage(n), stage_phase(n), NS, OFF_Q, &tmap_q, x.k_head, nq);
         if (stop) break;
         ++c;
         ++n;
@@ -428,12 +391,11 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         }
       };
 #pragma unroll 1
-      for (int i = max(n - NS_K, 0); i <= n; ++i) {
-        if (i < nv && i >= nv - NS_V) land(&m->full_v[stage_v(i)], phase_v(i));
-        if (i < nk && i >= nk - NS_K) land(&m->full_k[stage_k(i)], phase_k(i));
-        if (i < nq && i >= nq - NS_Q) land(&m->full_q[stage_q(i)], phase_q(i));
+      for (int i = max(n - NS, 0); i <= n; ++i) {
+        if (i < nv && i >= nv - NS_V) land(&m->full_v[stage_v(i)], stage_v_phase(i));
+        if (i < nk && i >= nk - NS) land(&m->full_k[stage(i)], stage_phase(i));
+        if (i < nq && i >= nq - NS) land(&m->full_q[stage(i)], stage_phase(i));
       }
-      if (ns > 0) land(&m->s_full, (ns - 1) & 1u);
     } else if (warp == WARP_MMA || warp == WARP_MMA_O) {
       const auto gave_up = [&]() { return uni(m->abort_flag) != 0; };  // (one answer for the whole warp)
       int it = 0, all = 0;  // chunks of all items that have been looked up
@@ -451,34 +413,30 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         // Test hook: a first, short wait for operands that cannot be there yet.
         if (a.poll_limit_first_wait && all > 0) {
           bool done = false;
-          for (uint32_t i = 0; i < a.poll_limit_first_wait && !done; ++i) done = mbar_test_wait(&m->w_ready[0], 0);
+          for (uint32_t i = 0; i < a.poll_limit_first_wait && !done; ++i) done = mbar_test_wait(&m->k_ready[0], 0);
           if (!done) m->abort_flag = 1;
         }
 #pragma unroll 1
         for (; n < all && !gave_up(); ++n) {
           if (n + 1 == all) look();
-          const uint32_t par = n & 1u, st = stage_k(n);
-          wait_bar(&m->full_k[st], phase_k(n), m);
+          const uint32_t par = n & 1u;
+          wait_bar(&m->v_ready[par], phase2(n), m);
           if (n > 0) wait_bar(&m->d_free, par ^ 1u, m);
 #pragma unroll 1
-          for (int s = 0; s < 4; ++s) {
-            const int i = 4 * n + s;
-            wait_bar(&m->w_ready[buf_w(i)], phase_w(i), m);
+          for (int half = 0; half < 2; ++half) {  // 32 tokens each, so that the next Kw can follow behind
+            wait_bar(&m->k_ready[half], par, m);
             tc_fence_after_sync();
             if (gave_up()) break;
             if (elect_one()) {
-              const uint32_t v = tm + COL_VW + buf_w(i) * (8 * VSPLIT), k = desc_lo_mn(sbase + OFF_K, BLOCK) + (st * TILE + s * 2048 >> 4);
-              if (s == 0)
-                mma16_ts<false>(tm + COL_D, v, k, ID_KV);
+              const uint32_t v = tm + COL_V + par * 32 + half * 16, kw = desc_lo_mn(sbase + OFF_KW, BLOCK) + half * (2 * 2048 >> 4);
+              if (half == 0)
+                mma16_ts<false>(tm + COL_D, v, kw, ID_KV);
               else
-                mma16_ts<true>(tm + COL_D, v, k, ID_KV);
+                mma16_ts<true>(tm + COL_D, v, kw, ID_KV);
 #pragma unroll
-              for (int part = 1; part < VSPLIT; ++part) mma16_ts<true>(tm + COL_D, v + part * 8, k, ID_KV);
-              mma_commit(&m->bar_w[buf_w(i)]);
-              if (s == 3) {
-                mma_commit(&m->bar_d);
-                mma_commit(&m->empty_k[st]);
-              }
+              for (int i = 1; i < 2 * KSPLIT; ++i)
+                mma16_ts<true>(tm + COL_D, v + (i & 1) * 8, kw + (((i >> 1) * TILE + (i & 1) * 2048) >> 4), ID_KV);
+              mma_commit(half == 0 ? &m->bar_kw : &m->bar_d);
             }
             __syncwarp();
           }
@@ -486,12 +444,13 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       } else if constexpr (WITH_O) {
         constexpr uint32_t ID_QK = idesc_bf16(64, 64), ID_QS = idesc_bf16(128, 64);
         const auto qk = [&](int i) {
-          wait_bar(&m->full_k[stage_k(i)], phase_k(i), m);
-          wait_bar(&m->full_q[stage_q(i)], phase_q(i), m);
+          const uint32_t st = stage(i);
+          wait_bar(&m->full_k[st], stage_phase(i), m);
+          wait_bar(&m->full_q[st], stage_phase(i), m);
           tc_fence_after_sync();
           if (gave_up()) return;
           if (elect_one()) {
-            const uint32_t q = desc_lo_k(sbase + OFF_Q) + stage_q(i) * (TILE >> 4), k = desc_lo_k(sbase + OFF_K) + stage_k(i) * (TILE >> 4);
+            const uint32_t q = desc_lo_k(sbase + OFF_Q) + st * (TILE >> 4), k = desc_lo_k(sbase + OFF_K) + st * (TILE >> 4);
             mma16_ss<false>(tm + COL_P, q, k, ID_QK);
 #pragma unroll
             for (int kk = 1; kk < 8; ++kk) {
@@ -499,7 +458,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
               mma16_ss<true>(tm + COL_P, q + o, k + o, ID_QK);
             }
             mma_commit(&m->bar_p);
-            mma_commit(&m->empty_k[stage_k(i)]);
+            mma_commit(&m->empty_k[st]);
           }
           __syncwarp();
         };
@@ -508,7 +467,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
 #pragma unroll 1
         for (n = -1; n < all && !gave_up(); ++n) {
           if (n + 1 == all) look();
-          const uint32_t par = n & 1u;
+          const uint32_t st = stage(n), par = n & 1u;
           if (!first) {
             // QS
             wait_bar(&m->s_ready, par, m);
@@ -516,7 +475,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
             tc_fence_after_sync();
             if (gave_up()) break;
             if (elect_one()) {
-              const uint32_t q = desc_lo_k(sbase + OFF_Q) + stage_q(n) * (TILE >> 4);
+              const uint32_t q = desc_lo_k(sbase + OFF_Q) + st * (TILE >> 4);
               const uint32_t d = tm + COL_OI;
               mma16_ts<false>(d, tm + COL_SH, q, ID_QS);
 #pragma unroll
@@ -525,19 +484,20 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
                 mma16_ts<true>(d, tm + (i < 8 ? COL_SH : COL_SL) + kk * 8, q + (((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4), ID_QS);
               }
               mma_commit(&m->bar_s);
-              mma_commit(&m->empty_q[stage_q(n)]);
+              mma_commit(&m->empty_q[st]);
             }
             __syncwarp();
             wait_bar(&m->p_ready, par, m);
-            tc_fence_after_sync();
-            if (gave_up()) break;
           }
           // the next chunk's QK ahead of this one's PV: its accumulator has been read, and the next P is waited for longest
           if (n + 1 < all) qk(n + 1);
           if (!first) {
             // PV: tokens 16 s ... 16 s + 15 reach the rows from 16 s on
+            wait_bar(&m->v_ready[par], phase2(n), m);
+            tc_fence_after_sync();
+            if (gave_up()) break;
             if (elect_one()) {
-              const uint32_t v = tm + COL_V, p = desc_lo_k(sbase + OFF_PH);
+              const uint32_t v = tm + COL_V + par * 32, p = desc_lo_k(sbase + OFF_PH);
               mma16_ts<false>(tm + COL_OT, v, p, idesc_bf16(128, 64));
 #pragma unroll
               for (int i = 1; i < 8; ++i) {
@@ -621,7 +581,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
             float h, l;
             sum_at(8 * b + 7, h, l);
             if (block == b + 1) bh = h, bl = l;
-            if (block <= b) two(&w.col[b * (b + 1) * 8 + 2 * lane], ex2f((h - gh[0]) + (l - gl[0])), ex2f((h - gh[1]) + (l - gl[1])));
+            if (block <= b) two(&w.col[b][2 * lane], ex2f((h - gh[0]) + (l - gl[0])), ex2f((h - gh[1]) + (l - gl[1])));
           }
           two(&w.row[2 * lane], a.q_scale * ex2f((gh[0] - bh) + (gl[0] - bl)), a.q_scale * ex2f((gh[1] - bh) + (gl[1] - bl)));
         }
@@ -664,7 +624,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           tc_fence_after_sync();
           const float r0 = w.row[t0], r1 = w.row[t1];
           const uint64_t rr0 = dpack2(r0, r0), rr1 = dpack2(r1, r1);
-          const float *const col = w.col + quad * (quad - 1) * 8 + 2 * tig;
+          const float *const col = w.col[quad > 0 ? quad - 1 : 0] + 2 * tig;
 #pragma unroll 1
           for (int s = 0; s < quad; ++s) {
             uint32_t p[8];
@@ -690,31 +650,21 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
                   dpack2(at(2, t1, i, h1, l1, hi.x, lo.x), at(3, t1, i + 1, h1, l1, hi.y, lo.y)));
             }
           }
-          // V^T, 32 columns of V per warp, as it is (once it has been looked at)
-          wait_bar(&m->v_ok[stage_v(n)], phase_v(n), m);
-#pragma unroll 2
-          for (int i = 0; i < 8; ++i) {
-            uint32_t r[4];
-            ldmatrix_x4_trans(r[0], r[1], r[2], r[3], v_place(smem_u32(smem + OFF_V + stage_v(n) * TILE), quad, i >> 1, i & 1, lane));
-            tmem_st_16x128b(tp - COL_P + COL_V + (i >> 1) * 8 + (static_cast<uint32_t>((i & 1) * 16) << 16), r);
-          }
-          tmem_st_wait();
           fence_smem_to_async();
           tc_fence_before_sync();
           arrive_warp(&m->p_ready, lane);
-          if (lane == 0) mbar_arrive(&m->empty_v[stage_v(n)]);
           if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
         }
       }
     }
-  } else if (warp < WARP_V) {
+  } else if (warp < WARP_K) {
     // ---- outputs ----
     regs_down<REGS_O>();
     if constexpr (WITH_O) {
       const int quad = warp & 3, g = lane >> 2, tig = lane & 3;
       const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
       const int64_t v_stride = static_cast<int64_t>(a.H_v) * D;
-      unsigned char *const ost = smem + OFF_O + quad * 2048;
+      unsigned char *const ost = smem + OFF_O + quad * 4096;
 #pragma unroll 1
       for (int it = 0; uni(take(it)); ++it) {
         const int tokens = m->items[it % RING].n;
@@ -727,27 +677,30 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
           wait_bar(&m->bar_o[n & 1], phase2(n), m);
           tc_fence_after_sync();
-          const bool has_bad = w.has_bad[quad] != 0;
-          const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
-          uint32_t y[4][8];  // bf16 pairs along the tokens: 16 columns (part & 1), 32 tokens (part >> 1)
-#pragma unroll
-          for (int part = 0; part < 4; ++part) {
+          const bool has_bad = (w.has_bad[quad * 2] | w.has_bad[quad * 2 + 1]) != 0;
+#pragma unroll 1
+          for (int part = 0; part < 4; ++part) {  // 16 columns of d_v (part & 1), 32 tokens (part >> 1)
             const int half = part & 1, tb = part >> 1;
             uint32_t oi[16], ot[16];
             const uint32_t at = tl + (static_cast<uint32_t>(half * 16) << 16) + tb * 32;
             tmem_ld_16x256b(at + COL_OI, oi);
             tmem_ld_16x256b(at + COL_OT, ot);
             tmem_ld_wait();
+            if (part == 3) {
+              tc_fence_before_sync();
+              arrive_warp(&m->o_free, lane);
+            }
             const int v0 = half * 16 + g;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const int t = tb * 32 + 8 * j + 2 * tig;
               const uint64_t e = *reinterpret_cast<const uint64_t *>(&w.eg[t]);
-              const float2 y0 = dunpack2(dfma2(e, pair(oi[4 * j], oi[4 * j + 1]), pair(ot[4 * j], ot[4 * j + 1])));
-              const float2 y1 = dunpack2(dfma2(e, pair(oi[4 * j + 2], oi[4 * j + 3]), pair(ot[4 * j + 2], ot[4 * j + 3])));
+              const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
+              float2 y0 = dunpack2(dfma2(e, pair(oi[4 * j], oi[4 * j + 1]), pair(ot[4 * j], ot[4 * j + 1])));
+              float2 y1 = dunpack2(dfma2(e, pair(oi[4 * j + 2], oi[4 * j + 3]), pair(ot[4 * j + 2], ot[4 * j + 3])));
               if constexpr (sizeof(OT) == 2) {
-                y[part][2 * j] = bf16x2(y0.x, y0.y);
-                y[part][2 * j + 1] = bf16x2(y1.x, y1.y);
+                ot[2 * j] = bf16x2(y0.x, y0.y);
+                ot[2 * j + 1] = bf16x2(y1.x, y1.y);
               } else {
                 OT *const p = o + t * v_stride + v0;
                 if (t < rows) {
@@ -760,46 +713,43 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
                 }
               }
             }
-          }
-          tc_fence_before_sync();
-          arrive_warp(&m->o_free, lane);
-          if constexpr (sizeof(OT) == 2) {
+            if constexpr (sizeof(OT) == 2) {
 #pragma unroll
-            for (int tb = 0; tb < 2; ++tb) {
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-#pragma unroll
-                for (int j = 0; j < 4; j += 2) {
-                  const uint32_t *const r = &y[2 * tb + half][2 * j];
-                  const int t = 8 * (j + (lane >> 4)) + (lane & 7), ch = half * 2 + (lane >> 3 & 1);
-                  stmatrix_x4_trans(smem_u32(ost) + t * 64 + ((ch ^ (t >> 1 & 3)) << 4), r[0], r[1], r[2], r[3]);
-                }
+              for (int j = 0; j < 4; j += 2) {
+                const int t = tb * 32 + 8 * (j + (lane >> 4)) + (lane & 7), ch = half * 2 + (lane >> 3 & 1);
+                stmatrix_x4_trans(smem_u32(ost) + t * 64 + ((ch ^ (t >> 1 & 3)) << 4), ot[2 * j], ot[2 * j + 1], ot[2 * j + 2], ot[2 * j + 3]);
               }
-              __syncwarp();
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int t = i * 8 + (lane >> 2), ch = lane & 3;
-                const uint4 z = *reinterpret_cast<const uint4 *>(ost + t * 64 + ((ch ^ (t >> 1 & 3)) << 4));
-                if (32 * tb + t < rows) *reinterpret_cast<uint4 *>(o + (32 * tb + t) * v_stride + ch * 8) = z;
-              }
-              __syncwarp();
             }
           }
-          if (has_bad) {  // a lane per column, over what the warp has just stored
-            __syncwarp();
+          __syncwarp();
+          if (has_bad) {  // a lane per column
             const OT nan = static_cast<OT>(__int_as_float(0x7fffffff));
 #pragma unroll 1
-            for (int t = w.bad[quad * 32 + lane]; t < rows && t < C; ++t) o[t * v_stride + lane] = nan;
+            for (int t = w.has_bad[quad * 2 + (lane >> 4)] ? w.bad[quad * 32 + lane] : C; t < rows && t < C; ++t) {
+              if constexpr (sizeof(OT) == 2)
+                *reinterpret_cast<OT *>(ost + t * 64 + ((lane >> 3 ^ (t >> 1 & 3)) << 4) + (lane & 7) * 2) = nan;
+              else
+                o[t * v_stride + lane] = nan;
+            }
+            __syncwarp();
+          }
+          if constexpr (sizeof(OT) == 2) {
+#pragma unroll 2
+            for (int i8 = 0; i8 < 8; ++i8) {
+              const int t = i8 * 8 + (lane >> 2), ch = lane & 3;
+              const uint4 y = *reinterpret_cast<const uint4 *>(ost + t * 64 + ((ch ^ (t >> 1 & 3)) << 4));
+              if (t < rows) *reinterpret_cast<uint4 *>(o + t * v_stride + ch * 8) = y;
+            }
+            __syncwarp();
           }
           arrive_warp(&m->dec_empty[slot(n)], lane);
         }
       }
     }
   } else if (warp < WARP_S) {
-    // ---- Vw ----
-    regs_down<REGS_V>();
-    const int vt = tid - WARP_V * 32, quad = warp & 3, tig = lane & 3;
-    const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
+    // ---- Kw ----
+    regs_down<REGS_K>();
+    const int kt = tid - WARP_K * 32;
 #pragma unroll 1
     for (int it = 0;; ++it) {
       if (any_of<1, 128>(!take(it))) break;  // (one answer for all four warps)
@@ -807,81 +757,42 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       release(it);
 #pragma unroll 1
       for (int c = 0; c < chunks_of(tokens); ++c, ++n) {
+        const uint32_t st = stage(n);
         const int rows = min(tokens - c * C, C);
-        Weights &w = m->wt[slot(n)];
-        wait_bar(&m->full_v[stage_v(n)], phase_v(n), m);
-        unsigned char *const tile = smem + OFF_V + stage_v(n) * TILE + (quad >> 1) * BLOCK;  // this warp's 32 columns: four of its 16-byte places
-        if (rows < C) {  // nothing from behind the last token: zero times a value that is none would be none
-          wait_bar(&m->full_k[stage_k(n)], phase_k(n), m);
-#pragma unroll 1
-          for (int t = rows + (lane >> 2); t < C; t += 8)
-            *reinterpret_cast<uint4 *>(tile + t * 128 + ((((quad & 1) * 4 + tig) ^ (t & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
-          // (QK may be reading this tile: what it makes of these rows is not used)
-#pragma unroll 1
-          for (int t = rows + (vt >> 4); t < C; t += 8)
-            *reinterpret_cast<uint4 *>(smem + OFF_K + stage_k(n) * TILE + (vt >> 3 & 1) * BLOCK + t * 128 + (vt & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-          fence_smem_to_async();
-          __syncwarp();
-        }
+        const Weights &w = m->wt[slot(n)];
         wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-        int first = C;  // of column `lane`: the first token with a value that is none
-        bool some = false;
+        // Kw, 32 tokens at a time
+        wait_bar(&m->full_k[st], stage_phase(n), m);
+        const unsigned char *const kr = smem + OFF_K + st * TILE + kt * 16;
+        unsigned char *const kw = smem + OFF_KW + kt * 16;
 #pragma unroll 1
-        for (int s = 0; s < 4; ++s) {  // 16 tokens each
-          const int i = 4 * n + s;
-          if (i >= WBUF) wait_bar(&m->bar_w[buf_w(i)], phase_w(i) ^ 1u, m);  // KV has read what was there
-          tc_fence_after_sync();
-          const uint64_t w0 = *reinterpret_cast<const uint64_t *>(&w.w[16 * s + 2 * tig]), w1 = *reinterpret_cast<const uint64_t *>(&w.w[16 * s + 8 + 2 * tig]);
-          const uint32_t to = tl + COL_VW + buf_w(i) * (8 * VSPLIT);
-          // A value that is none would reach every row of its column through products with weights that are zero, so it is taken out and
-          // remembered; 0 * x + sum is NaN from the first of them on.
-          bool looked = false;
-#pragma unroll 1
-          for (;;) {
-            __nv_bfloat162 probe = __floats2bfloat162_rn(0.f, 0.f);
-            const __nv_bfloat162 zero2 = probe;
+        for (int half = 0; half < 2; ++half) {
+          if (n > 0) wait_bar(half == 0 ? &m->bar_kw : &m->bar_d, (n - 1) & 1u, m);  // KV of the chunk before has read this half
+#pragma unroll 2
+          for (int i = 0; i < 4; ++i) {
+            const int row = (kt >> 3) + (half * 2 + (i & 1)) * 16;
+            const uint32_t at = ((i >> 1) * 4 + half * 2 + (i & 1)) * 2048;
+            const float f = w.w[row];
+            const uint64_t ff = dpack2(f, f);
+            uint4 y = *reinterpret_cast<const uint4 *>(kr + at);
+            if (row >= rows) y = make_uint4(0u, 0u, 0u, 0u);
+            uint64_t rest[4] = {dmul2(dpack2(bf_lo(y.x), bf_hi(y.x)), ff), dmul2(dpack2(bf_lo(y.y), bf_hi(y.y)), ff),
+                                dmul2(dpack2(bf_lo(y.z), bf_hi(y.z)), ff), dmul2(dpack2(bf_lo(y.w), bf_hi(y.w)), ff)};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {  // 16 columns of V each
-              uint32_t r[4];
-              ldmatrix_x4_trans(r[0], r[1], r[2], r[3], v_place(smem_u32(smem + OFF_V + stage_v(n) * TILE), quad, s, h, lane));
-              uint64_t rest[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                probe = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&r[j]), zero2, probe);
-                rest[j] = dmul2(dpack2(bf_lo(r[j]), bf_hi(r[j])), j < 2 ? w0 : w1);
-              }
-#pragma unroll
-              for (int part = 0; part < VSPLIT; ++part) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) r[j] = take_bf16x2(rest[j]);
-                tmem_st_16x128b(to + part * 8 + (static_cast<uint32_t>(h * 16) << 16), r);
-              }
+            for (int part = 0; part < KSPLIT; ++part) {
+              uint4 b;
+              b.x = take_bf16x2(rest[0]);
+              b.y = take_bf16x2(rest[1]);
+              b.z = take_bf16x2(rest[2]);
+              b.w = take_bf16x2(rest[3]);
+              *reinterpret_cast<uint4 *>(kw + part * TILE + at) = b;
             }
-            const bool none = __isnan(__low2float(probe)) || __isnan(__high2float(probe));
-            if (!__any_sync(0xffffffffu, none) || looked) break;
-            looked = some = true;
-#pragma unroll 1
-            for (int t = min(rows, 16 * s + 16) - 1; t >= 16 * s; --t) {
-              uint16_t *const e = reinterpret_cast<uint16_t *>(tile + t * 128 + ((((quad & 1) * 4 + (lane >> 3)) ^ (t & 7)) << 4) + (lane & 7) * 2);
-              if ((*e & 0x7F80u) == 0x7F80u) {
-                *e = 0;
-                if (first == C || first > t) first = t;
-              }
-            }
-            fence_smem_to_async();
-            __syncwarp();
           }
-          if (s == 3) {
-            if (some) w.bad[quad * 32 + lane] = first;
-            if (lane == 0) w.has_bad[quad] = some;
-          }
-          tmem_st_wait();
-          tc_fence_before_sync();
-          arrive_warp(&m->w_ready[buf_w(i)], lane);
+          fence_smem_to_async();
+          arrive_warp(&m->k_ready[half], lane);
         }
         if (lane == 0) {
-          mbar_arrive(&m->v_ok[stage_v(n)]);
-          mbar_arrive(&m->empty_v[stage_v(n)]);
+          mbar_arrive(&m->empty_k[st]);
           mbar_arrive(&m->dec_empty[slot(n)]);
         }
       }
@@ -892,61 +803,89 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     const int quad = warp & 3, half = (warp - WARP_S) >> 2;
     const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
     const int v = quad * 32 + lane, k0 = half * 64;
-    float *const mine = reinterpret_cast<float *>(smem + OFF_S) + k0 * D + v;  // this thread's place in the staged state
-    const bool leader = warp == WARP_S && lane == 0;
-    uint64_t S[32];
-    int ns = 0;               // states taken
-    float *dst = nullptr;     // where the last unit's state goes
-    bool leaving = false;     // the leader: it is on its way
-    const auto left = [&]() {
-      if (leaving) bulk_wait_read();
-      leaving = false;
-      mbar_arrive(&m->s_empty);
-    };
 #pragma unroll 1
     for (int it = 0;; ++it) {
-      const bool end = any_of<2, 256>(!take(it));  // (one answer for all eight warps)
-      if (end && any_of<2, 256>(m->abort_flag != 0)) break;  // after a time-out a unit is not written at all
-      Item x;
-      if (!end) {
-        x = m->items[it % RING];
-        release(it);
-      }
-      const bool from = !end && x.from != 0;
-      if (from) wait_bar(&m->s_full, ns++ & 1u, m);
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        float next[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) next[j] = 0.f;
-        if (from) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) next[j] = mine[(16 * b + j) * D];
-        }
-        if (dst) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float2 y = dunpack2(S[8 * b + j]);
-            mine[(16 * b + 2 * j) * D] = y.x;
-            mine[(16 * b + 2 * j + 1) * D] = y.y;
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) S[8 * b + j] = dpack2(next[2 * j], next[2 * j + 1]);
-      }
-      fence_smem_to_async();
-      asm volatile("bar.sync 2, 256;" ::: "memory");
-      if (leader && dst) {
-        for (int i = 0; i < 4; ++i) bulk_store(dst + i * (D * D / 4), sbase + OFF_S + i * (D * D), D * D);
-        bulk_commit();
-        leaving = true;
-      }
-      if (end) break;
+      if (any_of<2, 256>(!take(it))) break;  // (one answer for all eight warps)
+      const Item x = m->items[it % RING];
+      release(it);
+      uint64_t S[32];
       const int64_t seg_at = (static_cast<int64_t>(x.unit) * sp.nseg + x.seg) * (D * D);
+      const auto fetch = [&]() {
+        const float *const src = (x.from == 2 ? sp.seg_state + seg_at : a.state + x.state) + k0 * D + v;
+        if (x.from != 0) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) S[j] = dpack2(src[2 * j * D], src[(2 * j + 1) * D]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) S[j] = 0;
+        }
+      };
       float decay = 1.f;
+      bool fetched = false;
 #pragma unroll 1
       for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
-        const Weights &w = m->wt[slot(n)];
+        Weights &w = m->wt[slot(n)];
+        const uint32_t par = n & 1u;
+        const int rows = min(x.n - c * C, C);
+        // V^T, this warp's 16 columns.  A value that is none would reach every row of its column through products with weights that are
+        // zero, so it is taken out and remembered; 0 * x + sum is NaN from the first of them on.
+        wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
+        wait_bar(&m->full_v[stage_v(n)], stage_v_phase(n), m);
+        if (n > 1) {  // the products of the chunk before the last have read their V^T (their KV has been waited for)
+          if (WITH_O) wait_bar(&m->bar_o[par], phase2(n - 2), m);
+          tc_fence_after_sync();
+        }
+        {
+          unsigned char *const vt = smem + OFF_V + stage_v(n) * TILE + (quad >> 1) * BLOCK;
+          const int ch = (quad & 1) * 4 + half * 2;  // two of the 16-byte places of a row
+          if (rows < C) {  // nothing from behind the last token
+#pragma unroll 1
+            for (int t = rows + (lane >> 1); t < C; t += 16)
+              *reinterpret_cast<uint4 *>(vt + t * 128 + (((ch + (lane & 1)) ^ (t & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+            fence_smem_to_async();  // (the next tile lands here)
+            __syncwarp();
+          }
+          bool looked = false;
+          uint32_t r[16];
+#pragma unroll 1
+          for (;;) {
+            __nv_bfloat162 probe = __floats2bfloat162_rn(0.f, 0.f);
+            const __nv_bfloat162 zero2 = probe;
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+              const int t = 8 * (j + (lane >> 4)) + (lane & 7);
+              ldmatrix_x4_trans(r[2 * j], r[2 * j + 1], r[2 * j + 2], r[2 * j + 3],
+                                smem_u32(vt) + t * 128 + (((ch + (lane >> 3 & 1)) ^ (t & 7)) << 4));
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) probe = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&r[j]), zero2, probe);
+            const bool none = __isnan(__low2float(probe)) || __isnan(__high2float(probe));
+            if (!__any_sync(0xffffffffu, none) || looked) break;
+            looked = true;
+            if (lane < 16) {
+              int first = C;  // of this lane's column
+#pragma unroll 1
+              for (int t = rows - 1; t >= 0; --t) {
+                uint16_t *const e = reinterpret_cast<uint16_t *>(vt + t * 128 + (((ch + (lane >> 3)) ^ (t & 7)) << 4) + (lane & 7) * 2);
+                if ((*e & 0x7F80u) == 0x7F80u) {
+                  *e = 0;
+                  first = t;
+                }
+              }
+              w.bad[quad * 32 + half * 16 + lane] = first;
+            }
+            fence_smem_to_async();  // (the next tile lands here)
+            __syncwarp();
+          }
+          if (lane == 0) w.has_bad[quad * 2 + half] = looked;
+          tmem_st_16x128b(tl + COL_V + par * 32 + (static_cast<uint32_t>(half * 16) << 16), r);
+          tmem_st_wait();
+          tc_fence_before_sync();
+          arrive_warp(&m->v_ready[par], lane);
+          if (lane == 0) mbar_arrive(&m->empty_v[stage_v(n)]);
+        }
+        if (!fetched) fetch();
+        fetched = true;
         if constexpr (WITH_O) {
           if (n > 0) wait_bar(&m->bar_s, (n - 1) & 1u, m);  // QS of the chunk before has read its state
           tc_fence_after_sync();
@@ -962,12 +901,11 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           tc_fence_before_sync();
           arrive_warp(&m->s_ready, lane);
         }
-        wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
         float f = w.all;
         decay *= f;
         wait_bar(&m->bar_d, n & 1u, m);
         tc_fence_after_sync();
-        if (w.has_bad[quad] != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
+        if (w.has_bad[quad * 2 + (lane >> 4)] != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
         const uint64_t ff = dpack2(f, f);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
@@ -981,18 +919,27 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         tc_fence_before_sync();
         arrive_warp(&m->d_free, lane);
         if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
-        if (leader && c == 0) left();
       }
-      if (leader && chunks_of(x.n) == 0) left();
-      dst = nullptr;
+      if (!fetched) fetch();  // (no tokens)
+      // a unit is written as a whole or, after a time-out, not at all
+      if (any_of<2, 256>(m->abort_flag != 0)) break;
+      float *dst = nullptr;
       if (sp.phase == 1) {
         dst = sp.seg_state + seg_at + D * D;
-        if (leader) sp.seg_decay[static_cast<int64_t>(x.unit) * sp.nseg + x.seg] = decay;
+        if (warp == WARP_S && lane == 0) sp.seg_decay[static_cast<int64_t>(x.unit) * sp.nseg + x.seg] = decay;
       } else if (x.write) {
         dst = a.state + x.state;
       }
+      if (dst) {
+        dst += k0 * D + v;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float2 y = dunpack2(S[j]);
+          dst[2 * j * D] = y.x;
+          dst[(2 * j + 1) * D] = y.y;
+        }
+      }
     }
-    if (leader) bulk_wait();
   }
   stream_order_release();
   tc_fence_before_sync();

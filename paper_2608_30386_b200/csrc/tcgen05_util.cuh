@@ -64,21 +64,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const void *tmap,
       : "memory");
 }
 
-// Untiled load of `bytes` bytes (a multiple of 16; both addresses 16-byte aligned).
-__device__ __forceinline__ void bulk_load(uint32_t dst_smem, const void *src, uint32_t bytes, uint64_t *bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst_smem), "l"(src), "r"(bytes),
-               "r"(smem_u32(bar))
-               : "memory");
-}
-
-// Untiled store, likewise; the issuing thread commits it to a group and waits for that.
-__device__ __forceinline__ void bulk_store(void *dst, uint32_t src_smem, uint32_t bytes) {
-  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src_smem), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }  // the sources may be overwritten
-__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
 // One lane of a converged warp.  The compiler knows that a branch on this predicate runs with a single active thread, so the
 // tcgen05 instructions below it take their descriptors straight from uniform registers; behind `lane == 0` it has to allow
 // for several active threads with different operands and serialises every one of them in a loop.
@@ -140,10 +125,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
-// 16 lanes x 8 consecutive columns: thread (g = lane / 4, tig = lane % 4) holds, per 4 columns i, r[2i] = (row g, column 4i + tig) and
+// 16 lanes x 32 consecutive columns: thread (g = lane / 4, tig = lane % 4) holds, per 4 columns i, r[2i] = (row g, column 4i + tig) and
 // r[2i+1] = the same column of row g + 8, which is how ldmatrix spreads 16-bit tiles of eight by eight.
-__device__ __forceinline__ void tmem_st_16x128b(uint32_t taddr, const uint32_t (&r)[4]) {
-  asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+__device__ __forceinline__ void tmem_st_16x128b(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
 }
 // 32 lanes x 8 consecutive columns.
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
