@@ -15,9 +15,9 @@
 // as good as fp32.
 //
 // One thread block per SM walks over (request, layer, head) units, or over segments of long ones; roles of its warps:
-//   0       looks up the units; TMA: tiles of K, Q, V, three chunks ahead
+//   0       looks up the units (and clears the states of those without tokens); TMA: tiles of K, Q, V, three chunks ahead
 //   1, 3    issue the products: KV; QK, QS and PV (issue alone, at 60 to 100 cycles a product, filled one warp's time)
-//   2       sums of log-decays (as pairs of fp32), weights of a chunk
+//   2       announces the chunks to all others: sums of log-decays (as pairs of fp32), weights, where its unit's state is
 //   4 - 7   P: out of tensor memory, weighted, into its operand tiles
 //   8 - 11  outputs
 //   12 - 15 Kw
@@ -43,7 +43,7 @@ constexpr int kSms = 148;
 constexpr int NS = 3, NS_V = 2;  // stages of K and Q; of V
 constexpr int KSPLIT = 3;        // parts of Kw
 constexpr int RING = 4;  // chunks whose weights are kept, and units that are looked up ahead
-constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_MMA_O = 3, WARP_P = 4, WARP_O = 8, WARP_K = 12, WARP_S = 16, NWARP = 24;
+constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_P = 4, WARP_O = 8, WARP_K = 12, WARP_S = 16, NWARP = 24;
 // Registers of a thread, by groups of four warps: what the launch gives each (65,536 over all threads, in steps of 8), and how the roles
 // share it out.
 constexpr int REGS = 80, REGS_0 = 56, REGS_P = 72, REGS_O = 72, REGS_K = 72, REGS_S = 104;
@@ -63,7 +63,14 @@ constexpr uint32_t OFF_MISC = OFF_O + TILE;
 
 constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 320, COL_OT = 384, COL_V = 448;  // (V^T twice, by chunk parity)
 
-struct alignas(16) Weights {  // of one chunk (read in pairs)
+struct alignas(16) Chunk {
+  int32_t rows;          // its tokens; negative: there are no more chunks
+  int32_t first, last;   // of its unit
+  float all;             // e^{G_C}
+  const float *src;      // first: the unit's state; null: zero
+  float *dst, *decay;    // last: where its new state goes, and (a segment's) its decay; null: nowhere
+  int64_t out;           // its first output, in elements
+  // weights (read in pairs)
   float ghi[C], glo[C];  // G_t = ghi + glo, ghi a multiple of 2^-6: differences of ghi are exact
   float w[C];            // e^{G_C - G_i}; 0 behind the last token
   float eg[C];           // q_scale e^{G_t}
@@ -71,12 +78,11 @@ struct alignas(16) Weights {  // of one chunk (read in pairs)
   // e^{G_B - G_i}, neither above 1
   float row[C];          // q_scale e^{G_t - G_B}
   float col[3][3 * 16];  // e^{G_B - G_i}, B = 15, 31, 47
-  float all;             // e^{G_C}
   int32_t has_bad[8];    // V's columns of 16 hold values that are none:
   int32_t bad[D];        // the first token with one, per column (C: no such token)
 };
 // The states and tokens of one unit, or of one segment of it.
-struct Item {
+struct alignas(16) Item {
   int64_t state;   // offset of its state in floats
   int64_t tok0;    // its first token in the streams of the call
   int32_t unit, seg;
@@ -94,10 +100,11 @@ struct Misc {
   uint64_t bar_kw;                               // and the first half of KV
   uint64_t v_ready[2], k_ready[2], p_ready, s_ready;  // V^T (by chunk parity), the halves of Kw, P, the state are in place
   uint64_t o_free, d_free;                       // accumulators have been read
+  uint64_t s_whole;                              // the state's warps are all through with a unit
   uint64_t drain[2];
   uint32_t tmem_base;
   volatile uint32_t abort_flag;
-  Weights wt[RING];
+  Chunk ch[RING];
   uint16_t order[kMaxSorted];
 };
 constexpr uint32_t SMEM_BYTES = OFF_MISC + sizeof(Misc);
@@ -189,6 +196,18 @@ __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.al
 template <int N>
 __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
+// Which of N buffers, and the phase of its barriers, chunk by chunk.
+template <int N>
+struct Ring {
+  uint32_t i = 0, ph = 0;
+  __device__ __forceinline__ void step() {
+    if (++i == N) {
+      i = 0;
+      ph ^= 1u;
+    }
+  }
+};
+
 __device__ __forceinline__ int chunks_of(int n) { return (n + C - 1) / C; }
 // Segments that a request of `chunks` chunks really has.
 __device__ __forceinline__ int segments_of(const Split &sp, int chunks) {
@@ -239,6 +258,11 @@ __device__ __forceinline__ bool item_at(const DascDecayArgs &a, const Split &sp,
   return true;
 }
 
+// Where an item's state is read.
+__device__ __forceinline__ const float *state_of(const DascDecayArgs &a, const Split &sp, const Item &x) {
+  return x.from == 2 ? sp.seg_state + (static_cast<int64_t>(x.unit) * sp.nseg + x.seg) * (D * D) : a.state + x.state;
+}
+
 template <bool WITH_O, typename OT>
 __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_constant__ DascDecayArgs a, const __grid_constant__ Split sp,
                                                              const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
@@ -267,9 +291,9 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     mbar_init(&m->bar_kw, 1);
     for (int i = 0; i < RING; ++i) {
       mbar_init(&m->dec_full[i], 1);
-      mbar_init(&m->dec_empty[i], WITH_O ? 20 : 12);
+      mbar_init(&m->dec_empty[i], WITH_O ? 22 : 13);
       mbar_init(&m->item_full[i], 1);
-      mbar_init(&m->item_empty[i], WITH_O ? 23 : 14);
+      mbar_init(&m->item_empty[i], 1);
     }
     mbar_init(&m->bar_p, 1);
     mbar_init(&m->bar_s, 1);
@@ -278,6 +302,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     mbar_init(&m->s_ready, 8);
     mbar_init(&m->o_free, 4);
     mbar_init(&m->d_free, 8);
+    mbar_init(&m->s_whole, 8);
     mbar_init(&m->drain[0], 1);
     mbar_init(&m->drain[1], 1);
     m->abort_flag = 0;
@@ -312,113 +337,186 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
   tc_fence_after_sync();
   const uint32_t tm = static_cast<uint32_t>(uni(static_cast<int>(m->tmem_base)));
 
-  int n = 0;  // chunks so far: buffers and barrier phases go by it
-  // Item `it` of this block, once it has been looked up; false: there are no more, or a wait has run out.
-  const auto take = [&](int it) {
-    wait_bar(&m->item_full[it % RING], static_cast<uint32_t>(it) / RING & 1u, m);
-    return m->abort_flag == 0 && m->items[it % RING].n >= 0;
-  };
-  const auto release = [&](int it) { arrive_warp(&m->item_empty[it % RING], lane); };
-  const auto stage = [](int i) { return static_cast<uint32_t>(i) % NS; };
-  const auto stage_phase = [](int i) { return static_cast<uint32_t>(i) / NS & 1u; };
-  const auto stage_v = [](int i) { return static_cast<uint32_t>(i) % NS_V; };
-  const auto stage_v_phase = [](int i) { return static_cast<uint32_t>(i) / NS_V & 1u; };
   const auto phase2 = [](int i) { return static_cast<uint32_t>(i) >> 1 & 1u; };  // of what there are two of, by chunk parity
   const auto slot = [](int i) { return static_cast<uint32_t>(i) % RING; };
   const auto slot_phase = [](int i) { return static_cast<uint32_t>(i) / RING & 1u; };
+  // Chunk n, once it has been announced; false: there are no more, or a wait has run out.
+  const auto there = [&](int n) {
+    wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
+    return m->abort_flag == 0 && m->ch[slot(n)].rows >= 0;
+  };
+  // All roles count chunks, n: buffers and barrier phases go by it.
 
   if (warp < WARP_P) {
     regs_down<REGS_0>();
     if (warp == WARP_TMA) {
       // The next item is looked up, and its state brought into L2, behind the first loads of this one.
-      int nk = 0, nq = 0, nv = 0;  // tiles asked for
-      bool stop = false;
-      uint32_t k = 0;
-      int it = 0;
-      const auto publish = [&]() {
-        Item x;
-        while (!item_at(a, sp, m, sorted, k++, x)) {
-        }
-        if (it >= RING) wait_bar(&m->item_empty[it % RING], (static_cast<uint32_t>(it) / RING & 1u) ^ 1u, m);
-        if (lane == 0) m->items[it % RING] = x;
-        if (x.n >= 0 && x.from != 0 && lane < 4) {
-          const float *const src = x.from == 2 ? sp.seg_state + (static_cast<int64_t>(x.unit) * sp.nseg + x.seg) * (D * D) : a.state + x.state;
-          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + lane * (D * D / 4)), "n"(D * D) : "memory");
-        }
-        arrive_warp(&m->item_full[it % RING], lane);
-        ++it;
-        return x;
-      };
-      Item x, next;
       bool ask = true;
-      int c = 0, chunks = 0;
+      uint32_t k = 0;
+      int it = 0, n = 0, c = 0, chunks = 0;
+      Ring<NS> kq;
+      Item x, next;
 #pragma unroll 1
       for (;;) {
-        if (ask) next = publish();
-        ask = false;
+        if (ask) {
+          ask = false;
+#pragma unroll 1
+          for (;;) {
+            while (!item_at(a, sp, m, sorted, k++, next)) {
+            }
+            if (next.n != 0) break;
+            float4 *const st = reinterpret_cast<float4 *>(a.state + next.state);  // no tokens: its new state is zero
+#pragma unroll 1
+            for (int i = lane; i < D * D / 4; i += 32) st[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+          if (it >= RING) wait_bar(&m->item_empty[it % RING], (static_cast<uint32_t>(it) / RING & 1u) ^ 1u, m);
+          if (lane == 0) m->items[it % RING] = next;
+          if (next.n > 0 && next.from != 0 && lane < 4) bulk_prefetch(state_of(a, sp, next) + lane * (D * D / 4), D * D);
+          arrive_warp(&m->item_full[it % RING], lane);
+          ++it;
+        }
         if (c == chunks) {
           x = next;
           if (x.n < 0) break;
           chunks = chunks_of(x.n);
           c = 0;
           ask = true;
-          if (chunks == 0) continue;
         }
         const int32_t z = static_cast<int32_t>(x.tok0 + c * C);
-        const auto load = [&](uint64_t *empty, uint64_t *full, uint32_t st, uint32_t ph, int stages, uint32_t off, const CUtensorMap *map, int head,
-                              int &count) {
-          if (n >= stages) wait_bar(&empty[st], ph ^ 1u, m);
-          stop |= uni(m->abort_flag) != 0;
-          if (stop) return;
+#pragma unroll 1
+        for (int t = 0; t < (WITH_O ? 3 : 2); ++t) {  // V, K, Q
+          const uint32_t st = t == 0 ? n & 1u : kq.i, ph = t == 0 ? phase2(n) : kq.ph;
+          uint64_t *const full = (t == 0 ? m->full_v : t == 1 ? m->full_k : m->full_q) + st;
+          if (n >= (t == 0 ? NS_V : NS)) wait_bar((t == 0 ? m->empty_v : t == 1 ? m->empty_k : m->empty_q) + st, ph ^ 1u, m);
           if (lane == 0) {
-            mbar_expect_tx(&full[st], TILE);
-            tma_load_3d(sbase + off + st * TILE, map, 0, head, z, &full[st]);
-            tma_load_3d(sbase + off + st * TILE + BLOCK, map, 64, head, z, &full[st]);
+            const CUtensorMap *const map = t == 0 ? &tmap_v : t == 1 ? &tmap_k : &tmap_q;
+            const uint32_t to = sbase + (t == 0 ? OFF_V : t == 1 ? OFF_K : OFF_Q) + st * TILE;
+            const int head = t == 0 ? x.head : x.k_head;
+            mbar_expect_tx(full, TILE);
+            tma_load_3d(to, map, 0, head, z, full);
+            tma_load_3d(to + BLOCK, map, 64, head, z, full);
           }
-          ++count;
-        };
-        load(m->empty_v, m->full_v, stage_v(n), stage_v_phase(n), NS_V, OFF_V, &tmap_v, x.head, nv);
-        load(m->empty_k, m->full_k, stage(n), stage_phase(n), NS, OFF_K, &tmap_k, x.k_head, nk);
-        if (WITH_O) load(m->empty_q, m->full_q, stage(n), stage_phase(n), NS, OFF_Q, &tmap_q, x.k_head, nq);
-        if (stop) break;
+          if (uni(m->abort_flag)) break;
+        }
+        if (uni(m->abort_flag)) break;
+        kq.step();
         ++c;
         ++n;
       }
-      // Copies in flight land before the block ends, whoever has given up waiting for them.
+      // Copies in flight land before the block ends, whoever has given up waiting for them.  After a time-out, which tiles have been
+      // asked for is not known any more: a barrier that is not in use lets the bound on the polls run out.
+      const bool sure = uni(m->abort_flag) == 0;
       const auto land = [&](uint64_t *bar, uint32_t phase) {
 #pragma unroll 1
-        for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(bar, phase); ++p) {
+        for (uint32_t p = 0; p < (sure ? kMaxPolls : kMaxPolls >> 8) && !mbar_try_wait(bar, phase); ++p) {
         }
       };
 #pragma unroll 1
-      for (int i = max(n - NS, 0); i <= n; ++i) {
-        if (i < nv && i >= nv - NS_V) land(&m->full_v[stage_v(i)], stage_v_phase(i));
-        if (i < nk && i >= nk - NS) land(&m->full_k[stage(i)], stage_phase(i));
-        if (i < nq && i >= nq - NS) land(&m->full_q[stage(i)], stage_phase(i));
+      for (int i = max(n - NS, 0); i < (sure ? n : n + 1); ++i) {
+        const uint32_t st = static_cast<uint32_t>(i) % NS, ph = static_cast<uint32_t>(i) / NS & 1u;
+        if (i >= n - NS_V) land(&m->full_v[i & 1], phase2(i));
+        land(&m->full_k[st], ph);
+        if (WITH_O) land(&m->full_q[st], ph);
       }
-    } else if (warp == WARP_MMA || warp == WARP_MMA_O) {
-      const auto gave_up = [&]() { return uni(m->abort_flag) != 0; };  // (one answer for the whole warp)
-      int it = 0, all = 0;  // chunks of all items that have been looked up
-      const auto look = [&]() {  // the next item with tokens, if there is one
-        int chunks = 0;
-        while (chunks == 0 && uni(take(it))) {
-          chunks = uni(chunks_of(m->items[it % RING].n));
-          release(it++);
+    } else if (warp == WARP_DECAY) {
+      int n = 0;
+#pragma unroll 1
+      for (int it = 0;; ++it) {
+        wait_bar(&m->item_full[it % RING], static_cast<uint32_t>(it) / RING & 1u, m);
+        if (uni(m->abort_flag)) break;
+        const Item x = m->items[it % RING];
+        arrive_warp(&m->item_empty[it % RING], lane);
+        const float *g = (a.g_per_head ? a.g + x.lc * a.H_v + x.head : a.g + (x.tok0 + 2 * lane) * a.H_v + x.head);
+        const int64_t stride = a.g_per_head ? 0 : a.H_v;
+        const int chunks = x.n < 0 ? 1 : chunks_of(x.n);
+        float next[2];
+        next[0] = 2 * lane < x.n ? g[0] : 0.f;
+        next[1] = 2 * lane + 1 < x.n ? g[stride] : 0.f;
+#pragma unroll 1
+        for (int c = 0; c < chunks; ++c, ++n) {
+          const int left = x.n - c * C;
+          float cur[2] = {next[0], next[1]};
+          g += C * stride;
+          if (C + 2 * lane < left) next[0] = g[0];
+          if (C + 2 * lane + 1 < left) next[1] = g[stride];
+          if (n >= RING) wait_bar(&m->dec_empty[slot(n)], slot_phase(n) ^ 1u, m);
+          Chunk &w = m->ch[slot(n)];
+          if (lane == 0) {
+            w.rows = x.n < 0 ? -1 : min(left, C);
+            w.first = c == 0;
+            w.last = c == chunks - 1;
+            w.src = x.from != 0 ? state_of(a, sp, x) : nullptr;
+            const int64_t at = static_cast<int64_t>(x.unit) * sp.nseg + x.seg;
+            w.dst = sp.phase == 1 ? sp.seg_state + (at + 1) * (D * D) : x.write ? a.state + x.state : nullptr;
+            w.decay = sp.phase == 1 ? sp.seg_decay + at : nullptr;
+            w.out = ((x.tok0 + c * C) * a.H_v + x.head) * D;
+          }
+          // Log-decays in log2 units as pairs: hi a multiple of 2^-6, so that sums of 64 and their differences are exact (below -2048 a
+          // token forgets everything, and is clamped there), lo the rest, at most 2^-7 each.
+          float hi[2], lo[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            constexpr float L = 1.4426950408889634f, L_LO = static_cast<float>(1.4426950408889634 - static_cast<double>(L));
+            const float y = 2 * lane + j < left ? (cur[j] < -1400.f ? -1400.f : cur[j]) : 0.f;
+            const float p = y * L;
+            hi[j] = rintf(p * 64.f) * (1.f / 64.f);
+            lo[j] = (p - hi[j]) + fmaf(y, L, -p) + y * L_LO;
+          }
+          float sum_hi = hi[0] + hi[1], sum_lo = lo[0] + lo[1];
+#pragma unroll 1
+          for (int d = 1; d < 32; d <<= 1) {
+            const float y = __shfl_up_sync(0xffffffffu, sum_hi, d), z = __shfl_up_sync(0xffffffffu, sum_lo, d);
+            if (lane >= d) {
+              sum_hi += y;
+              sum_lo += z;
+            }
+          }
+          // sums up to this lane's tokens: gh + gl; two(at, h, l): e^{h + l - G} of both, times f
+          const float2 gh = make_float2(sum_hi - hi[1], sum_hi), gl = make_float2(sum_lo - lo[1], sum_lo);
+          const auto below = [&](float *at, float h, float l) {  // e^{h + l - G}
+            reinterpret_cast<float2 *>(at)[lane] = make_float2(ex2f((h - gh.x) + (l - gl.x)), ex2f((h - gh.y) + (l - gl.y)));
+          };
+          const auto above = [&](float *at, float h, float l) {  // q_scale e^{G - h - l}
+            reinterpret_cast<float2 *>(at)[lane] =
+                make_float2(a.q_scale * ex2f((gh.x - h) + (gl.x - l)), a.q_scale * ex2f((gh.y - h) + (gl.y - l)));
+          };
+          const float all_hi = __shfl_sync(0xffffffffu, sum_hi, 31), all_lo = __shfl_sync(0xffffffffu, sum_lo, 31);
+          below(w.w, all_hi, all_lo);
+          if (lane == 0) w.all = ex2f(all_hi + all_lo);
+          if (WITH_O) {
+            reinterpret_cast<float2 *>(w.ghi)[lane] = gh;
+            reinterpret_cast<float2 *>(w.glo)[lane] = gl;
+            above(w.eg, 0.f, 0.f);
+            const int block = lane >> 3;  // B: the last token before this lane's block of 16
+            const float bh = __shfl_sync(0xffffffffu, sum_hi, block * 8 - 1), bl = __shfl_sync(0xffffffffu, sum_lo, block * 8 - 1);
+            above(w.row, block == 0 ? 0.f : bh, block == 0 ? 0.f : bl);
+#pragma unroll 1
+            for (int b = 0; b < 3; ++b) {
+              const float h = __shfl_sync(0xffffffffu, sum_hi, 8 * b + 7), l = __shfl_sync(0xffffffffu, sum_lo, 8 * b + 7);
+              if (block <= b) below(w.col[b], h, l);
+            }
+          }
+          arrive_warp(&m->dec_full[slot(n)], lane);
         }
-        all += chunks;
+        if (x.n < 0) break;
+      }
+    } else {
+      const auto gave_up = [&]() { return uni(m->abort_flag) != 0; };  // (one answer for the whole warp)
+      const auto next = [&](int n) {  // is there a chunk n?
+        const bool yes = uni(there(n));
+        if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
+        return yes;
       };
       if (warp == WARP_MMA) {
         constexpr uint32_t ID_KV = idesc_bf16(128, 128, false, true);
-        look();
         // Test hook: a first, short wait for operands that cannot be there yet.
-        if (a.poll_limit_first_wait && all > 0) {
+        if (a.poll_limit_first_wait) {
           bool done = false;
           for (uint32_t i = 0; i < a.poll_limit_first_wait && !done; ++i) done = mbar_test_wait(&m->k_ready[0], 0);
           if (!done) m->abort_flag = 1;
         }
 #pragma unroll 1
-        for (; n < all && !gave_up(); ++n) {
-          if (n + 1 == all) look();
+        for (int n = 0; next(n); ++n) {
           const uint32_t par = n & 1u;
           wait_bar(&m->v_ready[par], phase2(n), m);
           if (n > 0) wait_bar(&m->d_free, par ^ 1u, m);
@@ -443,39 +541,21 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         }
       } else if constexpr (WITH_O) {
         constexpr uint32_t ID_QK = idesc_bf16(64, 64), ID_QS = idesc_bf16(128, 64);
-        const auto qk = [&](int i) {
-          const uint32_t st = stage(i);
-          wait_bar(&m->full_k[st], stage_phase(i), m);
-          wait_bar(&m->full_q[st], stage_phase(i), m);
-          tc_fence_after_sync();
-          if (gave_up()) return;
-          if (elect_one()) {
-            const uint32_t q = desc_lo_k(sbase + OFF_Q) + st * (TILE >> 4), k = desc_lo_k(sbase + OFF_K) + st * (TILE >> 4);
-            mma16_ss<false>(tm + COL_P, q, k, ID_QK);
-#pragma unroll
-            for (int kk = 1; kk < 8; ++kk) {
-              const uint32_t o = ((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4;
-              mma16_ss<true>(tm + COL_P, q + o, k + o, ID_QK);
-            }
-            mma_commit(&m->bar_p);
-            mma_commit(&m->empty_k[st]);
-          }
-          __syncwarp();
-        };
-        look();
-        bool first = true;
+        Ring<NS> kq;  // of the chunk QK is for
+        uint32_t q_before = 0;
+        bool more = next(0);
+        // QK of chunk n + 1 goes ahead of PV of chunk n: its accumulator has been read, and the next P is waited for longest
 #pragma unroll 1
-        for (n = -1; n < all && !gave_up(); ++n) {
-          if (n + 1 == all) look();
-          const uint32_t st = stage(n), par = n & 1u;
-          if (!first) {
+        for (int n = -1;; ++n) {
+          const uint32_t par = n & 1u;
+          if (n >= 0) {
             // QS
             wait_bar(&m->s_ready, par, m);
             if (n > 0) wait_bar(&m->o_free, par ^ 1u, m);
             tc_fence_after_sync();
             if (gave_up()) break;
             if (elect_one()) {
-              const uint32_t q = desc_lo_k(sbase + OFF_Q) + st * (TILE >> 4);
+              const uint32_t q = desc_lo_k(sbase + OFF_Q) + q_before * (TILE >> 4);
               const uint32_t d = tm + COL_OI;
               mma16_ts<false>(d, tm + COL_SH, q, ID_QS);
 #pragma unroll
@@ -484,19 +564,33 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
                 mma16_ts<true>(d, tm + (i < 8 ? COL_SH : COL_SL) + kk * 8, q + (((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4), ID_QS);
               }
               mma_commit(&m->bar_s);
-              mma_commit(&m->empty_q[st]);
+              mma_commit(&m->empty_q[q_before]);
             }
             __syncwarp();
+            more = next(n + 1);
             wait_bar(&m->p_ready, par, m);
-          }
-          // the next chunk's QK ahead of this one's PV: its accumulator has been read, and the next P is waited for longest
-          if (n + 1 < all) qk(n + 1);
-          if (!first) {
-            // PV: tokens 16 s ... 16 s + 15 reach the rows from 16 s on
             wait_bar(&m->v_ready[par], phase2(n), m);
-            tc_fence_after_sync();
-            if (gave_up()) break;
-            if (elect_one()) {
+          }
+          if (more) {
+            wait_bar(&m->full_k[kq.i], kq.ph, m);
+            wait_bar(&m->full_q[kq.i], kq.ph, m);
+          }
+          tc_fence_after_sync();
+          if (gave_up()) break;
+          if (elect_one()) {
+            if (more) {
+              const uint32_t q = desc_lo_k(sbase + OFF_Q) + kq.i * (TILE >> 4), k = desc_lo_k(sbase + OFF_K) + kq.i * (TILE >> 4);
+              mma16_ss<false>(tm + COL_P, q, k, ID_QK);
+#pragma unroll
+              for (int kk = 1; kk < 8; ++kk) {
+                const uint32_t o = ((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4;
+                mma16_ss<true>(tm + COL_P, q + o, k + o, ID_QK);
+              }
+              mma_commit(&m->bar_p);
+              mma_commit(&m->empty_k[kq.i]);
+            }
+            if (n >= 0) {
+              // PV: tokens 16 s ... 16 s + 15 reach the rows from 16 s on
               const uint32_t v = tm + COL_V + par * 32, p = desc_lo_k(sbase + OFF_PH);
               mma16_ts<false>(tm + COL_OT, v, p, idesc_bf16(128, 64));
 #pragma unroll
@@ -506,9 +600,11 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
               }
               mma_commit(&m->bar_o[par]);
             }
-            __syncwarp();
           }
-          first = false;
+          __syncwarp();
+          if (!more) break;
+          q_before = kq.i;
+          kq.step();
         }
       }
       // products in flight end before their memory is given back, whoever has given up waiting for them
@@ -518,80 +614,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
 #pragma unroll 1
       for (uint32_t p = 0; p < kMaxPolls && !mbar_try_wait(drain, 0); ++p) {
       }
-  } else if (warp == WARP_DECAY) {
-#pragma unroll 1
-    for (int it = 0; uni(take(it)); ++it) {
-      const Item x = m->items[it % RING];
-      release(it);
-      const float *const g = a.g_per_head ? a.g + x.lc * a.H_v + x.head : a.g + x.tok0 * a.H_v + x.head;
-      const int64_t stride = a.g_per_head ? 0 : a.H_v;
-      const auto fetch = [&](int c, float (&y)[2]) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int t = c * C + 2 * lane + j;
-          y[j] = t < x.n ? g[t * stride] : 0.f;
-        }
-      };
-      float cur[2], nxt[2];
-      fetch(0, cur);
-#pragma unroll 1
-      for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
-        fetch(c + 1, nxt);
-        if (n >= RING) wait_bar(&m->dec_empty[slot(n)], slot_phase(n) ^ 1u, m);
-        Weights &w = m->wt[slot(n)];
-        // Log-decays in log2 units as pairs: hi a multiple of 2^-6, so that sums of 64 and their differences are exact (below -2048 a
-        // token forgets everything, and is clamped there), lo the rest, at most 2^-7 each.
-        float hi[2], lo[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          constexpr float L = 1.4426950408889634f, L_LO = static_cast<float>(1.4426950408889634 - static_cast<double>(L));
-          const float x = cur[j] < -1400.f ? -1400.f : cur[j];
-          const float p = x * L;
-          hi[j] = rintf(p * 64.f) * (1.f / 64.f);
-          lo[j] = (p - hi[j]) + fmaf(x, L, -p) + x * L_LO;
-        }
-        float sum_hi = hi[0] + hi[1], sum_lo = lo[0] + lo[1];
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const float y = __shfl_up_sync(0xffffffffu, sum_hi, d), z = __shfl_up_sync(0xffffffffu, sum_lo, d);
-          if (lane >= d) {
-            sum_hi += y;
-            sum_lo += z;
-          }
-        }
-        const auto sum_at = [&](int l, float &h, float &l_) {  // up to lane l's second token
-          h = __shfl_sync(0xffffffffu, sum_hi, l);
-          l_ = __shfl_sync(0xffffffffu, sum_lo, l);
-        };
-        float all_hi, all_lo;
-        sum_at(31, all_hi, all_lo);
-        // this lane's tokens: sums up to the first and up to the second
-        const float gh[2] = {sum_hi - hi[1], sum_hi}, gl[2] = {sum_lo - lo[1], sum_lo};
-        const bool in[2] = {c * C + 2 * lane < x.n, c * C + 2 * lane + 1 < x.n};
-        const auto two = [](float *at, float x, float y) { *reinterpret_cast<float2 *>(at) = make_float2(x, y); };
-        two(&w.w[2 * lane], in[0] ? ex2f((all_hi - gh[0]) + (all_lo - gl[0])) : 0.f, in[1] ? ex2f((all_hi - gh[1]) + (all_lo - gl[1])) : 0.f);
-        if (WITH_O) {
-          two(&w.ghi[2 * lane], gh[0], gh[1]);
-          two(&w.glo[2 * lane], gl[0], gl[1]);
-          two(&w.eg[2 * lane], a.q_scale * ex2f(gh[0] + gl[0]), a.q_scale * ex2f(gh[1] + gl[1]));
-          const int block = lane >> 3;
-          float bh = 0.f, bl = 0.f;
-#pragma unroll
-          for (int b = 0; b < 3; ++b) {
-            float h, l;
-            sum_at(8 * b + 7, h, l);
-            if (block == b + 1) bh = h, bl = l;
-            if (block <= b) two(&w.col[b][2 * lane], ex2f((h - gh[0]) + (l - gl[0])), ex2f((h - gh[1]) + (l - gl[1])));
-          }
-          two(&w.row[2 * lane], a.q_scale * ex2f((gh[0] - bh) + (gl[0] - bl)), a.q_scale * ex2f((gh[1] - bh) + (gl[1] - bl)));
-        }
-        if (lane == 0) w.all = ex2f(all_hi + all_lo);
-        arrive_warp(&m->dec_full[slot(n)], lane);
-        cur[0] = nxt[0];
-        cur[1] = nxt[1];
-      }
     }
-  }
   } else if (warp < WARP_O) {
     // ---- P ----
     regs_down<REGS_P>();
@@ -600,61 +623,54 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       const uint32_t tp = tm + (static_cast<uint32_t>(quad * 32) << 16) + COL_P;
       const int t0 = quad * 16 + g, t1 = t0 + 8;  // this thread's rows; columns 16 s + 2 tig, + 1, + 8, + 9
       unsigned char *const ps = smem + OFF_PH + t0 * 128 + tig * 4;
-      const auto put = [&](int j, uint64_t y0, uint64_t y1) {  // columns 8 j + 2 tig, + 1
-        uint32_t hi, lo;
-        unsigned char *const p = ps + ((j ^ (t0 & 7)) << 4);
-        split2(y0, hi, lo);
-        *reinterpret_cast<uint32_t *>(p) = hi;
-        *reinterpret_cast<uint32_t *>(p + (OFF_PL - OFF_PH)) = lo;
-        split2(y1, hi, lo);
-        *reinterpret_cast<uint32_t *>(p + 8 * 128) = hi;
-        *reinterpret_cast<uint32_t *>(p + 8 * 128 + (OFF_PL - OFF_PH)) = lo;
-      };
-      const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
 #pragma unroll 1
-      for (int it = 0; uni(take(it)); ++it) {
-        const int tokens = m->items[it % RING].n;
-        release(it);
+      for (int n = 0; uni(there(n)); ++n) {
+        const Chunk &w = m->ch[slot(n)];
+        wait_bar(&m->bar_p, n & 1u, m);
+        if (n > 0) wait_bar(&m->bar_o[(n - 1) & 1], phase2(n - 1), m);  // PV of the chunk before has read its P
+        tc_fence_after_sync();
 #pragma unroll 1
-        for (int c = 0; c < chunks_of(tokens); ++c, ++n) {
-          const Weights &w = m->wt[slot(n)];
-          wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-          wait_bar(&m->bar_p, n & 1u, m);
-          if (n > 0) wait_bar(&m->bar_o[(n - 1) & 1], phase2(n - 1), m);  // PV of the chunk before has read its P
-          tc_fence_after_sync();
-          const float r0 = w.row[t0], r1 = w.row[t1];
-          const uint64_t rr0 = dpack2(r0, r0), rr1 = dpack2(r1, r1);
-          const float *const col = w.col[quad > 0 ? quad - 1 : 0] + 2 * tig;
-#pragma unroll 1
-          for (int s = 0; s < quad; ++s) {
-            uint32_t p[8];
-            tmem_ld_16x256b(tp + 16 * s, p);
-            const uint64_t c0 = *reinterpret_cast<const uint64_t *>(col + 16 * s), c1 = *reinterpret_cast<const uint64_t *>(col + 16 * s + 8);
+        for (int s = 0; s <= quad; ++s) {
+          uint32_t p[8];
+          tmem_ld_16x256b(tp + 16 * s, p);
+          uint64_t f[4];  // weights of p's pairs: rows t0, t1, columns + 0, 1; the same rows, columns + 8, 9
+          if (s < quad) {
+            const float r0 = w.row[t0], r1 = w.row[t1];
+            const uint64_t rr0 = dpack2(r0, r0), rr1 = dpack2(r1, r1);
+            const uint64_t *const col = reinterpret_cast<const uint64_t *>(&w.col[quad - 1][16 * s]) + tig;
+            f[0] = dmul2(rr0, col[0]);
+            f[1] = dmul2(rr1, col[0]);
+            f[2] = dmul2(rr0, col[4]);
+            f[3] = dmul2(rr1, col[4]);
             tmem_ld_wait();
-            put(2 * s, dmul2(pair(p[0], p[1]), dmul2(rr0, c0)), dmul2(pair(p[2], p[3]), dmul2(rr1, c0)));
-            put(2 * s + 1, dmul2(pair(p[4], p[5]), dmul2(rr0, c1)), dmul2(pair(p[6], p[7]), dmul2(rr1, c1)));
-          }
-          {
-            uint32_t p[8];
-            tmem_ld_16x256b(tp + 16 * quad, p);
-            const float h0 = w.ghi[t0], l0 = w.glo[t0], h1 = w.ghi[t1], l1 = w.glo[t1];
+          } else {
             tmem_ld_wait();
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              const int i = 16 * quad + 8 * b + 2 * tig;
+            for (int b = 0; b < 4; ++b) {
+              const int t = b & 1 ? t1 : t0, i = 16 * s + (b >> 1) * 8 + 2 * tig;
               const float2 hi = *reinterpret_cast<const float2 *>(&w.ghi[i]), lo = *reinterpret_cast<const float2 *>(&w.glo[i]);
-              const auto at = [&](int e, int t, int col, float ht, float lt, float hi_i, float lo_i) {
-                return col <= t ? __uint_as_float(p[4 * b + e]) * (a.q_scale * ex2f((ht - hi_i) + (lt - lo_i))) : 0.f;
-              };
-              put(2 * quad + b, dpack2(at(0, t0, i, h0, l0, hi.x, lo.x), at(1, t0, i + 1, h0, l0, hi.y, lo.y)),
-                  dpack2(at(2, t1, i, h1, l1, hi.x, lo.x), at(3, t1, i + 1, h1, l1, hi.y, lo.y)));
+              const float h = w.ghi[t], l = w.glo[t];
+              f[b] = dpack2(a.q_scale * ex2f((h - hi.x) + (l - lo.x)), a.q_scale * ex2f((h - hi.y) + (l - lo.y)));
+              // (masked places may hold anything, and above the diagonal weights may not be finite)
+              if (i > t) p[2 * b] = 0;
+              if (i + 1 > t) p[2 * b + 1] = 0;
+              const float2 y = dunpack2(f[b]);
+              f[b] = dpack2(i > t ? 0.f : y.x, i + 1 > t ? 0.f : y.y);
             }
           }
-          fence_smem_to_async();
-          tc_fence_before_sync();
-          arrive_warp(&m->p_ready, lane);
-          if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            uint32_t hi, lo;
+            split2(dmul2(dpack2(__uint_as_float(p[2 * b]), __uint_as_float(p[2 * b + 1])), f[b]), hi, lo);
+            unsigned char *const to = ps + (((2 * s + (b >> 1)) ^ (t0 & 7)) << 4) + (b & 1) * (8 * 128);
+            *reinterpret_cast<uint32_t *>(to) = hi;
+            *reinterpret_cast<uint32_t *>(to + (OFF_PL - OFF_PH)) = lo;
+          }
         }
+        fence_smem_to_async();
+        tc_fence_before_sync();
+        arrive_warp(&m->p_ready, lane);
+        if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
       }
     }
   } else if (warp < WARP_K) {
@@ -666,135 +682,115 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       const int64_t v_stride = static_cast<int64_t>(a.H_v) * D;
       unsigned char *const ost = smem + OFF_O + quad * 4096;
 #pragma unroll 1
-      for (int it = 0; uni(take(it)); ++it) {
-        const int tokens = m->items[it % RING].n;
-        OT *o = static_cast<OT *>(a.o) + (m->items[it % RING].tok0 * a.H_v + m->items[it % RING].head) * D + quad * 32;
-        release(it);
+      for (int n = 0; uni(there(n)); ++n) {
+        const Chunk &w = m->ch[slot(n)];
+        const int rows = w.rows;
+        OT *const o = static_cast<OT *>(a.o) + w.out + quad * 32;
+        wait_bar(&m->bar_o[n & 1], phase2(n), m);
+        if (uni(m->abort_flag)) break;
+        tc_fence_after_sync();
 #pragma unroll 1
-        for (int c = 0; c < chunks_of(tokens); ++c, ++n, o += C * v_stride) {
-          const Weights &w = m->wt[slot(n)];
-          const int rows = tokens - c * C;
-          wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-          wait_bar(&m->bar_o[n & 1], phase2(n), m);
-          tc_fence_after_sync();
-          const bool has_bad = (w.has_bad[quad * 2] | w.has_bad[quad * 2 + 1]) != 0;
-#pragma unroll 1
-          for (int part = 0; part < 4; ++part) {  // 16 columns of d_v (part & 1), 32 tokens (part >> 1)
-            const int half = part & 1, tb = part >> 1;
-            uint32_t oi[16], ot[16];
-            const uint32_t at = tl + (static_cast<uint32_t>(half * 16) << 16) + tb * 32;
-            tmem_ld_16x256b(at + COL_OI, oi);
-            tmem_ld_16x256b(at + COL_OT, ot);
-            tmem_ld_wait();
-            if (part == 3) {
-              tc_fence_before_sync();
-              arrive_warp(&m->o_free, lane);
-            }
-            const int v0 = half * 16 + g;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int t = tb * 32 + 8 * j + 2 * tig;
-              const uint64_t e = *reinterpret_cast<const uint64_t *>(&w.eg[t]);
-              const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
-              float2 y0 = dunpack2(dfma2(e, pair(oi[4 * j], oi[4 * j + 1]), pair(ot[4 * j], ot[4 * j + 1])));
-              float2 y1 = dunpack2(dfma2(e, pair(oi[4 * j + 2], oi[4 * j + 3]), pair(ot[4 * j + 2], ot[4 * j + 3])));
-              if constexpr (sizeof(OT) == 2) {
-                ot[2 * j] = bf16x2(y0.x, y0.y);
-                ot[2 * j + 1] = bf16x2(y1.x, y1.y);
-              } else {
-                OT *const p = o + t * v_stride + v0;
-                if (t < rows) {
-                  p[0] = y0.x;
-                  p[8] = y1.x;
-                }
-                if (t + 1 < rows) {
-                  p[v_stride] = y0.y;
-                  p[v_stride + 8] = y1.y;
-                }
-              }
-            }
-            if constexpr (sizeof(OT) == 2) {
-#pragma unroll
-              for (int j = 0; j < 4; j += 2) {
-                const int t = tb * 32 + 8 * (j + (lane >> 4)) + (lane & 7), ch = half * 2 + (lane >> 3 & 1);
-                stmatrix_x4_trans(smem_u32(ost) + t * 64 + ((ch ^ (t >> 1 & 3)) << 4), ot[2 * j], ot[2 * j + 1], ot[2 * j + 2], ot[2 * j + 3]);
-              }
-            }
+        for (int part = 0; part < 4; ++part) {  // 16 columns of d_v (part & 1), 32 tokens (part >> 1)
+          const int half = part & 1, tb = part >> 1;
+          uint32_t oi[16], ot[16];
+          const uint32_t at = tl + (static_cast<uint32_t>(half * 16) << 16) + tb * 32;
+          tmem_ld_16x256b(at + COL_OI, oi);
+          tmem_ld_16x256b(at + COL_OT, ot);
+          tmem_ld_wait();
+          if (part == 3) {
+            tc_fence_before_sync();
+            arrive_warp(&m->o_free, lane);
           }
-          __syncwarp();
-          if (has_bad) {  // a lane per column
-            const OT nan = static_cast<OT>(__int_as_float(0x7fffffff));
-#pragma unroll 1
-            for (int t = w.has_bad[quad * 2 + (lane >> 4)] ? w.bad[quad * 32 + lane] : C; t < rows && t < C; ++t) {
-              if constexpr (sizeof(OT) == 2)
-                *reinterpret_cast<OT *>(ost + t * 64 + ((lane >> 3 ^ (t >> 1 & 3)) << 4) + (lane & 7) * 2) = nan;
-              else
-                o[t * v_stride + lane] = nan;
+          const int v0 = half * 16 + g;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int t = tb * 32 + 8 * j + 2 * tig;
+            const uint64_t e = *reinterpret_cast<const uint64_t *>(&w.eg[t]);
+            const auto pair = [](uint32_t x, uint32_t y) { return dpack2(__uint_as_float(x), __uint_as_float(y)); };
+            const float2 y0 = dunpack2(dfma2(e, pair(oi[4 * j], oi[4 * j + 1]), pair(ot[4 * j], ot[4 * j + 1])));
+            const float2 y1 = dunpack2(dfma2(e, pair(oi[4 * j + 2], oi[4 * j + 3]), pair(ot[4 * j + 2], ot[4 * j + 3])));
+            if constexpr (sizeof(OT) == 2) {
+              ot[2 * j] = bf16x2(y0.x, y0.y);
+              ot[2 * j + 1] = bf16x2(y1.x, y1.y);
+            } else {
+              OT *const p = o + t * v_stride + v0;
+              if (t < rows) {
+                p[0] = y0.x;
+                p[8] = y1.x;
+              }
+              if (t + 1 < rows) {
+                p[v_stride] = y0.y;
+                p[v_stride + 8] = y1.y;
+              }
             }
-            __syncwarp();
           }
           if constexpr (sizeof(OT) == 2) {
-#pragma unroll 2
-            for (int i8 = 0; i8 < 8; ++i8) {
-              const int t = i8 * 8 + (lane >> 2), ch = lane & 3;
-              const uint4 y = *reinterpret_cast<const uint4 *>(ost + t * 64 + ((ch ^ (t >> 1 & 3)) << 4));
-              if (t < rows) *reinterpret_cast<uint4 *>(o + t * v_stride + ch * 8) = y;
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+              const int t = tb * 32 + 8 * (j + (lane >> 4)) + (lane & 7), ch = half * 2 + (lane >> 3 & 1);
+              stmatrix_x4_trans(smem_u32(ost) + t * 64 + ((ch ^ (t >> 1 & 3)) << 4), ot[2 * j], ot[2 * j + 1], ot[2 * j + 2], ot[2 * j + 3]);
             }
-            __syncwarp();
           }
-          arrive_warp(&m->dec_empty[slot(n)], lane);
         }
+        __syncwarp();
+        if constexpr (sizeof(OT) == 2) {
+#pragma unroll 4
+          for (int i8 = 0; i8 < 8; ++i8) {
+            const int t = i8 * 8 + (lane >> 2), ch = lane & 3;
+            const uint4 y = *reinterpret_cast<const uint4 *>(ost + t * 64 + ((ch ^ (t >> 1 & 3)) << 4));
+            if (t < rows) *reinterpret_cast<uint4 *>(o + t * v_stride + ch * 8) = y;
+          }
+          __syncwarp();
+        }
+        if (w.has_bad[quad * 2] | w.has_bad[quad * 2 + 1]) {  // a lane per column, over what the warp has just stored
+          const OT nan = static_cast<OT>(__int_as_float(0x7fffffff));
+#pragma unroll 1
+          for (int t = w.has_bad[quad * 2 + (lane >> 4)] ? w.bad[quad * 32 + lane] : C; t < rows; ++t) o[t * v_stride + lane] = nan;
+        }
+        arrive_warp(&m->dec_empty[slot(n)], lane);
       }
     }
   } else if (warp < WARP_S) {
     // ---- Kw ----
     regs_down<REGS_K>();
     const int kt = tid - WARP_K * 32;
+    Ring<NS> kq;
 #pragma unroll 1
-    for (int it = 0;; ++it) {
-      if (any_of<1, 128>(!take(it))) break;  // (one answer for all four warps)
-      const int tokens = m->items[it % RING].n;
-      release(it);
+    for (int n = 0; uni(there(n)); ++n, kq.step()) {
+      const Chunk &w = m->ch[slot(n)];
+      const int rows = w.rows;
+      wait_bar(&m->full_k[kq.i], kq.ph, m);
+      const unsigned char *const kr = smem + OFF_K + kq.i * TILE + kt * 16;
+      unsigned char *const kw = smem + OFF_KW + kt * 16;
 #pragma unroll 1
-      for (int c = 0; c < chunks_of(tokens); ++c, ++n) {
-        const uint32_t st = stage(n);
-        const int rows = min(tokens - c * C, C);
-        const Weights &w = m->wt[slot(n)];
-        wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-        // Kw, 32 tokens at a time
-        wait_bar(&m->full_k[st], stage_phase(n), m);
-        const unsigned char *const kr = smem + OFF_K + st * TILE + kt * 16;
-        unsigned char *const kw = smem + OFF_KW + kt * 16;
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          if (n > 0) wait_bar(half == 0 ? &m->bar_kw : &m->bar_d, (n - 1) & 1u, m);  // KV of the chunk before has read this half
+      for (int half = 0; half < 2; ++half) {  // 32 tokens at a time
+        if (n > 0) wait_bar(half == 0 ? &m->bar_kw : &m->bar_d, (n - 1) & 1u, m);  // KV of the chunk before has read this half
 #pragma unroll 2
-          for (int i = 0; i < 4; ++i) {
-            const int row = (kt >> 3) + (half * 2 + (i & 1)) * 16;
-            const uint32_t at = ((i >> 1) * 4 + half * 2 + (i & 1)) * 2048;
-            const float f = w.w[row];
-            const uint64_t ff = dpack2(f, f);
-            uint4 y = *reinterpret_cast<const uint4 *>(kr + at);
-            if (row >= rows) y = make_uint4(0u, 0u, 0u, 0u);
-            uint64_t rest[4] = {dmul2(dpack2(bf_lo(y.x), bf_hi(y.x)), ff), dmul2(dpack2(bf_lo(y.y), bf_hi(y.y)), ff),
-                                dmul2(dpack2(bf_lo(y.z), bf_hi(y.z)), ff), dmul2(dpack2(bf_lo(y.w), bf_hi(y.w)), ff)};
+        for (int i = 0; i < 4; ++i) {
+          const int row = (kt >> 3) + (half * 2 + (i & 1)) * 16;
+          const uint32_t at = ((i >> 1) * 4 + half * 2 + (i & 1)) * 2048;
+          const float f = w.w[row];
+          const uint64_t ff = dpack2(f, f);
+          uint4 y = *reinterpret_cast<const uint4 *>(kr + at);
+          if (row >= rows) y = make_uint4(0u, 0u, 0u, 0u);
+          uint64_t rest[4] = {dmul2(dpack2(bf_lo(y.x), bf_hi(y.x)), ff), dmul2(dpack2(bf_lo(y.y), bf_hi(y.y)), ff),
+                              dmul2(dpack2(bf_lo(y.z), bf_hi(y.z)), ff), dmul2(dpack2(bf_lo(y.w), bf_hi(y.w)), ff)};
 #pragma unroll
-            for (int part = 0; part < KSPLIT; ++part) {
-              uint4 b;
-              b.x = take_bf16x2(rest[0]);
-              b.y = take_bf16x2(rest[1]);
-              b.z = take_bf16x2(rest[2]);
-              b.w = take_bf16x2(rest[3]);
-              *reinterpret_cast<uint4 *>(kw + part * TILE + at) = b;
-            }
+          for (int part = 0; part < KSPLIT; ++part) {
+            uint4 b;
+            b.x = take_bf16x2(rest[0]);
+            b.y = take_bf16x2(rest[1]);
+            b.z = take_bf16x2(rest[2]);
+            b.w = take_bf16x2(rest[3]);
+            *reinterpret_cast<uint4 *>(kw + part * TILE + at) = b;
           }
-          fence_smem_to_async();
-          arrive_warp(&m->k_ready[half], lane);
         }
-        if (lane == 0) {
-          mbar_arrive(&m->empty_k[st]);
-          mbar_arrive(&m->dec_empty[slot(n)]);
-        }
+        fence_smem_to_async();
+        arrive_warp(&m->k_ready[half], lane);
+      }
+      if (lane == 0) {
+        mbar_arrive(&m->empty_k[kq.i]);
+        mbar_arrive(&m->dec_empty[slot(n)]);
       }
     }
   } else {
@@ -803,142 +799,131 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     const int quad = warp & 3, half = (warp - WARP_S) >> 2;
     const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
     const int v = quad * 32 + lane, k0 = half * 64;
+    uint64_t S[32];
+    float decay = 1.f;
+    uint32_t units = 0;
 #pragma unroll 1
-    for (int it = 0;; ++it) {
-      if (any_of<2, 256>(!take(it))) break;  // (one answer for all eight warps)
-      const Item x = m->items[it % RING];
-      release(it);
-      uint64_t S[32];
-      const int64_t seg_at = (static_cast<int64_t>(x.unit) * sp.nseg + x.seg) * (D * D);
-      const auto fetch = [&]() {
-        const float *const src = (x.from == 2 ? sp.seg_state + seg_at : a.state + x.state) + k0 * D + v;
-        if (x.from != 0) {
+    for (int n = 0; uni(there(n)); ++n) {
+      Chunk &w = m->ch[slot(n)];
+      const uint32_t par = n & 1u;
+      const int rows = w.rows;
+      // V^T, this warp's 16 columns.  A value that is none would reach every row of its column through products with weights that are
+      // zero, so it is taken out and remembered; 0 * x + sum is NaN from the first of them on.
+      wait_bar(&m->full_v[par], phase2(n), m);
+      // the products of the chunk before the last have read their V^T (their KV has been waited for)
+      if (WITH_O && n > 1) wait_bar(&m->bar_o[par], phase2(n - 2), m);
+      tc_fence_after_sync();
+      {
+        unsigned char *const vt = smem + OFF_V + par * TILE + (quad >> 1) * BLOCK;
+        const int ch = (quad & 1) * 4 + half * 2;  // two of the 16-byte places of a row
+        if (rows < C) {  // nothing from behind the last token
+#pragma unroll 1
+          for (int t = rows + (lane >> 1); t < C; t += 16)
+            *reinterpret_cast<uint4 *>(vt + t * 128 + (((ch + (lane & 1)) ^ (t & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+          fence_smem_to_async();  // (the next tile lands here)
+          __syncwarp();
+        }
+        bool looked = false;
+        uint32_t r[16];
+#pragma unroll 1
+        for (;;) {
+          __nv_bfloat162 probe = __floats2bfloat162_rn(0.f, 0.f);
+          const __nv_bfloat162 zero2 = probe;
+#pragma unroll
+          for (int j = 0; j < 8; j += 2) {
+            const int t = 8 * (j + (lane >> 4)) + (lane & 7);
+            ldmatrix_x4_trans(r[2 * j], r[2 * j + 1], r[2 * j + 2], r[2 * j + 3],
+                              smem_u32(vt) + t * 128 + (((ch + (lane >> 3 & 1)) ^ (t & 7)) << 4));
+          }
+#pragma unroll
+          for (int j = 0; j < 16; ++j) probe = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&r[j]), zero2, probe);
+          const bool none = __isnan(__low2float(probe)) || __isnan(__high2float(probe));
+          if (!__any_sync(0xffffffffu, none) || looked) break;
+          looked = true;
+          if (lane < 16) {
+            int first = C;  // of this lane's column
+#pragma unroll 1
+            for (int t = rows - 1; t >= 0; --t) {
+              uint16_t *const e = reinterpret_cast<uint16_t *>(vt + t * 128 + (((ch + (lane >> 3)) ^ (t & 7)) << 4) + (lane & 7) * 2);
+              if ((*e & 0x7F80u) == 0x7F80u) {
+                *e = 0;
+                first = t;
+              }
+            }
+            w.bad[quad * 32 + half * 16 + lane] = first;
+          }
+          fence_smem_to_async();  // (the next tile lands here)
+          __syncwarp();
+        }
+        if (lane == 0) w.has_bad[quad * 2 + half] = looked;
+        tmem_st_16x128b(tl + COL_V + par * 32 + (static_cast<uint32_t>(half * 16) << 16), r);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        arrive_warp(&m->v_ready[par], lane);
+        if (lane == 0) mbar_arrive(&m->empty_v[par]);
+      }
+      if (w.first) {
+        const float *const src = w.src + k0 * D + v;
+        decay = 1.f;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) S[j] = 0;
+        if (w.src) {
 #pragma unroll
           for (int j = 0; j < 32; ++j) S[j] = dpack2(src[2 * j * D], src[(2 * j + 1) * D]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) S[j] = 0;
         }
-      };
-      float decay = 1.f;
-      bool fetched = false;
-#pragma unroll 1
-      for (int c = 0; c < chunks_of(x.n); ++c, ++n) {
-        Weights &w = m->wt[slot(n)];
-        const uint32_t par = n & 1u;
-        const int rows = min(x.n - c * C, C);
-        // V^T, this warp's 16 columns.  A value that is none would reach every row of its column through products with weights that are
-        // zero, so it is taken out and remembered; 0 * x + sum is NaN from the first of them on.
-        wait_bar(&m->dec_full[slot(n)], slot_phase(n), m);
-        wait_bar(&m->full_v[stage_v(n)], stage_v_phase(n), m);
-        if (n > 1) {  // the products of the chunk before the last have read their V^T (their KV has been waited for)
-          if (WITH_O) wait_bar(&m->bar_o[par], phase2(n - 2), m);
-          tc_fence_after_sync();
-        }
-        {
-          unsigned char *const vt = smem + OFF_V + stage_v(n) * TILE + (quad >> 1) * BLOCK;
-          const int ch = (quad & 1) * 4 + half * 2;  // two of the 16-byte places of a row
-          if (rows < C) {  // nothing from behind the last token
-#pragma unroll 1
-            for (int t = rows + (lane >> 1); t < C; t += 16)
-              *reinterpret_cast<uint4 *>(vt + t * 128 + (((ch + (lane & 1)) ^ (t & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
-            fence_smem_to_async();  // (the next tile lands here)
-            __syncwarp();
-          }
-          bool looked = false;
-          uint32_t r[16];
-#pragma unroll 1
-          for (;;) {
-            __nv_bfloat162 probe = __floats2bfloat162_rn(0.f, 0.f);
-            const __nv_bfloat162 zero2 = probe;
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-              const int t = 8 * (j + (lane >> 4)) + (lane & 7);
-              ldmatrix_x4_trans(r[2 * j], r[2 * j + 1], r[2 * j + 2], r[2 * j + 3],
-                                smem_u32(vt) + t * 128 + (((ch + (lane >> 3 & 1)) ^ (t & 7)) << 4));
-            }
-#pragma unroll
-            for (int j = 0; j < 16; ++j) probe = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&r[j]), zero2, probe);
-            const bool none = __isnan(__low2float(probe)) || __isnan(__high2float(probe));
-            if (!__any_sync(0xffffffffu, none) || looked) break;
-            looked = true;
-            if (lane < 16) {
-              int first = C;  // of this lane's column
-#pragma unroll 1
-              for (int t = rows - 1; t >= 0; --t) {
-                uint16_t *const e = reinterpret_cast<uint16_t *>(vt + t * 128 + (((ch + (lane >> 3)) ^ (t & 7)) << 4) + (lane & 7) * 2);
-                if ((*e & 0x7F80u) == 0x7F80u) {
-                  *e = 0;
-                  first = t;
-                }
-              }
-              w.bad[quad * 32 + half * 16 + lane] = first;
-            }
-            fence_smem_to_async();  // (the next tile lands here)
-            __syncwarp();
-          }
-          if (lane == 0) w.has_bad[quad * 2 + half] = looked;
-          tmem_st_16x128b(tl + COL_V + par * 32 + (static_cast<uint32_t>(half * 16) << 16), r);
-          tmem_st_wait();
-          tc_fence_before_sync();
-          arrive_warp(&m->v_ready[par], lane);
-          if (lane == 0) mbar_arrive(&m->empty_v[stage_v(n)]);
-        }
-        if (!fetched) fetch();
-        fetched = true;
-        if constexpr (WITH_O) {
-          if (n > 0) wait_bar(&m->bar_s, (n - 1) & 1u, m);  // QS of the chunk before has read its state
-          tc_fence_after_sync();
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            uint32_t hi[8], lo[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) split2(S[b * 8 + j], hi[j], lo[j]);
-            tmem_st8(tl + COL_SH + half * 32 + b * 8, hi);
-            tmem_st8(tl + COL_SL + half * 32 + b * 8, lo);
-          }
-          tmem_st_wait();
-          tc_fence_before_sync();
-          arrive_warp(&m->s_ready, lane);
-        }
-        float f = w.all;
-        decay *= f;
-        wait_bar(&m->bar_d, n & 1u, m);
+      }
+      if constexpr (WITH_O) {
+        if (n > 0) wait_bar(&m->bar_s, (n - 1) & 1u, m);  // QS of the chunk before has read its state
         tc_fence_after_sync();
-        if (w.has_bad[quad * 2 + (lane >> 4)] != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
-        const uint64_t ff = dpack2(f, f);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-          uint32_t d[16];
-          tmem_ld16(tl + COL_D + k0 + b * 16, d);
-          tmem_ld_wait();
+          uint32_t hi[8], lo[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            S[b * 8 + j] = dfma2(S[b * 8 + j], ff, dpack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
+          for (int j = 0; j < 8; ++j) split2(S[b * 8 + j], hi[j], lo[j]);
+          tmem_st8(tl + COL_SH + half * 32 + b * 8, hi);
+          tmem_st8(tl + COL_SL + half * 32 + b * 8, lo);
         }
+        tmem_st_wait();
         tc_fence_before_sync();
-        arrive_warp(&m->d_free, lane);
-        if (lane == 0) mbar_arrive(&m->dec_empty[slot(n)]);
+        arrive_warp(&m->s_ready, lane);
       }
-      if (!fetched) fetch();  // (no tokens)
-      // a unit is written as a whole or, after a time-out, not at all
-      if (any_of<2, 256>(m->abort_flag != 0)) break;
-      float *dst = nullptr;
-      if (sp.phase == 1) {
-        dst = sp.seg_state + seg_at + D * D;
-        if (warp == WARP_S && lane == 0) sp.seg_decay[static_cast<int64_t>(x.unit) * sp.nseg + x.seg] = decay;
-      } else if (x.write) {
-        dst = a.state + x.state;
-      }
-      if (dst) {
-        dst += k0 * D + v;
+      float f = w.all;
+      decay *= f;
+      wait_bar(&m->bar_d, par, m);
+      tc_fence_after_sync();
+      if (w.has_bad[quad * 2 + (lane >> 4)] != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
+      const uint64_t ff = dpack2(f, f);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const float2 y = dunpack2(S[j]);
-          dst[2 * j * D] = y.x;
-          dst[(2 * j + 1) * D] = y.y;
-        }
+      for (int b = 0; b < 4; ++b) {
+        uint32_t d[16];
+        tmem_ld16(tl + COL_D + k0 + b * 16, d);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          S[b * 8 + j] = dfma2(S[b * 8 + j], ff, dpack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
       }
+      tc_fence_before_sync();
+      arrive_warp(&m->d_free, lane);
+      if (w.last) {
+        // A unit is written as a whole or, after a time-out, not at all: every warp that has got through it arrives, and it is written
+        // if all have.
+        if (uni(m->abort_flag)) break;
+        arrive_warp(&m->s_whole, lane);
+        wait_bar(&m->s_whole, units & 1u, m);
+        if (!uni(mbar_test_wait(&m->s_whole, units & 1u))) break;
+        ++units;
+        if (w.dst) {
+          float *const dst = w.dst + k0 * D + v;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const float2 y = dunpack2(S[j]);
+            dst[2 * j * D] = y.x;
+            dst[(2 * j + 1) * D] = y.y;
+          }
+        }
+        if (w.decay && warp == WARP_S && lane == 0) *w.decay = decay;
+      }
+      arrive_warp(&m->dec_empty[slot(n)], lane);
     }
   }
   stream_order_release();
