@@ -802,12 +802,13 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     uint64_t S[32];
     float decay = 1.f;
     uint32_t units = 0;
-#pragma unroll 1
-    for (int n = 0; uni(there(n)); ++n) {
+    // V^T of chunk n, if there is one.
+    const auto values = [&](int n) {
+      if (!uni(there(n))) return false;
       Chunk &w = m->ch[slot(n)];
       const uint32_t par = n & 1u;
       const int rows = w.rows;
-      // V^T, this warp's 16 columns.  A value that is none would reach every row of its column through products with weights that are
+      // This warp's 16 columns.  A value that is none would reach every row of its column through products with weights that are
       // zero, so it is taken out and remembered; 0 * x + sum is NaN from the first of them on.
       wait_bar(&m->full_v[par], phase2(n), m);
       // the products of the chunk before the last have read their V^T (their KV has been waited for)
@@ -862,68 +863,81 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
         arrive_warp(&m->v_ready[par], lane);
         if (lane == 0) mbar_arrive(&m->empty_v[par]);
       }
-      if (w.first) {
-        const float *const src = w.src + k0 * D + v;
-        decay = 1.f;
+      return true;
+    };
+    // V^T goes a chunk ahead: a chunk's own products are under way meanwhile.
+    bool more = false;
+#pragma unroll 1
+    for (int n = -1;; ++n) {
+      Chunk &w = m->ch[slot(n)];
+      if (n >= 0) {
+        if (w.first) {
+          const float *const src = w.src + k0 * D + v;
+          decay = 1.f;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) S[j] = 0;
-        if (w.src) {
+          for (int j = 0; j < 32; ++j) S[j] = 0;
+          if (w.src) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) S[j] = dpack2(src[2 * j * D], src[(2 * j + 1) * D]);
-        }
-      }
-      if constexpr (WITH_O) {
-        if (n > 0) wait_bar(&m->bar_s, (n - 1) & 1u, m);  // QS of the chunk before has read its state
-        tc_fence_after_sync();
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          uint32_t hi[8], lo[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) split2(S[b * 8 + j], hi[j], lo[j]);
-          tmem_st8(tl + COL_SH + half * 32 + b * 8, hi);
-          tmem_st8(tl + COL_SL + half * 32 + b * 8, lo);
-        }
-        tmem_st_wait();
-        tc_fence_before_sync();
-        arrive_warp(&m->s_ready, lane);
-      }
-      float f = w.all;
-      decay *= f;
-      wait_bar(&m->bar_d, par, m);
-      tc_fence_after_sync();
-      if (w.has_bad[quad * 2 + (lane >> 4)] != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
-      const uint64_t ff = dpack2(f, f);
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        uint32_t d[16];
-        tmem_ld16(tl + COL_D + k0 + b * 16, d);
-        tmem_ld_wait();
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          S[b * 8 + j] = dfma2(S[b * 8 + j], ff, dpack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
-      }
-      tc_fence_before_sync();
-      arrive_warp(&m->d_free, lane);
-      if (w.last) {
-        // A unit is written as a whole or, after a time-out, not at all: every warp that has got through it arrives, and it is written
-        // if all have.
-        if (uni(m->abort_flag)) break;
-        arrive_warp(&m->s_whole, lane);
-        wait_bar(&m->s_whole, units & 1u, m);
-        if (!uni(mbar_test_wait(&m->s_whole, units & 1u))) break;
-        ++units;
-        if (w.dst) {
-          float *const dst = w.dst + k0 * D + v;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float2 y = dunpack2(S[j]);
-            dst[2 * j * D] = y.x;
-            dst[(2 * j + 1) * D] = y.y;
+            for (int j = 0; j < 32; ++j) S[j] = dpack2(src[2 * j * D], src[(2 * j + 1) * D]);
           }
         }
-        if (w.decay && warp == WARP_S && lane == 0) *w.decay = decay;
+        if constexpr (WITH_O) {
+          if (n > 0) wait_bar(&m->bar_s, (n - 1) & 1u, m);  // QS of the chunk before has read its state
+          tc_fence_after_sync();
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            uint32_t hi[8], lo[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) split2(S[b * 8 + j], hi[j], lo[j]);
+            tmem_st8(tl + COL_SH + half * 32 + b * 8, hi);
+            tmem_st8(tl + COL_SL + half * 32 + b * 8, lo);
+          }
+          tmem_st_wait();
+          tc_fence_before_sync();
+          arrive_warp(&m->s_ready, lane);
+        }
       }
-      arrive_warp(&m->dec_empty[slot(n)], lane);
+      more = values(n + 1);
+      if (n >= 0) {
+        float f = w.all;
+        decay *= f;
+        wait_bar(&m->bar_d, n & 1u, m);
+        tc_fence_after_sync();
+        if (w.has_bad[quad * 2 + (lane >> 4)] != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
+        const uint64_t ff = dpack2(f, f);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          uint32_t d[16];
+          tmem_ld16(tl + COL_D + k0 + b * 16, d);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            S[b * 8 + j] = dfma2(S[b * 8 + j], ff, dpack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
+        }
+        tc_fence_before_sync();
+        arrive_warp(&m->d_free, lane);
+        if (w.last) {
+          // A unit is written as a whole or, after a time-out, not at all: every warp that has got through it arrives, and it is written
+          // if all have.
+          if (uni(m->abort_flag)) break;
+          arrive_warp(&m->s_whole, lane);
+          wait_bar(&m->s_whole, units & 1u, m);
+          if (!uni(mbar_test_wait(&m->s_whole, units & 1u))) break;
+          ++units;
+          if (w.dst) {
+            float *const dst = w.dst + k0 * D + v;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const float2 y = dunpack2(S[j]);
+              dst[2 * j * D] = y.x;
+              dst[(2 * j + 1) * D] = y.y;
+            }
+          }
+          if (w.decay && warp == WARP_S && lane == 0) *w.decay = decay;
+        }
+        arrive_warp(&m->dec_empty[slot(n)], lane);
+      }
+      if (!more) break;
     }
   }
   stream_order_release();
