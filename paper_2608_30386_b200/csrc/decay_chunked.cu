@@ -865,22 +865,36 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       }
       return true;
     };
+    // The state goes where it belongs, and the next unit's takes its place (null: from nowhere), 16 values of a thread at a time, so that the loads
+    // are under way beside the stores.
+    const auto exchange = [&](float *dst, const float *src) {
+      const bool out = dst != nullptr, in = src != nullptr;
+      dst += k0 * D + v;
+      src += k0 * D + v;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        if (out) {
+#pragma unroll
+          for (int j = 8 * b; j < 8 * b + 8; ++j) {
+            const float2 y = dunpack2(S[j]);
+            dst[2 * j * D] = y.x;
+            dst[(2 * j + 1) * D] = y.y;
+          }
+        }
+#pragma unroll
+        for (int j = 8 * b; j < 8 * b + 8; ++j) S[j] = 0;
+        if (in) {
+#pragma unroll
+          for (int j = 8 * b; j < 8 * b + 8; ++j) S[j] = dpack2(src[2 * j * D], src[(2 * j + 1) * D]);
+        }
+      }
+    };
     // V^T goes a chunk ahead: a chunk's own products are under way meanwhile.
     bool more = false;
 #pragma unroll 1
     for (int n = -1;; ++n) {
       Chunk &w = m->ch[slot(n)];
       if (n >= 0) {
-        if (w.first) {
-          const float *const src = w.src + k0 * D + v;
-          decay = 1.f;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) S[j] = 0;
-          if (w.src) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) S[j] = dpack2(src[2 * j * D], src[(2 * j + 1) * D]);
-          }
-        }
         if constexpr (WITH_O) {
           if (n > 0) wait_bar(&m->bar_s, (n - 1) & 1u, m);  // QS of the chunk before has read its state
           tc_fence_after_sync();
@@ -924,18 +938,14 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           wait_bar(&m->s_whole, units & 1u, m);
           if (!uni(mbar_test_wait(&m->s_whole, units & 1u))) break;
           ++units;
-          if (w.dst) {
-            float *const dst = w.dst + k0 * D + v;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float2 y = dunpack2(S[j]);
-              dst[2 * j * D] = y.x;
-              dst[(2 * j + 1) * D] = y.y;
-            }
-          }
+          exchange(w.dst, more ? m->ch[slot(n + 1)].src : nullptr);
           if (w.decay && warp == WARP_S && lane == 0) *w.decay = decay;
+          decay = 1.f;
         }
         arrive_warp(&m->dec_empty[slot(n)], lane);
+      }
+      else if (more) {
+        exchange(nullptr, m->ch[0].src);
       }
       if (!more) break;
     }
