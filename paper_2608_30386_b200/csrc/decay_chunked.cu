@@ -66,7 +66,8 @@ constexpr uint32_t COL_D = 0, COL_SH = 128, COL_SL = 192, COL_P = 256, COL_OI = 
 struct alignas(16) Chunk {
   int32_t rows;          // its tokens; negative: there are no more chunks
   int32_t first, last;   // of its unit
-  float all;             // e^{G_C}
+  float all, all_lo;     // e^{G_C}, and what it is short of it
+  float log;             // G_C
   const float *src;      // first: the unit's state; null: zero
   float *dst, *decay;    // last: where its new state goes, and (a segment's) its decay; null: nowhere
   int64_t out;           // its first output, in elements
@@ -180,10 +181,6 @@ __device__ __forceinline__ uint32_t take_bf16x2(uint64_t &xy) {
   xy = dsub2(xy, dpack2(bf_lo(b), bf_hi(b)));
   return b;
 }
-__device__ __forceinline__ void split2(uint64_t xy, uint32_t &hi, uint32_t &lo) {
-  hi = take_bf16x2(xy);
-  lo = take_bf16x2(xy);
-}
 __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t &r0, uint32_t &r1, uint32_t &r2, uint32_t &r3, uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
 }
@@ -267,6 +264,7 @@ template <bool WITH_O, typename OT>
 __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_constant__ DascDecayArgs a, const __grid_constant__ Split sp,
                                                              const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                                                              const __grid_constant__ CUtensorMap tmap_v) {
+  constexpr int OSPLIT = sizeof(OT) == 2 ? 1 : 2;  // parts of P and of the state on the way to the outputs
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sbase = smem_u32(smem);
   Misc *const m = reinterpret_cast<Misc *>(smem + OFF_MISC);
@@ -482,7 +480,19 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           };
           const float all_hi = __shfl_sync(0xffffffffu, sum_hi, 31), all_lo = __shfl_sync(0xffffffffu, sum_lo, 31);
           below(w.w, all_hi, all_lo);
-          if (lane == 0) w.all = ex2f(all_hi + all_lo);
+          if (lane == 0) {
+            // The state is multiplied by e^{G_C} once per chunk: half an ulp, the same every time where the decay is, is 5e-6 of a state that
+            // lasts 10^4 tokens.  Slow decay is 1 + d with d good to its own last bits, and the rest of the sum kept.
+            w.log = all_hi + all_lo;
+            float f = ex2f(w.log), f_lo = 0.f;
+            if (w.log > -1.f) {
+              const float d = expm1f(w.log * 0.6931471805599453f);
+              f = 1.f + d;
+              f_lo = d - (f - 1.f);
+            }
+            w.all = f;
+            w.all_lo = f_lo;
+          }
           if (WITH_O) {
             reinterpret_cast<float2 *>(w.ghi)[lane] = gh;
             reinterpret_cast<float2 *>(w.glo)[lane] = gl;
@@ -559,7 +569,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
               const uint32_t d = tm + COL_OI;
               mma16_ts<false>(d, tm + COL_SH, q, ID_QS);
 #pragma unroll
-              for (int i = 1; i < 16; ++i) {
+              for (int i = 1; i < 8 * OSPLIT; ++i) {
                 const int kk = i & 7;
                 mma16_ts<true>(d, tm + (i < 8 ? COL_SH : COL_SL) + kk * 8, q + (((kk >> 2) * BLOCK + (kk & 3) * 32) >> 4), ID_QS);
               }
@@ -594,7 +604,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
               const uint32_t v = tm + COL_V + par * 32, p = desc_lo_k(sbase + OFF_PH);
               mma16_ts<false>(tm + COL_OT, v, p, idesc_bf16(128, 64));
 #pragma unroll
-              for (int i = 1; i < 8; ++i) {
+              for (int i = 1; i < 4 * OSPLIT; ++i) {
                 const uint32_t s = i & 3;
                 mma16_ts<true>(tm + COL_OT + 16 * s, v + 8 * s, p + (((i < 4 ? 0 : OFF_PL - OFF_PH) + s * 2048 + s * 32) >> 4), idesc_bf16(128, 64 - 16 * s));
               }
@@ -660,11 +670,10 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           }
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
-            uint32_t hi, lo;
-            split2(dmul2(dpack2(__uint_as_float(p[2 * b]), __uint_as_float(p[2 * b + 1])), f[b]), hi, lo);
+            uint64_t rest = dmul2(dpack2(__uint_as_float(p[2 * b]), __uint_as_float(p[2 * b + 1])), f[b]);
             unsigned char *const to = ps + (((2 * s + (b >> 1)) ^ (t0 & 7)) << 4) + (b & 1) * (8 * 128);
-            *reinterpret_cast<uint32_t *>(to) = hi;
-            *reinterpret_cast<uint32_t *>(to + (OFF_PL - OFF_PH)) = lo;
+#pragma unroll
+            for (int part = 0; part < OSPLIT; ++part) *reinterpret_cast<uint32_t *>(to + part * (OFF_PL - OFF_PH)) = take_bf16x2(rest);
           }
         }
         fence_smem_to_async();
@@ -800,7 +809,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
     const uint32_t tl = tm + (static_cast<uint32_t>(quad * 32) << 16);
     const int v = quad * 32 + lane, k0 = half * 64;
     uint64_t S[32];
-    float decay = 1.f;
+    float decay = 0.f;  // the unit's, in log2 units
     uint32_t units = 0;
     // V^T of chunk n, if there is one.
     const auto values = [&](int n) {
@@ -900,11 +909,16 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           tc_fence_after_sync();
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
-            uint32_t hi[8], lo[8];
+            uint64_t rest[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) split2(S[b * 8 + j], hi[j], lo[j]);
-            tmem_st8(tl + COL_SH + half * 32 + b * 8, hi);
-            tmem_st8(tl + COL_SL + half * 32 + b * 8, lo);
+            for (int j = 0; j < 8; ++j) rest[j] = S[b * 8 + j];
+#pragma unroll
+            for (int part = 0; part < OSPLIT; ++part) {
+              uint32_t r[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) r[j] = take_bf16x2(rest[j]);
+              tmem_st8(tl + COL_SH + part * (COL_SL - COL_SH) + half * 32 + b * 8, r);
+            }
           }
           tmem_st_wait();
           tc_fence_before_sync();
@@ -914,11 +928,12 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
       more = values(n + 1);
       if (n >= 0) {
         float f = w.all;
-        decay *= f;
+        const float f_lo = w.all_lo;
+        decay += w.log;
         wait_bar(&m->bar_d, n & 1u, m);
         tc_fence_after_sync();
         if (w.has_bad[quad * 2 + (lane >> 4)] != 0 && w.bad[v] < C) f = __int_as_float(0x7fffffff);  // the column is none from here on
-        const uint64_t ff = dpack2(f, f);
+        const uint64_t ff = dpack2(f, f), ll = dpack2(f_lo, f_lo);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           uint32_t d[16];
@@ -926,7 +941,7 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           tmem_ld_wait();
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            S[b * 8 + j] = dfma2(S[b * 8 + j], ff, dpack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
+            S[b * 8 + j] = dfma2(S[b * 8 + j], ff, dfma2(S[b * 8 + j], ll, dpack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1]))));
         }
         tc_fence_before_sync();
         arrive_warp(&m->d_free, lane);
@@ -939,8 +954,8 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
           if (!uni(mbar_test_wait(&m->s_whole, units & 1u))) break;
           ++units;
           exchange(w.dst, more ? m->ch[slot(n + 1)].src : nullptr);
-          if (w.decay && warp == WARP_S && lane == 0) *w.decay = decay;
-          decay = 1.f;
+          if (w.decay && warp == WARP_S && lane == 0) *w.decay = exp2f(decay);
+          decay = 0.f;
         }
         arrive_warp(&m->dec_empty[slot(n)], lane);
       }

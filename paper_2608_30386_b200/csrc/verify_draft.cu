@@ -16,7 +16,7 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int NT = 512, NW = NT / 32;
+constexpr int NT = 256, NW = NT / 32;
 constexpr int TILE = 128;  // entries of a row that a warp takes at once: four per lane
 
 template <typename T>
@@ -48,7 +48,7 @@ __device__ __forceinline__ void load4(const T *row, int i, int vocab, float (&x)
 }
 
 template <typename T, bool VEC, int CL>
-__global__ void __launch_bounds__(NT) verify_draft_kernel(const __grid_constant__ DascVerifyArgs a) {
+__global__ void __launch_bounds__(NT, 4) verify_draft_kernel(const __grid_constant__ DascVerifyArgs a) {
   __shared__ double warp_sum[NW], s_before, s_threshold;
   __shared__ int s_count, s_winner;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -190,38 +190,47 @@ __global__ void __launch_bounds__(NT) verify_draft_kernel(const __grid_constant_
   if (gw != winner) return;
   double before = s_before;
   const double threshold = s_threshold;
-  int token = -1, last_some = -1;
-  for (int t = first; t < last && token < 0; ++t) {
+  // the first tile that takes it over (or the last one with any weight)
+  int found = -1;
+  double found_before = before;
+  bool over = false;
+#pragma unroll 4
+  for (int t = first; t < last; ++t) {
     double w[4];
     weights(t, w);
-    double incl = (w[0] + w[1]) + (w[2] + w[3]);
+    double sum = (w[0] + w[1]) + (w[2] + w[3]);
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const double y = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += y;
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (!over && sum > 0.0) {
+      found = t;
+      found_before = before;
+      over = before + sum > threshold;
     }
-    const double excl = __shfl_up_sync(0xffffffffu, incl, 1);
-    double x = before + (lane > 0 ? excl : 0.0);
-    int here = -1, any = -1;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x += w[j];
-      if (w[j] > 0.0) {
-        any = j;
-        if (here < 0 && x > threshold) here = j;
-      }
-    }
-    const uint32_t hit = __ballot_sync(0xffffffffu, here >= 0), some_here = __ballot_sync(0xffffffffu, any >= 0);
-    if (hit) {
-      const int l = __ffs(hit) - 1;
-      token = t * TILE + l * 4 + __shfl_sync(0xffffffffu, here, l);
-    } else if (some_here) {
-      const int l = 31 - __clz(some_here);
-      last_some = t * TILE + l * 4 + __shfl_sync(0xffffffffu, any, l);
-    }
-    before += __shfl_sync(0xffffffffu, incl, 31);
+    before += sum;
   }
-  if (lane == 0) a.out[r * a.out_stride + count] = token >= 0 ? token : last_some;
+  double w[4];
+  weights(found, w);
+  double incl = (w[0] + w[1]) + (w[2] + w[3]);
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const double y = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += y;
+  }
+  const double excl = __shfl_up_sync(0xffffffffu, incl, 1);
+  double x = found_before + (lane > 0 ? excl : 0.0);
+  int here = -1, any = -1;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x += w[j];
+    if (w[j] > 0.0) {
+      any = j;
+      if (here < 0 && x > threshold) here = j;
+    }
+  }
+  // (sums in another order may stay a last bit below: then the last entry with any weight is the one)
+  const uint32_t hit = __ballot_sync(0xffffffffu, here >= 0), some = __ballot_sync(0xffffffffu, any >= 0);
+  const int l = hit ? __ffs(hit) - 1 : 31 - __clz(some);
+  if (lane == l) a.out[r * a.out_stride + count] = found * TILE + l * 4 + (hit ? here : any);
 }
 
 template <typename T, bool VEC, int CL>
