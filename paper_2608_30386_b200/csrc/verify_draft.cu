@@ -3,12 +3,14 @@
 // two tokens by more than many of them weigh.
 //
 // Split: a request is one cluster of CL thread blocks, each of which owns a contiguous part of the row, and in it each warp a
-// contiguous run of tiles.  One pass sums the weights per warp; the sums meet through distributed shared memory in a fixed
-// order, every block finds the one warp whose part holds the threshold, and that warp goes over its own few tiles again (they
-// are in L2).  One launch, no workspace, nothing depends on the order of arrival.
+// contiguous run of tiles.  One pass sums the weights per tile and per warp; the warps' sums meet through distributed shared memory in
+// a fixed order, every block finds the one warp whose part holds the threshold, that warp finds the tile among its sums and reads
+// this one tile again.  One launch, no workspace, nothing depends on the order of arrival.
 // Bound: one pass over a row of the target, and one of the drafter where a token does not stand.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
+
+#include <type_traits>
 
 #include "decay_common.cuh"
 
@@ -16,8 +18,9 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int NT = 256, NW = NT / 32;
+constexpr int NT = 512, NW = NT / 32;
 constexpr int TILE = 128;  // entries of a row that a warp takes at once: four per lane
+constexpr int SUMS = 64;   // sums that a warp keeps: one per tile, or per few tiles of a very long row
 
 template <typename T>
 __device__ __forceinline__ float prob(T x) {
@@ -48,8 +51,8 @@ __device__ __forceinline__ void load4(const T *row, int i, int vocab, float (&x)
 }
 
 template <typename T, bool VEC, int CL>
-__global__ void __launch_bounds__(NT, 4) verify_draft_kernel(const __grid_constant__ DascVerifyArgs a) {
-  __shared__ double warp_sum[NW], s_before, s_threshold;
+__global__ void __launch_bounds__(NT, 2) verify_draft_kernel(const __grid_constant__ DascVerifyArgs a) {
+  __shared__ double warp_sum[NW], tile_sum[NW][SUMS], s_before, s_threshold;
   __shared__ int s_count, s_winner;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r = blockIdx.x / CL, rank = blockIdx.x % CL;
@@ -93,7 +96,7 @@ __global__ void __launch_bounds__(NT, 4) verify_draft_kernel(const __grid_consta
   }
 
   const int tiles = (a.vocab + TILE - 1) / TILE, per_warp = (tiles + CL * NW - 1) / (CL * NW);
-  const int gw = rank * NW + warp;
+  const int gw = rank * NW + warp, group = (per_warp + SUMS - 1) / SUMS;  // tiles per sum
   const int first = min(gw * per_warp, tiles), last = min(first + per_warp, tiles);
   auto weights = [&](int tile, double (&w)[4]) {
     const int i = tile * TILE + lane * 4;
@@ -111,14 +114,30 @@ __global__ void __launch_bounds__(NT, 4) verify_draft_kernel(const __grid_consta
   constexpr int PER = (CL * NW + 31) / 32;
   for (int attempt = 0; attempt < 2; ++attempt) {
     double sum = 0.0;
-#pragma unroll 4
-    for (int t = first; t < last; ++t) {
-      double w[4];
-      weights(t, w);
-      sum += (w[0] + w[1]) + (w[2] + w[3]);
-    }
+    const auto keep = [&](int i, double x) {
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+      if (lane == 0) tile_sum[warp][i] = x;
+      sum += x;
+    };
+    if (group == 1) {
+#pragma unroll 4
+      for (int t = first; t < last; ++t) {
+        double w[4];
+        weights(t, w);
+        keep(t - first, (w[0] + w[1]) + (w[2] + w[3]));
+      }
+    } else {
+      for (int t = first; t < last; t += group) {
+        double x = 0.0;
+        for (int u = t; u < min(t + group, last); ++u) {
+          double w[4];
+          weights(u, w);
+          x += (w[0] + w[1]) + (w[2] + w[3]);
+        }
+        keep((t - first) / group, x);
+      }
+    }
     if (lane == 0) warp_sum[warp] = sum;
     cluster.sync();
     double x[PER];  // lane l of the first warp: the sums of warps PER l ... of the cluster
@@ -190,47 +209,53 @@ __global__ void __launch_bounds__(NT, 4) verify_draft_kernel(const __grid_consta
   if (gw != winner) return;
   double before = s_before;
   const double threshold = s_threshold;
-  // the first tile that takes it over (or the last one with any weight)
-  int found = -1;
-  double found_before = before;
-  bool over = false;
-#pragma unroll 4
-  for (int t = first; t < last; ++t) {
+  // the first of this warp's sums that takes it over, or the last one that is not zero
+  int at = -1;
+  double at_before = before;
+  for (int i = 0; first + i * group < last; ++i) {
+    const double x = tile_sum[warp][i];
+    if (x > 0.0) {
+      at = i;
+      at_before = before;
+      if (before + x > threshold) break;
+    }
+    before += x;
+  }
+  // and the first of its entries (sums in another order may stay a last bit below: then the last entry with any weight)
+  before = at_before;
+  int token = -1, last_some = -1;
+  const int begin = first + at * group;
+  for (int t = begin; t < min(begin + group, last) && token < 0; ++t) {
     double w[4];
     weights(t, w);
-    double sum = (w[0] + w[1]) + (w[2] + w[3]);
+    double incl = (w[0] + w[1]) + (w[2] + w[3]);
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (!over && sum > 0.0) {
-      found = t;
-      found_before = before;
-      over = before + sum > threshold;
+    for (int d = 1; d < 32; d <<= 1) {
+      const double y = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += y;
     }
-    before += sum;
-  }
-  double w[4];
-  weights(found, w);
-  double incl = (w[0] + w[1]) + (w[2] + w[3]);
+    const double excl = __shfl_up_sync(0xffffffffu, incl, 1);
+    double x = before + (lane > 0 ? excl : 0.0);
+    int here = -1, any = -1;
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const double y = __shfl_up_sync(0xffffffffu, incl, d);
-    if (lane >= d) incl += y;
-  }
-  const double excl = __shfl_up_sync(0xffffffffu, incl, 1);
-  double x = found_before + (lane > 0 ? excl : 0.0);
-  int here = -1, any = -1;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    x += w[j];
-    if (w[j] > 0.0) {
-      any = j;
-      if (here < 0 && x > threshold) here = j;
+    for (int j = 0; j < 4; ++j) {
+      x += w[j];
+      if (w[j] > 0.0) {
+        any = j;
+        if (here < 0 && x > threshold) here = j;
+      }
     }
+    const uint32_t hit = __ballot_sync(0xffffffffu, here >= 0), some = __ballot_sync(0xffffffffu, any >= 0);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      token = t * TILE + l * 4 + __shfl_sync(0xffffffffu, here, l);
+    } else if (some) {
+      const int l = 31 - __clz(some);
+      last_some = t * TILE + l * 4 + __shfl_sync(0xffffffffu, any, l);
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
   }
-  // (sums in another order may stay a last bit below: then the last entry with any weight is the one)
-  const uint32_t hit = __ballot_sync(0xffffffffu, here >= 0), some = __ballot_sync(0xffffffffu, any >= 0);
-  const int l = hit ? __ffs(hit) - 1 : 31 - __clz(some);
-  if (lane == l) a.out[r * a.out_stride + count] = found * TILE + l * 4 + (hit ? here : any);
+  if (lane == 0) a.out[r * a.out_stride + count] = token >= 0 ? token : last_some;
 }
 
 template <typename T, bool VEC, int CL>
@@ -243,7 +268,16 @@ int launch_type(const DascVerifyArgs &a, void *stream) {
   // four entries per load where every row starts on their boundary
   auto even = [](const void *p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0 && stride % 4 == 0; };
   const bool vec = even(a.target, a.target_stride) && (!a.draft || even(a.draft, a.draft_stride));
-  return vec ? launch<T, true, 8>(a, stream) : launch<T, false, 8>(a, stream);
+  // as many blocks per request as still fit the GPU at once, two per SM
+  const auto with = [&](auto cl) {
+    constexpr int CL = decltype(cl)::value;
+    return vec ? launch<T, true, CL>(a, stream) : launch<T, false, CL>(a, stream);
+  };
+  constexpr int kPlaces = 2 * 148;
+  if (a.n_req * int64_t{8} <= kPlaces) return with(std::integral_constant<int, 8>{});
+  if (a.n_req * int64_t{4} <= kPlaces) return with(std::integral_constant<int, 4>{});
+  if (a.n_req * int64_t{2} <= kPlaces) return with(std::integral_constant<int, 2>{});
+  return with(std::integral_constant<int, 1>{});
 }
 
 }  // namespace
