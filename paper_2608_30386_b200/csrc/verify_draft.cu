@@ -29,8 +29,11 @@ __device__ __forceinline__ float prob(T x) {
   else
     return x;
 }
-// A probability that is none counts as nothing.
-__device__ __forceinline__ double clean(float x) { return x > 0.f && x < __int_as_float(0x7f800000) ? static_cast<double>(x) : 0.0; }
+// A probability that is none (negative, infinite, NaN) counts as nothing.
+__device__ __forceinline__ float clean(float x) {
+  x = fmaxf(x, 0.f);
+  return x < __int_as_float(0x7f800000) ? x : 0.f;
+}
 
 // four entries of a row, from entry i on; 0 behind the end
 template <typename T, bool VEC>
@@ -98,46 +101,53 @@ __global__ void __launch_bounds__(NT, 2) verify_draft_kernel(const __grid_consta
   const int tiles = (a.vocab + TILE - 1) / TILE, per_warp = (tiles + CL * NW - 1) / (CL * NW);
   const int gw = rank * NW + warp, group = (per_warp + SUMS - 1) / SUMS;  // tiles per sum
   const int first = min(gw * per_warp, tiles), last = min(first + per_warp, tiles);
+  // max(p - q, 0), exact in 64 bits
   auto weights = [&](int tile, double (&w)[4]) {
     const int i = tile * TILE + lane * 4;
-    float p[4], q[4] = {0.f, 0.f, 0.f, 0.f};
+    float p[4], q[4];
     load4<T, VEC>(prow, i, a.vocab, p);
     if (qrow) load4<T, VEC>(qrow, i, a.vocab, q);
+    const bool other = qrow || taken >= 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const double d = clean(p[j]) - (i + j == taken ? 1.0 : clean(q[j]));
-      w[j] = d > 0.0 ? d : 0.0;
+      p[j] = clean(p[j]);
+      w[j] = p[j];
+      if (other) w[j] -= static_cast<double>(fminf(p[j], qrow ? clean(q[j]) : (i + j == taken ? 1.f : 0.f)));
     }
   };
 
   cg::cluster_group cluster = cg::this_cluster();
   constexpr int PER = (CL * NW + 31) / 32;
   for (int attempt = 0; attempt < 2; ++attempt) {
+    // Four sums at a time: their loads are in flight together, and the lanes' parts fold into one another, so that lanes 8 j .. 8 j + 7
+    // end with sum j (six exchanges for four sums, not twenty).
     double sum = 0.0;
-    const auto keep = [&](int i, double x) {
+    for (int i = 0; first + i * group < last; i += 4) {
+      double x[4] = {0.0, 0.0, 0.0, 0.0};
+      for (int u = 0; u < group; ++u) {
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-      if (lane == 0) tile_sum[warp][i] = x;
-      sum += x;
-    };
-    if (group == 1) {
-#pragma unroll 4
-      for (int t = first; t < last; ++t) {
-        double w[4];
-        weights(t, w);
-        keep(t - first, (w[0] + w[1]) + (w[2] + w[3]));
-      }
-    } else {
-      for (int t = first; t < last; t += group) {
-        double x = 0.0;
-        for (int u = t; u < min(t + group, last); ++u) {
-          double w[4];
-          weights(u, w);
-          x += (w[0] + w[1]) + (w[2] + w[3]);
+        for (int j = 0; j < 4; ++j) {
+          const int t = first + (i + j) * group + u;
+          if (t < last) {
+            double w[4];
+            weights(t, w);
+            x[j] += (w[0] + w[1]) + (w[2] + w[3]);
+          }
         }
-        keep((t - first) / group, x);
       }
+      const bool up = lane & 16, up2 = lane & 8;
+      double y0 = up ? x[2] : x[0], y1 = up ? x[3] : x[1];
+      y0 += __shfl_xor_sync(0xffffffffu, up ? x[0] : x[2], 16);
+      y1 += __shfl_xor_sync(0xffffffffu, up ? x[1] : x[3], 16);
+      double z = up2 ? y1 : y0;
+      z += __shfl_xor_sync(0xffffffffu, up2 ? y0 : y1, 8);
+#pragma unroll
+      for (int d = 4; d > 0; d >>= 1) z += __shfl_xor_sync(0xffffffffu, z, d);
+      if (lane % 8 == 0) tile_sum[warp][i + lane / 8] = z;
+      sum += z;
     }
+    sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 8);
     if (lane == 0) warp_sum[warp] = sum;
     cluster.sync();
     double x[PER];  // lane l of the first warp: the sums of warps PER l ... of the cluster
