@@ -41,6 +41,11 @@ __device__ __forceinline__ DecayRange decay_range(const DascDecayArgs &a, int r)
   return {b, n};
 }
 
+// `bytes` bytes (a multiple of 16) into L2 only.
+__device__ __forceinline__ void bulk_prefetch(const void *src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
+}
+
 // packed pairs of fp32 (one instruction per pair)
 __device__ __forceinline__ uint64_t dpack2(float lo, float hi) {
   uint64_t r;

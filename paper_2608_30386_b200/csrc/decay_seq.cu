@@ -1,23 +1,26 @@
-// Linear attention with a decay per head, token by token in fp32 on the CUDA cores:
+// Linear attention with a decay per head in fp32 on the CUDA cores:
 //     S <- exp(g_t) S + k_t v_t^T,   o_t = q_scale S^T q_t.
 // One token per request (decoding) is this recurrence with the state on its way from and to memory; a few tokens (drafts)
 // and the shapes and types the chunked kernel does not take run through the same registers.
 //
+// Several tokens go through the state together.  With P_t the product of the group's decays up to token t and D_ts of those behind s up to t,
+//     o_t = P_t S^T q_t + sum_{s <= t} D_ts (q_t . k_s) v_s,   then S <- P_n S + sum_s (D_ns k_s) v_s^T:
+// one multiplication per value of the state and token for the outputs and one for the state, where the recurrence has three, and
+// none for the state after the last group of a call that does not keep it.
+//
 // Split: columns of the state do not interact, so a thread block owns NCOL columns of one (request, layer, head) state, all
 // of it in registers: a thread holds ROWS rows of four columns.  The read-out sums over rows, which are spread over
-// RG groups of threads: partial sums meet in shared memory once per group of TB tokens, in a fixed order.
+// RG groups of threads: partial sums meet in shared memory once per group of TB tokens, in a fixed order.  Decays multiply, they are not
+// differences of sums: exp(-inf) is a zero like any other.
 // Bound: bytes of the state (128 KB read and written per 128 x 128 head and call).
 #include <cuda_runtime.h>
-
-#include <type_traits>
 
 #include "decay_common.cuh"
 
 namespace {
 
-constexpr int NT = 128;  // threads per block
 constexpr int TB = 8;    // tokens per group
-constexpr int kFew = 16;  // tokens over which decays may be rounded
+constexpr int kAhead = 2 * 148;
 
 template <typename T>
 __device__ __forceinline__ float to_float(T x) {
@@ -41,26 +44,33 @@ __device__ __forceinline__ void cp_async4(void *smem, const void *gmem) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(smem))), "l"(gmem) : "memory");
 }
 
+// 128 x 128 values are held by 256 threads, all else by 128: at most 64 registers of state per thread
+template <int DK, int NCOL>
+constexpr int kThreads = DK * NCOL > 128 * 64 ? 256 : 128;
+
 template <int DK, int NCOL, bool STEP, typename IO>
 struct Smem {
+  static constexpr int NT = kThreads<DK, NCOL>;
   static constexpr int N = STEP ? 1 : TB;
   static constexpr int RG = NT / (NCOL / 4);
   alignas(16) uint64_t kk[N][DK], qq[N][DK];  // each value twice: operands of the packed instructions
   alignas(16) float v[N][NCOL];
   alignas(16) float part[N][RG][NCOL];
-  float alpha[N], alpha_lo[N];
+  float alpha[N], alpha_lo[N];  // a single token's decay
+  float upto[N];                // P_t
+  float qk[N][N];               // D_ts q_scale q_t . k_s
   // the next group, as it comes from memory
   alignas(16) IO raw_q[STEP ? 1 : N][STEP ? 8 : DK], raw_k[STEP ? 1 : N][STEP ? 8 : DK], raw_v[STEP ? 1 : N][STEP ? 8 : NCOL];
   alignas(16) float raw_g[N];
 };
 
 template <int DK, int NCOL, bool STEP, typename IO, typename OT>
-__global__ void __launch_bounds__(NT, 3) decay_seq_kernel(const __grid_constant__ DascDecayArgs a) {
-  constexpr int LPR = NCOL / 4, RG = NT / LPR, ROWS = DK / RG;
+__global__ void __launch_bounds__((kThreads<DK, NCOL>), (kThreads<DK, NCOL> == 256 ? 2 : 3)) decay_seq_kernel(const __grid_constant__ DascDecayArgs a) {
+  constexpr int NT = kThreads<DK, NCOL>, LPR = NCOL / 4, RG = NT / LPR, ROWS = DK / RG;
   using Sm = Smem<DK, NCOL, STEP, IO>;
   extern __shared__ __align__(16) unsigned char smem_raw[];
   Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
-  const int tid = threadIdx.x, cg = tid % LPR, rg = tid / LPR;
+  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, cg = tid % LPR, rg = tid / LPR;
   const int parts = a.d_v / NCOL;
   const int part = blockIdx.x % parts, unit = blockIdx.x / parts;
   const int h = unit % a.H_v, lc = unit / a.H_v % a.n_layers_in_call, r = unit / (a.H_v * a.n_layers_in_call);
@@ -118,32 +128,34 @@ __global__ void __launch_bounds__(NT, 3) decay_seq_kernel(const __grid_constant_
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   // A decay rounded to fp32 is off by up to half an ulp, the same every time where the decay is constant: 6e-4 of a state that lasts 10^4
-  // tokens.  So beyond a few tokens what alpha is short of is carried along (1 + d, d good to its own last bits).
-  auto token = [&](int t, auto whole) {
-    const float al = sm.alpha[t], lo = sm.alpha_lo[t];
-    const uint64_t aa = dpack2(al, al), ll = dpack2(lo, lo);
-    const auto step = [&](uint64_t &s, uint64_t kv) {
-      if constexpr (decltype(whole)::value) kv = dfma2(s, ll, kv);
-      s = dfma2(s, aa, kv);
-    };
-    const ulonglong2 vv = *reinterpret_cast<const ulonglong2 *>(&sm.v[t][cg * 4]);
+  // tokens.  So what it is short of is carried along (1 + d, d good to its own last bits).
+  auto decay = [&](float g, float &hi, float &lo) {
+    const float d = expm1f(g), a1 = 1.f + d;
+    const bool slow = g > -0.7f;
+    hi = slow ? a1 : expf(g);
+    lo = slow ? d - (a1 - 1.f) : 0.f;
+  };
+  auto token = [&]() {  // a single one
+    const uint64_t aa = dpack2(sm.alpha[0], sm.alpha[0]), ll = dpack2(sm.alpha_lo[0], sm.alpha_lo[0]);
+    const auto step = [&](uint64_t &s, uint64_t kv) { s = dfma2(s, aa, dfma2(s, ll, kv)); };
+    const ulonglong2 vv = *reinterpret_cast<const ulonglong2 *>(&sm.v[0][cg * 4]);
     uint64_t o0 = 0, o1 = 0;
 #pragma unroll
     for (int i = 0; i < ROWS; i += 2) {
-      const ulonglong2 kk = *reinterpret_cast<const ulonglong2 *>(&sm.kk[t][rg * ROWS + i]);
+      const ulonglong2 kk = *reinterpret_cast<const ulonglong2 *>(&sm.kk[0][rg * ROWS + i]);
       step(S[i][0], dmul2(kk.x, vv.x));
       step(S[i][1], dmul2(kk.x, vv.y));
       step(S[i + 1][0], dmul2(kk.y, vv.x));
       step(S[i + 1][1], dmul2(kk.y, vv.y));
       if (STEP || a.o) {
-        const ulonglong2 qq = *reinterpret_cast<const ulonglong2 *>(&sm.qq[t][rg * ROWS + i]);
+        const ulonglong2 qq = *reinterpret_cast<const ulonglong2 *>(&sm.qq[0][rg * ROWS + i]);
         o0 = dfma2(S[i][0], qq.x, o0);
         o1 = dfma2(S[i][1], qq.x, o1);
         o0 = dfma2(S[i + 1][0], qq.y, o0);
         o1 = dfma2(S[i + 1][1], qq.y, o1);
       }
     }
-    if (STEP || a.o) *reinterpret_cast<ulonglong2 *>(&sm.part[t][rg][cg * 4]) = make_ulonglong2(o0, o1);
+    if (STEP || a.o) *reinterpret_cast<ulonglong2 *>(&sm.part[0][rg][cg * 4]) = make_ulonglong2(o0, o1);
   };
   auto store_state = [&]() {
 #pragma unroll
@@ -153,11 +165,18 @@ __global__ void __launch_bounds__(NT, 3) decay_seq_kernel(const __grid_constant_
     }
   };
   auto outputs = [&](int t0, int cnt) {
+#pragma unroll 2
     for (int i = tid; i < cnt * NCOL; i += NT) {
       const int t = i / NCOL, c = i % NCOL;
       float x = 0.f;
 #pragma unroll
       for (int j = 0; j < RG; ++j) x += sm.part[t][j][c];
+      if (!STEP && n > 1) {
+        x *= sm.upto[t];
+#pragma unroll
+        for (int s = 0; s < TB; ++s)
+          if (s <= t) x = fmaf(sm.qk[t][s % Sm::N], sm.v[s % Sm::N][c], x);
+      }
       go[(t0 + t) * v_stride + c] = from_float<OT>(x);
     }
   };
@@ -169,40 +188,144 @@ __global__ void __launch_bounds__(NT, 3) decay_seq_kernel(const __grid_constant_
       sm.qq[0][i] = dpack2(q, q);
     }
     for (int i = tid; i < NCOL; i += NT) sm.v[0][i] = to_float<IO>(gv[i]);
-    if (tid == 0) sm.alpha[0] = expf(*gg);
+    if (tid == 0) decay(*gg, sm.alpha[0], sm.alpha_lo[0]);
     __syncthreads();
-    token(0, std::false_type{});
+    token();
     store_state();
     __syncthreads();
     outputs(0, 1);
   } else {
     if (n > 0) stage(0);
+    // the state of a unit that a block of the next wave works on starts on its way into L2
+    const int ahead = unit + kAhead / parts;
+    if (tid == NT - 1 && part == 0 && ahead < a.n_req * a.n_layers_in_call * a.H_v && !merge) {
+      const int ah = ahead % a.H_v, al = ahead / a.H_v % a.n_layers_in_call, ar = ahead / (a.H_v * a.n_layers_in_call);
+      const int other = a.req_idx[ar];
+      if (other >= 0 && !(a.from_zero && a.from_zero[ar] != 0))
+        bulk_prefetch(a.state + other * a.req_stride + (a.layer_begin + al) * a.layer_stride + static_cast<int64_t>(ah) * DK * a.d_v, DK * a.d_v * 4);
+    }
     for (int t0 = 0; t0 < n; t0 += TB) {
       const int cnt = min(TB, n - t0);
       asm volatile("cp.async.wait_all;" ::: "memory");
       __syncthreads();
+      const bool update = write || t0 + TB < n;
+      // every warp for itself: lane t < cnt holds token t's decay, the other lanes 1
+      const float g = lane < cnt ? sm.raw_g[lane] : 0.f;
+      float alpha, lo;
+      decay(g, alpha, lo);
+      if (tid == 0) {
+        sm.alpha[0] = alpha;
+        sm.alpha_lo[0] = lo;
+      }
+      float upto = alpha, behind = __shfl_down_sync(0xffffffffu, alpha, 1);  // products of the decays up to a token, and behind it
+#pragma unroll
+      for (int d = 1; d < TB; d <<= 1) {
+        const float x = __shfl_up_sync(0xffffffffu, upto, d), y = __shfl_down_sync(0xffffffffu, behind, d);
+        if (lane >= d) upto *= x;
+        behind *= y;  // (lanes from cnt on: 1)
+      }
+      if (tid < TB) sm.upto[tid] = upto;
+      // The whole group's decay of the state, with what a rounded factor is short of.  The sum G of the logarithms is off by an ulp
+      // or so, which costs what it is multiplied with a relative G 2^-23, and leaves e^G of it.
+      float all_hi = g, all_lo;
+#pragma unroll
+      for (int d = 1; d < TB; d <<= 1) all_hi += __shfl_xor_sync(0xffffffffu, all_hi, d);
+      decay(__shfl_sync(0xffffffffu, all_hi, 0), all_hi, all_lo);
       for (int i = tid; i < cnt * DK; i += NT) {
         const int t = i / DK, c = i % DK;
-        const float k = to_float<IO>(sm.raw_k[t][c]);
-        sm.kk[t][c] = dpack2(k, k);
+        const float d = __shfl_sync(0xffffffffu, behind, t);  // (t is the same in all of a warp)
+        if (update) {
+          const float k = to_float<IO>(sm.raw_k[t][c]) * d;
+          sm.kk[t][c] = dpack2(k, k);
+        }
         if (a.o) {
           const float q = to_float<IO>(sm.raw_q[t][c]) * a.q_scale;
           sm.qq[t][c] = dpack2(q, q);
         }
       }
       for (int i = tid; i < cnt * NCOL; i += NT) sm.v[i / NCOL][i % NCOL] = to_float<IO>(sm.raw_v[i / NCOL][i % NCOL]);
-      if (tid < cnt) {
-        const float g = sm.raw_g[tid], d = expm1f(g), a1 = 1.f + d;
-        const bool slow = n > kFew && g > -0.7f;
-        sm.alpha[tid] = slow ? a1 : expf(g);
-        sm.alpha_lo[tid] = slow ? d - (a1 - 1.f) : 0.f;
+      if (a.o && n > 1) {
+        // D_ts q_t . k_s: a warp has one or two tokens t; its lanes' parts of the 8 or 16 sums fold into one another
+        constexpr int PER = DK / 32, OWN = TB / (NT / 32), V = OWN * TB;
+        struct alignas(sizeof(IO) * PER) Part {
+          IO x[PER];
+        };
+        float x[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = 0.f;
+        Part q[OWN];
+#pragma unroll
+        for (int o = 0; o < OWN; ++o) q[o] = *reinterpret_cast<const Part *>(&sm.raw_q[OWN * warp + o][lane * PER]);
+#pragma unroll
+        for (int s = 0; s < TB; ++s) {
+          const Part k = *reinterpret_cast<const Part *>(&sm.raw_k[s][lane * PER]);
+#pragma unroll
+          for (int o = 0; o < OWN; ++o)
+#pragma unroll
+            for (int j = 0; j < PER; ++j) x[o * TB + s] = fmaf(to_float<IO>(q[o].x[j]), to_float<IO>(k.x[j]), x[o * TB + s]);
+        }
+#pragma unroll
+        for (int w = V / 2; w > 0; w >>= 1) {
+          const int other = w * 32 / V;
+          const bool up = lane & other;
+#pragma unroll
+          for (int j = 0; j < w; ++j) {
+            const float mine = up ? x[j + w] : x[j];
+            x[j] = mine + __shfl_xor_sync(0xffffffffu, up ? x[j] : x[j + w], other);
+          }
+        }
+#pragma unroll
+        for (int d = 16 / V; d > 0; d >>= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], d);
+        const int at = lane / (32 / V), t = OWN * warp + at / TB, s = at % TB;
+        float d = 1.f;
+#pragma unroll
+        for (int u = 1; u < TB; ++u) {
+          const float y = __shfl_sync(0xffffffffu, alpha, u);
+          if (u > s && u <= t) d *= y;
+        }
+        if (s <= t && lane % (32 / V) == 0) sm.qk[t][s] = x[0] * a.q_scale * d;
       }
       __syncthreads();
       if (t0 + TB < n) stage(t0 + TB);
-      if (n > kFew)
-        for (int t = 0; t < cnt; ++t) token(t, std::true_type{});
-      else
-        for (int t = 0; t < cnt; ++t) token(t, std::false_type{});
+      if (n == 1) {
+        token();
+      } else {
+        if (a.o) {
+#pragma unroll 2
+          for (int t = 0; t < cnt; ++t) {
+            uint64_t o0 = 0, o1 = 0;
+#pragma unroll
+            for (int i = 0; i < ROWS; i += 2) {
+              const ulonglong2 qq = *reinterpret_cast<const ulonglong2 *>(&sm.qq[t][rg * ROWS + i]);
+              o0 = dfma2(S[i][0], qq.x, o0);
+              o1 = dfma2(S[i][1], qq.x, o1);
+              o0 = dfma2(S[i + 1][0], qq.y, o0);
+              o1 = dfma2(S[i + 1][1], qq.y, o1);
+            }
+            *reinterpret_cast<ulonglong2 *>(&sm.part[t][rg][cg * 4]) = make_ulonglong2(o0, o1);
+          }
+        }
+        if (update) {
+          const uint64_t hi = dpack2(all_hi, all_hi), ll = dpack2(all_lo, all_lo);
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) {
+            S[i][0] = dfma2(S[i][0], hi, dmul2(S[i][0], ll));
+            S[i][1] = dfma2(S[i][1], hi, dmul2(S[i][1], ll));
+          }
+#pragma unroll 2
+          for (int t = 0; t < cnt; ++t) {
+            const ulonglong2 vv = *reinterpret_cast<const ulonglong2 *>(&sm.v[t][cg * 4]);
+#pragma unroll
+            for (int i = 0; i < ROWS; i += 2) {
+              const ulonglong2 kk = *reinterpret_cast<const ulonglong2 *>(&sm.kk[t][rg * ROWS + i]);
+              S[i][0] = dfma2(kk.x, vv.x, S[i][0]);
+              S[i][1] = dfma2(kk.x, vv.y, S[i][1]);
+              S[i + 1][0] = dfma2(kk.y, vv.x, S[i + 1][0]);
+              S[i + 1][1] = dfma2(kk.y, vv.y, S[i + 1][1]);
+            }
+          }
+        }
+      }
       if (a.o) {
         __syncthreads();
         outputs(t0, cnt);  // (the next group's partial sums come behind two barriers)
@@ -217,6 +340,7 @@ template <int DK, int NCOL, bool STEP, typename IO, typename OT>
 int launch(const DascDecayArgs &a, void *stream) {
   const int64_t blocks = static_cast<int64_t>(a.n_req) * a.n_layers_in_call * a.H_v * (a.d_v / NCOL);
   if (blocks > 2147483647LL) return static_cast<int>(cudaErrorInvalidConfiguration);
+  constexpr int NT = kThreads<DK, NCOL>;
   constexpr size_t smem = sizeof(Smem<DK, NCOL, STEP, IO>);
   auto kernel = decay_seq_kernel<DK, NCOL, STEP, IO, OT>;
   if (smem > 48 * 1024) {
@@ -235,8 +359,10 @@ template <int DK, typename IO, typename OT>
 int launch_cols(const DascDecayArgs &a, void *stream) {
   const int64_t units = static_cast<int64_t>(a.n_req) * a.n_layers_in_call * a.H_v;
   // the widest part of the columns that still gives every SM a block or two
-  if constexpr (DK <= 64)  // (128 x 128 values do not fit the registers of 128 threads beside what a token needs)
-    if (a.d_v % 128 == 0 && units * (a.d_v / 128) >= 2 * 148) return launch_form<DK, 128, IO, OT>(a, stream);
+  if (a.d_v % 128 == 0 && units * (a.d_v / 128) >= 2 * 148) {
+    if (a.cu_seqlens) return launch<DK, 128, false, IO, OT>(a, stream);
+    if constexpr (DK <= 64) return launch<DK, 128, true, IO, OT>(a, stream);
+  }
   if (a.d_v % 64 == 0 && units * (a.d_v / 64) >= 2 * 148) return launch_form<DK, 64, IO, OT>(a, stream);
   return launch_form<DK, 32, IO, OT>(a, stream);
 }

@@ -64,11 +64,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const void *tmap,
       : "memory");
 }
 
-// `bytes` bytes (a multiple of 16) into L2 only.
-__device__ __forceinline__ void bulk_prefetch(const void *src, uint32_t bytes) {
-  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
-}
-
 // One lane of a converged warp.  The compiler knows that a branch on this predicate runs with a single active thread, so the
 // tcgen05 instructions below it take their descriptors straight from uniform registers; behind `lane == 0` it has to allow
 // for several active threads with different operands and serialises every one of them in a loop.
