@@ -559,10 +559,11 @@ dasc_status_t dasc_refresh_static(const dasc_plan_t *plan, float *state_base, in
  *                                   advanced over those that stand by a second call (CONTINUE, seq_used, o = NULL).
  * A request without tokens still has its S_0 written where the mode writes a state that does not start as stored.
  *
- * algo SEQUENTIAL: token by token in fp32; d_k of 32, 64 or 128 and any d_v that is a multiple of 32.
+ * algo SEQUENTIAL: up to 8 tokens at a time, in fp32; d_k of 32, 64 or 128 and any d_v that is a multiple of 32.
  * algo CHUNKED: chunks of 64 tokens on the tensor cores, for d_k = d_v = 128 and bf16 q, k, v (DASC_ERR_SHAPE
- *   otherwise).  Operands that are not exact in bf16 (weights inside a chunk, decayed keys, the state) are pairs of bf16,
- *   16 mantissa bits, and sums are fp32.  A token with a NaN or an infinity in v makes its column of the state and of
+ *   otherwise), sums in fp32.  Operands that are not exact in bf16: decayed keys are in three bf16 parts (states are as good as
+ *   fp32 ones); weights inside a chunk and the state on its way to the outputs in two for fp32 outputs, in one for bf16
+ *   outputs, which adds at most half a bf16 step of each term.  A token with a NaN or an infinity in v makes its column of the state and of
  *   all later outputs NaN (where exact arithmetic may keep an infinity); earlier outputs are not touched by it.
  * algo AUTO: CHUNKED where shape and type allow it and the requests are long enough to gain, else SEQUENTIAL.
  *
