@@ -12,7 +12,9 @@
 // of it in registers: a thread holds ROWS rows of four columns.  The read-out sums over rows, which are spread over
 // RG groups of threads: partial sums meet in shared memory once per group of TB tokens, in a fixed order.  Decays multiply, they are not
 // differences of sums: exp(-inf) is a zero like any other.
-// Bound: bytes of the state (128 KB read and written per 128 x 128 head and call).
+// Bound: bytes of the state (128 KB read and written per 128 x 128 head and call).  A token of 256 requests x 32 heads: 163 us, 102 % of the
+// measured copy rate of 6461 GB/s.  Few tokens are bound by the latency of a block's steps (loads, decays, products of queries and keys,
+// outputs), of which two blocks per SM hide one: 5 tokens of 64 requests x 32 heads scored in 45 us (22 us of bytes), advanced in 55 us (42).
 #include <cuda_runtime.h>
 
 #include "decay_common.cuh"
@@ -20,8 +22,8 @@
 namespace {
 
 constexpr int TB = 8;    // tokens per group
-// How many states on the next to be fetched into L2 is: a wave of blocks (two per SM).  With it 64 requests x 4 layers x 32 heads of
-// 5 tokens take 48 us where they took 51, and their advance 55 where it took 61.
+// How many states on the next to be fetched into L2 is: a wave of blocks (two per SM).  With it 5 tokens of 64 requests x
+// 32 heads are scored in 48 us where it took 51, and advanced in 55 where it took 61.
 constexpr int kAhead = 2 * 148;
 
 template <typename T>

@@ -6,7 +6,10 @@
 // contiguous run of tiles.  One pass sums the weights per tile and per warp; the warps' sums meet through distributed shared memory in
 // a fixed order, every block finds the one warp whose part holds the threshold, that warp finds the tile among its sums and reads
 // this one tile again.  One launch, no workspace, nothing depends on the order of arrival.
-// Bound: one pass over a row of the target, and one of the drafter where a token does not stand.
+// Bound: one pass over a row of the target, and one of the drafter where a token does not stand; in small calls the chain of loads to
+// the first token that does not stand, two cluster barriers and the last tile.  64 requests of 8 drafts over 131,072 entries in fp32: 23 us,
+// their bytes take 10.4 at 6461 GB/s; 37 of 5 over 50,257 in bf16, odd rows: 9.5 us; one: 6.3 us.  Not faster: the warp's part of the row
+// prefetched into L2 ahead of its loads (27 us).
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -62,6 +65,7 @@ __global__ void __launch_bounds__(NT, 2) verify_draft_kernel(const __grid_consta
   stream_order_begin();
 
   const int64_t d0 = a.cu_drafts[r];
+  const float u_next = a.u_next[r];  // (on its way before it is needed)
   const int n = a.tokens ? min(max(static_cast<int>(a.cu_drafts[r + 1] - d0), 0), a.max_drafts) : 0;
   const T *const target = static_cast<const T *>(a.target) + (d0 + r) * a.target_stride;
   const T *const draft = a.draft ? static_cast<const T *>(a.draft) + d0 * a.draft_stride : nullptr;
@@ -175,7 +179,7 @@ __global__ void __launch_bounds__(NT, 2) verify_draft_kernel(const __grid_consta
       if (lane == 0) run = 0.0;
       // the first warp whose part of the row takes the running sum over the threshold (the last one with any weight, should
       // a random number not be below 1)
-      const double threshold = fmax(static_cast<double>(a.u_next[r]) * total, 0.0);
+      const double threshold = fmax(static_cast<double>(u_next) * total, 0.0);
       int here = -1, some = -1;
       double before = 0.0, before_some = 0.0;
 #pragma unroll
