@@ -12,9 +12,9 @@
 // of it in registers: a thread holds ROWS rows of four columns.  The read-out sums over rows, which are spread over
 // RG groups of threads: partial sums meet in shared memory once per group of TB tokens, in a fixed order.  Decays multiply, they are not
 // differences of sums: exp(-inf) is a zero like any other.
-// Bound: bytes of the state (128 KB read and written per 128 x 128 head and call).  A token of 256 requests x 32 heads: 163 us, 102 % of the
-// measured copy rate of 6461 GB/s.  Few tokens are bound by the latency of a block's steps (loads, decays, products of queries and keys,
-// outputs), of which two blocks per SM hide one: 5 tokens of 64 requests x 32 heads scored in 45 us (22 us of bytes), advanced in 55 us (42).
+// Bound: bytes of the state (128 KB read and written per 128 x 128 head and call).  A token of 256 requests x 32 heads: 163 us, 101 % of the
+// measured copy rate of 6567 GB/s.  Few tokens are bound by the latency of a block's steps (loads, decays, products of queries and keys,
+// outputs), of which two blocks per SM hide one: 5 tokens of 64 requests x 32 heads scored in 45 us (22 us of bytes), advanced in 55 us (41).
 #include <cuda_runtime.h>
 
 #include "decay_common.cuh"

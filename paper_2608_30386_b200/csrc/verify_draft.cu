@@ -8,7 +8,7 @@
 // this one tile again.  One launch, no workspace, nothing depends on the order of arrival.
 // Bound: one pass over a row of the target, and one of the drafter where a token does not stand; in small calls the chain of loads to
 // the first token that does not stand, two cluster barriers and the last tile.  64 requests of 8 drafts over 131,072 entries in fp32: 23 us,
-// their bytes take 10.4 at 6461 GB/s; 37 of 5 over 50,257 in bf16, odd rows: 9.5 us; one: 6.3 us.  Not faster: the warp's part of the row
+// their bytes take 10.2 at 6567 GB/s; 37 of 5 over 50,257 in bf16, odd rows: 9.5 us; one: 6.3 us.  Not faster: the warp's part of the row
 // prefetched into L2 ahead of its loads (27 us).
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
