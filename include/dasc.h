@@ -572,6 +572,7 @@ dasc_status_t dasc_refresh_static(const dasc_plan_t *plan, float *state_base, in
  *   captured graphs replayed together) each need their own.
  * dasc_decay_status: after the stream has been synchronised, DASC_OK or DASC_ERR_TIMEOUT if a bounded device-side wait of
  *   the last call with this workspace gave up (the states of the requests concerned are not written).  Copies device -> host.
+ *   A call without requests or layers launches nothing and leaves the workspace as it was.
  * Errors: as for dasc_refresh, before any launch.  The plan must be of kind GDN (DASC_ERR_UNSUPPORTED otherwise).
  * Sums run in a fixed order: equal calls give equal bits.
  */
