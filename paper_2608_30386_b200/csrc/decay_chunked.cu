@@ -29,8 +29,8 @@
 // Bound: with every SM at work, power (the SM clock settles at 1.45 to 1.6 of 1.965 GHz), so fewer products and instructions count, not idle
 // cycles; and the roles' code as a whole, which runs at an instruction per cycle and scheduler up to 32 KB and at a third of that
 // beyond (unrolled to 142 KB, its warps waited for instructions 5.5 times as long as they issued them, at 58 KB 0.6 times).
-// Measured, 32 heads, bf16 outputs: 64 requests of 256 tokens x 4 layers 730 us (the bytes take 410 us at 6567 GB/s), 64 requests of 1 to
-// 1023 tokens 346 us, one of 32,768 tokens 486 us.
+// Measured, 32 heads, bf16 outputs: 64 requests of 256 tokens x 4 layers 748 us (the bytes take 410 us at 6567 GB/s), 64 requests of 1 to
+// 1023 tokens 350 us, one of 32,768 tokens 491 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
