@@ -349,3 +349,36 @@ def test_prompts_and_drafts_over_states_from_the_pool():
     check(drafts, run(drafts, mode=SCORE), expected(drafts, mode=SCORE), False)
     assert torch.equal(drafts.state, got)
     check(drafts, run(drafts, used=[1, 5, 3], want_o=False), expected(drafts, used=[1, 5, 3]), False)
+
+
+def test_calls_without_requests_or_layers():
+    case = make_case(55, [20, 3])
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    state = case.state.clone()
+    empty = [x[:, :0] for x in (case.q, case.k, case.v, case.g)]
+    dasc.dasc_decay_attn(case.plan, state, *case.strides, none, *empty, torch.zeros(1, dtype=torch.int32, device="cuda"), 0, 0, o=empty[2])
+    dasc.dasc_decay_step(case.plan, state, *case.strides, none, *empty, empty[2])
+    dasc.dasc_decay_attn(case.plan, state, *case.strides, case.req, *(x[:0] for x in (case.q, case.k, case.v, case.g)), case.cu.cuda(), case.T, 20, layer_begin=1,
+                         layer_end=1)
+    dasc.dasc_verify_draft(torch.zeros(0, 5, device="cuda"), None, none, torch.zeros(1, dtype=torch.int32, device="cuda"), none.float(), none.float(),
+                           torch.zeros(0, 3, dtype=torch.int32, device="cuda"), none)
+    torch.cuda.synchronize()
+    assert torch.equal(state, case.state)
+
+
+@pytest.mark.parametrize("algo", [SEQ, CHUNKED])
+def test_a_state_that_hardly_decays_does_not_drift(algo):
+    """A factor rounded to fp32 would be off by the same half ulp (up to 2^-25) at each of n applications: n 2^-25 of a state that nothing is added to.
+    Here 8192 tokens of zero keys are run at several decays, so all of the error is the factors': token by token, rounded, it would come to
+    2^-12 for some of them.  With what the factor is short of carried along, an application is off by the rounding of the state
+    itself (2^-24, both ways about as often) and the sum of log-decays by an ulp.  1024 groups of 8 tokens (128 chunks of 64): at most 1024 * 2^-24 even
+    if all roundings went one way, and 2^-22 * G for the exponents' relative error, G <= 1 in all."""
+    n = 8192
+    case = make_case(56, [n], H_v=4, H_k=4, decay="head", spare=0)
+    g = torch.tensor([[-1.1e-5, -3.3e-5, -7.7e-5, -1.2e-4]], device="cuda")
+    case.g = g
+    case.k = torch.zeros_like(case.k)
+    state, _ = run(case, algo=algo, want_o=False)
+    want = case.state.double() * torch.exp(g.double() * n)[0].view(1, 1, 4, 1, 1)
+    err = ((state.double() - want).abs() / want.abs()).max()
+    assert float(err) <= 1024 * 2.0 ** -24 + 2.0 ** -22

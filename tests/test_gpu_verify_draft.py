@@ -156,3 +156,19 @@ def test_strided_rows_and_outputs_and_too_many_drafts():
     same(call(wide[:, :777], wide_d[:, :777], tokens, cu, ua, un, 5, stride=9), want)
     # five drafts where two are allowed: cut to two
     same(call(target, draft, tokens, cu, [0.0] * 9, un, 2), define(target, draft, tokens, cu, [0.0] * 9, un, 2))
+
+
+@pytest.mark.parametrize("R", [32, 33, 64, 65, 148, 149])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_numbers_of_requests(R, dtype):
+    target, draft, tokens, cu, ua, un = make(R, [r % 4 for r in range(R)], 2003, dtype)
+    for q in (draft, None):
+        same(call(target, q, tokens, cu, ua, un, 3), define(target, q, tokens, cu, ua, un, 3))
+
+
+@pytest.mark.parametrize("R,V", [(1, 2 ** 20 + 129), (2, 1300001), (149, 131072 + 4), (150, 140001), (66, 262144 + 1000)])
+def test_rows_so_long_that_a_sum_stands_for_several_tiles(R, V):
+    target, draft, tokens, cu, ua, un = make(R + V, [2] + [0] * (R - 1), V, spread=1.0)
+    same(call(target, draft, tokens, cu, ua, un, 2), define(target, draft, tokens, cu, ua, un, 2))
+    un = [0.999999] * R
+    same(call(target, draft, tokens, cu, [1.0, 1.0], un, 2), define(target, draft, tokens, cu, [1.0, 1.0], un, 2))
