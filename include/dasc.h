@@ -562,9 +562,9 @@ dasc_status_t dasc_refresh_static(const dasc_plan_t *plan, float *state_base, in
  * algo SEQUENTIAL: up to 8 tokens at a time, in fp32; d_k of 32, 64 or 128 and any d_v that is a multiple of 32.
  * algo CHUNKED: chunks of 64 tokens on the tensor cores, for d_k = d_v = 128 and bf16 q, k, v (DASC_ERR_SHAPE
  *   otherwise), sums in fp32.  Operands that are not exact in bf16: decayed keys are in three bf16 parts (states are as good as
- *   fp32 ones); weights inside a chunk and the state on its way to the outputs in two for fp32 outputs, in one for bf16
- *   outputs, which adds at most half a bf16 step of each term.  A token with a NaN or an infinity in v makes its column of the state and of
- *   all later outputs NaN (where exact arithmetic may keep an infinity); earlier outputs are not touched by it.
+ *   fp32 ones); weights inside a chunk and the state on its way to the outputs in two (2^-16 of each term).  A token with a NaN or
+ *   an infinity in v makes its column of the state and of all later outputs NaN (where exact arithmetic may keep an infinity);
+ *   earlier outputs are not touched by it.
  * algo AUTO: CHUNKED where shape and type allow it and the requests are long enough to gain, else SEQUENTIAL.
  *
  * workspace: DEVICE scratch of at least dasc_decay_workspace_bytes() for these sizes, 256-byte aligned, private to the call until

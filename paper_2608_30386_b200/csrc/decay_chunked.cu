@@ -11,9 +11,9 @@
 // V, K and Q are exact in bf16: Q and K are used as they land, V^T goes to tensor memory (the tensor core's reads of shared memory are
 // what bounds the products: 128 x 64 x 16 takes 49 cycles with both operands there, 33 with one of them in tensor memory).
 // A value in n parts of bf16 (x rounded, the rest rounded, ...) is good to 2^-8n.  What the fp32 state is summed from stays at fp32's
-// precision: Kw is in three parts (in pairs the state of 256 tokens is off by 2.4e-6, in three parts by 3e-7).  On the way to fp32 outputs P
-// and S_0 are pairs; where outputs are rounded to bf16, they are in one part: each term is off by at most half a bf16 step of its own, as the
-// sum is by the rounding (outputs measure 0.0023 from exact ones, 0.0017 with everything in fp32, and calls take 12 to 15 % less time than with pairs).
+// precision: Kw is in three parts (in pairs the state of 256 tokens is off by 2.4e-6, in three parts by 3e-7).  On the way to the outputs P and
+// S_0 are pairs, for bf16 outputs too: these are then off by their own rounding (0.0017) and nothing else, where one part takes them to
+// 0.0023, 1.4 times as far, in 5 to 11 % less time.
 //
 // One thread block per SM walks over (request, layer, head) units, or over segments of long ones; roles of its warps:
 //   0       looks up the units (and clears the states of those without tokens); TMA: tiles of K, Q, V, three chunks ahead
@@ -29,8 +29,8 @@
 // Bound: with every SM at work, power (the SM clock settles at 1.45 to 1.6 of 1.965 GHz), so fewer products and instructions count, not idle
 // cycles; and the roles' code as a whole, which runs at an instruction per cycle and scheduler up to 32 KB and at a third of that
 // beyond (unrolled to 142 KB, its warps waited for instructions 5.5 times as long as they issued them, at 58 KB 0.6 times).
-// Measured, 32 heads, bf16 outputs: 64 requests of 256 tokens x 4 layers 748 us (the bytes take 410 us at 6567 GB/s), 64 requests of 1 to
-// 1023 tokens 350 us, one of 32,768 tokens 491 us.
+// Measured, 32 heads, bf16 outputs: 64 requests of 256 tokens x 4 layers 784 us (the bytes take 410 us at 6567 GB/s), 64 requests of 1 to
+// 1023 tokens 386 us, one of 32,768 tokens 528 us.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -47,7 +47,7 @@ using namespace tc5;
 constexpr int C = 64, D = 128;
 constexpr int kSms = 148;
 constexpr int NS = 3, NS_V = 2;  // stages of K and Q; of V
-constexpr int KSPLIT = 3;        // parts of Kw
+constexpr int KSPLIT = 3, OSPLIT = 2;  // parts of Kw; of P and of the state on the way to the outputs
 constexpr int RING = 4;  // chunks whose weights are kept, and units that are looked up ahead
 constexpr int WARP_TMA = 0, WARP_MMA = 1, WARP_DECAY = 2, WARP_P = 4, WARP_O = 8, WARP_K = 12, WARP_S = 16, NWARP = 24;
 // Registers of a thread, by groups of four warps: what the launch gives each (65,536 over all threads, in steps of 8), and how the roles
@@ -256,7 +256,6 @@ template <bool WITH_O, typename OT>
 __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_constant__ DascDecayArgs a, const __grid_constant__ Split sp,
                                                              const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                                                              const __grid_constant__ CUtensorMap tmap_v) {
-  constexpr int OSPLIT = sizeof(OT) == 2 ? 1 : 2;  // parts of P and of the state on the way to the outputs
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sbase = smem_u32(smem);
   Misc *const m = reinterpret_cast<Misc *>(smem + OFF_MISC);
