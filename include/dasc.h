@@ -567,9 +567,11 @@ dasc_status_t dasc_refresh_static(const dasc_plan_t *plan, float *state_base, in
  *   earlier outputs are not touched by it.
  * algo AUTO: CHUNKED where shape and type allow it and the requests are long enough to gain, else SEQUENTIAL.
  *
- * workspace: DEVICE scratch of at least dasc_decay_workspace_bytes() for these sizes, 256-byte aligned, private to the call until
- *   it completes; needs no initialisation; NULL where that size is 0.  Two calls that may overlap (two streams, two
- *   captured graphs replayed together) each need their own.
+ * workspace: DEVICE scratch of at least dasc_decay_workspace_bytes() for these sizes or larger ones, 256-byte aligned, private to
+ *   the call until it completes; needs no initialisation; NULL where that size is 0 (fp32 streams need none in any case).  Two
+ *   calls that may overlap (two streams, two captured graphs replayed together) each need their own.
+ * dasc_decay_workspace_bytes: never falls as n_req, n_layers_in_call, total_tokens or max_seqlen grow, so a buffer for the
+ *   largest batch and the longest request serves every call up to these; 64 MiB and 6 KiB at most.
  * dasc_decay_status: after the stream has been synchronised, DASC_OK or DASC_ERR_TIMEOUT if a bounded device-side wait of
  *   the last call with this workspace gave up (the states of the requests concerned are not written).  Copies device -> host.
  *   A call without requests or layers launches nothing and leaves the workspace as it was.

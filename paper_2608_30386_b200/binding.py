@@ -537,7 +537,7 @@ def dasc_refresh_static(plan: Plan, state: torch.Tensor, layer_stride: int, req_
 
 def dasc_decay_workspace_bytes(plan: Plan, n_req: int, n_layers_in_call: int, total_tokens: int, max_seqlen: int,
                                algo: int = ALGO_AUTO) -> int:
-    """Bytes of workspace of ``dasc_decay_attn`` for these sizes (0: none)."""
+    """Bytes of workspace of ``dasc_decay_attn`` for these sizes and all smaller ones (0: none)."""
     out = C.c_size_t()
     _check(lib().dasc_decay_workspace_bytes(plan.handle, n_req, n_layers_in_call, total_tokens, max_seqlen, algo, C.byref(out)),
            "dasc_decay_workspace_bytes")

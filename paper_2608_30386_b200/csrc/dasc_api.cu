@@ -844,9 +844,10 @@ dasc_status_t dasc_decay_workspace_bytes(const dasc_plan_t *plan, int32_t n_req,
                                          int32_t max_seqlen, int32_t algo, size_t *out) {
   if (!plan || !out || n_req < 0 || n_layers_in_call < 0 || total_tokens < 0) return DASC_ERR_INVALID_ARG;
   if (algo != DASC_ALGO_AUTO && algo != DASC_ALGO_SEQUENTIAL && algo != DASC_ALGO_CHUNKED) return DASC_ERR_INVALID_ARG;
-  const bool chunked = algo != DASC_ALGO_SEQUENTIAL && decay_chunked_shape(plan, n_layers_in_call, total_tokens) &&
+  // (also for streams too long for the chunked kernel: a smaller call may use it)
+  const bool chunked = algo != DASC_ALGO_SEQUENTIAL && chunked_shape_ok(plan) && total_tokens > 0 &&
                        (algo == DASC_ALGO_CHUNKED || max_seqlen > kDecayShort);
-  *out = chunked ? dasc_decay_chunked_workspace_bytes(n_req, n_layers_in_call, plan->info.n_v_heads, total_tokens, max_seqlen) : 0;
+  *out = chunked ? dasc_decay_chunked_workspace_bound(n_req, n_layers_in_call, plan->info.n_v_heads, total_tokens, max_seqlen) : 0;
   return DASC_OK;
 }
 

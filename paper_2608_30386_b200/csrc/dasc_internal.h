@@ -156,8 +156,10 @@ constexpr int kDecayStatusWords = 512;
 // Both return a cudaError_t as int, or -1 if the shape has no kernel.
 int dasc_launch_decay_seq(const DascDecayArgs &a, void *stream);
 int dasc_launch_decay_chunked(const DascDecayArgs &a, void *stream);
-// Bytes of workspace of the chunked kernel: status words, and the states of the segments where it splits requests.
+// Bytes of workspace of the chunked kernel: status words, and the states of the segments where it splits requests.  The first is what a
+// call needs, the second what no call up to these sizes needs more than.
 size_t dasc_decay_chunked_workspace_bytes(int32_t n_req, int32_t n_layers_in_call, int32_t H_v, int64_t total_tokens, int32_t max_seqlen);
+size_t dasc_decay_chunked_workspace_bound(int32_t n_req, int32_t n_layers_in_call, int32_t H_v, int64_t total_tokens, int32_t max_seqlen);
 
 // verify_draft.cu
 struct DascVerifyArgs {

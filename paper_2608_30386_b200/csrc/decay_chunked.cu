@@ -1020,16 +1020,20 @@ EncodeTiledFn encode_tiled_fn() {
 struct SplitSizes {
   int32_t nseg, seg_chunks;
 };
+constexpr int64_t kMaxSplitUnits = 2 * kSms, kMaxSegments = 16, kMaxSplitItems = 1024, kMinSplitChunks = 16, kMinSegmentChunks = 4;
+int64_t longest_chunks(int64_t total_tokens, int32_t max_seqlen) {
+  return (std::max<int64_t>(std::min<int64_t>(max_seqlen, total_tokens), 1) + C - 1) / C;
+}
 SplitSizes split_sizes(int32_t n_req, int32_t layers, int32_t H_v, int64_t total_tokens, int32_t max_seqlen) {
   const int64_t units = static_cast<int64_t>(n_req) * layers * H_v;
-  const int64_t longest = (std::max<int64_t>(std::min<int64_t>(max_seqlen, total_tokens), 1) + C - 1) / C;
+  const int64_t longest = longest_chunks(total_tokens, max_seqlen);
   SplitSizes best{1, static_cast<int32_t>(longest)};
-  if (units == 0 || units > 2 * kSms || longest < 16) return best;
+  if (units == 0 || units > kMaxSplitUnits || longest < kMinSplitChunks) return best;
   const double even = static_cast<double>(std::min<int64_t>(total_tokens / C + n_req, longest * n_req)) * layers * H_v / longest;  // units as long as the longest
   double cost = 0;
-  for (int nseg = 1; nseg <= 16 && units * nseg <= 1024 && n_req * nseg <= kMaxSorted; ++nseg) {
+  for (int nseg = 1; nseg <= kMaxSegments && units * nseg <= kMaxSplitItems && n_req * nseg <= kMaxSorted; ++nseg) {
     const int64_t chunks = (longest + nseg - 1) / nseg;
-    if (nseg > 1 && chunks < 4) break;
+    if (nseg > 1 && chunks < kMinSegmentChunks) break;
     const double rounds = std::max(1.0, static_cast<double>(static_cast<int64_t>((even * nseg + kSms - 1) / kSms)));
     const double t = rounds * chunks * (nseg > 1 ? 1.6 : 1.0) + (nseg > 1 ? 10.0 : 0.0);
     if (nseg == 1 || t < cost) {
@@ -1051,14 +1055,23 @@ cudaError_t launch(const DascDecayArgs &a, const Split &sp, const CUtensorMap &q
 
 }  // namespace
 
+static size_t workspace_of(int64_t segments) {
+  return kDecayStatusWords * sizeof(uint32_t) + (segments * sizeof(float) + 255) / 256 * 256 + segments * D * D * sizeof(float);
+}
+
 size_t dasc_decay_chunked_workspace_bytes(int32_t n_req, int32_t n_layers_in_call, int32_t H_v, int64_t total_tokens, int32_t max_seqlen) {
   const SplitSizes s = split_sizes(n_req, n_layers_in_call, H_v, total_tokens, max_seqlen);
-  size_t bytes = kDecayStatusWords * sizeof(uint32_t);
-  if (s.nseg > 1) {
-    const size_t segs = static_cast<size_t>(n_req) * n_layers_in_call * H_v * s.nseg;
-    bytes += (segs * sizeof(float) + 255) / 256 * 256 + segs * D * D * sizeof(float);
-  }
-  return bytes;
+  return workspace_of(s.nseg > 1 ? static_cast<int64_t>(n_req) * n_layers_in_call * H_v * s.nseg : 0);
+}
+
+// Few long requests are split where many are not, so a call may need more than a larger one.  The most that any call up to these sizes
+// needs: as many units as are split at all, times as many segments as the longest request may have.
+size_t dasc_decay_chunked_workspace_bound(int32_t n_req, int32_t n_layers_in_call, int32_t H_v, int64_t total_tokens, int32_t max_seqlen) {
+  const int64_t longest = longest_chunks(total_tokens, max_seqlen);
+  if (longest < kMinSplitChunks) return workspace_of(0);
+  const int64_t units = std::min(static_cast<int64_t>(n_req) * n_layers_in_call * H_v, kMaxSplitUnits / H_v * H_v);
+  const int64_t segments = std::min(kMaxSegments, (longest - 1) / (kMinSegmentChunks - 1));  // ceil(longest / n) >= kMinSegmentChunks
+  return workspace_of(std::min(units * segments, kMaxSplitItems));
 }
 
 int dasc_launch_decay_chunked(const DascDecayArgs &args, void *stream) {

@@ -1,0 +1,44 @@
+"""A workspace of dasc_decay_attn that is sized once, for the largest calls, serves every smaller one."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_30386_b200 as dasc
+from decay_helpers import make_case, run
+
+
+def query(plan, n_req, layers, total, longest, algo=dasc.ALGO_AUTO):
+    return dasc.dasc_decay_workspace_bytes(plan, n_req, layers, total, longest, algo)
+
+
+@pytest.mark.parametrize("heads", [1, 4, 32, 48, 300])
+def test_the_size_never_falls_as_a_call_grows(heads):
+    n = 4 * heads
+    plan = dasc.dasc_plan(dasc.GDN, 4, heads, heads, 128, 128, np.zeros(n, np.float32), np.zeros(n, np.float32), device=-1)
+    rng = random.Random(heads)
+    for algo in (dasc.ALGO_AUTO, dasc.ALGO_CHUNKED):
+        assert query(plan, 64, 1, 64 * 32768, 32768, algo) >= query(plan, 1, 1, 32768, 32768, algo) >= query(plan, 1, 1, 2048, 2048, algo) > 0
+        for _ in range(2000):
+            small = [rng.randint(1, 40), rng.randint(1, 4), int(2 ** rng.uniform(0, 20)), int(2 ** rng.uniform(0, 16))]
+            large = [x + rng.choice([0, 0, 1, x, 7 * x]) for x in small]
+            large[1] = min(large[1], 4)
+            assert query(plan, *large, algo) >= query(plan, *small, algo), (small, large)
+        # streams so long that a call falls back to the other form do not make it fall either
+        assert query(plan, 1, 4, 2 ** 31 - 1, 32768, algo) >= query(plan, 1, 1, 32768, 32768, algo)
+
+
+@pytest.mark.gpu
+def test_one_workspace_for_calls_of_every_size():
+    H, most, longest = 20, 16, 2100
+    plan = make_case(70, [1], L=2, H_v=H, H_k=H).plan
+    size = query(plan, most, 2, most * longest, longest)
+    memory = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    for lens in ([2085], [300] * most, [1100, 40], [1024, 1025, 1500], [70], [1400] * 7, [3, 5], [2100] * 14):
+        case = make_case(71, lens, L=2, H_v=H, H_k=H)
+        for layers in ((0, 1), (0, 2)):
+            want = run(case, layers=layers)
+            got = run(case, layers=layers, workspace=memory[:size])
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (lens, layers)
+    assert bool((memory[size:] == 0x5A).all())
