@@ -549,6 +549,8 @@ dasc_status_t dasc_refresh_static(const dasc_plan_t *plan, float *state_base, in
  *          state is not read, so it may hold anything)
  *   req_idx    DEVICE int32[n_req]: which dense state each request owns (distinct).  A negative entry is padding: the
  *          request's state and its rows of o are left as they were.
+ *   layer_stride, req_stride  states that are written must not overlap: neither stride may be below a layer's dense size where
+ *          there are several layers, or several requests (DASC_ERR_INVALID_ARG); that one does not run into the other is up to the caller
  *   max_seqlen an upper bound on any request's token count; it chooses kernels and the split of long requests and limits
  *          nothing
  * mode:

@@ -808,8 +808,9 @@ dasc_status_t decay_validate(const dasc_plan_t *plan, float *state_base, int64_t
   if (total_tokens > 0 && (!k || !v || !g || (o && !q))) return DASC_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || (reinterpret_cast<uintptr_t>(g) & 3u)) return DASC_ERR_INVALID_ARG;
   if (layer_stride < 0 || req_stride < 0 || layer_stride % 4 || req_stride % 4) return DASC_ERR_INVALID_ARG;
-  if (layers > 1 && layer_stride < plan->info.dense_floats_per_layer && req_stride < plan->info.dense_floats_per_layer)
-    return DASC_ERR_INVALID_ARG;  // layers of one request would overlap
+  const int64_t dense = plan->info.dense_floats_per_layer;
+  if (mode != DASC_DECAY_SCORE && ((layers > 1 && layer_stride < dense) || (n_req > 1 && req_stride < dense)))
+    return DASC_ERR_INVALID_ARG;  // layers of one request, or requests in one layer, would overlap and be written from several blocks
   if (const dasc_status_t ds = check_device(plan); ds != DASC_OK) return ds;
   a->H_v = plan->info.n_v_heads;
   a->H_k = plan->info.n_k_heads;
