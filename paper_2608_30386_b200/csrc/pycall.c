@@ -229,9 +229,13 @@ static int current_device(int64_t *out) {
   return r;
 }
 
-/* A tensor's address (None: NULL; an int is an address and taken as it is).  It has to be on device `dev`, of type `dtype` (NULL: bf16
- * or fp32, which *io says), contiguous unless `any_layout`, and to hold at least `need` values. */
+/* A tensor's address (None: NULL; an int is an address and taken as it is where there is one type it can be of).  It has to be on device
+ * `dev`, of type `dtype` (NULL: bf16 or fp32, which *io says), contiguous unless `any_layout`, and to hold at least `need` values. */
 static int as_tensor(PyObject *o, const char *name, int64_t dev, PyObject *dtype, int any_layout, double need, int32_t *io, void **out) {
+  if (!dtype && PyLong_Check(o)) {
+    PyErr_Format(PyExc_TypeError, "%s has to be a tensor: an address does not say whether its values are bf16 or fp32", name);
+    return -1;
+  }
   if (o == Py_None || PyLong_Check(o)) return as_ptr(o, out);
   int64_t x;
   PyObject *v = PyObject_GetAttr(o, s_dtype);
