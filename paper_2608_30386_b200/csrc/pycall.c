@@ -229,6 +229,27 @@ static int current_device(int64_t *out) {
   return r;
 }
 
+/* Is the tensor on device `dev`, and contiguous (unless `any_layout`)? */
+static int is_placed(PyObject *o, const char *name, int64_t dev, int any_layout) {
+  int64_t x;
+  if (method_i64(o, s_get_device, &x)) return -1;
+  if (x != dev) {
+    PyErr_Format(PyExc_ValueError, "%s is not on the current CUDA device", name);
+    return -1;
+  }
+  if (any_layout) return 0;
+  PyObject *v = PyObject_CallMethodNoArgs(o, s_is_contiguous);
+  if (!v) return -1;
+  const int yes = PyObject_IsTrue(v);
+  Py_DECREF(v);
+  if (yes < 0) return -1;
+  if (!yes) {
+    PyErr_Format(PyExc_ValueError, "%s is not contiguous", name);
+    return -1;
+  }
+  return 0;
+}
+
 /* A tensor's address (None: NULL; an int is an address and taken as it is where there is one type it can be of).  It has to be on device
  * `dev`, of type `dtype` (NULL: bf16 or fp32, which *io says), contiguous unless `any_layout`, and to hold at least `need` values. */
 static int as_tensor(PyObject *o, const char *name, int64_t dev, PyObject *dtype, int any_layout, double need, int32_t *io, void **out) {
@@ -245,22 +266,7 @@ static int as_tensor(PyObject *o, const char *name, int64_t dev, PyObject *dtype
   Py_DECREF(v);
   if (!ok) return -1;
   if (io) *io = bf16 ? DASC_IO_BF16 : DASC_IO_FP32;
-  if (method_i64(o, s_get_device, &x)) return -1;
-  if (x != dev) {
-    PyErr_Format(PyExc_ValueError, "%s is not on the current CUDA device", name);
-    return -1;
-  }
-  if (!any_layout) {
-    v = PyObject_CallMethodNoArgs(o, s_is_contiguous);
-    if (!v) return -1;
-    const int yes = PyObject_IsTrue(v);
-    Py_DECREF(v);
-    if (yes < 0) return -1;
-    if (!yes) {
-      PyErr_Format(PyExc_ValueError, "%s is not contiguous", name);
-      return -1;
-    }
-  }
+  if (is_placed(o, name, dev, any_layout)) return -1;
   if (need > 0) {
     if (method_i64(o, s_numel, &x)) return -1;
     if ((double)x < need) {
@@ -344,8 +350,8 @@ static PyObject *py_decay_attn(PyObject *self, PyObject *const *a, Py_ssize_t n)
     return NULL;
   }
   if (as_tensor(a[17], "seq_used", r.dev, g_int32, 0, (double)r.n_req, NULL, &used) ||
-      as_tensor(a[18], "from_zero", r.dev, g_int32, 0, (double)r.n_req, NULL, &zero) || as_ptr(a[21], &ws) || nbytes(a[21], &ws_bytes) ||
-      as_stream(a[22], &stream))
+      as_tensor(a[18], "from_zero", r.dev, g_int32, 0, (double)r.n_req, NULL, &zero) || (a[21] != Py_None && is_placed(a[21], "workspace", r.dev, 0)) ||
+      as_ptr(a[21], &ws) || nbytes(a[21], &ws_bytes) || as_stream(a[22], &stream))
     return NULL;
   dasc_status_t st;
   Py_BEGIN_ALLOW_THREADS

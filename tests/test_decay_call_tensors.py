@@ -56,3 +56,10 @@ def test_a_call_with_nothing_wrong_reaches_the_library():
 def test_an_address_does_not_say_of_which_type_its_values_are(name):
     with pytest.raises(TypeError, match=f"^{name} "):
         attn(**{name: P})
+
+
+@pytest.mark.parametrize("bad, message", [(dict(device=-1), "device"), (dict(device=1), "device"), (dict(contiguous=False), "contiguous")])
+def test_a_workspace_is_looked_at_like_every_other_tensor(bad, message):
+    """On the host, on another device, or a strided view, whose count of values says nothing about how far it reaches."""
+    with pytest.raises(ValueError, match=f"^workspace .*{message}"):
+        attn(workspace=Tensor(4096, dtype=torch.uint8, **bad))
