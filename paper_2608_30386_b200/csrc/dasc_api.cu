@@ -874,8 +874,10 @@ dasc_status_t dasc_decay_attn(const dasc_plan_t *plan, float *state_base, int64_
   if (algo == DASC_ALGO_CHUNKED && !shape_ok) return DASC_ERR_SHAPE;
   const bool fits = shape_ok && decay_chunked_shape(plan, a.n_layers_in_call, total_tokens);
   if (algo == DASC_ALGO_CHUNKED && !fits && total_tokens > 0) return DASC_ERR_SHAPE;
-  const bool usable = workspace && !(reinterpret_cast<uintptr_t>(workspace) & 255u) && workspace_bytes >= kDecayStatusWords * sizeof(uint32_t);
-  a.workspace = usable ? workspace : nullptr;
+  // the status is written where dasc_decay_status looks for it, whichever form runs and whether it needs a workspace or not
+  if (reinterpret_cast<uintptr_t>(workspace) & 3u) return DASC_ERR_WORKSPACE;
+  a.workspace = workspace_bytes >= kDecayStatusWords * sizeof(uint32_t) ? workspace : nullptr;
+  const bool usable = a.workspace && !(reinterpret_cast<uintptr_t>(workspace) & 255u);
   if (fits && (algo == DASC_ALGO_CHUNKED || (algo == DASC_ALGO_AUTO && max_seqlen > kDecayShort))) {
     if (!usable || workspace_bytes < dasc_decay_chunked_workspace_bytes(n_req, a.n_layers_in_call, a.H_v, total_tokens, max_seqlen))
       return DASC_ERR_WORKSPACE;

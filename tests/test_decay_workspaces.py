@@ -42,3 +42,25 @@ def test_one_workspace_for_calls_of_every_size():
             got = run(case, layers=layers, workspace=memory[:size])
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (lens, layers)
     assert bool((memory[size:] == 0x5A).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("offset", [0, 4, 16, 252])
+def test_the_status_is_that_of_the_last_call_where_the_workspace_is_not_aligned(offset):
+    """The form that needs no workspace takes any that begins at a whole word, and the status that it leaves there is its own."""
+    case = make_case(72, [5, 3])
+    memory = torch.full((8192,), 0xFF, dtype=torch.uint8, device="cuda")
+    run(case, algo=dasc.ALGO_SEQUENTIAL, workspace=memory[offset:offset + 4096])  # (looks at the status)
+    assert bool((memory[:offset] == 0xFF).all()) and bool((memory[offset + 4096:] == 0xFF).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("algo", [dasc.ALGO_SEQUENTIAL, dasc.ALGO_CHUNKED])
+@pytest.mark.parametrize("offset", [1, 2, 255])
+def test_a_workspace_between_words_is_refused(algo, offset):
+    case = make_case(73, [5, 3])
+    memory = torch.full((8192,), 0xFF, dtype=torch.uint8, device="cuda")
+    with pytest.raises(dasc.DascError) as e:
+        run(case, algo=algo, workspace=memory[offset:offset + 4096])
+    assert e.value.status == dasc.binding.ERR_WORKSPACE
+    assert bool((memory == 0xFF).all())
