@@ -778,9 +778,11 @@ bool decay_shape_ok(const dasc_plan_t *plan) {
   return (k == 32 || k == 64 || k == 128) && plan->info.d_v % 32 == 0;
 }
 
-// Requests of at most this many tokens (by the caller's bound) run in fp32 under AUTO.  Measured with 32 heads, fp32 / chunks, in us:
-// 6 tokens of 1, 8 and 64 requests 10 / 14, 21 / 21 and 80 / 74, 8 tokens 12 / 14, 23 / 21 and 88 / 74, 12 tokens 12 / 14, 29 / 21
-// and 113 / 74, 24 tokens 16 / 14, 39 / 23 and 170 / 82.
+// Requests of at most this many tokens (by the caller's bound) run in fp32 under AUTO.  Measured with 32 heads, from a cold L2, fp32 / chunks, in
+// us: 4 tokens of 1, 8 and 64 requests 10 / 14, 21 / 22 and 72 / 77, 6 tokens 10 / 14, 21 / 23 and 82 / 76, 8 tokens 12 / 14, 23 / 23
+// and 88 / 78, 12 tokens 12 / 14, 29 / 23 and 113 / 78, 24 tokens 16 / 14, 39 / 23 and 168 / 82.  The crossing moves from 16 tokens of one request to 5
+// of 64; the rule goes by length alone, at the crossing of 8 requests, so that how drafts are computed does not depend on how many
+// others are in the batch.  6 to 8 tokens of 64 requests pay 8 to 13 % for that.
 constexpr int kDecayShort = 8;
 bool decay_chunked_shape(const dasc_plan_t *plan, int32_t layers, int64_t total_tokens) {
   return chunked_shape_ok(plan) && total_tokens > 0 && static_cast<double>(layers) * total_tokens <= INT32_MAX;  // (32-bit token coordinates)

@@ -28,7 +28,9 @@
 // to QS; KV itself does not depend on the state.
 // Bound: with every SM at work, power (the SM clock settles at 1.45 to 1.6 of 1.965 GHz), so fewer products and instructions count, not idle
 // cycles; and the roles' code as a whole, which runs at an instruction per cycle and scheduler up to 32 KB and at a third of that
-// beyond (unrolled to 142 KB, its warps waited for instructions 5.5 times as long as they issued them, at 58 KB 0.6 times).
+// beyond (unrolled to 142 KB, its warps waited for instructions 5.5 times as long as they issued them, at 61 KB 1.1 times); and what a unit
+// costs beside its chunks, chiefly the exchange of the state between its last product and the next unit's first: 14.2 us for a unit of four
+// chunks in a batch, where a chunk of a long request takes 2.5.
 // Measured, 32 heads, bf16 outputs: 64 requests of 256 tokens x 4 layers 784 us (the bytes take 410 us at 6567 GB/s), 64 requests of 1 to
 // 1023 tokens 386 us, one of 32,768 tokens 528 us.
 #include <cuda.h>
@@ -79,7 +81,7 @@ struct alignas(16) Chunk {
   int64_t out;           // its first output, in elements
   // weights (read in pairs)
   float ghi[C], glo[C];  // G_t = ghi + glo, ghi a multiple of 2^-6: differences of ghi are exact
-  float w[C];            // e^{G_C - G_i}; 0 behind the last token
+  float w[C];            // e^{G_C - G_i} (behind the last token 1: those keys are left out where Kw is made)
   float eg[C];           // q_scale e^{G_t}
   // P's weights outside its diagonal blocks of 16 x 16 are products: with B the last token before t's block, e^{G_t - G_B} times
   // e^{G_B - G_i}, neither above 1
@@ -444,8 +446,8 @@ __global__ void __launch_bounds__(NT, 1) decay_chunked_kernel(const __grid_const
             w.decay = sp.phase == 1 ? sp.seg_decay + at : nullptr;
             w.out = ((x.tok0 + c * C) * a.H_v + x.head) * D;
           }
-          // Log-decays in log2 units as pairs: hi a multiple of 2^-6, so that sums of 64 and their differences are exact (below -2048 a
-          // token forgets everything, and is clamped there), lo the rest, at most 2^-7 each.
+          // Log-decays in log2 units as pairs: hi a multiple of 2^-6, so that sums of 64 and their differences are exact (at -1400,
+          // 2020 in log2 units, a token forgets everything, and is clamped there), lo the rest, at most 2^-7 each.
           float hi[2], lo[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
@@ -1016,7 +1018,13 @@ EncodeTiledFn encode_tiled_fn() {
 }
 
 // How long requests are split: into as many segments as make the longest chain of chunks on one SM shortest, by the caller's bound on
-// the length.  All but the last segment are then run twice (their states first, without outputs).
+// the length.  All but the last segment are then run twice (their states first, without outputs).  The model counts time in chunks with
+// outputs (2.4 to 2.5 us): one without takes 0.58 to 0.60 of it (148 heads of 8192 tokens, 184 against 315 us), so a split chunk counts 1.6, and the two
+// more launches and the join about 10 (2048 tokens of 32 heads in 4 segments: 52 us, 31 of them chunks).  Measured, us, unsplit / as the model has it /
+// the best of up to 16 segments: 32 heads of 32,768 tokens 1124 / 462 / 457, of 8192 320 / 153 / 151, of 2048 77 / 52 / 52, of 1024 42 / 42 / 37; 4 heads
+// of 4096 169 / 41 / 38; 4, 8 and 9 requests of 32 heads and 2048 or 4096 tokens are best left whole, as it has them (two segments of four
+// requests 221 against 153).  One of 32,768 beside 8 of 100 1218 / 722 / 665: the model weighs the batch, not its one long request,
+// and with more units than twice the SMs nothing is split however long one of them is.
 struct SplitSizes {
   int32_t nseg, seg_chunks;
 };

@@ -15,6 +15,7 @@
 // Bound: bytes of the state (128 KB read and written per 128 x 128 head and call).  A token of 256 requests x 32 heads: 163 us, 101 % of the
 // measured copy rate of 6567 GB/s.  Few tokens are bound by the latency of a block's steps (loads, decays, products of queries and keys,
 // outputs), of which two blocks per SM hide one: 5 tokens of 64 requests x 32 heads scored in 45 us (22 us of bytes), advanced in 55 us (41).
+// With 128 rows and columns two blocks per SM leave 128 registers, of which groups of tokens spill 11 to 15 (44 to 60 bytes).
 #include <cuda_runtime.h>
 
 #include "decay_common.cuh"
@@ -22,8 +23,8 @@
 namespace {
 
 constexpr int TB = 8;    // tokens per group
-// How many states on the next to be fetched into L2 is: a wave of blocks (two per SM).  With it 5 tokens of 64 requests x
-// 32 heads are scored in 48 us where it took 51, and advanced in 55 where it took 61.
+// How many states on the next to be fetched into L2 is: a wave of blocks (two per SM).  It took 5 tokens of 64 requests x
+// 32 heads, scored, from 51 to 48 us (45 since), and advanced from 61 to 55.
 constexpr int kAhead = 2 * 148;
 
 template <typename T>

@@ -8,7 +8,7 @@
 // this one tile again.  One launch, no workspace, nothing depends on the order of arrival.
 // Bound: one pass over a row of the target, and one of the drafter where a token does not stand; in small calls the chain of loads to
 // the first token that does not stand, two cluster barriers and the last tile.  64 requests of 8 drafts over 131,072 entries in fp32: 23 us,
-// their bytes take 10.2 at 6567 GB/s; 37 of 5 over 50,257 in bf16, odd rows: 9.5 us; one: 6.3 us.  Not faster: the warp's part of the row
+// their bytes take 10.2 at 6567 GB/s; 37 of 5 over 50,257 in bf16, odd rows: 9.2 us; one: 6.7 us (calls one behind the other).  Not faster: the warp's part of the row
 // prefetched into L2 ahead of its loads (27 us).
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -283,7 +283,7 @@ int launch_type(const DascVerifyArgs &a, void *stream) {
   auto even = [](const void *p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0 && stride % 4 == 0; };
   const bool vec = even(a.target, a.target_stride) && (!a.draft || even(a.draft, a.draft_stride));
   // As many blocks per request as still fit the GPU at once, two per SM (not every GPC holds a whole number of clusters of 4 or 8).
-  // Measured over 131072 entries in us with 8 / 4 / 2 / 1 blocks: 32 requests 21 / 27 / 41 / 70, 37 requests 31 / 29 / 41 / 70, 64 requests
+  // Measured over 131072 entries, 4 drafts each, every call from a cold L2 (unlike the figures at the top), in us with 8 / 4 / 2 / 1 blocks: 32 requests 21 / 27 / 41 / 70, 37 requests 31 / 29 / 41 / 70, 64 requests
   // 35 / 31 / 43 / 72, 148 requests 74 / 68 / 53 / 78, 296 requests 129 / 109 / 90 / 87.
   const auto with = [&](auto cl) {
     constexpr int CL = decltype(cl)::value;
