@@ -566,7 +566,7 @@ dasc_status_t dasc_refresh_static(const dasc_plan_t *plan, float *state_base, in
  *   otherwise), sums in fp32.  Operands that are not exact in bf16: decayed keys are in three bf16 parts (states are as good as
  *   fp32 ones); weights inside a chunk and the state on its way to the outputs in two (2^-16 of each term).  A token with a NaN or
  *   an infinity in v makes its column of the state and of all later outputs NaN (where exact arithmetic may keep an infinity);
- *   earlier outputs are not touched by it.
+ *   earlier outputs are not touched by it.  An infinity in q, k or a state may be a NaN where exact arithmetic has an infinity.
  * algo AUTO: CHUNKED where shape and type allow it and the requests are long enough to gain, else SEQUENTIAL.
  *
  * workspace: DEVICE scratch of at least dasc_decay_workspace_bytes() for these sizes or larger ones, 256-byte aligned, private to
