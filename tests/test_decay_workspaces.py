@@ -64,3 +64,41 @@ def test_a_workspace_between_words_is_refused(algo, offset):
         run(case, algo=algo, workspace=memory[offset:offset + 4096])
     assert e.value.status == dasc.binding.ERR_WORKSPACE
     assert bool((memory == 0xFF).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("o_dtype", [torch.float32, torch.bfloat16])
+def test_long_requests_one_behind_the_other_in_one_workspace_and_replayed(o_dtype):
+    """Calls that are split into segments, on one stream with nothing between them, as they are and from a graph."""
+    cases = [make_case(74, [2085, 7], H_v=8, H_k=4), make_case(75, [1100, 1300], H_v=8, H_k=4, decay="head")]
+    size = max(query(c.plan, 2, 1, c.T, max(c.lens)) for c in cases)
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+    want = [run(c, o_dtype=o_dtype) for c in cases]
+    states, outs = [c.state.clone() for c in cases], [torch.zeros_like(w[1]) for w in want]
+    cus = [c.cu.cuda() for c in cases]
+
+    def calls():
+        for c, state, o, cu in zip(cases, states, outs, cus):
+            dasc.dasc_decay_attn(c.plan, state, *c.strides, c.req, c.q, c.k, c.v, c.g, cu, c.T, max(c.lens), q_scale=0.7, o=o, workspace=ws,
+                                 decay=dasc.DECAY_PER_HEAD if c.g.dim() == 2 else dasc.DECAY_PER_TOKEN)
+
+    def check_and_start_again():
+        torch.cuda.synchronize()
+        assert dasc.dasc_decay_status(ws) == 0
+        for c, state, o, w in zip(cases, states, outs, want):
+            owned = c.req.long()
+            assert torch.equal(state[owned], w[0][owned]) and torch.equal(o[:, :c.T], w[1][:, :c.T])
+            state.copy_(c.state)
+            o.zero_()
+        torch.cuda.synchronize()
+
+    calls()
+    check_and_start_again()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+        calls()
+        graph.capture_end()
+    for _ in range(3):
+        graph.replay()
+        check_and_start_again()
