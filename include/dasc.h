@@ -13,6 +13,10 @@
  *                 device linear attention with a decay per head (no delta correction) over the same states: prompts, single tokens
  *   dasc_verify_draft
  *                 device how many drafted tokens of each request stand, and its next token
+ *   dasc_delta_step / dasc_delta_draft
+ *                 device the recurrence of dasc_refresh for single tokens (decoding) and drafted ones (scored, or advanced over)
+ *   dasc_beam_select / dasc_beam_reorder
+ *                 device beam search: the best continuations, and slots and states of the beams they continue
  *
  * Conventions
  *   - No exception crosses this boundary; every call returns a dasc_status_t.
@@ -628,6 +632,85 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
                                 int32_t dtype, int32_t vocab, const int32_t *tokens, const int32_t *cu_drafts,
                                 const float *u_accept, const float *u_next, int32_t n_req, int32_t max_drafts, int32_t *out,
                                 int64_t out_stride, int32_t *n_kept, void *cuda_stream);
+
+/*
+ * The gated delta rule (Eq. 1) in decoding: the recurrence and layouts of dasc_refresh, for plans of either kind, in fp32.  States, q, k, v,
+ * g (any g <= 0, -infinity: everything before the token is forgotten), beta, o, req_idx and strides as for dasc_refresh and
+ * dasc_decay_attn: a negative req_idx is padding (state and rows of o stay as they were), and neither stride may be below a layer's
+ * dense size where it reaches states that are written.  d_k of 32, 64 or 128 and any d_v that is a multiple of 32 (DASC_ERR_SHAPE
+ * otherwise).  No workspace.  Sums run in a fixed order: equal calls give equal bits.
+ *
+ * dasc_delta_step: one token per request; token r of the streams ([Lc][n_req][heads][d]) belongs to request r; o is required.
+ *   src_idx    DEVICE int32[n_req] or NULL: beams.  Request r then starts from the state of slot src_idx[r] and writes slot req_idx[r]
+ *              (dasc_beam_reorder gives both).  Requests come in groups of beam_width (1 .. 32, divides n_req); beams of one group that
+ *              continue the same state read it once.  A slot that is written by a beam may be read only by beams
+ *              that start from this beam's own source, and beams of different groups share no source; a negative src_idx is padding.  beam_width
+ *              is not looked at where src_idx is NULL.
+ *
+ * dasc_delta_draft: each request's token range, made for a few tokens (drafts; for prompts and suffixes dasc_refresh is the faster call); any
+ *   number of tokens is right.  cu_seqlens, seq_used, from_zero as for dasc_decay_attn.  max_seqlen is an upper bound on any
+ *   request's token count; it limits nothing.
+ *   mode DASC_DRAFT_ADVANCE  every state is advanced and written back; o may be NULL, and then q
+ *   mode DASC_DRAFT_SCORE    outputs only, no state is written.  A recurrent state cannot be rewound the way a KV cache can,
+ *                            so drafts are scored first, then verified (dasc_verify_draft), and the state is advanced over those that stand
+ *                            by a second call (ADVANCE, seq_used = n_kept, o = NULL).
+ *   A request without tokens still has its state set to zero by ADVANCE where from_zero says so.  A token with a NaN or an infinity in v reaches its own
+ *   column of the state and of later outputs only; one in k, g or beta reaches everything behind it.
+ * Errors: as for dasc_decay_attn, before any launch (g of a KDA plan has to be 16-byte aligned).
+ */
+typedef enum { DASC_DRAFT_ADVANCE = 0, DASC_DRAFT_SCORE = 1 } dasc_draft_mode_t;
+dasc_status_t dasc_delta_step(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride,
+                              const int32_t *req_idx, const int32_t *src_idx, int32_t beam_width, const void *q, const void *k,
+                              const void *v, int32_t io_dtype, const float *g, const float *beta, int32_t n_req,
+                              int32_t layer_begin, int32_t layer_end, float q_scale, void *o, int32_t o_dtype, void *cuda_stream);
+dasc_status_t dasc_delta_draft(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride,
+                               const int32_t *req_idx, const void *q, const void *k, const void *v, int32_t io_dtype,
+                               const float *g, const float *beta, const int32_t *cu_seqlens, const int32_t *seq_used,
+                               const int32_t *from_zero, int32_t n_req, int64_t total_tokens, int32_t max_seqlen,
+                               int32_t layer_begin, int32_t layer_end, float q_scale, void *o, int32_t o_dtype, int32_t mode,
+                               void *cuda_stream);
+
+/*
+ * Beam search: the n_out best continuations of each request over its `width` beams and the vocabulary, from logits:
+ *     s(b, v) = scores[b] + x_bv - log sum_w exp(x_bw)          in 64-bit arithmetic, exponentials in fp32
+ * best first; among equal ones the lower beam, then the larger logit, then the lower token.
+ *   logits   DEVICE [n_req * width][vocab], bf16 or fp32 (`dtype`), logits_stride >= vocab elements between rows.  What is not a finite number (a
+ *            masked token's -infinity, a NaN) is no continuation and has no weight in the sum.
+ *   scores   DEVICE fp32[n_req][width]: log-probabilities of the beams so far; a beam whose score is not finite has no continuation (at the
+ *            start one beam has score 0, the others -infinity)
+ *   ended    DEVICE int32[n_req][width] or NULL: a beam where it is != 0 is complete; its row of logits is not read and its one
+ *            continuation is end_token with the score it has
+ *   end_token  in [0, vocab) where `ended` is given; -1 (no such token) where only out_ended is; not looked at without both
+ *   out_scores fp32, out_parent int32 (the beam, 0 .. width-1), out_token int32: DEVICE [n_req][n_out].  Where there are fewer
+ *            continuations than n_out, the last entries are -infinity, -1, -1.
+ *   out_ended  DEVICE int32[n_req][n_out] or NULL: 1 where the beam had ended, the token is end_token, or there is no continuation
+ * width <= 32, n_out <= 64 (DASC_ERR_SHAPE otherwise).  With n_out == width, out_scores may be scores and out_ended may be ended.
+ * The current device must be the one that holds the buffers.  One launch, no workspace; equal calls give equal bits.
+ */
+dasc_status_t dasc_beam_select(const void *logits, int64_t logits_stride, int32_t dtype, int32_t vocab, const float *scores,
+                               const int32_t *ended, int32_t end_token, int32_t n_req, int32_t width, int32_t n_out,
+                               float *out_scores, int32_t *out_parent, int32_t *out_token, int32_t *out_ended, void *cuda_stream);
+
+/*
+ * States behind the beams of a selection: new beam i of a request continues its beam parent[i], and gets a slot of the active-state pool that
+ * holds this beam's state.  Per request, of the new beams that continue the same one the lowest keeps its slot; every other one gets, in ascending
+ * order, the slots of the beams that nobody continues, and the states (layers [layer_begin, layer_end)) and convolution blobs of
+ * these alone are copied, as bits.  The slots of a request stay the same set.
+ *   req_idx  DEVICE int32[n_req][width]: slot of each beam, all distinct
+ *   parent   DEVICE int32[n_req][width]: out_parent of a selection with n_out == width.  A negative entry (or one that is no beam): the new
+ *            beam gets a slot and nothing is copied to it.
+ *   new_idx  DEVICE int32[n_req][width], written: slots of the new beams
+ *   src_idx  DEVICE int32[n_req][width] or NULL, written: the slot that held each new beam's state before the call (-1: none)
+ *            The four arrays must not overlap.
+ *   state_base  NULL: no states are copied; new_idx and src_idx then go to dasc_delta_step, which reads each state where it is
+ *   conv_base   DEVICE or NULL: convolution blobs of conv_bytes, conv_stride_bytes apart, as for dasc_conv_store
+ * A negative slot (padding) is passed on and never copied.  Strides and alignment as for dasc_delta_step; width <= 32 (DASC_ERR_SHAPE
+ * otherwise).  No workspace.
+ */
+dasc_status_t dasc_beam_reorder(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride, void *conv_base,
+                                int64_t conv_stride_bytes, int64_t conv_bytes, const int32_t *req_idx, const int32_t *parent,
+                                int32_t n_req, int32_t width, int32_t layer_begin, int32_t layer_end, int32_t *new_idx,
+                                int32_t *src_idx, void *cuda_stream);
 
 const char *dasc_status_string(dasc_status_t status);
 /* "major.minor.patch" of this library. */

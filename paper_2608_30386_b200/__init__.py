@@ -15,4 +15,5 @@ from .binding import (  # noqa: F401
     dasc_debug_refresh_form,
     DECAY_CONTINUE, DECAY_PER_HEAD, DECAY_PER_TOKEN, DECAY_SCORE, DECAY_SCRATCH_MERGE_LOCAL, dasc_decay_attn, dasc_decay_status,
     dasc_decay_step, dasc_decay_workspace_bytes, dasc_verify_draft,
+    DRAFT_ADVANCE, DRAFT_SCORE, dasc_beam_reorder, dasc_beam_select, dasc_delta_draft, dasc_delta_step,
 )

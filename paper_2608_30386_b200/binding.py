@@ -27,6 +27,7 @@ REFRESH_CONTINUE, REFRESH_SCRATCH_MERGE_LOCAL = 0, 1
 ALGO_AUTO, ALGO_SEQUENTIAL, ALGO_CHUNKED = 0, 1, 2
 DECAY_PER_TOKEN, DECAY_PER_HEAD = 0, 1
 DECAY_CONTINUE, DECAY_SCRATCH_MERGE_LOCAL, DECAY_SCORE = 0, 1, 2
+DRAFT_ADVANCE, DRAFT_SCORE = 0, 1
 
 OK, ERR_INVALID_ARG, ERR_SHAPE, ERR_UNSUPPORTED, ERR_ALLOC, ERR_CUDA, ERR_WORKSPACE, ERR_TIMEOUT, ERR_DOMAIN = range(9)
 
@@ -41,6 +42,7 @@ EXPORTS = (
     "dasc_refresh_counters", "dasc_debug_set_refresh_poll_limit", "dasc_debug_refresh_form",
     "dasc_refresh_workspace_bytes", "dasc_refresh", "dasc_refresh_status", "dasc_refresh_window", "dasc_refresh_static",
     "dasc_decay_workspace_bytes", "dasc_decay_attn", "dasc_decay_status", "dasc_decay_step", "dasc_verify_draft",
+    "dasc_delta_step", "dasc_delta_draft", "dasc_beam_select", "dasc_beam_reorder",
     "dasc_status_string", "dasc_version",
 )
 
@@ -151,6 +153,19 @@ def lib() -> C.CDLL:
                                       C.c_float, C.c_void_p, C.c_int32, C.c_void_p]
         L.dasc_verify_draft.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p,
                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64,
+                                        C.c_void_p, C.c_void_p]
+        L.dasc_delta_step.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32,
+                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
+                                      C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_int32, C.c_void_p]
+        L.dasc_delta_draft.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_void_p,
+                                       C.c_int32, C.c_int32, C.c_void_p]
+        L.dasc_beam_select.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
+                                       C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_void_p]
+        L.dasc_beam_reorder.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
+                                        C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                         C.c_void_p, C.c_void_p]
         L.dasc_status_string.restype = C.c_char_p
         L.dasc_status_string.argtypes = [C.c_int]
@@ -594,3 +609,76 @@ def dasc_verify_draft(target: torch.Tensor, draft: torch.Tensor | None, tokens: 
         ds = vocab if n_drafts <= 1 else ds  # (a stride that nothing is reached by says nothing)
     _check((_native or _call()).verify_draft(target, vocab if rows <= 1 else ts, draft, ds, vocab, tokens, cu_drafts, u_accept, u_next,
                                              width - 1, out, width if n_out <= 1 else os_, n_kept, stream), "dasc_verify_draft")
+
+
+def dasc_delta_step(plan: Plan, state: torch.Tensor, layer_stride: int, req_stride: int, req_idx: torch.Tensor, q: torch.Tensor,
+                    k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, beta: torch.Tensor, o: torch.Tensor, *,
+                    src_idx: torch.Tensor | None = None, beam_width: int = 1, layer_begin: int = 0, layer_end: int | None = None,
+                    q_scale: float = 1.0, stream=None):
+    """The gated delta rule for one token per request: streams [layers in the call][n_req][heads][d], states in place.  With
+    ``src_idx`` (int32 [n_req], device) request r continues the state of slot ``src_idx[r]`` and writes slot ``req_idx[r]``, in groups of
+    ``beam_width`` beams: what ``dasc_beam_reorder`` gives when it copies no states.  A negative ``req_idx`` is padding."""
+    _check((_native or _call()).delta_step(
+        plan.handle, state, layer_stride, req_stride, req_idx, q, k, v, g, beta, layer_begin,
+        plan.info.n_layers if layer_end is None else layer_end, q_scale, o, src_idx, beam_width, stream), "dasc_delta_step")
+
+
+def dasc_delta_draft(plan: Plan, state: torch.Tensor, layer_stride: int, req_stride: int, req_idx: torch.Tensor,
+                     q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
+                     cu_seqlens: torch.Tensor, total_tokens: int, max_seqlen: int, *, seq_used: torch.Tensor | None = None,
+                     from_zero: torch.Tensor | None = None, layer_begin: int = 0, layer_end: int | None = None, q_scale: float = 1.0,
+                     o: torch.Tensor | None = None, mode: int = DRAFT_ADVANCE, stream=None):
+    """The gated delta rule over a few tokens per request: outputs into ``o`` and the states left alone (``DRAFT_SCORE``), or the states
+    advanced in place (``DRAFT_ADVANCE``; ``o`` and then ``q`` may be None), over ``seq_used`` tokens of each request where given, for instance
+    ``dasc_verify_draft``'s ``n_kept``.  ``from_zero`` and a negative ``req_idx`` as for ``dasc_decay_attn``."""
+    _check((_native or _call()).delta_draft(
+        plan.handle, state, layer_stride, req_stride, req_idx, q, k, v, g, beta, layer_begin,
+        plan.info.n_layers if layer_end is None else layer_end, q_scale, o, cu_seqlens, total_tokens, max_seqlen, seq_used, from_zero, mode,
+        stream), "dasc_delta_draft")
+
+
+def dasc_beam_select(logits: torch.Tensor, scores: torch.Tensor, out_scores: torch.Tensor, out_parent: torch.Tensor,
+                     out_token: torch.Tensor, *, ended: torch.Tensor | None = None, out_ended: torch.Tensor | None = None,
+                     end_token: int = -1, stream=None):
+    """The best continuations of each request's beams.  ``logits`` [n_req, width, vocab] (or [n_req * width, vocab]), bf16 or fp32, rows may be
+    strided; ``scores`` fp32 [n_req, width], ``ended`` int32 alike; ``out_scores``, ``out_parent``, ``out_token`` (and ``out_ended``)
+    [n_req, n_out] are written.  Scores and ended beams may be updated in place where n_out is the width."""
+    (n_req, width), n_out, vocab = scores.shape, out_scores.shape[-1], logits.shape[-1]
+    for x in (out_scores, out_parent, out_token, out_ended):
+        if x is not None and tuple(x.shape) != (n_req, n_out):
+            raise ValueError("the outputs need one row of continuations per request")
+    if ended is not None and ended.shape != scores.shape:
+        raise ValueError("ended needs an entry per beam")
+    if tuple(logits.shape[:-1]) not in ((n_req, width), (n_req * width,)):
+        raise ValueError("logits needs a row of the vocabulary per beam")
+    stride = vocab
+    if n_req * width > 1 and vocab > 0:
+        stride = logits.stride(-2) if logits.dim() == 2 or width > 1 else logits.stride(0)
+        if logits.dim() == 3 and n_req > 1 and width > 1 and logits.stride(0) != width * stride:
+            raise ValueError("the rows of logits have to be evenly spaced")
+    if logits.stride(-1) != 1 and vocab > 1:
+        raise ValueError("the rows of logits have to be dense")
+    _check((_native or _call()).beam_select(logits, stride, vocab, scores, ended, end_token, n_req, width, n_out, out_scores, out_parent, out_token,
+                                            out_ended, stream), "dasc_beam_select")
+
+
+def dasc_beam_reorder(plan: Plan, state: torch.Tensor | None, layer_stride: int, req_stride: int, req_idx: torch.Tensor,
+                      parent: torch.Tensor, new_idx: torch.Tensor, *, src_idx: torch.Tensor | None = None,
+                      conv: torch.Tensor | None = None, layer_begin: int = 0, layer_end: int | None = None, stream=None):
+    """Slots and states of the beams of a selection: ``req_idx`` and ``parent`` int32 [n_req, width] are read, ``new_idx`` (and ``src_idx``) are
+    written, and the states of beams that are continued more than once are copied to slots that nobody continues.  ``state`` None:
+    slots only, for ``dasc_delta_step`` with ``src_idx``.  ``conv`` [slots, ...]: a convolution blob per slot that goes along, rows of a multiple of
+    16 bytes."""
+    n_req, width = req_idx.shape
+    for x in (parent, new_idx, src_idx):
+        if x is not None and x.shape != req_idx.shape:
+            raise ValueError("req_idx, parent, new_idx and src_idx need an entry per beam")
+    conv_stride = conv_bytes = 0
+    if conv is not None:
+        if conv.dim() < 2 or not conv[0].is_contiguous():
+            raise ValueError("conv needs a dense blob per slot")
+        conv_bytes = conv[0].numel() * conv.element_size()
+        conv_stride = conv.stride(0) * conv.element_size() if conv.shape[0] > 1 else conv_bytes
+    _check((_native or _call()).beam_reorder(
+        plan.handle, state, layer_stride, req_stride, conv, conv_stride, conv_bytes, req_idx, parent, n_req, width, layer_begin,
+        plan.info.n_layers if layer_end is None else layer_end, new_idx, src_idx, stream), "dasc_beam_reorder")

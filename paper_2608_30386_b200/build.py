@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libdasc.so")
 CALL = os.path.join(HERE, "_dasccall.so")   # CPython entry to the library's device calls
 CALL_SOURCE = "pycall.c"
 SOURCES = ["dasc_api.cu", "plan_host.cpp", "pack_restore.cu", "codec_int8.cu", "refresh_seq.cu", "refresh_chunked.cu",
-           "decay_seq.cu", "decay_chunked.cu", "verify_draft.cu"]
+           "decay_seq.cu", "decay_chunked.cu", "verify_draft.cu", "delta_decode.cu", "beam.cu"]
 # sources compiled several times, side by side: object name and define of each translation unit
 UNITS = {"refresh_seq.cu": [(f"refresh_seq_{d}", f"-DDASC_SEQ_DIM={d}") for d in (128, 64, 32)]}
 HEADERS = [os.path.join(ROOT, "include", "dasc.h"), os.path.join(CSRC, "dasc_internal.h"),

@@ -94,6 +94,15 @@ dasc_status_t check_device(const dasc_plan_t *plan) {
   return dev == plan->info.device ? DASC_OK : DASC_ERR_INVALID_ARG;
 }
 
+// Where there is no plan to say which device the buffers are on: is this one on the current device?
+dasc_status_t check_buffer_device(const void *p) {
+  int dev = -1;
+  cudaPointerAttributes at{};
+  if (cudaGetDevice(&dev) != cudaSuccess) return DASC_ERR_CUDA;
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) return DASC_ERR_CUDA;
+  return at.type == cudaMemoryTypeUnregistered || (at.type == cudaMemoryTypeDevice && at.device != dev) ? DASC_ERR_INVALID_ARG : DASC_OK;
+}
+
 dasc_status_t check_copy_args(const dasc_plan_t *plan, const void *state, int64_t layer_stride, int64_t req_stride,
                               const void *idx_a, const void *pool, int64_t *slot_stride, const void *idx_b,
                               int32_t n_pairs, int64_t min_slot_floats = -1) {
@@ -924,12 +933,7 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
   if (reinterpret_cast<uintptr_t>(target) % esz || reinterpret_cast<uintptr_t>(draft) % esz) return DASC_ERR_INVALID_ARG;
   if (target_stride < vocab || (draft && draft_stride < vocab) || out_stride < static_cast<int64_t>(max_drafts) + 1)
     return DASC_ERR_INVALID_ARG;
-  // there is no plan to say which device the buffers are on
-  int dev = -1;
-  cudaPointerAttributes at{};
-  if (cudaGetDevice(&dev) != cudaSuccess) return DASC_ERR_CUDA;
-  if (cudaPointerGetAttributes(&at, target) != cudaSuccess) return DASC_ERR_CUDA;
-  if (at.type == cudaMemoryTypeUnregistered || (at.type == cudaMemoryTypeDevice && at.device != dev)) return DASC_ERR_INVALID_ARG;
+  if (const dasc_status_t ds = check_buffer_device(target); ds != DASC_OK) return ds;
   DascVerifyArgs a{};
   a.target = target;
   a.target_stride = target_stride;
@@ -947,6 +951,179 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
   a.out_stride = out_stride;
   a.n_kept = n_kept;
   return dasc_launch_verify_draft(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
+}
+
+// ---- the gated delta rule for single and drafted tokens --------------------------------------------------------------------------
+
+namespace {
+
+// Every argument check of dasc_delta_step and dasc_delta_draft (cu_seqlens given there), before anything is launched.
+dasc_status_t delta_validate(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride, const int32_t *req_idx,
+                             const void *q, const void *k, const void *v, int32_t io_dtype, const float *g, const float *beta, int32_t n_req,
+                             int64_t total_tokens, int32_t layer_begin, int32_t layer_end, float q_scale, void *o, int32_t o_dtype, bool score,
+                             DascDeltaArgs *a) {
+  if (!plan || plan->info.device < 0) return DASC_ERR_INVALID_ARG;
+  if (n_req < 0 || total_tokens < 0) return DASC_ERR_INVALID_ARG;
+  if (layer_begin < 0 || layer_end < layer_begin || layer_end > plan->info.n_layers) return DASC_ERR_INVALID_ARG;
+  if (io_dtype != DASC_IO_BF16 && io_dtype != DASC_IO_FP32) return DASC_ERR_INVALID_ARG;
+  if (o && o_dtype != DASC_IO_BF16 && o_dtype != DASC_IO_FP32) return DASC_ERR_INVALID_ARG;
+  if (!decay_shape_ok(plan)) return DASC_ERR_SHAPE;
+  const int32_t layers = layer_end - layer_begin;
+  if (total_tokens > INT32_MAX || static_cast<double>(n_req) * layers * plan->info.n_v_heads * (plan->info.d_v / 32) > INT32_MAX)
+    return DASC_ERR_SHAPE;
+  if (n_req == 0 || layers == 0) return DASC_OK;
+  if (!state_base || !req_idx || !aligned16(state_base)) return DASC_ERR_INVALID_ARG;
+  if (total_tokens > 0 && (!k || !v || !g || !beta || (o && !q))) return DASC_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o)) return DASC_ERR_INVALID_ARG;
+  const bool kda = plan->info.kind == DASC_KDA;
+  if ((reinterpret_cast<uintptr_t>(g) & (kda ? 15u : 3u)) || (reinterpret_cast<uintptr_t>(beta) & 3u)) return DASC_ERR_INVALID_ARG;
+  if (layer_stride < 0 || req_stride < 0 || layer_stride % 4 || req_stride % 4) return DASC_ERR_INVALID_ARG;
+  const int64_t dense = plan->info.dense_floats_per_layer;
+  if (!score && ((layers > 1 && layer_stride < dense) || (n_req > 1 && req_stride < dense)))
+    return DASC_ERR_INVALID_ARG;  // layers of one request, or requests in one layer, would overlap and be written from several blocks
+  if (const dasc_status_t ds = check_device(plan); ds != DASC_OK) return ds;
+  a->H_v = plan->info.n_v_heads;
+  a->H_k = plan->info.n_k_heads;
+  a->d_k = plan->info.d_k;
+  a->d_v = plan->info.d_v;
+  a->kda = kda;
+  a->state = state_base;
+  a->layer_stride = layer_stride;
+  a->req_stride = req_stride;
+  a->req_idx = req_idx;
+  a->q = q;
+  a->k = k;
+  a->v = v;
+  a->io_bf16 = io_dtype == DASC_IO_BF16;
+  a->g = g;
+  a->beta = beta;
+  a->n_req = n_req;
+  a->total_tokens = total_tokens;
+  a->layer_begin = layer_begin;
+  a->n_layers_in_call = layers;
+  a->q_scale = q_scale;
+  a->o = o;
+  a->o_bf16 = o_dtype == DASC_IO_BF16;
+  a->score = score;
+  return DASC_OK;
+}
+
+}  // namespace
+
+dasc_status_t dasc_delta_step(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride,
+                              const int32_t *req_idx, const int32_t *src_idx, int32_t beam_width, const void *q, const void *k,
+                              const void *v, int32_t io_dtype, const float *g, const float *beta, int32_t n_req,
+                              int32_t layer_begin, int32_t layer_end, float q_scale, void *o, int32_t o_dtype, void *cuda_stream) {
+  TraceRange trace("dasc_delta_step");
+  DascDeltaArgs a{};
+  if (src_idx && (beam_width < 1 || beam_width > kBeamMaxWidth || (n_req > 0 && n_req % beam_width))) return DASC_ERR_INVALID_ARG;
+  const dasc_status_t st = delta_validate(plan, state_base, layer_stride, req_stride, req_idx, q, k, v, io_dtype, g, beta, n_req, n_req,
+                                          layer_begin, layer_end, q_scale, o, o_dtype, false, &a);
+  if (st != DASC_OK || n_req == 0 || layer_end == layer_begin) return st;
+  if (!o) return DASC_ERR_INVALID_ARG;
+  a.src_idx = src_idx;
+  a.beam_width = src_idx ? beam_width : 1;
+  return dasc_launch_delta(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
+}
+
+dasc_status_t dasc_delta_draft(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride,
+                               const int32_t *req_idx, const void *q, const void *k, const void *v, int32_t io_dtype,
+                               const float *g, const float *beta, const int32_t *cu_seqlens, const int32_t *seq_used,
+                               const int32_t *from_zero, int32_t n_req, int64_t total_tokens, int32_t max_seqlen,
+                               int32_t layer_begin, int32_t layer_end, float q_scale, void *o, int32_t o_dtype, int32_t mode,
+                               void *cuda_stream) {
+  TraceRange trace("dasc_delta_draft");
+  DascDeltaArgs a{};
+  if (mode != DASC_DRAFT_ADVANCE && mode != DASC_DRAFT_SCORE) return DASC_ERR_INVALID_ARG;
+  if (max_seqlen < 0 || (mode == DASC_DRAFT_SCORE && !o)) return DASC_ERR_INVALID_ARG;
+  const dasc_status_t st = delta_validate(plan, state_base, layer_stride, req_stride, req_idx, q, k, v, io_dtype, g, beta, n_req, total_tokens,
+                                          layer_begin, layer_end, q_scale, o, o_dtype, mode == DASC_DRAFT_SCORE, &a);
+  if (st != DASC_OK || n_req == 0 || layer_end == layer_begin) return st;
+  if (!cu_seqlens) return DASC_ERR_INVALID_ARG;
+  a.cu_seqlens = cu_seqlens;
+  a.seq_used = seq_used;
+  a.from_zero = from_zero;
+  return dasc_launch_delta(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
+}
+
+// ---- beam search -------------------------------------------------------------------------------------------------------------------
+
+dasc_status_t dasc_beam_select(const void *logits, int64_t logits_stride, int32_t dtype, int32_t vocab, const float *scores,
+                               const int32_t *ended, int32_t end_token, int32_t n_req, int32_t width, int32_t n_out,
+                               float *out_scores, int32_t *out_parent, int32_t *out_token, int32_t *out_ended, void *cuda_stream) {
+  TraceRange trace("dasc_beam_select");
+  if (n_req < 0 || vocab <= 0 || width < 1 || n_out < 1) return DASC_ERR_INVALID_ARG;
+  if (dtype != DASC_IO_BF16 && dtype != DASC_IO_FP32) return DASC_ERR_INVALID_ARG;
+  if (width > kBeamMaxWidth || n_out > kBeamMaxOut || n_req > INT32_MAX / 64 || vocab > INT32_MAX / 64) return DASC_ERR_SHAPE;
+  if ((ended || out_ended) && (end_token < -1 || end_token >= vocab)) return DASC_ERR_INVALID_ARG;
+  if (ended && end_token < 0) return DASC_ERR_INVALID_ARG;
+  if (n_req == 0) return DASC_OK;
+  if (!logits || !scores || !out_scores || !out_parent || !out_token) return DASC_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(logits) % (dtype == DASC_IO_BF16 ? 2 : 4) || logits_stride < vocab) return DASC_ERR_INVALID_ARG;
+  for (const void *p : {static_cast<const void *>(scores), static_cast<const void *>(ended), static_cast<const void *>(out_scores),
+                        static_cast<const void *>(out_parent), static_cast<const void *>(out_token), static_cast<const void *>(out_ended)})
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return DASC_ERR_INVALID_ARG;
+  if (n_out != width && (out_scores == scores || (ended && out_ended == ended))) return DASC_ERR_INVALID_ARG;
+  if (const dasc_status_t ds = check_buffer_device(logits); ds != DASC_OK) return ds;
+  DascBeamSelectArgs a{};
+  a.logits = logits;
+  a.stride = logits_stride;
+  a.bf16 = dtype == DASC_IO_BF16;
+  a.vocab = vocab;
+  a.scores = scores;
+  a.ended = ended;
+  a.end_token = ended || out_ended ? end_token : -1;
+  a.n_req = n_req;
+  a.width = width;
+  a.n_out = n_out;
+  a.out_scores = out_scores;
+  a.out_parent = out_parent;
+  a.out_token = out_token;
+  a.out_ended = out_ended;
+  return dasc_launch_beam_select(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
+}
+
+dasc_status_t dasc_beam_reorder(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride, void *conv_base,
+                                int64_t conv_stride_bytes, int64_t conv_bytes, const int32_t *req_idx, const int32_t *parent,
+                                int32_t n_req, int32_t width, int32_t layer_begin, int32_t layer_end, int32_t *new_idx,
+                                int32_t *src_idx, void *cuda_stream) {
+  TraceRange trace("dasc_beam_reorder");
+  if (!plan || plan->info.device < 0) return DASC_ERR_INVALID_ARG;
+  if (n_req < 0 || width < 1) return DASC_ERR_INVALID_ARG;
+  if (layer_begin < 0 || layer_end < layer_begin || layer_end > plan->info.n_layers) return DASC_ERR_INVALID_ARG;
+  if (width > kBeamMaxWidth) return DASC_ERR_SHAPE;
+  if (n_req == 0) return DASC_OK;
+  if (!req_idx || !parent || !new_idx || new_idx == req_idx || src_idx == req_idx || new_idx == parent || src_idx == parent || new_idx == src_idx)
+    return DASC_ERR_INVALID_ARG;
+  DascBeamReorderArgs a{};
+  const int64_t dense = plan->info.dense_floats_per_layer;
+  const int32_t layers = layer_end - layer_begin;
+  if (state_base) {
+    if (!aligned16(state_base) || layer_stride < 0 || req_stride < 0 || layer_stride % 4 || req_stride % 4) return DASC_ERR_INVALID_ARG;
+    if ((layers > 1 && layer_stride < dense) || (static_cast<int64_t>(n_req) * width > 1 && req_stride < dense)) return DASC_ERR_INVALID_ARG;
+    if (dense / 4 > INT32_MAX) return DASC_ERR_SHAPE;
+    a.state = state_base;
+    a.layer_stride = layer_stride;
+    a.req_stride = req_stride;
+    a.layer_begin = layer_begin;
+    a.n_layers_in_call = layers;
+    a.layer_vecs = static_cast<uint32_t>(dense / 4);
+  }
+  if (conv_base) {
+    if (!aligned16(conv_base) || conv_bytes < 0 || conv_bytes % 16 || conv_stride_bytes % 16 || conv_stride_bytes < conv_bytes) return DASC_ERR_INVALID_ARG;
+    if (conv_bytes / 16 > INT32_MAX) return DASC_ERR_SHAPE;
+    a.conv = conv_base;
+    a.conv_stride = conv_stride_bytes;
+    a.conv_vecs = static_cast<uint32_t>(conv_bytes / 16);
+  }
+  if (const dasc_status_t ds = check_device(plan); ds != DASC_OK) return ds;
+  a.req_idx = req_idx;
+  a.parent = parent;
+  a.n_req = n_req;
+  a.width = width;
+  a.new_idx = new_idx;
+  a.src_idx = src_idx;
+  return dasc_launch_beam_reorder(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
 }
 
 const char *dasc_status_string(dasc_status_t s) {

@@ -174,3 +174,54 @@ struct DascVerifyArgs {
   int32_t *n_kept;
 };
 int dasc_launch_verify_draft(const DascVerifyArgs &a, void *stream);
+
+// delta_decode.cu: the gated delta rule for single tokens (cu_seqlens null) and drafted ones.
+struct DascDeltaArgs {
+  int32_t H_v, H_k, d_k, d_v, kda;
+  float *state;
+  int64_t layer_stride, req_stride;
+  const int32_t *req_idx;
+  const int32_t *src_idx;     // single tokens: device, [n_req], or null: which state each beam continues
+  int32_t beam_width;         // beams per request where src_idx is given, at most 32
+  const void *q, *k, *v;
+  int32_t io_bf16;
+  const float *g, *beta;
+  const int32_t *cu_seqlens;  // null: one token per request, token r is request r's
+  const int32_t *seq_used;    // device, [n_req], or null: tokens of each request that are run
+  const int32_t *from_zero;   // device, [n_req], or null: != 0 starts from a zero state
+  int32_t n_req;
+  int64_t total_tokens;
+  int32_t layer_begin, n_layers_in_call;
+  float q_scale;
+  void *o;
+  int32_t o_bf16;
+  int32_t score;              // drafts: 1 = states are not written
+};
+int dasc_launch_delta(const DascDeltaArgs &a, void *stream);  // cudaError_t as int, or -1 if the shape has no kernel
+
+// beam.cu
+constexpr int kBeamMaxWidth = 32, kBeamMaxOut = 64;
+struct DascBeamSelectArgs {
+  const void *logits;
+  int64_t stride;
+  int32_t bf16, vocab;
+  const float *scores;
+  const int32_t *ended;  // or null
+  int32_t end_token, n_req, width, n_out;
+  float *out_scores;
+  int32_t *out_parent, *out_token, *out_ended;
+  int32_t segments, seg_slices, slice_len, per_block;  // set by the launcher: segments of a row, slices of a segment, their length, segments per block
+};
+int dasc_launch_beam_select(const DascBeamSelectArgs &a, void *stream);
+struct DascBeamReorderArgs {
+  float *state;  // or null
+  int64_t layer_stride, req_stride;
+  void *conv;    // or null
+  int64_t conv_stride;  // bytes
+  const int32_t *req_idx, *parent;
+  int32_t n_req, width, layer_begin, n_layers_in_call;
+  int32_t *new_idx, *src_idx;
+  uint32_t layer_vecs, conv_vecs;                   // vectors of 16 bytes
+  uint32_t piece_vecs, layer_pieces, pieces;        // set by the launcher: what a thread block copies of each state
+};
+int dasc_launch_beam_reorder(DascBeamReorderArgs a, void *stream);

@@ -400,12 +400,147 @@ static PyObject *py_verify_draft(PyObject *self, PyObject *const *a, Py_ssize_t 
   return PyLong_FromLong(st);
 }
 
+/* ---- the gated delta rule for single and drafted tokens, beam search ---- */
+
+/* plan, state, layer_stride, req_stride, req_idx, q, k, v, g, beta, layer_begin, layer_end, q_scale, o */
+struct delta_args {
+  void *plan, *state, *req, *q, *k, *v, *g, *beta, *o;
+  int64_t dev, ls, rs, n_req;
+  int32_t lb, le, n_req32, io, o_io;
+  float q_scale;
+};
+static int delta_parse(struct delta_args *r, PyObject *const *a, int64_t tokens /* < 0: one per request */) {
+  dasc_plan_info_t info;
+  int64_t lb, le;
+  int32_t io_q = -1, io_k = -1, io_v = -1;
+  r->o_io = DASC_IO_FP32;
+  if (as_ptr(a[0], &r->plan) || current_device(&r->dev) || as_index(a[2], &r->ls) || as_index(a[3], &r->rs) || as_index(a[10], &lb) ||
+      as_index(a[11], &le) || as_float(a[12], &r->q_scale) || as_i32(lb, "layer_begin", &r->lb) || as_i32(le, "layer_end", &r->le))
+    return -1;
+  if (dasc_plan_info(r->plan, &info) != DASC_OK) {
+    PyErr_SetString(PyExc_ValueError, "no plan");
+    return -1;
+  }
+  if (PyLong_Check(a[4]) || a[4] == Py_None) {
+    PyErr_SetString(PyExc_TypeError, "req_idx has to be a tensor");
+    return -1;
+  }
+  if (method_i64(a[4], s_numel, &r->n_req) || as_i32(r->n_req, "n_req", &r->n_req32)) return -1;
+  const double rows = ((double)le - (double)lb) * (double)(tokens < 0 ? r->n_req : tokens);
+  const double qk = rows * info.n_k_heads * info.d_k, vo = rows * info.n_v_heads * info.d_v, heads = rows * info.n_v_heads;
+  if (as_tensor(a[1], "state", r->dev, g_fp32, 1, 0, NULL, &r->state) || as_tensor(a[4], "req_idx", r->dev, g_int32, 0, 0, NULL, &r->req) ||
+      as_tensor(a[5], "q", r->dev, NULL, 0, qk, &io_q, &r->q) || as_tensor(a[6], "k", r->dev, NULL, 0, qk, &io_k, &r->k) ||
+      as_tensor(a[7], "v", r->dev, NULL, 0, vo, &io_v, &r->v) ||
+      as_tensor(a[8], "g", r->dev, g_fp32, 0, info.kind == DASC_KDA ? heads * info.d_k : heads, NULL, &r->g) ||
+      as_tensor(a[9], "beta", r->dev, g_fp32, 0, heads, NULL, &r->beta))
+    return -1;
+  r->io = io_k == -1 ? DASC_IO_FP32 : io_k;
+  if ((io_q != -1 && io_q != r->io) || (io_v != -1 && io_v != r->io)) {
+    PyErr_SetString(PyExc_TypeError, "q, k and v have to be of one type");
+    return -1;
+  }
+  return as_tensor(a[13], "o", r->dev, NULL, 0, vo, &r->o_io, &r->o);
+}
+
+/* delta_parse's arguments, then src_idx, beam_width, stream */
+static PyObject *py_delta_step(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  struct delta_args r;
+  void *src, *stream;
+  int64_t width;
+  int32_t width32;
+  if (arg_count(n, 17) || delta_parse(&r, a, -1) || as_tensor(a[14], "src_idx", r.dev, g_int32, 0, (double)r.n_req, NULL, &src) ||
+      as_index(a[15], &width) || as_i32(width, "beam_width", &width32) || as_stream(a[16], &stream))
+    return NULL;
+  dasc_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = dasc_delta_step(r.plan, r.state, r.ls, r.rs, r.req, src, width32, r.q, r.k, r.v, r.io, r.g, r.beta, r.n_req32, r.lb, r.le, r.q_scale, r.o, r.o_io,
+                       stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+/* delta_parse's arguments, then cu_seqlens, total_tokens, max_seqlen, seq_used, from_zero, mode, stream */
+static PyObject *py_delta_draft(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  struct delta_args r;
+  void *cu, *used, *zero, *stream;
+  int64_t total, longest, mode, n_cu;
+  int32_t most, mode32;
+  if (arg_count(n, 21) || as_count(a[15], &total) || as_count(a[16], &longest) || as_index(a[19], &mode) || as_i32(longest, "max_seqlen", &most) ||
+      as_i32(mode, "mode", &mode32))
+    return NULL;
+  if (delta_parse(&r, a, total < 0 ? 0 : total) || as_tensor(a[14], "cu_seqlens", r.dev, g_int32, 0, 1, NULL, &cu) || method_i64(a[14], s_numel, &n_cu))
+    return NULL;
+  if (n_cu != r.n_req + 1) {
+    PyErr_Format(PyExc_ValueError, "cu_seqlens holds %lld values for %lld requests", (long long)n_cu, (long long)r.n_req);
+    return NULL;
+  }
+  if (as_tensor(a[17], "seq_used", r.dev, g_int32, 0, (double)r.n_req, NULL, &used) ||
+      as_tensor(a[18], "from_zero", r.dev, g_int32, 0, (double)r.n_req, NULL, &zero) || as_stream(a[20], &stream))
+    return NULL;
+  dasc_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = dasc_delta_draft(r.plan, r.state, r.ls, r.rs, r.req, r.q, r.k, r.v, r.io, r.g, r.beta, cu, used, zero, r.n_req32, total, most, r.lb, r.le, r.q_scale,
+                        r.o, r.o_io, mode32, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+/* logits, logits_stride, vocab, scores, ended, end_token, n_req, width, n_out, out_scores, out_parent, out_token, out_ended, stream; rows of logits may be
+ * further apart than they are long, so the caller has looked at their shape */
+static PyObject *py_beam_select(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  void *logits, *scores, *ended, *os, *op, *ot, *oe, *stream;
+  int64_t dev, stride, x[5];
+  int32_t io = DASC_IO_FP32, i[5];
+  static const char *const names[5] = {"vocab", "end_token", "n_req", "width", "n_out"};
+  static const int at[5] = {2, 5, 6, 7, 8};
+  if (arg_count(n, 14) || current_device(&dev) || as_index(a[1], &stride)) return NULL;
+  for (int j = 0; j < 5; ++j)
+    if (as_index(a[at[j]], &x[j]) || as_i32(x[j], names[j], &i[j])) return NULL;
+  const double beams = (double)i[2] * i[3], outs = (double)i[2] * i[4];
+  if (as_tensor(a[0], "logits", dev, NULL, 1, 0, &io, &logits) || as_tensor(a[3], "scores", dev, g_fp32, 0, beams, NULL, &scores) ||
+      as_tensor(a[4], "ended", dev, g_int32, 0, beams, NULL, &ended) || as_tensor(a[9], "out_scores", dev, g_fp32, 0, outs, NULL, &os) ||
+      as_tensor(a[10], "out_parent", dev, g_int32, 0, outs, NULL, &op) || as_tensor(a[11], "out_token", dev, g_int32, 0, outs, NULL, &ot) ||
+      as_tensor(a[12], "out_ended", dev, g_int32, 0, outs, NULL, &oe) || as_stream(a[13], &stream))
+    return NULL;
+  dasc_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = dasc_beam_select(logits, stride, io, i[0], scores, ended, i[1], i[2], i[3], i[4], os, op, ot, oe, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+/* plan, state, layer_stride, req_stride, conv, conv_stride_bytes, conv_bytes, req_idx, parent, n_req, width, layer_begin, layer_end, new_idx, src_idx,
+ * stream */
+static PyObject *py_beam_reorder(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  void *plan, *state, *conv, *req, *parent, *to, *src, *stream;
+  int64_t dev, ls, rs, cs, cb, x[4];
+  int32_t i[4];
+  static const char *const names[4] = {"n_req", "width", "layer_begin", "layer_end"};
+  if (arg_count(n, 16) || as_ptr(a[0], &plan) || current_device(&dev) || as_index(a[2], &ls) || as_index(a[3], &rs) || as_index(a[5], &cs) ||
+      as_index(a[6], &cb))
+    return NULL;
+  for (int j = 0; j < 4; ++j)
+    if (as_index(a[9 + j], &x[j]) || as_i32(x[j], names[j], &i[j])) return NULL;
+  const double beams = (double)i[0] * i[1];
+  if (as_tensor(a[1], "state", dev, g_fp32, 1, 0, NULL, &state) || (a[4] != Py_None && !PyLong_Check(a[4]) && is_placed(a[4], "conv", dev, 1)) ||
+      as_ptr(a[4], &conv) || as_tensor(a[7], "req_idx", dev, g_int32, 0, beams, NULL, &req) ||
+      as_tensor(a[8], "parent", dev, g_int32, 0, beams, NULL, &parent) || as_tensor(a[13], "new_idx", dev, g_int32, 0, beams, NULL, &to) ||
+      as_tensor(a[14], "src_idx", dev, g_int32, 0, beams, NULL, &src) || as_stream(a[15], &stream))
+    return NULL;
+  dasc_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = dasc_beam_reorder(plan, state, ls, rs, conv, cs, cb, req, parent, i[0], i[1], i[2], i[3], to, src, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
 #define M(name, fn) {name, (PyCFunction)(void (*)(void))fn, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {
     M("init", py_init), M("pack", py_pack), M("pack_padded", py_pack_padded), M("pack_int8", py_pack_int8),
     M("restore", py_restore), M("restore_padded", py_restore_padded), M("restore_int8", py_restore_int8),
     M("refresh", py_refresh), M("refresh_window", py_refresh_window),
-    M("decay_attn", py_decay_attn), M("decay_step", py_decay_step), M("verify_draft", py_verify_draft), {NULL, NULL, 0, NULL}};
+    M("decay_attn", py_decay_attn), M("decay_step", py_decay_step), M("verify_draft", py_verify_draft),
+    M("delta_step", py_delta_step), M("delta_draft", py_delta_draft), M("beam_select", py_beam_select), M("beam_reorder", py_beam_reorder), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dasccall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__dasccall(void) {
