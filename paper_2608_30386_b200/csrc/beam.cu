@@ -4,10 +4,11 @@
 // request's width x vocab continuations are wanted.  Inside a beam they are ordered like the logits themselves, so each part of a row gives its best n_out
 // by 64-bit keys (logit, then lower token) while it sums exponentials, all from one pass over the row, and the few that are left meet with their beams' sums.
 // Split: a request is a cluster of CL thread blocks; the rows of its beams are cut into segments, alike for all rows, which the blocks take in
-// order, a slice of at most NT * EPT entries in registers at a time.  Sums are kept by segment and added up in their order, so that equal rows have
-// equal sums whichever blocks they fell to.  A lower bound on the slice's n_out-th best entry comes from the maxima of groups of threads (there are at least
-// n_out groups); the entries above it, a few dozen as a rule, go to shared memory and are ranked there by counting.  Where more of them tie or the
-// bound is poor, the n_out-th key is found by bisection.  Nothing depends on the order of arrival.
+// order.  A block goes through a segment in rounds of 64 bytes per thread, the next round's loads in flight.  Sums are kept by segment and added up in
+// their order, so that equal rows have equal sums whichever blocks they fell to.  A lower bound on the segment's n_out-th best entry comes from the
+// maxima of groups of threads (there are at least n_out groups); the entries above it, a few dozen as a rule, go to shared memory and are ranked
+// there by counting at the segment's end.  Where too many tie or the bound is poor, a round's n_out-th key is found by bisection.  The first block
+// ranks what all of them have left.  Nothing depends on the order of arrival.
 //
 // Reordering.  The lowest new beam of each continued one keeps its slot; the others get the slots of beams that nobody continues, and only these are copied: sources
 // stay as they are and every destination is a slot that nobody reads, so nothing has to wait for anything and there is no second buffer.
@@ -24,12 +25,11 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int NT = 512, NW = NT / 32;
-constexpr int EPT = 32;              // entries of a slice per thread
-constexpr int SLICE = NT * EPT;
-constexpr int CAP = 512;             // entries above the bound that are ranked at once
+constexpr int WORDS = 16;            // 32-bit words of a row that a thread holds at a time
+constexpr int CAP = 512;             // entries above the bound that are collected before they are ranked
 constexpr int MAXW = kBeamMaxWidth, MAXN = kBeamMaxOut;  // beams per request, continuations wanted
-constexpr int MAXS = 16, MAXCL = 8;  // segments of a row, thread blocks of a request
-constexpr float kNone = -__builtin_huge_valf();
+constexpr int MAXS = 16;             // segments of a row
+constexpr float kNone = -__builtin_huge_valf(), kLog2e = 1.44269504f;
 
 // 32 bits that order like the value
 __device__ __forceinline__ uint32_t order32(float x) {
@@ -42,328 +42,417 @@ __device__ __forceinline__ uint64_t order64(double x) {
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 __device__ __forceinline__ double value64(uint64_t o) { return __longlong_as_double(static_cast<long long>(o >> 63 ? o & 0x7FFFFFFFFFFFFFFFull : ~o)); }
-// larger logit first, then lower token
+// larger logit first, then lower token; 0 is below every key
 __device__ __forceinline__ uint64_t key_of(float x, int token) { return static_cast<uint64_t>(order32(x)) << 32 | (0xFFFFFFFFu - static_cast<uint32_t>(token)); }
 __device__ __forceinline__ int token_of(uint64_t key) { return static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(key)); }
+__device__ __forceinline__ float logit_of(uint64_t key) { return value32(static_cast<uint32_t>(key >> 32)); }
 
-__device__ __forceinline__ float clean(float x) { return fabsf(x) < __int_as_float(0x7f800000) ? x : kNone; }
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < __int_as_float(0x7f800000); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float warp_min(float x) {
+  float y;
+  asm("redux.sync.min.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
 
-struct Pick {
-  uint64_t total;  // order64 of s; 0: none
+struct Entry {
+  uint64_t total;  // order64 of s
   uint64_t key;
   int beam, pad;
 };
+__device__ __forceinline__ bool ahead(const Entry &a, const Entry &b) {
+  return a.total != b.total ? a.total > b.total : a.beam != b.beam ? a.beam < b.beam : a.key > b.key;
+}
 
 struct SelectSmem {
   uint64_t cand[CAP + MAXN];
-  uint64_t list[MAXW][MAXN];  // this block's best of each beam, best first
-  int count[MAXW];
   float top[MAXW * MAXS];     // of each segment (those of this block): the largest logit, and the sum of exponentials relative to it
   double sum[MAXW * MAXS];
   float group_max[NW * 4], warp_sum[NW];
-  int n_cand, n_above;
+  int n_cand, n_above, n_entries;
   float score[MAXW];
-  int ended[MAXW];
+  int ended[MAXW], count[MAXW];
   double lse[MAXW];
-  Pick pick[MAXN];            // this block's best over its beams
-  int n_pick;
-  Pick all[MAXCL * MAXN];     // first block: every block's
-  int n_all[MAXCL];
 };
+// behind it: uint64_t list[beams per block][n_out], best first; then a round's words where they are searched for the n_out-th key, and at the end
+// in the first block Entry entry[lists of all blocks][n_out]
 
-// The best entry over the lanes: largest total; among equal ones the lower beam, the larger key.  Lanes without one have total 0.
-__device__ __forceinline__ int best_lane(uint64_t total, int beam, uint64_t key) {
-  const uint32_t hi = static_cast<uint32_t>(total >> 32), lo = static_cast<uint32_t>(total);
-  uint32_t m = __ballot_sync(0xffffffffu, hi == __reduce_max_sync(0xffffffffu, hi));
-  auto narrow = [&](uint32_t x) {  // of the lanes in m, those with the largest x
-    const uint32_t in = m >> (threadIdx.x & 31) & 1u;
-    const uint32_t best = __reduce_max_sync(0xffffffffu, in ? x : 0u);
-    m = __ballot_sync(0xffffffffu, in && x == best);
-  };
-  if (m & (m - 1)) narrow(lo);
-  if (m & (m - 1)) narrow(MAXW - static_cast<uint32_t>(beam));
-  if (m & (m - 1)) narrow(static_cast<uint32_t>(key >> 32));
-  if (m & (m - 1)) narrow(static_cast<uint32_t>(key));
-  return __ffs(m) - 1;
-}
-
-// entries of a row, four or eight per load where rows are aligned
+// A thread's part of a round: where entries of a row are, and how they come from memory
 template <typename T, bool VEC>
-struct Slice {
-  static constexpr int VW = VEC ? 16 / static_cast<int>(sizeof(T)) : 1, LOADS = EPT / VW;
+struct Round {
+  static constexpr bool PACKED = VEC && sizeof(T) == 2;
+  static constexpr int EPT = PACKED ? 2 * WORDS : WORDS, SIZE = NT * EPT;  // entries per thread, and per block
+  static constexpr int VW = VEC ? 16 / static_cast<int>(sizeof(T)) : 1;     // entries per load
   static __device__ __forceinline__ int index(int e) { return (e / VW * NT + static_cast<int>(threadIdx.x)) * VW + e % VW; }
-  // entries `from` .. `from + len - 1` of the row; kNone behind them and where there is no finite number
-  static __device__ __forceinline__ void load(const T *row, int from, int len, float (&x)[EPT]) {
+  static __device__ __forceinline__ uint32_t bits(T x) {
+    if constexpr (sizeof(T) == 2)
+      return static_cast<uint32_t>(__bfloat16_as_ushort(x)) << 16;
+    else
+      return __float_as_uint(x);
+  }
+  // the `len` entries from `row` on (no more than SIZE of them); -infinity behind them
+  static __device__ __forceinline__ void load(const T *row, int len, uint32_t (&w)[WORDS]) {
+    constexpr uint32_t kPad = PACKED ? 0xFF80FF80u : 0xFF800000u;
 #pragma unroll
-    for (int l = 0; l < LOADS; ++l) {
+    for (int l = 0; l < EPT / VW; ++l) {
       const int i = (l * NT + static_cast<int>(threadIdx.x)) * VW;
       if constexpr (!VEC) {
-        float y = kNone;
-        if (i < len) {
-          if constexpr (sizeof(T) == 2)
-            y = __bfloat162float(row[from + i]);
-          else
-            y = row[from + i];
-        }
-        x[l] = y;
+        w[l] = i < len ? bits(row[i]) : kPad;
       } else if (i + VW <= len) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(row + from + i);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if constexpr (sizeof(T) == 2) {
-            x[l * VW + 2 * j] = __uint_as_float(w[j] << 16);
-            x[l * VW + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-          } else {
-            x[l * VW + j] = __uint_as_float(w[j]);
-          }
-        }
+        const uint4 v = *reinterpret_cast<const uint4 *>(row + i);
+        w[4 * l] = v.x, w[4 * l + 1] = v.y, w[4 * l + 2] = v.z, w[4 * l + 3] = v.w;
       } else {
 #pragma unroll
-        for (int j = 0; j < VW; ++j) {
-          float y = kNone;
-          if (i + j < len) {
-            if constexpr (sizeof(T) == 2)
-              y = __bfloat162float(row[from + i + j]);
-            else
-              y = row[from + i + j];
+        for (int j = 0; j < 4; ++j) {
+          w[4 * l + j] = kPad;
+          if constexpr (PACKED) {
+            if (i + 2 * j < len) w[4 * l + j] = 0xFF800000u | bits(row[i + 2 * j]) >> 16;
+            if (i + 2 * j + 1 < len) w[4 * l + j] = (w[4 * l + j] & 0xFFFFu) | bits(row[i + 2 * j + 1]);
+          } else {
+            if (i + j < len) w[4 * l + j] = bits(row[i + j]);
           }
-          x[l * VW + j] = y;
         }
       }
     }
+  }
+  static __device__ __forceinline__ float get(const uint32_t (&w)[WORDS], int e) {
+    if constexpr (PACKED)
+      return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+    else
+      return __uint_as_float(w[e]);
+  }
+  static __device__ __forceinline__ float max(const uint32_t (&w)[WORDS]) {
+    if constexpr (PACKED) {
+      uint32_t m = w[0];
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) x[e] = clean(x[e]);
+      for (int i = 1; i < WORDS; ++i) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i]));
+      return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+    } else {
+      float m = __uint_as_float(w[0]);
+#pragma unroll
+      for (int i = 1; i < WORDS; ++i) m = fmaxf(m, __uint_as_float(w[i]));
+      return m;
+    }
+  }
+  // what is not a finite number becomes -infinity
+  static __device__ __forceinline__ void clean(uint32_t (&w)[WORDS]) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      if constexpr (PACKED) {
+        const float lo = get(w, 2 * i), hi = get(w, 2 * i + 1);
+        w[i] = __byte_perm(__float_as_uint(finite(lo) ? lo : kNone), __float_as_uint(finite(hi) ? hi : kNone), 0x7632);
+      } else {
+        w[i] = finite(get(w, i)) ? w[i] : 0xFF800000u;
+      }
+    }
+  }
+  // sum of e^(x - ref); differences first, since a product with log2 e ahead of them would be off by the same amount in all of a row's terms
+  static __device__ __forceinline__ float sum(const uint32_t (&w)[WORDS], float ref) {
+    const uint64_t r = dpack2(ref, ref), l = dpack2(kLog2e, kLog2e);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < EPT; e += 2) {
+      const float2 y = dunpack2(dmul2(dsub2(dpack2(get(w, e), get(w, e + 1)), r), l));
+      s[e % 4] += ex2(y.x);
+      s[e % 4 + 1] += ex2(y.y);
+    }
+    return (s[0] + s[1]) + (s[2] + s[3]);
   }
 };
 
+// A round with too many entries above the bound: the N largest keys above `floor` of its words (which each thread has left in shared memory) are
+// collected behind the `held` ones from before (at most CAP / 2); returns how many there are now.  Called by the whole block.
+template <typename Rd>
+__device__ __noinline__ int collect_best(SelectSmem &sm, const uint32_t *words, float bound, float top, int from, uint64_t floor, int held, int N) {
+  const int tid = threadIdx.x;
+  auto value = [&](int e) {
+    if constexpr (Rd::PACKED) {
+      const uint32_t x = words[e / 2 * NT + tid];
+      return __uint_as_float(e & 1 ? x & 0xFFFF0000u : x << 16);
+    } else {
+      return __uint_as_float(words[e * NT + tid]);
+    }
+  };
+  auto at_least = [&](uint64_t t) {  // how many keys there are from t on
+    int c = 0;
+#pragma unroll 4
+    for (int e = 0; e < Rd::EPT; ++e) {
+      const float x = value(e);
+      if (x >= bound && x > kNone) {
+        const uint64_t key = key_of(x, from + Rd::index(e));
+        c += key >= t && key > floor;
+      }
+    }
+    c = __reduce_add_sync(0xffffffffu, c);
+    __syncthreads();
+    if (tid == 0) sm.n_above = 0;
+    __syncthreads();
+    if (tid % 32 == 0 && c) atomicAdd(&sm.n_above, c);
+    __syncthreads();
+    return sm.n_above;
+  };
+  // Keys lie between these two, so that the bits they share need not be found; where fewer than N are above the bound, which many share
+  // (a row of one value, a mask of the lowest one), only the places of those that tie.
+  uint64_t low = key_of(bound, from + Rd::SIZE - 1), high = key_of(top, from);
+  if (bound < top) {
+    if (at_least(key_of(bound, 0) + 1) < N)
+      high = key_of(bound, from);
+  }
+  const int bits = low == high ? 0 : 64 - __clzll(static_cast<long long>(low ^ high));
+  uint64_t t = bits == 64 ? 0 : high >> bits << bits;
+  for (int bit = bits - 1; bit >= 0; --bit) {
+    const uint64_t trial = t | 1ull << bit;
+    if (at_least(trial) >= N) t = trial;
+  }
+  __syncthreads();
+  if (tid == 0) sm.n_cand = held;
+  __syncthreads();
+  for (int e = 0; e < Rd::EPT; ++e) {
+    const float x = value(e);
+    if (x >= bound && x > kNone) {
+      const uint64_t key = key_of(x, from + Rd::index(e));
+      if (key >= t && key > floor) {
+        const int at = atomicAdd(&sm.n_cand, 1);
+        if (at < CAP) sm.cand[at] = key;
+      }
+    }
+  }
+  __syncthreads();
+  return sm.n_cand;
+}
+
 template <typename T, bool VEC, int CL>
-__global__ void __launch_bounds__(NT) beam_select_kernel(const __grid_constant__ DascBeamSelectArgs a) {
-  using Sl = Slice<T, VEC>;
-  __shared__ SelectSmem sm;
+__global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constant__ DascBeamSelectArgs a) {
+  using Rd = Round<T, VEC>;
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  SelectSmem &sm = *reinterpret_cast<SelectSmem *>(smem_raw);
+  uint64_t *const list = reinterpret_cast<uint64_t *>(smem_raw + sizeof(SelectSmem));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r = blockIdx.x / CL, rank = blockIdx.x % CL;
   const int W = a.width, N = a.n_out;
   stream_order_begin();
 
   if (tid < W) {
-    sm.score[tid] = a.scores[static_cast<int64_t>(r) * W + tid];
-    sm.ended[tid] = a.ended ? a.ended[static_cast<int64_t>(r) * W + tid] != 0 : 0;
+    const float score = a.scores[static_cast<int64_t>(r) * W + tid];
+    sm.score[tid] = score;
+    // 0: its row counts, 1: it has ended, 2: it has no continuation
+    sm.ended[tid] = !finite(score) ? 2 : a.ended && a.ended[static_cast<int64_t>(r) * W + tid] != 0 ? 1 : 0;
     sm.count[tid] = 0;
   }
+  if (tid == 0) sm.n_cand = sm.n_entries = 0;
   __syncthreads();
 
   const int groups = N <= NW ? 1 : N <= 2 * NW ? 2 : 4;  // per warp
-  const int first = rank * a.per_block, last = min(first + a.per_block, W * a.segments);
-  for (int step = 0; step < (last - first) * a.seg_slices; ++step) {
-    const int item = first + step / a.seg_slices, b = item / a.segments;
-    const bool opens = step % a.seg_slices == 0;
-    const float seg_top = opens ? kNone : sm.top[item];
-    const int from = (item % a.segments * a.seg_slices + step % a.seg_slices) * a.slice_len, len = min(a.slice_len, a.vocab - from);
-    if (len <= 0 || sm.ended[b] || !(fabsf(sm.score[b]) < __int_as_float(0x7f800000))) continue;  // (the same for the whole block)
-    float x[EPT];
-    Sl::load(static_cast<const T *>(a.logits) + (static_cast<int64_t>(r) * W + b) * a.stride, from, len, x);
-    float m = x[0];
+  const int first = min(rank * a.per_block, W * a.segments), last = min(first + a.per_block, W * a.segments), first_beam = first / a.segments;
+  const T *const rows = static_cast<const T *>(a.logits) + static_cast<int64_t>(r) * W * a.stride;
+  // (segment, round) one behind the other; rows that do not count are passed over
+  auto segment_len = [&](int item) { return min(a.segment_len, a.vocab - item % a.segments * a.segment_len); };
+  auto skip = [&](int item) {
+    while (item < last && sm.ended[item / a.segments]) ++item;
+    return item;
+  };
+  auto load = [&](int item, int base, uint32_t(&w)[WORDS]) {
+    if (item < last)
+      Rd::load(rows + item / a.segments * a.stride + item % a.segments * a.segment_len + base, min(segment_len(item) - base, Rd::SIZE), w);
+  };
+  int item = skip(first), base = 0;
+  uint32_t w[WORDS], ahead_w[WORDS];
+  load(item, base, ahead_w);
+  int held = 0;              // entries collected up to now
+  float m = kNone, s = 0.f;  // this thread's largest logit of the segment, and sum of exponentials relative to it
+  while (item < last) {
 #pragma unroll
-    for (int e = 1; e < EPT; ++e) m = fmaxf(m, x[e]);
-    float g = m;
-    for (int d = 1; d < 32 / groups; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
-    if (lane % (32 / groups) == 0) sm.group_max[warp * groups + lane / (32 / groups)] = g;
-    if (tid == 0) sm.n_cand = 0;
+    for (int i = 0; i < WORDS; ++i) w[i] = ahead_w[i];
+    const int b = item / a.segments, from = item % a.segments * a.segment_len + base;
+    const bool ends = base + Rd::SIZE >= segment_len(item);
+    const int next_item = ends ? skip(item + 1) : item, next_base = ends ? 0 : base + Rd::SIZE;
+    load(next_item, next_base, ahead_w);
+
+    float mr = Rd::max(w), mn = fmaxf(m, mr), ref = mn == kNone ? 0.f : mn, part = Rd::sum(w, ref);
+    // A NaN, or an infinity.  Looked at as bits: a sum of ex2 is taken to be at least 0 by the assembler, and `!(part >= 0)` for never true.
+    if (__float_as_uint(part) >= 0x7F800000u) {
+      Rd::clean(w);
+      mr = Rd::max(w), mn = fmaxf(m, mr), ref = mn == kNone ? 0.f : mn, part = Rd::sum(w, ref);
+    }
+    s = fmaf(s, ex2((m - ref) * kLog2e), part);
+    m = mn;
+    if (groups == 1) {
+      const float g = warp_max(m);
+      if (lane == 0) sm.group_max[warp] = g;
+    } else {
+      float g = m;
+      for (int d = 1; d < 32 / groups; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
+      if (lane % (32 / groups) == 0) sm.group_max[warp * groups + lane / (32 / groups)] = g;
+    }
     __syncthreads();
-    float top = kNone, bound = -kNone;
-    for (int i = lane; i < NW * groups; i += 32) {
-      top = fmaxf(top, sm.group_max[i]);
-      bound = fminf(bound, sm.group_max[i]);
+    // N groups of threads each have an entry of this segment at least as large as `bound`
+    float low = sm.group_max[lane % (NW * groups)], high = low;
+    if (groups == 4) {
+      low = fminf(low, sm.group_max[32 + lane]);
+      high = fmaxf(high, sm.group_max[32 + lane]);
     }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-      bound = fminf(bound, __shfl_xor_sync(0xffffffffu, bound, d));
-    }
+    const float bound = warp_min(low), top = warp_max(high);
+    uint64_t *const best = list + (b - first_beam) * N;
     const int have = sm.count[b];
-    if (have == N) bound = fmaxf(bound, value32(static_cast<uint32_t>(sm.list[b][N - 1] >> 32) + 1));  // (slices come in order: equal ones lose)
-    if (top > kNone) {
-      // sum of exponentials relative to the segment's largest logit so far
-      const float ref = fmaxf(top, seg_top);
-      float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+    const uint64_t floor = have == N ? best[N - 1] : 0;
+    if (mr >= bound && mr > kNone) {
 #pragma unroll
-      for (int e = 0; e < EPT; e += 4) {
-        s0 += exp2f((x[e] - ref) * 1.44269504f);
-        s1 += exp2f((x[e + 1] - ref) * 1.44269504f);
-        s2 += exp2f((x[e + 2] - ref) * 1.44269504f);
-        s3 += exp2f((x[e + 3] - ref) * 1.44269504f);
-      }
-      float s = (s0 + s1) + (s2 + s3);
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-      if (lane == 0) sm.warp_sum[warp] = s;
-      if (m >= bound) {
-#pragma unroll
-        for (int e = 0; e < EPT; ++e)
-          if (x[e] >= bound && x[e] > kNone) {
+      for (int e = 0; e < Rd::EPT; ++e) {
+        const float x = Rd::get(w, e);
+        if (x >= bound && x > kNone) {
+          const uint64_t key = key_of(x, from + Rd::index(e));
+          if (key > floor) {
             const int at = atomicAdd(&sm.n_cand, 1);
-            if (at < CAP) sm.cand[at] = key_of(x[e], from + Sl::index(e));
+            if (at < CAP) sm.cand[at] = key;
           }
+        }
       }
+    }
+    if (ends) {
+      float x = s * ex2((m - (top == kNone ? 0.f : top)) * kLog2e);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+      if (lane == 0) sm.warp_sum[warp] = x;
+      m = kNone;
+      s = 0.f;
     }
     __syncthreads();
-    if (!(top > kNone)) {  // (the same for the whole block: no logit of this slice counts)
-      if (opens && tid == 0) sm.top[item] = kNone;
-      __syncthreads();
-      continue;
-    }
     int n = sm.n_cand;
     if (n > CAP) {
-      // The N-th largest key, bit by bit from the top.
-      uint64_t t = 0;
-      for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t trial = t | 1ull << bit;
-        int c = 0;
+      uint32_t *const words = reinterpret_cast<uint32_t *>(list + a.block_beams * N);
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) c += x[e] > kNone && key_of(x[e], from + Sl::index(e)) >= trial;
-        c = __reduce_add_sync(0xffffffffu, c);
-        __syncthreads();
-        if (tid == 0) sm.n_above = 0;
-        __syncthreads();
-        if (lane == 0 && c) atomicAdd(&sm.n_above, c);
-        __syncthreads();
-        if (sm.n_above >= N) t = trial;
+      for (int i = 0; i < WORDS; ++i) words[i * NT + tid] = w[i];
+      n = collect_best<Rd>(sm, words, bound, top, from, floor, held, N);
+    }
+    if (ends && warp == 0) {
+      double x = lane < NW ? sm.warp_sum[lane] : 0.0;
+#pragma unroll
+      for (int d = NW / 2; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+      if (lane == 0) {
+        sm.top[item] = top;
+        sm.sum[item] = x;
       }
-      if (tid == 0) sm.n_cand = 0;
+    }
+    if (ends || n > CAP / 2) {
+      // what has been collected joins the beam's list; eight lanes count how many are ahead of each
+      for (int i = tid; i < have; i += NT) sm.cand[n + i] = best[i];
       __syncthreads();
+      const int total = n + have;
+      for (int i0 = 0; i0 < total; i0 += NT / 8) {
+        const int i = i0 + tid / 8;
+        const uint64_t k = i < total ? sm.cand[i] : 0;
+        int place = 0;
+        for (int j = tid % 8; j < total; j += 8) place += sm.cand[j] > k;
 #pragma unroll
-      for (int e = 0; e < EPT; ++e)
-        if (x[e] > kNone && key_of(x[e], from + Sl::index(e)) >= t) {
-          const int at = atomicAdd(&sm.n_cand, 1);
-          if (at < CAP) sm.cand[at] = key_of(x[e], from + Sl::index(e));
-        }
+        for (int d = 4; d > 0; d >>= 1) place += __shfl_xor_sync(0xffffffffu, place, d);
+        if (i < total && tid % 8 == 0 && place < N) best[place] = k;
+      }
+      if (tid == 0) {
+        sm.count[b] = min(total, N);
+        sm.n_cand = 0;
+      }
       __syncthreads();
-      n = min(sm.n_cand, CAP);
+      n = 0;
     }
-    if (tid < have) sm.cand[n + tid] = sm.list[b][tid];
-    if (tid == 0) {
-      const float ref = fmaxf(top, seg_top);
-      double s = 0.0;
-      for (int i = 0; i < NW; ++i) s += sm.warp_sum[i];
-      sm.sum[item] = seg_top > kNone ? sm.sum[item] * exp(static_cast<double>(seg_top) - ref) + s : s;
-    }
-    __syncthreads();
-    const int total = n + have;
-    for (int i = tid; i < total; i += NT) {
-      const uint64_t k = sm.cand[i];
-      int place = 0;
-      for (int j = 0; j < total; ++j) place += sm.cand[j] > k;
-      if (place < N) sm.list[b][place] = k;
-    }
-    if (tid == 0) {
-      sm.count[b] = min(total, N);
-      sm.top[item] = fmaxf(top, seg_top);
-    }
-    __syncthreads();
+    held = n;
+    item = next_item;
+    base = next_base;
   }
 
-  // every row's sum, from all blocks
+  // The first block takes the lists and sums of all of them.
   cg::cluster_group cluster = cg::this_cluster();
   cluster.sync();
-  if (tid < W) {
-    float top = kNone;
-    double s = 0.0;
-    if (!sm.ended[tid] && fabsf(sm.score[tid]) < __int_as_float(0x7f800000)) {
+  Entry *const entry = reinterpret_cast<Entry *>(list + a.block_beams * N);
+  if (rank == 0) {
+    if (tid < W && sm.ended[tid] == 0) {
+      float top = kNone;
       for (int i = tid * a.segments; i < (tid + 1) * a.segments; ++i) top = fmaxf(top, cluster.map_shared_rank(sm.top, i / a.per_block)[i]);
+      double x = 0.0;
       if (top > kNone)
         for (int i = tid * a.segments; i < (tid + 1) * a.segments; ++i) {
           const float t = cluster.map_shared_rank(sm.top, i / a.per_block)[i];
-          if (t > kNone) s += cluster.map_shared_rank(sm.sum, i / a.per_block)[i] * exp(static_cast<double>(t) - top);
+          if (t > kNone) x += cluster.map_shared_rank(sm.sum, i / a.per_block)[i] * exp(static_cast<double>(t) - top);
         }
+      sm.lse[tid] = static_cast<double>(top) + log(x);
     }
-    sm.lse[tid] = static_cast<double>(top) + log(s);
-  }
-  __syncthreads();
-  // this block's best: lane b holds the best of beam b that is left
-  if (warp == 0) {
-    int at = 0, n = 0;
-    uint64_t key = 0, total = 0;
-    const bool mine = lane < W;
-    const bool over = mine && sm.ended[lane];
-    const bool counts = mine && fabsf(sm.score[lane]) < __int_as_float(0x7f800000);
-    auto head = [&]() {
-      total = key = 0;
-      if (!counts) return;
-      if (over) {
-        if (rank == 0 && at == 0) {
-          total = order64(sm.score[lane]);
-          key = key_of(0.f, a.end_token);
-        }
-      } else if (at < sm.count[lane]) {
-        key = sm.list[lane][at];
-        total = order64(static_cast<double>(sm.score[lane]) + (static_cast<double>(value32(static_cast<uint32_t>(key >> 32))) - sm.lse[lane]));
-      }
-    };
-    head();
-    for (; n < N; ++n) {
-      const int l = best_lane(total, lane, key);
-      if (__shfl_sync(0xffffffffu, total, l) == 0) break;
-      if (lane == l) {
-        sm.pick[n].total = total;
-        sm.pick[n].key = key;
-        sm.pick[n].beam = lane;
-        ++at;
-        head();
-      }
-    }
-    if (lane == 0) sm.n_pick = n;
-  }
-  cluster.sync();
-  if (rank == 0) {
-    if (tid < CL) sm.n_all[tid] = *cluster.map_shared_rank(&sm.n_pick, tid);
     __syncthreads();
-    for (int i = tid; i < CL * N; i += NT) {
-      const int c = i / N, j = i % N;
-      if (j < sm.n_all[c]) sm.all[i] = cluster.map_shared_rank(sm.pick, c)[j];
+    for (int i = tid; i < CL * a.block_beams * N; i += NT) {
+      const int c = i / (a.block_beams * N), j = i % (a.block_beams * N), its_first = c * a.per_block / a.segments, b = its_first + j / N;
+      if (c * a.per_block < W * a.segments && b * a.segments < min((c + 1) * a.per_block, W * a.segments) && j % N < cluster.map_shared_rank(sm.count, c)[b]) {
+        Entry e;
+        e.key = cluster.map_shared_rank(list, c)[j];
+        e.total = order64(static_cast<double>(sm.score[b]) + (static_cast<double>(logit_of(e.key)) - sm.lse[b]));
+        e.beam = b;
+        entry[atomicAdd(&sm.n_entries, 1)] = e;
+      }
+    }
+    if (tid < W && sm.ended[tid] == 1) {
+      Entry e;
+      e.key = key_of(0.f, a.end_token);
+      e.total = order64(sm.score[tid]);
+      e.beam = tid;
+      entry[atomicAdd(&sm.n_entries, 1)] = e;
     }
   }
   cluster.sync();  // (no block ends while the first one still reads it)
-  if (rank == 0 && warp == 0) {
-    int at = 0;
-    Pick p{};
-    auto head = [&]() {
-      p.total = 0;
-      p.beam = 0;
-      if (lane < CL && at < sm.n_all[lane % MAXCL]) p = sm.all[lane * N + at];
-    };
-    head();
-    const int64_t out = static_cast<int64_t>(r) * N;
-    for (int n = 0; n < N; ++n) {
-      const int l = best_lane(p.total, p.beam, p.key);
-      const bool none = __shfl_sync(0xffffffffu, p.total, l) == 0;
-      if (lane == l) {
-        const int token = none ? -1 : token_of(p.key);
-        a.out_scores[out + n] = none ? kNone : static_cast<float>(value64(p.total));
-        a.out_parent[out + n] = none ? -1 : p.beam;
-        a.out_token[out + n] = token;
-        if (a.out_ended) a.out_ended[out + n] = none || sm.ended[p.beam] || token == a.end_token;
-        if (!none) {
-          ++at;
-          head();
-        }
-      }
+  if (rank != 0) return;
+  const int total = sm.n_entries;
+  const int64_t out = static_cast<int64_t>(r) * N;
+  for (int i0 = 0; i0 < total; i0 += NT / 8) {
+    const int i = i0 + tid / 8;
+    const Entry e = entry[min(i, total - 1)];
+    int place = 0;
+    for (int j = tid % 8; j < total; j += 8) place += ahead(entry[j], e);
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) place += __shfl_xor_sync(0xffffffffu, place, d);
+    if (i < total && tid % 8 == 0 && place < N) {
+      const int token = token_of(e.key);
+      a.out_scores[out + place] = static_cast<float>(value64(e.total));
+      a.out_parent[out + place] = e.beam;
+      a.out_token[out + place] = token;
+      if (a.out_ended) a.out_ended[out + place] = sm.ended[e.beam] == 1 || token == a.end_token;
     }
+  }
+  for (int i = total + tid; i < N; i += NT) {
+    a.out_scores[out + i] = kNone;
+    a.out_parent[out + i] = a.out_token[out + i] = -1;
+    if (a.out_ended) a.out_ended[out + i] = 1;
   }
 }
 
 template <typename T, bool VEC, int CL>
 int select(DascBeamSelectArgs a, void *stream) {
-  // segments of a row: as many as fill whole rounds of the cluster's blocks
-  const int need = (a.vocab + SLICE - 1) / SLICE;
-  a.seg_slices = (need + MAXS - 1) / MAXS;
-  const int least = (need + a.seg_slices - 1) / a.seg_slices, rounds = (a.width * least + CL - 1) / CL;
-  a.segments = std::min(MAXS, std::max(least, rounds * CL / a.width));
-  const int slices = a.segments * a.seg_slices;
-  a.slice_len = ((a.vocab + slices - 1) / slices + 7) / 8 * 8;
-  a.segments = (a.vocab + a.slice_len * a.seg_slices - 1) / (a.slice_len * a.seg_slices);
+  // Segments of a row, the same for all rows: whole rounds as far as possible.  A segment's end costs its block about as much as another round.
+  using Rd = Round<T, VEC>;
+  int64_t least = INT64_MAX;
+  for (int n = 1; n <= MAXS; ++n) {
+    const int64_t len = ((a.vocab + n - 1) / n + 7) / 8 * 8, cost = (static_cast<int64_t>(a.width) * n + CL - 1) / CL * ((len + Rd::SIZE - 1) / Rd::SIZE + 1);
+    if (cost < least) {
+      least = cost;
+      a.segment_len = static_cast<int32_t>(len);
+    }
+  }
+  a.segments = (a.vocab + a.segment_len - 1) / a.segment_len;
   a.per_block = (a.width * a.segments + CL - 1) / CL;
-  return static_cast<int>(launch_clusters(beam_select_kernel<T, VEC, CL>, dim3(static_cast<unsigned>(a.n_req) * CL), dim3(NT), CL, 0, stream, a));
+  a.block_beams = std::min(a.width, (a.per_block + a.segments - 2) / a.segments + 1);
+  // lists of this block's beams; entries of all lists and of the beams that have ended (a beam that is in several blocks has not)
+  const size_t smem = sizeof(SelectSmem) + static_cast<size_t>(a.block_beams) * sizeof(uint64_t) * a.n_out +
+                      std::max(static_cast<size_t>(a.width + CL) * sizeof(Entry) * a.n_out, NT * WORDS * sizeof(uint32_t));
+  auto kernel = beam_select_kernel<T, VEC, CL>;
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return static_cast<int>(e);
+  }
+  return static_cast<int>(launch_clusters(kernel, dim3(static_cast<unsigned>(a.n_req) * CL), dim3(NT), CL, smem, stream, a));
 }
 
 template <typename T>
