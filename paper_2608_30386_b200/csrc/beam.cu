@@ -29,7 +29,10 @@ constexpr int WORDS = 16;            // 32-bit words of a row that a thread hold
 constexpr int CAP = 512;             // entries above the bound that are collected before they are ranked
 constexpr int MAXW = kBeamMaxWidth, MAXN = kBeamMaxOut;  // beams per request, continuations wanted
 constexpr int MAXS = 16;             // segments of a row
+constexpr int GROUPS = 64;           // of NT / 64 threads, whose maxima bound the n_out-th best entry; at least MAXN
 constexpr float kNone = -__builtin_huge_valf(), kLog2e = 1.44269504f;
+template <typename T>
+constexpr float kLowest = sizeof(T) == 2 ? -3.38953139e38f : -3.40282347e38f;  // the type's lowest finite value
 
 // 32 bits that order like the value
 __device__ __forceinline__ uint32_t order32(float x) {
@@ -53,17 +56,16 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ uint64_t dadd2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ __forceinline__ float warp_max(float x) {
   float y;
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float warp_min(float x) {
-  float y;
-  asm("redux.sync.min.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 struct Entry {
   uint64_t total;  // order64 of s
   uint64_t key;
@@ -77,7 +79,7 @@ struct SelectSmem {
   uint64_t cand[CAP + MAXN];
   float top[MAXW * MAXS];     // of each segment (those of this block): the largest logit, and the sum of exponentials relative to it
   double sum[MAXW * MAXS];
-  float group_max[NW * 4], warp_sum[NW];
+  float group_max[GROUPS], bound, warp_top[NW], warp_sum[NW];
   int n_cand, n_above, n_entries;
   float score[MAXW];
   int ended[MAXW], count[MAXW];
@@ -99,26 +101,39 @@ struct Round {
     else
       return __float_as_uint(x);
   }
-  // the `len` entries from `row` on (no more than SIZE of them); -infinity behind them
+  // the first `len` entries from `row` on, at most SIZE; -infinity behind them
   static __device__ __forceinline__ void load(const T *row, int len, uint32_t (&w)[WORDS]) {
     constexpr uint32_t kPad = PACKED ? 0xFF80FF80u : 0xFF800000u;
+    const T *const mine = row + static_cast<int>(threadIdx.x) * VW;
+    if (len >= SIZE) {
+#pragma unroll
+      for (int l = 0; l < EPT / VW; ++l) {
+        if constexpr (VEC) {
+          const uint4 v = *reinterpret_cast<const uint4 *>(mine + l * NT * VW);
+          w[4 * l] = v.x, w[4 * l + 1] = v.y, w[4 * l + 2] = v.z, w[4 * l + 3] = v.w;
+        } else {
+          w[l] = bits(mine[l * NT]);
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int l = 0; l < EPT / VW; ++l) {
-      const int i = (l * NT + static_cast<int>(threadIdx.x)) * VW;
+      const int left = len - (l * NT + static_cast<int>(threadIdx.x)) * VW;
       if constexpr (!VEC) {
-        w[l] = i < len ? bits(row[i]) : kPad;
-      } else if (i + VW <= len) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(row + i);
+        w[l] = left > 0 ? bits(mine[l * NT]) : kPad;
+      } else if (left >= VW) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(mine + l * NT * VW);
         w[4 * l] = v.x, w[4 * l + 1] = v.y, w[4 * l + 2] = v.z, w[4 * l + 3] = v.w;
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           w[4 * l + j] = kPad;
           if constexpr (PACKED) {
-            if (i + 2 * j < len) w[4 * l + j] = 0xFF800000u | bits(row[i + 2 * j]) >> 16;
-            if (i + 2 * j + 1 < len) w[4 * l + j] = (w[4 * l + j] & 0xFFFFu) | bits(row[i + 2 * j + 1]);
+            if (2 * j < left) w[4 * l + j] = 0xFF800000u | bits(mine[l * NT * VW + 2 * j]) >> 16;
+            if (2 * j + 1 < left) w[4 * l + j] = (w[4 * l + j] & 0xFFFFu) | bits(mine[l * NT * VW + 2 * j + 1]);
           } else {
-            if (i + j < len) w[4 * l + j] = bits(row[i + j]);
+            if (j < left) w[4 * l + j] = bits(mine[l * NT * VW + j]);
           }
         }
       }
@@ -158,21 +173,87 @@ struct Round {
   // sum of e^(x - ref); differences first, since a product with log2 e ahead of them would be off by the same amount in all of a row's terms
   static __device__ __forceinline__ float sum(const uint32_t (&w)[WORDS], float ref) {
     const uint64_t r = dpack2(ref, ref), l = dpack2(kLog2e, kLog2e);
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    uint64_t s[2] = {0, 0};
 #pragma unroll
     for (int e = 0; e < EPT; e += 2) {
       const float2 y = dunpack2(dmul2(dsub2(dpack2(get(w, e), get(w, e + 1)), r), l));
-      s[e % 4] += ex2(y.x);
-      s[e % 4 + 1] += ex2(y.y);
+      s[e / 2 % 2] = dadd2(s[e / 2 % 2], dpack2(ex2(y.x), ex2(y.y)));
     }
-    return (s[0] + s[1]) + (s[2] + s[3]);
+    const float2 t = dunpack2(dadd2(s[0], s[1]));
+    return t.x + t.y;
+  }
+  // which entries are at least `bound` (one of the type's values): bit place(e) for entry e
+  static __device__ __forceinline__ uint32_t at_least(const uint32_t (&w)[WORDS], float bound) {
+    uint32_t hits = 0;
+    if constexpr (PACKED) {
+      const uint32_t b = __byte_perm(__float_as_uint(bound), 0, 0x3232);
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        uint32_t yes;
+        asm("set.ge.u32.bf16x2 %0, %1, %2;" : "=r"(yes) : "r"(w[i]), "r"(b));
+        hits |= yes & 0x00010001u << i;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) hits |= __uint_as_float(w[i]) >= bound ? 1u << i : 0u;
+    }
+    return hits;
+  }
+  static __device__ __forceinline__ int entry(int place) { return PACKED ? 2 * (place % WORDS) + place / WORDS : place; }
+  // entry e, which differs from thread to thread
+  static __device__ __forceinline__ float pick(const uint32_t (&w)[WORDS], int e) {
+    uint32_t x = w[0];
+#pragma unroll
+    for (int i = 1; i < WORDS; ++i) x = (PACKED ? e / 2 : e) == i ? w[i] : x;
+    return __uint_as_float(!PACKED || e & 1 ? (PACKED ? x & 0xFFFF0000u : x) : x << 16);
   }
 };
 
-// A round with too many entries above the bound: the N largest keys above `floor` of its words (which each thread has left in shared memory) are
-// collected behind the `held` ones from before (at most CAP / 2); returns how many there are now.  Called by the whole block.
+// The `n` keys that have been collected join the `have` ones of a list, of which the N best stay, best first; eight lanes count how many are
+// ahead of each.  Called by the whole block behind a barrier, and ends with one; returns how many the list has now.
+__device__ __noinline__ int join_list(SelectSmem &sm, uint64_t *best, int n, int have, int N) {
+  const int tid = threadIdx.x, total = n + have;
+  if (tid < have) sm.cand[n + tid] = best[tid];
+  __syncthreads();
+  for (int i0 = 0; i0 < total; i0 += NT / 8) {
+    const int i = i0 + tid / 8;
+    const uint64_t k = i < total ? sm.cand[i] : 0;
+    int place = 0;
+    for (int j = tid % 8; j < total; j += 8) place += sm.cand[j] > k;
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) place += __shfl_xor_sync(0xffffffffu, place, d);
+    if (i < total && tid % 8 == 0 && place < N) best[place] = k;
+  }
+  if (tid == 0) sm.n_cand = 0;
+  __syncthreads();
+  return min(total, N);
+}
+
+// A warp's share of a segment's sum, relative to its own largest logit.
+__device__ __forceinline__ void share_sum(SelectSmem &sm, float m, float s) {
+  const float top = warp_max(m);
+  float x = s * ex2((m - (top == kNone ? 0.f : top)) * kLog2e);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+  if (threadIdx.x % 32 == 0) {
+    sm.warp_top[threadIdx.x / 32] = top;
+    sm.warp_sum[threadIdx.x / 32] = x;
+  }
+}
+// one more round's part of a thread's sum
 template <typename Rd>
-__device__ __noinline__ int collect_best(SelectSmem &sm, const uint32_t *words, float bound, float top, int from, uint64_t floor, int held, int N) {
+__device__ __forceinline__ float add_sum(const uint32_t (&w)[WORDS], float &m, float &s) {
+  const float mr = Rd::max(w), mn = fmaxf(m, mr), ref = mn == kNone ? 0.f : mn;
+  s = fmaf(s, ex2((m - ref) * kLog2e), Rd::sum(w, ref));
+  m = mn;
+  return mr;
+}
+
+// A segment with a NaN or an infinity, or in which more entries were above the bound than there is room for (many that tie, or a poor bound): once more, a round at
+// a time, each with the keys above the N-th best so far, of which at most N are collected.  `words`: a round's words in shared memory.  Called by the
+// whole block behind a barrier; leaves the warps' sums and returns how many the list has.
+template <typename Rd, typename T>
+__device__ __noinline__ int rescan(SelectSmem &sm, uint32_t *words, const T *row, int len, int from, uint64_t *best, int have, int N) {
   const int tid = threadIdx.x;
   auto value = [&](int e) {
     if constexpr (Rd::PACKED) {
@@ -182,52 +263,56 @@ __device__ __noinline__ int collect_best(SelectSmem &sm, const uint32_t *words, 
       return __uint_as_float(words[e * NT + tid]);
     }
   };
-  auto at_least = [&](uint64_t t) {  // how many keys there are from t on
-    int c = 0;
+  float m = kNone, s = 0.f;
+  for (int base = 0; base < len; base += Rd::SIZE) {
+    uint32_t w[WORDS];
+    Rd::load(row + base, len - base, w);
+    Rd::clean(w);
+    add_sum<Rd>(w, m, s);
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) words[i * NT + tid] = w[i];  // (each thread reads its own)
+    const int at = from + base;
+    auto at_least = [&](uint64_t t) {  // how many keys there are from t on
+      int c = 0;
 #pragma unroll 4
+      for (int e = 0; e < Rd::EPT; ++e) {
+        const float x = value(e);
+        c += x > kNone && key_of(x, at + Rd::index(e)) >= t;
+      }
+      c = __reduce_add_sync(0xffffffffu, c);
+      __syncthreads();
+      if (tid == 0) sm.n_above = 0;
+      __syncthreads();
+      if (tid % 32 == 0 && c) atomicAdd(&sm.n_above, c);
+      __syncthreads();
+      return sm.n_above;
+    };
+    uint64_t t = have == N ? best[N - 1] + 1 : 1;
+    int n = at_least(t);
+    if (n == 0) continue;
+    if (n > CAP) {  // the N-th largest key, bit by bit from the top
+      t = 0;
+      for (int bit = 63; bit >= 0; --bit)
+        if (at_least(t | 1ull << bit) >= N) t |= 1ull << bit;
+    }
+    __syncthreads();
+    if (tid == 0) sm.n_cand = 0;
+    __syncthreads();
     for (int e = 0; e < Rd::EPT; ++e) {
       const float x = value(e);
-      if (x >= bound && x > kNone) {
-        const uint64_t key = key_of(x, from + Rd::index(e));
-        c += key >= t && key > floor;
-      }
+      const uint64_t key = key_of(x, at + Rd::index(e));
+      if (x > kNone && key >= t) sm.cand[atomicAdd(&sm.n_cand, 1)] = key;  // (at most CAP of them, or N)
     }
-    c = __reduce_add_sync(0xffffffffu, c);
     __syncthreads();
-    if (tid == 0) sm.n_above = 0;
+    n = sm.n_cand;
     __syncthreads();
-    if (tid % 32 == 0 && c) atomicAdd(&sm.n_above, c);
-    __syncthreads();
-    return sm.n_above;
-  };
-  // Keys lie between these two, so that the bits they share need not be found; where fewer than N are above the bound, which many share
-  // (a row of one value, a mask of the lowest one), only the places of those that tie.
-  uint64_t low = key_of(bound, from + Rd::SIZE - 1), high = key_of(top, from);
-  if (bound < top) {
-    if (at_least(key_of(bound, 0) + 1) < N)
-      high = key_of(bound, from);
+    have = join_list(sm, best, n, have, N);
   }
-  const int bits = low == high ? 0 : 64 - __clzll(static_cast<long long>(low ^ high));
-  uint64_t t = bits == 64 ? 0 : high >> bits << bits;
-  for (int bit = bits - 1; bit >= 0; --bit) {
-    const uint64_t trial = t | 1ull << bit;
-    if (at_least(trial) >= N) t = trial;
-  }
+  share_sum(sm, m, s);
   __syncthreads();
-  if (tid == 0) sm.n_cand = held;
+  if (tid == 0) sm.n_cand = 0;
   __syncthreads();
-  for (int e = 0; e < Rd::EPT; ++e) {
-    const float x = value(e);
-    if (x >= bound && x > kNone) {
-      const uint64_t key = key_of(x, from + Rd::index(e));
-      if (key >= t && key > floor) {
-        const int at = atomicAdd(&sm.n_cand, 1);
-        if (at < CAP) sm.cand[at] = key;
-      }
-    }
-  }
-  __syncthreads();
-  return sm.n_cand;
+  return have;
 }
 
 template <typename T, bool VEC, int CL>
@@ -251,121 +336,119 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
   if (tid == 0) sm.n_cand = sm.n_entries = 0;
   __syncthreads();
 
-  const int groups = N <= NW ? 1 : N <= 2 * NW ? 2 : 4;  // per warp
   const int first = min(rank * a.per_block, W * a.segments), last = min(first + a.per_block, W * a.segments), first_beam = first / a.segments;
-  const T *const rows = static_cast<const T *>(a.logits) + static_cast<int64_t>(r) * W * a.stride;
-  // (segment, round) one behind the other; rows that do not count are passed over
-  auto segment_len = [&](int item) { return min(a.segment_len, a.vocab - item % a.segments * a.segment_len); };
-  auto skip = [&](int item) {
-    while (item < last && sm.ended[item / a.segments]) ++item;
-    return item;
+  // where this block is: a segment of a beam's row, and how many of its entries are left; rows that do not count are passed over
+  struct Place {
+    const T *row;
+    int item, beam, segment, left;
   };
-  auto load = [&](int item, int base, uint32_t(&w)[WORDS]) {
-    if (item < last)
-      Rd::load(rows + item / a.segments * a.stride + item % a.segments * a.segment_len + base, min(segment_len(item) - base, Rd::SIZE), w);
+  auto open = [&](Place &p) {
+    p.left = min(a.segment_len, a.vocab - p.segment * a.segment_len);
+    p.row = static_cast<const T *>(a.logits) + (static_cast<int64_t>(r) * W + p.beam) * a.stride + p.segment * a.segment_len;
   };
-  int item = skip(first), base = 0;
+  auto skip = [&](Place &p) {
+    while (p.item < last && sm.ended[p.beam]) {
+      p.item += a.segments - p.segment;
+      p.segment = 0;
+      ++p.beam;
+    }
+    if (p.item < last) open(p);
+  };
+  auto advance = [&](Place &p) {
+    p.row += Rd::SIZE;
+    p.left -= Rd::SIZE;
+    if (p.left <= 0) {
+      ++p.item;
+      if (++p.segment == a.segments) {
+        p.segment = 0;
+        ++p.beam;
+      }
+      skip(p);
+    }
+  };
+  Place next{nullptr, first, first_beam, first - first_beam * a.segments, 0};
+  skip(next);
   uint32_t w[WORDS], ahead_w[WORDS];
-  load(item, base, ahead_w);
-  int held = 0;              // entries collected up to now
+  if (next.item < last) Rd::load(next.row, next.left, ahead_w);
   float m = kNone, s = 0.f;  // this thread's largest logit of the segment, and sum of exponentials relative to it
-  while (item < last) {
+  int round = 0;
+  volatile float *const group_max = sm.group_max, *const shared_bound = &sm.bound;
+  while (next.item < last) {
+    const Place at = next;
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) w[i] = ahead_w[i];
-    const int b = item / a.segments, from = item % a.segments * a.segment_len + base;
-    const bool ends = base + Rd::SIZE >= segment_len(item);
-    const int next_item = ends ? skip(item + 1) : item, next_base = ends ? 0 : base + Rd::SIZE;
-    load(next_item, next_base, ahead_w);
+    advance(next);
+    if (next.item < last) Rd::load(next.row, next.left, ahead_w);
 
-    float mr = Rd::max(w), mn = fmaxf(m, mr), ref = mn == kNone ? 0.f : mn, part = Rd::sum(w, ref);
-    // A NaN, or an infinity.  Looked at as bits: a sum of ex2 is taken to be at least 0 by the assembler, and `!(part >= 0)` for never true.
-    if (__float_as_uint(part) >= 0x7F800000u) {
-      Rd::clean(w);
-      mr = Rd::max(w), mn = fmaxf(m, mr), ref = mn == kNone ? 0.f : mn, part = Rd::sum(w, ref);
-    }
-    s = fmaf(s, ex2((m - ref) * kLog2e), part);
-    m = mn;
-    if (groups == 1) {
-      const float g = warp_max(m);
-      if (lane == 0) sm.group_max[warp] = g;
+    const float mr = add_sum<Rd>(w, m, s);
+    uint64_t *const best = list + (at.beam - first_beam) * N;
+    const int have = sm.count[at.beam];
+    uint64_t floor = 0;
+    float bound;
+    if (have == N) {
+      floor = best[N - 1];
+      bound = logit_of(floor);
     } else {
+      // At any time once all groups of threads have left the largest entry they have seen of this segment, the N-th largest of those is at most
+      // the segment's N-th best entry.  Found to 16 bits of order32; all warps look for it in the first round, then one of them now and then.
       float g = m;
-      for (int d = 1; d < 32 / groups; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
-      if (lane % (32 / groups) == 0) sm.group_max[warp * groups + lane / (32 / groups)] = g;
-    }
-    __syncthreads();
-    // N groups of threads each have an entry of this segment at least as large as `bound`
-    float low = sm.group_max[lane % (NW * groups)], high = low;
-    if (groups == 4) {
-      low = fminf(low, sm.group_max[32 + lane]);
-      high = fmaxf(high, sm.group_max[32 + lane]);
-    }
-    const float bound = warp_min(low), top = warp_max(high);
-    uint64_t *const best = list + (b - first_beam) * N;
-    const int have = sm.count[b];
-    const uint64_t floor = have == N ? best[N - 1] : 0;
-    if (mr >= bound && mr > kNone) {
 #pragma unroll
-      for (int e = 0; e < Rd::EPT; ++e) {
-        const float x = Rd::get(w, e);
-        if (x >= bound && x > kNone) {
-          const uint64_t key = key_of(x, from + Rd::index(e));
-          if (key > floor) {
-            const int at = atomicAdd(&sm.n_cand, 1);
-            if (at < CAP) sm.cand[at] = key;
-          }
+      for (int d = 1; d < NT / GROUPS; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
+      if (lane % (NT / GROUPS) == 0) group_max[tid / (NT / GROUPS)] = g;
+      if (round == 0) __syncthreads();
+      if (round == 0 || ((round & (round - 1)) == 0 && warp == round % NW)) {
+        const uint32_t x = order32(group_max[lane]), y = order32(group_max[lane + 32]);
+        uint32_t t = 0;
+        for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
+          const uint32_t trial = t | bit;
+          if (__popc(__ballot_sync(0xffffffffu, x >= trial)) + __popc(__ballot_sync(0xffffffffu, y >= trial)) >= N) t = trial;
+        }
+        *shared_bound = fmaxf(t == 0 ? kNone : value32(t), kLowest<T>);  // (the same from all warps of the first round, or larger from a later one)
+        __syncwarp();
+      }
+      bound = *shared_bound;
+    }
+    if (mr >= bound) {
+      for (uint32_t hits = Rd::at_least(w, bound); hits; hits &= hits - 1) {
+        const int e = Rd::entry(__ffs(hits) - 1);
+        const uint64_t key = key_of(Rd::pick(w, e), at.segment * a.segment_len + round * Rd::SIZE + Rd::index(e));
+        if (key > floor) {
+          const int to = atomicAdd(&sm.n_cand, 1);
+          if (to < CAP) sm.cand[to] = key;
         }
       }
     }
-    if (ends) {
-      float x = s * ex2((m - (top == kNone ? 0.f : top)) * kLog2e);
+    ++round;
+    if (next.item != at.item) {  // the segment's end
+      share_sum(sm, m, s);
+      // a NaN or an infinity, looked at as bits: a sum of ex2 is taken to be at least 0 by the assembler, and `!(s >= 0)` for never true
+      const bool odd = __syncthreads_or(__float_as_uint(s) >= 0x7F800000u);
+      const int n = sm.n_cand;
+      int now;
+      if (odd || n > CAP) {
+        const int from = at.segment * a.segment_len;
+        __syncthreads();
+        now = rescan<Rd>(sm, reinterpret_cast<uint32_t *>(list + a.block_beams * N), at.row - (round - 1) * Rd::SIZE, min(a.segment_len, a.vocab - from), from,
+                         best, have, N);
+      } else {
+        now = join_list(sm, best, n, have, N);
+      }
+      if (warp == 0) {
+        const float its = lane < NW ? sm.warp_top[lane] : kNone, top = warp_max(its);
+        double x = its > kNone ? sm.warp_sum[lane] * exp(static_cast<double>(its) - top) : 0.0;
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-      if (lane == 0) sm.warp_sum[warp] = x;
+        for (int d = NW / 2; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        if (lane == 0) {
+          sm.top[at.item] = top;
+          sm.sum[at.item] = x;
+          sm.count[at.beam] = now;
+        }
+      }
       m = kNone;
       s = 0.f;
-    }
-    __syncthreads();
-    int n = sm.n_cand;
-    if (n > CAP) {
-      uint32_t *const words = reinterpret_cast<uint32_t *>(list + a.block_beams * N);
-#pragma unroll
-      for (int i = 0; i < WORDS; ++i) words[i * NT + tid] = w[i];
-      n = collect_best<Rd>(sm, words, bound, top, from, floor, held, N);
-    }
-    if (ends && warp == 0) {
-      double x = lane < NW ? sm.warp_sum[lane] : 0.0;
-#pragma unroll
-      for (int d = NW / 2; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-      if (lane == 0) {
-        sm.top[item] = top;
-        sm.sum[item] = x;
-      }
-    }
-    if (ends || n > CAP / 2) {
-      // what has been collected joins the beam's list; eight lanes count how many are ahead of each
-      for (int i = tid; i < have; i += NT) sm.cand[n + i] = best[i];
+      round = 0;
       __syncthreads();
-      const int total = n + have;
-      for (int i0 = 0; i0 < total; i0 += NT / 8) {
-        const int i = i0 + tid / 8;
-        const uint64_t k = i < total ? sm.cand[i] : 0;
-        int place = 0;
-        for (int j = tid % 8; j < total; j += 8) place += sm.cand[j] > k;
-#pragma unroll
-        for (int d = 4; d > 0; d >>= 1) place += __shfl_xor_sync(0xffffffffu, place, d);
-        if (i < total && tid % 8 == 0 && place < N) best[place] = k;
-      }
-      if (tid == 0) {
-        sm.count[b] = min(total, N);
-        sm.n_cand = 0;
-      }
-      __syncthreads();
-      n = 0;
     }
-    held = n;
-    item = next_item;
-    base = next_base;
   }
 
   // The first block takes the lists and sums of all of them.
@@ -463,8 +546,9 @@ int select_type(const DascBeamSelectArgs &a, void *stream) {
     return vec ? select<T, true, CL>(a, stream) : select<T, false, CL>(a, stream);
   };
   constexpr int kPlaces = 2 * 148;
-  if (a.n_req * int64_t{8} <= kPlaces) return with(std::integral_constant<int, 8>{});
-  if (a.n_req * int64_t{4} <= kPlaces) return with(std::integral_constant<int, 4>{});
+  constexpr int kClustered = kPlaces * 7 / 8;  // (not every GPC holds a whole number of clusters of 4 or 8)
+  if (a.n_req * int64_t{8} <= kClustered) return with(std::integral_constant<int, 8>{});
+  if (a.n_req * int64_t{4} <= kClustered) return with(std::integral_constant<int, 4>{});
   if (a.n_req * int64_t{2} <= kPlaces) return with(std::integral_constant<int, 2>{});
   return with(std::integral_constant<int, 1>{});
 }
