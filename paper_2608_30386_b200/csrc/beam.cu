@@ -26,10 +26,9 @@ namespace {
 
 constexpr int NT = 512, NW = NT / 32;
 constexpr int WORDS = 16;            // 32-bit words of a row that a thread holds at a time
-constexpr int CAP = 512;             // entries above the bound that are collected before they are ranked
 constexpr int MAXW = kBeamMaxWidth, MAXN = kBeamMaxOut;  // beams per request, continuations wanted
 constexpr int MAXS = 16;             // segments of a row
-constexpr int GROUPS = 64;           // of NT / 64 threads, whose maxima bound the n_out-th best entry; at least MAXN
+constexpr int CHUNKS = 16;           // parts of a thread's entries of a segment
 constexpr float kNone = -__builtin_huge_valf(), kLog2e = 1.44269504f;
 template <typename T>
 constexpr float kLowest = sizeof(T) == 2 ? -3.38953139e38f : -3.40282347e38f;  // the type's lowest finite value
@@ -76,17 +75,18 @@ __device__ __forceinline__ bool ahead(const Entry &a, const Entry &b) {
 }
 
 struct SelectSmem {
-  uint64_t cand[CAP + MAXN];
-  float top[MAXW * MAXS];     // of each segment (those of this block): the largest logit, and the sum of exponentials relative to it
-  double sum[MAXW * MAXS];
-  float group_max[GROUPS], bound, warp_top[NW], warp_sum[NW];
-  int n_cand, n_above, n_entries;
-  float score[MAXW];
-  int ended[MAXW], count[MAXW];
+  double reference[MAXW * MAXS], sum[MAXW * MAXS];  // of each segment (those of this block): the sum of exponentials is e^reference times sum
   double lse[MAXW];
+  float score[MAXW];
+  int ended[MAXW];
+  float warp_top[MAXW][NW], warp_sum[MAXW][NW];  // the warps' shares of each of this block's segments
+  uint32_t best_of[NT], bound;  // 16 or 32 bits of order of each thread's largest value
+  int n_hits[MAXW], odd[MAXW];  // of each of this block's segments
+  int n_above, n_entries, n_left;
+  unsigned long long any_bit, all_bits;
+  uint16_t chunk[CHUNKS][NT];   // the largest entry of each thread's chunks, 16 bits of order32
 };
-// behind it: uint64_t list[beams per block][n_out], best first; then a round's words where they are searched for the n_out-th key, and at the end
-// in the first block Entry entry[lists of all blocks][n_out]
+// behind it: uint64_t hit[segments of this block][a.budget], then in the first block Entry entry[all of them]
 
 // A thread's part of a round: where entries of a row are, and how they come from memory
 template <typename T, bool VEC>
@@ -94,7 +94,8 @@ struct Round {
   static constexpr bool PACKED = VEC && sizeof(T) == 2;
   static constexpr int EPT = PACKED ? 2 * WORDS : WORDS, SIZE = NT * EPT;  // entries per thread, and per block
   static constexpr int VW = VEC ? 16 / static_cast<int>(sizeof(T)) : 1;     // entries per load
-  static __device__ __forceinline__ int index(int e) { return (e / VW * NT + static_cast<int>(threadIdx.x)) * VW + e % VW; }
+  static __device__ __forceinline__ int index(int e, int thread) { return (e / VW * NT + thread) * VW + e % VW; }
+  static __device__ __forceinline__ int index(int e) { return index(e, static_cast<int>(threadIdx.x)); }
   static __device__ __forceinline__ uint32_t bits(T x) {
     if constexpr (sizeof(T) == 2)
       return static_cast<uint32_t>(__bfloat16_as_ushort(x)) << 16;
@@ -170,114 +171,111 @@ struct Round {
       }
     }
   }
-  // sum of e^(x - ref); differences first, since a product with log2 e ahead of them would be off by the same amount in all of a row's terms
-  static __device__ __forceinline__ float sum(const uint32_t (&w)[WORDS], float ref) {
-    const uint64_t r = dpack2(ref, ref), l = dpack2(kLog2e, kLog2e);
+  // sum of 2^(x log2 e - c).  With log2 e rounded to l this is the sum of e^((x - c / l)(1 + d)), d = 1.3e-8: all that d touches are differences from
+  // the reference c / l, so it is as good as one that subtracts first, for half of the instructions.
+  static __device__ __forceinline__ float sum(const uint32_t (&w)[WORDS], float c) {
+    const uint64_t r = dpack2(-c, -c), l = dpack2(kLog2e, kLog2e);
     uint64_t s[2] = {0, 0};
 #pragma unroll
     for (int e = 0; e < EPT; e += 2) {
-      const float2 y = dunpack2(dmul2(dsub2(dpack2(get(w, e), get(w, e + 1)), r), l));
+      const float2 y = dunpack2(dfma2(dpack2(get(w, e), get(w, e + 1)), l, r));
       s[e / 2 % 2] = dadd2(s[e / 2 % 2], dpack2(ex2(y.x), ex2(y.y)));
     }
     const float2 t = dunpack2(dadd2(s[0], s[1]));
     return t.x + t.y;
   }
-  // which entries are at least `bound` (one of the type's values): bit place(e) for entry e
-  static __device__ __forceinline__ uint32_t at_least(const uint32_t (&w)[WORDS], float bound) {
-    uint32_t hits = 0;
-    if constexpr (PACKED) {
-      const uint32_t b = __byte_perm(__float_as_uint(bound), 0, 0x3232);
-#pragma unroll
-      for (int i = 0; i < WORDS; ++i) {
-        uint32_t yes;
-        asm("set.ge.u32.bf16x2 %0, %1, %2;" : "=r"(yes) : "r"(w[i]), "r"(b));
-        hits |= yes & 0x00010001u << i;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < WORDS; ++i) hits |= __uint_as_float(w[i]) >= bound ? 1u << i : 0u;
-    }
-    return hits;
-  }
-  static __device__ __forceinline__ int entry(int place) { return PACKED ? 2 * (place % WORDS) + place / WORDS : place; }
-  // entry e, which differs from thread to thread
-  static __device__ __forceinline__ float pick(const uint32_t (&w)[WORDS], int e) {
-    uint32_t x = w[0];
-#pragma unroll
-    for (int i = 1; i < WORDS; ++i) x = (PACKED ? e / 2 : e) == i ? w[i] : x;
-    return __uint_as_float(!PACKED || e & 1 ? (PACKED ? x & 0xFFFF0000u : x) : x << 16);
-  }
 };
 
-// The `n` keys that have been collected join the `have` ones of a list, of which the N best stay, best first; eight lanes count how many are
-// ahead of each.  Called by the whole block behind a barrier, and ends with one; returns how many the list has now.
-__device__ __noinline__ int join_list(SelectSmem &sm, uint64_t *best, int n, int have, int N) {
-  const int tid = threadIdx.x, total = n + have;
-  if (tid < have) sm.cand[n + tid] = best[tid];
-  __syncthreads();
-  for (int i0 = 0; i0 < total; i0 += NT / 8) {
-    const int i = i0 + tid / 8;
-    const uint64_t k = i < total ? sm.cand[i] : 0;
-    int place = 0;
-    for (int j = tid % 8; j < total; j += 8) place += sm.cand[j] > k;
-#pragma unroll
-    for (int d = 4; d > 0; d >>= 1) place += __shfl_xor_sync(0xffffffffu, place, d);
-    if (i < total && tid % 8 == 0 && place < N) best[place] = k;
-  }
-  if (tid == 0) sm.n_cand = 0;
-  __syncthreads();
-  return min(total, N);
-}
-
-// A warp's share of a segment's sum, relative to its own largest logit.
-__device__ __forceinline__ void share_sum(SelectSmem &sm, float m, float s) {
-  const float top = warp_max(m);
-  float x = s * ex2((m - (top == kNone ? 0.f : top)) * kLog2e);
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-  if (threadIdx.x % 32 == 0) {
-    sm.warp_top[threadIdx.x / 32] = top;
-    sm.warp_sum[threadIdx.x / 32] = x;
-  }
-}
+// Sums of exponentials are relative to 2^c with c = round(m log2 e), m the largest logit of what they are over.
+__device__ __forceinline__ float reference(float m) { return m == kNone ? 0.f : __fmul_rn(m, kLog2e); }  // (not part of a multiply-add)
 // one more round's part of a thread's sum
 template <typename Rd>
 __device__ __forceinline__ float add_sum(const uint32_t (&w)[WORDS], float &m, float &s) {
-  const float mr = Rd::max(w), mn = fmaxf(m, mr), ref = mn == kNone ? 0.f : mn;
-  s = fmaf(s, ex2((m - ref) * kLog2e), Rd::sum(w, ref));
+  const float mr = Rd::max(w), mn = fmaxf(m, mr), c = reference(mn);
+  const float part = Rd::sum(w, c), more = fmaf(s, ex2(reference(m) - c), part);
+  s = m == kNone ? part : more;
   m = mn;
   return mr;
 }
+// A segment's sum of the threads': each warp leaves its share, and a warp adds them up at the end.  `plain`: they are relative to e^m itself.
+__device__ __forceinline__ void share_sum(SelectSmem &sm, int local, float m, float x) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+  if (threadIdx.x % 32 == 0) {
+    sm.warp_top[local][threadIdx.x / 32] = m;
+    sm.warp_sum[local][threadIdx.x / 32] = x;
+  }
+}
+__device__ __forceinline__ double warp_max(double x) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) x = fmax(x, __shfl_xor_sync(0xffffffffu, x, d));
+  return x;
+}
+__device__ __forceinline__ double warp_sum(double x) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+  return x;
+}
+// Sums x relative to e^ref, one per lane, as one: `top` is what it is relative to (-infinity: no lane has any).
+__device__ __forceinline__ double add_up(double ref, double x, double &top) {
+  top = warp_max(ref);
+  return warp_sum(ref > -INFINITY ? x * exp(ref - top) : 0.0);
+}
+__device__ __forceinline__ void join_sums(SelectSmem &sm, int local, int item, bool plain) {
+  const int lane = threadIdx.x % 32;
+  const float m = lane < NW ? sm.warp_top[local][lane] : kNone;
+  double top;
+  const double x = add_up(m == kNone ? -INFINITY : plain ? m : reference(m) * (1.0 / static_cast<double>(kLog2e)),
+                          lane < NW ? sm.warp_sum[local][lane] : 0.0, top);
+  if (lane == 0) {
+    sm.reference[item] = top;
+    sm.sum[item] = x;
+  }
+}
 
-// A segment with a NaN or an infinity, or in which more entries were above the bound than there is room for (many that tie, or a poor bound): once more, a round at
-// a time, each with the keys above the N-th best so far, of which at most N are collected.  `words`: a round's words in shared memory.  Called by the
-// whole block behind a barrier; leaves the warps' sums and returns how many the list has.
+// A segment with a NaN, an infinity or a logit that is too large to be a power of two, or in which more entries were above the bound than there is room for (many that
+// tie): once more, with differences from the largest logit, and its N best keys bit by bit from the top.  Called by the whole block; returns how many there are.
 template <typename Rd, typename T>
-__device__ __noinline__ int rescan(SelectSmem &sm, uint32_t *words, const T *row, int len, int from, uint64_t *best, int have, int N) {
+__device__ __noinline__ int rescan(SelectSmem &sm, const T *row, int len, int from, int local, uint64_t *hit, int N) {
   const int tid = threadIdx.x;
-  auto value = [&](int e) {
-    if constexpr (Rd::PACKED) {
-      const uint32_t x = words[e / 2 * NT + tid];
-      return __uint_as_float(e & 1 ? x & 0xFFFF0000u : x << 16);
-    } else {
-      return __uint_as_float(words[e * NT + tid]);
-    }
-  };
-  float m = kNone, s = 0.f;
+  float m = kNone;
   for (int base = 0; base < len; base += Rd::SIZE) {
     uint32_t w[WORDS];
     Rd::load(row + base, len - base, w);
     Rd::clean(w);
-    add_sum<Rd>(w, m, s);
+    m = fmaxf(m, Rd::max(w));
+  }
+  m = warp_max(m);
+  float s = 0.f;
+  for (int base = 0; base < len; base += Rd::SIZE) {
+    uint32_t w[WORDS];
+    Rd::load(row + base, len - base, w);
+    Rd::clean(w);
 #pragma unroll
-    for (int i = 0; i < WORDS; ++i) words[i * NT + tid] = w[i];  // (each thread reads its own)
+    for (int e = 0; e < Rd::EPT; ++e) s += ex2((Rd::get(w, e) - (m == kNone ? 0.f : m)) * kLog2e);
+  }
+  share_sum(sm, local, m, s);
+  // The N best of the rounds so far are in `hit`, `least` of them the last; each round's better ones join them.
+  int have = 0;
+  uint64_t least = 0;
+  for (int base = 0; base < len; base += Rd::SIZE) {
+    uint32_t w[WORDS];
+    Rd::load(row + base, len - base, w);
+    Rd::clean(w);
     const int at = from + base;
-    auto at_least = [&](uint64_t t) {  // how many keys there are from t on
-      int c = 0;
-#pragma unroll 4
-      for (int e = 0; e < Rd::EPT; ++e) {
-        const float x = value(e);
-        c += x > kNone && key_of(x, at + Rd::index(e)) >= t;
+    const uint64_t old = tid < have ? hit[tid] : 0;
+    auto at_least = [&](uint64_t t) {  // how many keys there are from t on, this round's and the old ones
+      const float v = value32(static_cast<uint32_t>(t >> 32));
+      const uint32_t low = static_cast<uint32_t>(t), last = 0xFFFFFFFFu - static_cast<uint32_t>(at);
+      int c = old >= t;
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) asm volatile("" : "+r"(w[i]));  // (nothing is kept from one bit to the next)
+      if (low == 0) {
+#pragma unroll
+        for (int e = 0; e < Rd::EPT; ++e) c += Rd::get(w, e) >= v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < Rd::EPT; ++e) c += Rd::get(w, e) > v || (Rd::get(w, e) == v && last - Rd::index(e) >= low);
       }
       c = __reduce_add_sync(0xffffffffu, c);
       __syncthreads();
@@ -287,32 +285,85 @@ __device__ __noinline__ int rescan(SelectSmem &sm, uint32_t *words, const T *row
       __syncthreads();
       return sm.n_above;
     };
-    uint64_t t = have == N ? best[N - 1] + 1 : 1;
-    int n = at_least(t);
-    if (n == 0) continue;
-    if (n > CAP) {  // the N-th largest key, bit by bit from the top
-      t = 0;
-      for (int bit = 63; bit >= 0; --bit)
-        if (at_least(t | 1ull << bit) >= N) t |= 1ull << bit;
+    if (have == N && at_least(least + 1) < N) continue;
+    uint64_t t = static_cast<uint64_t>(order32(kLowest<T>)) << 32;  // all of them
+    if (at_least(t) > N) {
+      // bit by bit from the top, those that differ between keys
+      if (tid == 0) sm.any_bit = 0, sm.all_bits = ~0ull;
+      __syncthreads();
+      uint64_t any = old, all = old ? old : ~0ull;
+#pragma unroll
+      for (int e = 0; e < Rd::EPT; ++e) {
+        const float x = Rd::get(w, e);
+        const uint64_t key = key_of(x, at + Rd::index(e));
+        if (x > kNone) any |= key, all &= key;
+      }
+      atomicOr(&sm.any_bit, any);
+      atomicAnd(&sm.all_bits, all);
+      __syncthreads();
+      t = sm.all_bits;
+      for (uint64_t bits = sm.any_bit ^ sm.all_bits; bits;) {
+        const uint64_t bit = 1ull << (63 - __clzll(static_cast<long long>(bits)));
+        if (at_least((t & ~(bit - 1)) | bit) >= N) t |= bit;
+        bits ^= bit;
+      }
     }
     __syncthreads();
-    if (tid == 0) sm.n_cand = 0;
+    if (tid == 0) sm.n_left = 0;
     __syncthreads();
+    if (old >= t) hit[atomicAdd(&sm.n_left, 1)] = old;
+#pragma unroll
     for (int e = 0; e < Rd::EPT; ++e) {
-      const float x = value(e);
+      const float x = Rd::get(w, e);
       const uint64_t key = key_of(x, at + Rd::index(e));
-      if (x > kNone && key >= t) sm.cand[atomicAdd(&sm.n_cand, 1)] = key;  // (at most CAP of them, or N)
+      if (x > kNone && key >= t) hit[atomicAdd(&sm.n_left, 1)] = key;  // (N of them at most)
     }
     __syncthreads();
-    n = sm.n_cand;
+    have = sm.n_left;
+    least = t;
     __syncthreads();
-    have = join_list(sm, best, n, have, N);
   }
-  share_sum(sm, m, s);
   __syncthreads();
-  if (tid == 0) sm.n_cand = 0;
-  __syncthreads();
+  if (tid == 0) sm.n_left = 0;
   return have;
+}
+
+// A lower bound on the N-th largest of many values, of which each thread has left its largest in `best_of` (0: none): the threads are G >= N groups, every G-th
+// one together so that neighbours are apart, and the N-th largest of the groups' maxima is at most that.  By the whole block; `bound` is set behind the
+// next barrier.
+template <int G>
+__device__ __forceinline__ void nth_of_groups(const uint32_t *best_of, int N, uint32_t *bound) {
+  constexpr int PER = G / 32;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  uint32_t x[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    x[i] = best_of[lane + 32 * i];
+#pragma unroll
+    for (int j = 1; j < NT / G; ++j) x[i] = max(x[i], best_of[lane + 32 * i + G * j]);
+  }
+#pragma unroll
+  for (int i = 0; i < G / NW; ++i) {  // this warp's share of them: is it the one?
+    const int g = warp * (G / NW) + i;
+    uint32_t v = x[0];
+#pragma unroll
+    for (int j = 1; j < PER; ++j) v = g / 32 == j ? x[j] : v;
+    v = __shfl_sync(0xffffffffu, v, g % 32);
+    int above = 0, from = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      above += __popc(__ballot_sync(0xffffffffu, x[j] > v));
+      from += __popc(__ballot_sync(0xffffffffu, x[j] >= v));
+    }
+    if (above < N && from >= N && lane == 0) *bound = v;
+  }
+}
+__device__ __forceinline__ void find_bound(SelectSmem &sm, int N) {
+  static_assert(MAXN <= 128, "a group for every n_out");
+  if (N <= 32)
+    nth_of_groups<64>(sm.best_of, N, &sm.bound);  // (with many values, 64 ln 2 = 44 of them are above it where N = 32, 18 where N = 16)
+  else
+    nth_of_groups<128>(sm.best_of, N, &sm.bound);
 }
 
 template <typename T, bool VEC, int CL>
@@ -320,7 +371,7 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
   using Rd = Round<T, VEC>;
   extern __shared__ __align__(16) unsigned char smem_raw[];
   SelectSmem &sm = *reinterpret_cast<SelectSmem *>(smem_raw);
-  uint64_t *const list = reinterpret_cast<uint64_t *>(smem_raw + sizeof(SelectSmem));
+  uint64_t *const hit = reinterpret_cast<uint64_t *>(smem_raw + sizeof(SelectSmem));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r = blockIdx.x / CL, rank = blockIdx.x % CL;
   const int W = a.width, N = a.n_out;
@@ -331,151 +382,111 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
     sm.score[tid] = score;
     // 0: its row counts, 1: it has ended, 2: it has no continuation
     sm.ended[tid] = !finite(score) ? 2 : a.ended && a.ended[static_cast<int64_t>(r) * W + tid] != 0 ? 1 : 0;
-    sm.count[tid] = 0;
   }
-  if (tid == 0) sm.n_cand = sm.n_entries = 0;
+  if (tid < MAXW) sm.n_hits[tid] = sm.odd[tid] = 0;
+  if (tid == 0) sm.n_entries = sm.n_left = 0;
   __syncthreads();
 
-  const int first = min(rank * a.per_block, W * a.segments), last = min(first + a.per_block, W * a.segments), first_beam = first / a.segments;
-  // where this block is: a segment of a beam's row, and how many of its entries are left; rows that do not count are passed over
-  struct Place {
-    const T *row;
-    int item, beam, segment, left;
+  const int first = min(rank * a.per_block, W * a.segments), last = min(first + a.per_block, W * a.segments);
+  const int each = (a.segment_len + Rd::SIZE * CHUNKS - 1) / (Rd::SIZE * CHUNKS);  // rounds per chunk
+  auto row_of = [&](int item) {
+    return static_cast<const T *>(a.logits) + (static_cast<int64_t>(r) * W + item / a.segments) * a.stride + item % a.segments * a.segment_len;
   };
-  auto open = [&](Place &p) {
-    p.left = min(a.segment_len, a.vocab - p.segment * a.segment_len);
-    p.row = static_cast<const T *>(a.logits) + (static_cast<int64_t>(r) * W + p.beam) * a.stride + p.segment * a.segment_len;
-  };
-  auto skip = [&](Place &p) {
-    while (p.item < last && sm.ended[p.beam]) {
-      p.item += a.segments - p.segment;
-      p.segment = 0;
-      ++p.beam;
-    }
-    if (p.item < last) open(p);
-  };
-  auto advance = [&](Place &p) {
-    p.row += Rd::SIZE;
-    p.left -= Rd::SIZE;
-    if (p.left <= 0) {
-      ++p.item;
-      if (++p.segment == a.segments) {
-        p.segment = 0;
-        ++p.beam;
+  for (int item = first; item < last; ++item) {
+    if (sm.ended[item / a.segments]) continue;  // (the same for the whole block)
+    const int from = item % a.segments * a.segment_len, len = min(a.segment_len, a.vocab - from);
+    const T *const row = row_of(item);
+    // One pass over the segment: this thread's largest logit and its sum of exponentials, and the largest of each chunk of its entries.
+    float m = kNone, s = 0.f, top = kNone;
+    int chunks = 0, left = each;
+    auto leave = [&](float x) {
+      top = fmaxf(top, x);
+      if (--left == 0) {
+        sm.chunk[chunks++][tid] = static_cast<uint16_t>(order32(top) >> 16);
+        left = each;
+        top = kNone;
       }
-      skip(p);
+    };
+    for (int base = 0; base < len; base += 2 * Rd::SIZE) {  // two rounds' loads at a time
+      uint32_t w[2][WORDS];
+      Rd::load(row + base, len - base, w[0]);
+      if (base + Rd::SIZE < len) Rd::load(row + base + Rd::SIZE, len - base - Rd::SIZE, w[1]);
+      leave(add_sum<Rd>(w[0], m, s));
+      if (base + Rd::SIZE < len) leave(add_sum<Rd>(w[1], m, s));
     }
-  };
-  Place next{nullptr, first, first_beam, first - first_beam * a.segments, 0};
-  skip(next);
-  uint32_t w[WORDS], ahead_w[WORDS];
-  if (next.item < last) Rd::load(next.row, next.left, ahead_w);
-  float m = kNone, s = 0.f;  // this thread's largest logit of the segment, and sum of exponentials relative to it
-  int round = 0;
-  volatile float *const group_max = sm.group_max, *const shared_bound = &sm.bound;
-  while (next.item < last) {
-    const Place at = next;
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) w[i] = ahead_w[i];
-    advance(next);
-    if (next.item < last) Rd::load(next.row, next.left, ahead_w);
-
-    const float mr = add_sum<Rd>(w, m, s);
-    uint64_t *const best = list + (at.beam - first_beam) * N;
-    const int have = sm.count[at.beam];
-    uint64_t floor = 0;
-    float bound;
-    if (have == N) {
-      floor = best[N - 1];
-      bound = logit_of(floor);
-    } else {
-      // At any time once all groups of threads have left the largest entry they have seen of this segment, the N-th largest of those is at most
-      // the segment's N-th best entry.  Found to 16 bits of order32; all warps look for it in the first round, then one of them now and then.
-      float g = m;
-#pragma unroll
-      for (int d = 1; d < NT / GROUPS; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
-      if (lane % (NT / GROUPS) == 0) group_max[tid / (NT / GROUPS)] = g;
-      if (round == 0) __syncthreads();
-      if (round == 0 || ((round & (round - 1)) == 0 && warp == round % NW)) {
-        const uint32_t x = order32(group_max[lane]), y = order32(group_max[lane + 32]);
-        uint32_t t = 0;
-        for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
-          const uint32_t trial = t | bit;
-          if (__popc(__ballot_sync(0xffffffffu, x >= trial)) + __popc(__ballot_sync(0xffffffffu, y >= trial)) >= N) t = trial;
-        }
-        *shared_bound = fmaxf(t == 0 ? kNone : value32(t), kLowest<T>);  // (the same from all warps of the first round, or larger from a later one)
-        __syncwarp();
-      }
-      bound = *shared_bound;
-    }
-    if (mr >= bound) {
-      for (uint32_t hits = Rd::at_least(w, bound); hits; hits &= hits - 1) {
-        const int e = Rd::entry(__ffs(hits) - 1);
-        const uint64_t key = key_of(Rd::pick(w, e), at.segment * a.segment_len + round * Rd::SIZE + Rd::index(e));
-        if (key > floor) {
-          const int to = atomicAdd(&sm.n_cand, 1);
-          if (to < CAP) sm.cand[to] = key;
+    if (left != each) sm.chunk[chunks++][tid] = static_cast<uint16_t>(order32(top) >> 16);
+    sm.best_of[tid] = order32(m) >> 16;
+    const float high = warp_max(m);
+    share_sum(sm, item - first, high, m == kNone ? 0.f : s * ex2(reference(m) - reference(high)));
+    // a NaN or an infinity, looked at as bits: a sum of ex2 is taken to be at least 0 by the assembler, and `!(s >= 0)` for never true
+    const bool odd = __syncthreads_or(__float_as_uint(s) >= 0x7F800000u);
+    find_bound(sm, N);
+    if (tid == 0) sm.odd[item - first] = odd;
+    __syncthreads();
+    const uint32_t t = max(sm.bound, order32(kLowest<T>) >> 16);
+    if (odd) continue;
+    // The few chunks that may hold one of the best are read again, an entry per lane.
+    const float bound = value32(t << 16);
+    volatile int *const hits = &sm.n_hits[item - first];
+    for (int c = 0; c < chunks && *hits <= a.budget; ++c) {  // (too many: all of it once more, see rescan)
+      for (uint32_t who = __ballot_sync(0xffffffffu, sm.chunk[c][tid] >= t); who; who &= who - 1) {
+        const int thread = warp * 32 + __ffs(who) - 1;
+        for (int i = lane; i < each * Rd::EPT; i += 32) {
+          const int at = (c * each + i / Rd::EPT) * Rd::SIZE + Rd::index(i % Rd::EPT, thread);
+          const float x = at < len ? __uint_as_float(Rd::bits(row[at])) : kNone;
+          if (x >= bound) {
+            const int to = atomicAdd(const_cast<int *>(hits), 1);
+            if (to < a.budget) hit[(item - first) * a.budget + to] = key_of(x, from + at);
+          }
         }
       }
-    }
-    ++round;
-    if (next.item != at.item) {  // the segment's end
-      share_sum(sm, m, s);
-      // a NaN or an infinity, looked at as bits: a sum of ex2 is taken to be at least 0 by the assembler, and `!(s >= 0)` for never true
-      const bool odd = __syncthreads_or(__float_as_uint(s) >= 0x7F800000u);
-      const int n = sm.n_cand;
-      int now;
-      if (odd || n > CAP) {
-        const int from = at.segment * a.segment_len;
-        __syncthreads();
-        now = rescan<Rd>(sm, reinterpret_cast<uint32_t *>(list + a.block_beams * N), at.row - (round - 1) * Rd::SIZE, min(a.segment_len, a.vocab - from), from,
-                         best, have, N);
-      } else {
-        now = join_list(sm, best, n, have, N);
-      }
-      if (warp == 0) {
-        const float its = lane < NW ? sm.warp_top[lane] : kNone, top = warp_max(its);
-        double x = its > kNone ? sm.warp_sum[lane] * exp(static_cast<double>(its) - top) : 0.0;
-#pragma unroll
-        for (int d = NW / 2; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-        if (lane == 0) {
-          sm.top[at.item] = top;
-          sm.sum[at.item] = x;
-          sm.count[at.beam] = now;
-        }
-      }
-      m = kNone;
-      s = 0.f;
-      round = 0;
-      __syncthreads();
     }
   }
-
-  // The first block takes the lists and sums of all of them.
-  cg::cluster_group cluster = cg::this_cluster();
-  cluster.sync();
-  Entry *const entry = reinterpret_cast<Entry *>(list + a.block_beams * N);
-  if (rank == 0) {
-    if (tid < W && sm.ended[tid] == 0) {
-      float top = kNone;
-      for (int i = tid * a.segments; i < (tid + 1) * a.segments; ++i) top = fmaxf(top, cluster.map_shared_rank(sm.top, i / a.per_block)[i]);
-      double x = 0.0;
-      if (top > kNone)
-        for (int i = tid * a.segments; i < (tid + 1) * a.segments; ++i) {
-          const float t = cluster.map_shared_rank(sm.top, i / a.per_block)[i];
-          if (t > kNone) x += cluster.map_shared_rank(sm.sum, i / a.per_block)[i] * exp(static_cast<double>(t) - top);
-        }
-      sm.lse[tid] = static_cast<double>(top) + log(x);
+  __syncthreads();
+  for (int item = first; item < last; ++item) {
+    const bool again = sm.odd[item - first] || sm.n_hits[item - first] > a.budget;  // (the same for the whole block)
+    if (!again) continue;
+    const int from = item % a.segments * a.segment_len;
+    const int n = rescan<Rd>(sm, row_of(item), min(a.segment_len, a.vocab - from), from, item - first, hit + (item - first) * a.budget, N);
+    if (tid == 0) {
+      sm.n_hits[item - first] = n;
+      sm.odd[item - first] = 1;
     }
     __syncthreads();
-    for (int i = tid; i < CL * a.block_beams * N; i += NT) {
-      const int c = i / (a.block_beams * N), j = i % (a.block_beams * N), its_first = c * a.per_block / a.segments, b = its_first + j / N;
-      if (c * a.per_block < W * a.segments && b * a.segments < min((c + 1) * a.per_block, W * a.segments) && j % N < cluster.map_shared_rank(sm.count, c)[b]) {
+  }
+  for (int item = first + warp; item < last; item += NW)
+    if (!sm.ended[item / a.segments]) join_sums(sm, item - first, item, sm.odd[item - first]);
+
+  // The first block takes the hits and sums of all of them.
+  cg::cluster_group cluster = cg::this_cluster();
+  cluster.sync();
+  Entry *const entry = reinterpret_cast<Entry *>(hit + (a.per_block * a.budget + 1) / 2 * 2);
+  uint64_t mine = 0;  // this thread's best total
+  if (rank == 0) {
+    for (int b = warp; b < W; b += NW)
+      if (sm.ended[b] == 0) {
+        const int item = b * a.segments + lane, c = item / a.per_block;
+        double ref = -INFINITY, x = 0.0, top;
+        if (lane < a.segments) {
+          ref = cluster.map_shared_rank(sm.reference, c)[item];
+          x = cluster.map_shared_rank(sm.sum, c)[item];
+        }
+        x = add_up(ref, x, top);
+        if (lane == 0) sm.lse[b] = top + log(x);
+      }
+    __syncthreads();
+    for (int item = warp; item < W * a.segments; item += NW) {
+      const int c = item / a.per_block, local = item % a.per_block, b = item / a.segments, n = cluster.map_shared_rank(sm.n_hits, c)[local];
+      int to = 0;
+      if (lane == 0 && n > 0) to = atomicAdd(&sm.n_entries, n);
+      to = __shfl_sync(0xffffffffu, to, 0);
+      for (int i = lane; i < n; i += 32) {
         Entry e;
-        e.key = cluster.map_shared_rank(list, c)[j];
+        e.key = cluster.map_shared_rank(hit, c)[local * a.budget + i];
         e.total = order64(static_cast<double>(sm.score[b]) + (static_cast<double>(logit_of(e.key)) - sm.lse[b]));
         e.beam = b;
-        entry[atomicAdd(&sm.n_entries, 1)] = e;
+        entry[to + i] = e;
+        mine = max(mine, e.total);
       }
     }
     if (tid < W && sm.ended[tid] == 1) {
@@ -484,17 +495,34 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
       e.total = order64(sm.score[tid]);
       e.beam = tid;
       entry[atomicAdd(&sm.n_entries, 1)] = e;
+      mine = max(mine, e.total);
     }
   }
   cluster.sync();  // (no block ends while the first one still reads it)
   if (rank != 0) return;
-  const int total = sm.n_entries;
+  // Those that may be among the N best by 32 bits of their totals; where there are few, all.
+  int total = sm.n_entries;
+  uint16_t *const kept = sm.chunk[0];  // (indexes of at most MAXW * budget of them)
+  if (total > NT / 8) {
+    sm.best_of[tid] = static_cast<uint32_t>(mine >> 32);
+    __syncthreads();
+    find_bound(sm, N);
+    __syncthreads();
+    const uint32_t t = sm.bound;
+    for (int i = tid; i < total; i += NT)
+      if (static_cast<uint32_t>(entry[i].total >> 32) >= t) kept[atomicAdd(&sm.n_left, 1)] = static_cast<uint16_t>(i);
+    __syncthreads();
+    total = sm.n_left;
+  } else {
+    for (int i = tid; i < total; i += NT) kept[i] = static_cast<uint16_t>(i);
+    __syncthreads();
+  }
   const int64_t out = static_cast<int64_t>(r) * N;
-  for (int i0 = 0; i0 < total; i0 += NT / 8) {
+  for (int i0 = 0; i0 < total; i0 += NT / 8) {  // eight lanes count how many are ahead of each
     const int i = i0 + tid / 8;
-    const Entry e = entry[min(i, total - 1)];
+    const Entry e = entry[kept[min(i, total - 1)]];
     int place = 0;
-    for (int j = tid % 8; j < total; j += 8) place += ahead(entry[j], e);
+    for (int j = tid % 8; j < total; j += 8) place += ahead(entry[kept[j]], e);
 #pragma unroll
     for (int d = 4; d > 0; d >>= 1) place += __shfl_xor_sync(0xffffffffu, place, d);
     if (i < total && tid % 8 == 0 && place < N) {
@@ -516,20 +544,23 @@ template <typename T, bool VEC, int CL>
 int select(DascBeamSelectArgs a, void *stream) {
   // Segments of a row, the same for all rows: whole rounds as far as possible.  A segment's end costs its block about as much as another round.
   using Rd = Round<T, VEC>;
+  constexpr size_t kEntries = 40 * 1024;  // bytes of entries that leave room for two blocks per SM
   int64_t least = INT64_MAX;
   for (int n = 1; n <= MAXS; ++n) {
-    const int64_t len = ((a.vocab + n - 1) / n + 7) / 8 * 8, cost = (static_cast<int64_t>(a.width) * n + CL - 1) / CL * ((len + Rd::SIZE - 1) / Rd::SIZE + 1);
-    if (cost < least) {
+    const int64_t len = ((a.vocab + n - 1) / n + 7) / 8 * 8, per_block = (static_cast<int64_t>(a.width) * n + CL - 1) / CL;
+    const int64_t cost = per_block * ((len + Rd::SIZE - 1) / Rd::SIZE + 1);
+    if (cost < least && (n == 1 || (per_block <= MAXW && a.width * n * (2 * a.n_out + 64) * sizeof(Entry) <= kEntries))) {
       least = cost;
       a.segment_len = static_cast<int32_t>(len);
     }
   }
   a.segments = (a.vocab + a.segment_len - 1) / a.segment_len;
   a.per_block = (a.width * a.segments + CL - 1) / CL;
-  a.block_beams = std::min(a.width, (a.per_block + a.segments - 2) / a.segments + 1);
-  // lists of this block's beams; entries of all lists and of the beams that have ended (a beam that is in several blocks has not)
-  const size_t smem = sizeof(SelectSmem) + static_cast<size_t>(a.block_beams) * sizeof(uint64_t) * a.n_out +
-                      std::max(static_cast<size_t>(a.width + CL) * sizeof(Entry) * a.n_out, NT * WORDS * sizeof(uint32_t));
+  // hits per segment: about 1.1 n_out are to be expected, more where good tokens are neighbours
+  a.budget = std::max(2 * a.n_out + 64, std::min(4 * a.n_out + 128, static_cast<int>(kEntries / sizeof(Entry)) / (a.width * a.segments)));
+  // hits of this block's segments; entries of all segments, a beam that has ended has none but its own
+  const size_t smem = sizeof(SelectSmem) + static_cast<size_t>(a.per_block * a.budget + 1) / 2 * 16 +
+                      static_cast<size_t>(a.width * a.segments) * a.budget * sizeof(Entry);
   auto kernel = beam_select_kernel<T, VEC, CL>;
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));

@@ -210,7 +210,7 @@ struct DascBeamSelectArgs {
   int32_t end_token, n_req, width, n_out;
   float *out_scores;
   int32_t *out_parent, *out_token, *out_ended;
-  int32_t segments, segment_len, per_block, block_beams;  // set by the launcher: segments of a row, their length, segments and beams per thread block
+  int32_t segments, segment_len, per_block, budget;  // set by the launcher: segments of a row, their length, segments per thread block, hits per segment
 };
 int dasc_launch_beam_select(const DascBeamSelectArgs &a, void *stream);
 struct DascBeamReorderArgs {
