@@ -195,27 +195,29 @@ struct DraftShape {
   static constexpr int WARPS = NCOL / 16, NT = NCOL > 32 ? WARPS * 32 : 128, BLOCKS = DK / 8;  // (a narrow part has two warps that only prepare)
 };
 
-template <int DK, int NCOL, bool KDA, typename IO>
-struct DraftSmem {
-  static constexpr int GN = KDA ? DK : 4, BLOCKS = DK / 8;
-  // operands as the lanes take them, the rounded parts and what they are short of; a block's 32 lanes and 64 bytes that spread the writes over the banks
-  alignas(16) float4 key_query[2][BLOCKS][36];  // P_t k_t and q_scale P_t q_t of token t = lane / 4: rows 2 m (key, query), 2 m + 1 (key, query)
-  alignas(16) float4 last[BLOCKS][36];          // D_ns k_s: row lane / 4, tokens m and m + 4 rounded, and what they are short of
+// What a group of tokens brings to a state's NCOL columns, and the rows it is made from.
+template <int DK, int NCOL>
+struct Operands {
+  // as the lanes take them, the rounded parts and what they are short of; a block's 32 lanes and 64 bytes that spread the writes over the banks
+  alignas(16) float4 key_query[2][DK / 8][36];  // P_t k_t and q_scale P_t q_t of token t = lane / 4: rows 2 m (key, query), 2 m + 1 (key, query)
+  alignas(16) float4 last[DK / 8][36];          // D_ns k_s: row lane / 4, tokens m and m + 4 rounded, and what they are short of
   alignas(16) float hi[DK], lo[DK];             // the group's decay
   alignas(16) float v[TB][NCOL], u[TB][NCOL];
-  alignas(16) float alpha[TB][KDA ? DK : 1];
   alignas(16) float kk[TB][TB], qk[TB][TB];     // k_t . D_ts k_s for s < t, q_scale q_t . D_ts k_s for s <= t, 0 for later s
   float beta[TB];
-  // the next group as it comes from memory
-  alignas(16) IO raw_q[TB][DK], raw_k[TB][DK], raw_v[TB][NCOL];
-  alignas(16) float raw_g[TB][GN], raw_beta[TB];
+};
+template <int DK, int NCOL, bool KDA, typename IO>
+struct RawRows {  // as they come from memory
+  alignas(16) IO q[TB][DK], k[TB][DK], v[TB][NCOL];
+  alignas(16) float g[TB][KDA ? DK : 4], beta[TB];
+};
+template <int DK, int NCOL, bool KDA, typename IO>
+struct DraftSmem {
+  Operands<DK, NCOL> op;
+  RawRows<DK, NCOL, KDA, IO> raw;
 };
 
-__device__ __forceinline__ float to_tf32(float x) {
-  uint32_t y;
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(y) : "f"(x));
-  return __uint_as_float(y);
-}
+__device__ __forceinline__ float to_tf32(float x) { return __uint_as_float((__float_as_uint(x) + 0x1000u) & 0xFFFFE000u); }  // (an infinity stays one)
 __device__ __forceinline__ void mma_tf32(float (&d)[4], const float4 &a, float b0, float b1) {
   asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -223,28 +225,26 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], const float4 &a, float b
         "r"(__float_as_uint(b1)));
 }
 
-template <int DK, int NCOL, bool KDA, typename IO, typename OT>
-__global__ void __launch_bounds__((DraftShape<DK, NCOL>::NT), (512 / DraftShape<DK, NCOL>::NT)) delta_draft_kernel(const __grid_constant__ DascDeltaArgs a) {
-  using Sh = DraftShape<DK, NCOL>;
-  using Sm = DraftSmem<DK, NCOL, KDA, IO>;
-  constexpr int NT = Sh::NT, BLOCKS = Sh::BLOCKS;
-  extern __shared__ __align__(16) unsigned char smem_raw[];
-  Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
-  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, m = lane % 4, nn = lane / 4;
-  // A block takes every gridDim.x-th part of a state; what the next one needs is on its way while one is worked on.
-  const int parts = a.d_v / NCOL, jobs = static_cast<int>(static_cast<int64_t>(a.n_req) * a.n_layers_in_call * a.H_v * parts);  // (below 2^31: launch)
-  struct Job {
-    int r, lc, h, part, req, begin, n;
-    bool zero;
-  };
-  auto look_up = [&](int64_t job) {
-    Job x{0, 0, 0, 0, -1, 0, 0, false};
-    if (job < jobs) {
-      const int i = static_cast<int>(job);
-      x.part = i % parts;
-      x.h = i / parts % a.H_v;
-      x.lc = i / (parts * a.H_v) % a.n_layers_in_call;
-      x.r = i / (parts * a.H_v) / a.n_layers_in_call;
+// A block takes every gridDim.x-th part of a state; what the next one needs is on its way while one is worked on.
+struct Job {
+  int part, h, lc, r;  // counted up in this order
+  int req, begin, n;
+  bool zero;
+};
+template <int DK, int NCOL>
+struct JobWalk {
+  const DascDeltaArgs &a;
+  const int dv, parts;
+  const Job stride;
+  __device__ __forceinline__ explicit JobWalk(const DascDeltaArgs &args)
+      : a(args), dv(NCOL == 128 ? 128 : args.d_v), parts(dv / NCOL), stride(digits(static_cast<int>(gridDim.x))) {}  // (128 columns at once: only where that is all)
+  __device__ __forceinline__ Job digits(int i) const {
+    return Job{i % parts, i / parts % a.H_v, i / (parts * a.H_v) % a.n_layers_in_call, i / (parts * a.H_v) / a.n_layers_in_call, -1, 0, 0, false};
+  }
+  __device__ __forceinline__ void look_up(Job &x) const {
+    x.req = -1;
+    x.n = 0;
+    if (x.r < a.n_req) {
       x.req = a.req_idx[x.r];
       x.begin = a.cu_seqlens[x.r];
       x.n = max(a.cu_seqlens[x.r + 1] - x.begin, 0);
@@ -252,134 +252,140 @@ __global__ void __launch_bounds__((DraftShape<DK, NCOL>::NT), (512 / DraftShape<
       if (x.req < 0) x.n = 0;
       x.zero = a.from_zero && a.from_zero[x.r] != 0;
     }
-    return x;
-  };
-  auto state_of = [&](const Job &x) {
-    return a.state + x.req * a.req_stride + (a.layer_begin + x.lc) * a.layer_stride + static_cast<int64_t>(x.h) * DK * a.d_v + x.part * NCOL;
-  };
-  const bool write = !a.score;
-  const int64_t qk_stride = static_cast<int64_t>(a.H_k) * DK, v_stride = static_cast<int64_t>(a.H_v) * a.d_v;
-  stream_order_wait();
-
-  auto stage = [&](const Job &x, int t0) {  // a group's rows as they are, 16 bytes per copy
-    const int cnt = min(TB, x.n - t0), hk = x.h / (a.H_v / a.H_k);
-    const int64_t tok = static_cast<int64_t>(x.lc) * a.total_tokens + x.begin + t0;
-    const IO *const gq = static_cast<const IO *>(a.q) + (tok * a.H_k + hk) * DK;
-    const IO *const gk = static_cast<const IO *>(a.k) + (tok * a.H_k + hk) * DK;
-    const IO *const gv = static_cast<const IO *>(a.v) + (tok * a.H_v + x.h) * a.d_v + x.part * NCOL;
-    const float *const gg = a.g + (tok * a.H_v + x.h) * (KDA ? DK : 1);
-    const float *const gb = a.beta + tok * a.H_v + x.h;
-    constexpr int QV = DK * sizeof(IO) / 16, VV = NCOL * sizeof(IO) / 16, GV = DK / 4;
-    for (int i = tid; i < cnt * QV; i += NT) {
-      const int t = i / QV, j = i % QV * (16 / sizeof(IO));
-      cp_async16(&sm.raw_k[t][j], gk + t * qk_stride + j);
-      if (a.o) cp_async16(&sm.raw_q[t][j], gq + t * qk_stride + j);
-    }
-    for (int i = tid; i < cnt * VV; i += NT) {
-      const int t = i / VV, j = i % VV * (16 / sizeof(IO));
-      cp_async16(&sm.raw_v[t][j], gv + t * v_stride + j);
-    }
-    if constexpr (KDA) {
-      for (int i = tid; i < cnt * GV; i += NT) cp_async16(&sm.raw_g[i / GV][i % GV * 4], gg + static_cast<int64_t>(i / GV) * a.H_v * DK + i % GV * 4);
-    } else {
-      if (tid < cnt) cp_async4(&sm.raw_g[tid][0], gg + static_cast<int64_t>(tid) * a.H_v);
-    }
-    if (tid < cnt) cp_async4(&sm.raw_beta[tid], gb + static_cast<int64_t>(tid) * a.H_v);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-
-  Job now = look_up(blockIdx.x);
-  stage(now, 0);
-  for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
-  const Job next = look_up(job + gridDim.x);
-  const int n = now.n;
-  const bool holds = warp < Sh::WARPS;
-  float *const st = state_of(now) + static_cast<int64_t>(2 * m) * a.d_v + warp * 16 + 2 * nn;
-  OT *const go = static_cast<OT *>(a.o) + ((static_cast<int64_t>(now.lc) * a.total_tokens + now.begin) * a.H_v + now.h) * a.d_v + now.part * NCOL;
-  uint64_t S[BLOCKS][2];  // rows 8 b + 2 m and the one behind it; columns 2 nn, 2 nn + 1
-#pragma unroll
-  for (int b = 0; b < BLOCKS; ++b) {
-    float2 x = make_float2(0.f, 0.f), y = x;
-    if (holds && !now.zero && n > 0) {
-      x = *reinterpret_cast<const float2 *>(st + static_cast<int64_t>(8 * b) * a.d_v);
-      y = *reinterpret_cast<const float2 *>(st + static_cast<int64_t>(8 * b + 1) * a.d_v);
-    }
-    S[b][0] = dpack2(x.x, y.x);
-    S[b][1] = dpack2(x.y, y.y);
   }
+  __device__ __forceinline__ Job first() const {
+    Job x = digits(static_cast<int>(blockIdx.x));
+    look_up(x);
+    return x;
+  }
+  __device__ __forceinline__ Job after(const Job &x) const {  // gridDim.x behind x
+    Job y = x;
+    y.part += stride.part;
+    bool carry = y.part >= parts;
+    y.part -= carry ? parts : 0;
+    y.h += stride.h + carry;
+    carry = y.h >= a.H_v;
+    y.h -= carry ? a.H_v : 0;
+    y.lc += stride.lc + carry;
+    carry = y.lc >= a.n_layers_in_call;
+    y.lc -= carry ? a.n_layers_in_call : 0;
+    y.r += stride.r + carry;
+    look_up(y);
+    return y;
+  }
+  __device__ __forceinline__ float *state_of(const Job &x) const {
+    return a.state + x.req * a.req_stride + (a.layer_begin + x.lc) * a.layer_stride + (x.h * DK * dv + x.part * NCOL);
+  }
+};
 
-  for (int t0 = 0; t0 < n; t0 += TB) {
-    const int cnt = min(TB, n - t0);
-    const bool update = write || t0 + TB < n;
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncthreads();
-    for (int i = tid; i < cnt * (KDA ? DK : 1); i += NT) {
-      if constexpr (KDA)
-        sm.alpha[i / DK][i % DK] = expf(sm.raw_g[i / DK][i % DK]);
-      else
-        sm.alpha[i][0] = expf(sm.raw_g[i][0]);
+// The rows of `cnt` tokens of a job from token t0 on, as they are, 16 bytes per copy, by NT threads (the first ones of the block; offsets between eight
+// tokens are below 2^31: launch).
+template <int DK, int NCOL, bool KDA, typename IO, int NT>
+__device__ __forceinline__ void copy_rows(RawRows<DK, NCOL, KDA, IO> &raw, const DascDeltaArgs &a, const Job &x, int cnt, int t0) {
+  const int tid = threadIdx.x, dv = NCOL == 128 ? 128 : a.d_v, group = a.H_v / a.H_k, v_stride = a.H_v * dv;
+  if (cnt > 0) {
+    const int64_t tok = static_cast<int64_t>(x.lc) * a.total_tokens + (x.begin + t0), row = tok * a.H_v + x.h;
+    const int64_t key = (tok * a.H_k + x.h / group) * DK;
+    constexpr int VE = 16 / sizeof(IO), QV = DK / VE, VV = NCOL / VE, GV = DK / 4;
+    const int qk_stride = a.H_k * DK;
+    const IO *const gk = static_cast<const IO *>(a.k) + key, *const gq = static_cast<const IO *>(a.q) + key;
+#pragma unroll
+    for (int i = tid; i < TB * QV * 2; i += NT) {
+      const int t = i / QV % TB, j = i % QV * VE;
+      const bool query = i >= TB * QV;
+      if (t < cnt && !(query && !a.o)) cp_async16(query ? &raw.q[t][j] : &raw.k[t][j], (query ? gq : gk) + t * qk_stride + j);
     }
-    for (int i = tid; i < cnt * NCOL; i += NT) sm.v[i / NCOL][i % NCOL] = to_float<IO>(sm.raw_v[i / NCOL][i % NCOL]);
-    if (tid < cnt) sm.beta[tid] = sm.raw_beta[tid];
-    __syncthreads();
-    // keys and queries behind the group's start, and keys decayed to its end: a thread per channel and kind
-    for (int i = tid; i < 3 * DK; i += NT) {
+    const IO *const gv = static_cast<const IO *>(a.v) + row * dv + x.part * NCOL;
+#pragma unroll
+    for (int i = tid; i < TB * VV; i += NT)
+      if (i / VV < cnt) cp_async16(&raw.v[i / VV][i % VV * VE], gv + i / VV * v_stride + i % VV * VE);
+    const float *const gg = a.g + row * (KDA ? DK : 1);
+    if constexpr (KDA) {
+#pragma unroll
+      for (int i = tid; i < TB * GV; i += NT)
+        if (i / GV < cnt) cp_async16(&raw.g[i / GV][i % GV * 4], gg + i / GV * (a.H_v * DK) + i % GV * 4);
+    } else {
+      if (tid < cnt) cp_async4(&raw.g[tid][0], gg + tid * a.H_v);
+    }
+    if (tid >= NT - 32 && tid - (NT - 32) < cnt) cp_async4(&raw.beta[tid - (NT - 32)], a.beta + row + (tid - (NT - 32)) * a.H_v);
+  }
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+
+// The group's `cnt` tokens as operands, by NT threads (the first ones of the block).
+template <int DK, int NCOL, bool KDA, typename IO, int NT>
+__device__ __forceinline__ void prepare(Operands<DK, NCOL> &op, const RawRows<DK, NCOL, KDA, IO> &raw, int cnt, bool update, bool want, float q_scale) {
+  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+  // Half of the warps: keys and queries behind the group's start, and keys decayed to its end, a thread per channel and kind.  Decays of several tokens
+  // are exponentials of sums of their logarithms, always over the tokens between two points (-infinity is like any other number there); a factor e^G is off
+  // by 2^-24 |G| or so of itself, 2^-25 at most.
+  if (tid < NT / 2) {
+    const int kinds = update ? 3 : 2;
+    for (int i = tid; i < kinds * DK; i += NT / 2) {
       const int c = i % DK, what = i / DK, b = c / 8;
       if (what < 2) {
-        const IO(*const raw)[DK] = what ? sm.raw_q : sm.raw_k;
-        float p = what ? a.q_scale : 1.f;
-        float *const to = reinterpret_cast<float *>(&sm.key_query[0][b][c % 8 / 2]) + c % 2 * 2 + what, *const short_of = to + BLOCKS * 36 * 4;
+        const IO(*const rows)[DK] = what ? raw.q : raw.k;
+        const float scale = what ? q_scale : 1.f;
+        float G = 0.f;
+        float *const to = reinterpret_cast<float *>(&op.key_query[0][b][c % 8 / 2]) + c % 2 * 2 + what, *const short_of = to + (DK / 8) * 36 * 4;
 #pragma unroll
         for (int t = 0; t < TB; ++t) {
           float x = 0.f;
-          if (t < cnt && (what == 0 || a.o)) {
-            p *= sm.alpha[t][KDA ? c : 0];
-            x = p * to_float<IO>(raw[t][c]);
+          if (t < cnt && (what == 0 || want)) {
+            G += raw.g[t][KDA ? c : 0];
+            x = __expf(G) * (to_float<IO>(rows[t][c]) * scale);
           }
           const float hi = to_tf32(x);
           to[t * 16] = hi;
           short_of[t * 16] = x - hi;
         }
-      } else if (update) {
-        float d = 1.f, sum = 0.f, hi, lo;
-        float *const to = reinterpret_cast<float *>(&sm.last[b][c % 8 * 4]);
+      } else {
+        float G = 0.f, hi, lo;
+        float *const to = reinterpret_cast<float *>(&op.last[b][c % 8 * 4]);
 #pragma unroll
         for (int t = TB - 1; t >= 0; --t) {
           float x = 0.f;
           if (t < cnt) {
-            x = d * to_float<IO>(sm.raw_k[t][c]);
-            d *= sm.alpha[t][KDA ? c : 0];
-            sum += sm.raw_g[t][KDA ? c : 0];
+            x = __expf(G) * to_float<IO>(raw.k[t][c]);
+            G += raw.g[t][KDA ? c : 0];
           }
           hi = to_tf32(x);
           to[t % 4 * 4 + t / 4] = hi;
           to[t % 4 * 4 + t / 4 + 2] = x - hi;
         }
-        decay_factor(sum, hi, lo);
-        sm.hi[c] = hi;
-        sm.lo[c] = lo;
+        decay_factor(G, hi, lo);
+        op.hi[c] = hi;
+        op.lo[c] = lo;
       }
     }
-    // Products between tokens: a warp has one token t or more; its lanes' parts of the 16 sums fold into one another.
-    constexpr int PER = DK / 32;
-    for (int t = warp; t < TB; t += NT / 32) {
-      float x[2 * TB], k[PER], q[PER], d[PER];
+  } else {
+    // The others: products between tokens.  A warp has one token t or more; its lanes' parts of the 16 sums fold into one another.
+    constexpr int PER = DK / 32, HALF = NT / 64;
+    for (int i = tid - NT / 2; i < cnt * NCOL; i += NT / 2) op.v[i / NCOL][i % NCOL] = to_float<IO>(raw.v[i / NCOL][i % NCOL]);
+    if (tid - NT / 2 < cnt) op.beta[tid - NT / 2] = raw.beta[tid - NT / 2];
+    for (int t = warp - HALF; t < TB; t += HALF) {
+      if (t >= cnt) {
+        if (lane < 2 * TB) (lane < TB ? op.kk : op.qk)[t][lane % TB] = 0.f;
+        continue;
+      }
+      float x[2 * TB], k[PER], q[PER], G[PER];
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
-        k[j] = t < cnt ? to_float<IO>(sm.raw_k[t][lane * PER + j]) : 0.f;
-        q[j] = t < cnt && a.o ? to_float<IO>(sm.raw_q[t][lane * PER + j]) * a.q_scale : 0.f;
-        d[j] = 1.f;
+        k[j] = to_float<IO>(raw.k[t][lane * PER + j]);
+        q[j] = want ? to_float<IO>(raw.q[t][lane * PER + j]) * q_scale : 0.f;
+        G[j] = 0.f;
       }
 #pragma unroll
       for (int s = TB - 1; s >= 0; --s) {
         x[s] = x[TB + s] = 0.f;
-        if (s <= t && t < cnt) {
+        if (s <= t) {
+          float d = __expf(G[0]);
 #pragma unroll
           for (int j = 0; j < PER; ++j) {
-            const float e = d[j] * to_float<IO>(sm.raw_k[s][lane * PER + j]);
+            const float e = (KDA ? __expf(G[j]) : d) * to_float<IO>(raw.k[s][lane * PER + j]);
             x[s] = fmaf(k[j], e, x[s]);
             x[TB + s] = fmaf(q[j], e, x[TB + s]);
-            d[j] *= sm.alpha[s][KDA ? lane * PER + j : 0];
+            G[j] += raw.g[s][KDA ? lane * PER + j : 0];
           }
         }
       }
@@ -393,112 +399,157 @@ __global__ void __launch_bounds__((DraftShape<DK, NCOL>::NT), (512 / DraftShape<
         }
       }
       x[0] += __shfl_xor_sync(0xffffffffu, x[0], 16);
-      if (lane < 2 * TB) (lane < TB ? sm.kk : sm.qk)[t][lane % TB] = lane == t ? 0.f : x[0];
+      if (lane < 2 * TB) (lane < TB ? op.kk : op.qk)[t][lane % TB] = lane == t ? 0.f : x[0];
     }
-    __syncthreads();
-    if (t0 + TB < n)
-      stage(now, t0 + TB);
-    else
-      stage(next, 0);
-    if (t0 == 0 && tid == NT - 1 && next.n > 0 && !next.zero) {  // and its rows of the state come as far as L2
-      if (parts == 1) {
-        bulk_prefetch(state_of(next), DK * NCOL * 4);
-      } else {
-#pragma unroll 1
-        for (int i = 0; i < DK; ++i) asm volatile("prefetch.global.L2 [%0];" ::"l"(state_of(next) + static_cast<int64_t>(i) * a.d_v));
+  }
+}
+
+// A warp's 16 columns of a group, the first of which is `c0` of the block's.  `state(b)` gives its lanes' part of block b, row 2 m in x and row 2 m + 1 in y;
+// `store(b, x, y)` takes what it becomes, where `update`.  Outputs go to `o`, v_stride apart, where `want`.
+template <int DK, int NCOL, typename OT, typename State, typename Store>
+__device__ __forceinline__ void run_group(Operands<DK, NCOL> &op, int cnt, int c0, bool update, bool want, OT *o, int64_t v_stride, State state, Store store) {
+  const int lane = threadIdx.x % 32, m = lane % 4, nn = lane / 4;
+  // S^T (P_t k_t) and S^T (P_t q_t) of token t = nn, columns 4 m .. 4 m + 3
+  float big[2][4] = {}, one[2][4] = {}, two[2][4] = {};
+#pragma unroll
+  for (int b = 0; b < DK / 8; ++b) {
+    const float4 hi = op.key_query[0][b][lane], lo = op.key_query[1][b][lane];
+    float2 row[2];
+    state(b, row[0], row[1]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float x0 = j ? row[0].y : row[0].x, x1 = j ? row[1].y : row[1].x, r0 = to_tf32(x0), r1 = to_tf32(x1);
+      mma_tf32(big[j], hi, r0, r1);
+      mma_tf32(one[j], lo, r0, r1);
+      mma_tf32(two[j], hi, x0 - r0, x1 - r1);
+    }
+  }
+  float x[4], y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int j = i % 2, at = i / 2;
+    x[i] = (one[j][at] + two[j][at]) + big[j][at];
+    y[i] = (one[j][at + 2] + two[j][at + 2]) + big[j][at + 2];
+  }
+  // u_t, one token after the other, and outputs as the u_s come by
+  const int c = c0 + 4 * m;
+  const bool valid = nn < cnt;
+  const float beta = valid ? op.beta[nn] : 0.f;
+  const float4 v = valid ? *reinterpret_cast<const float4 *>(&op.v[nn][c]) : make_float4(0.f, 0.f, 0.f, 0.f);
+  x[0] = beta * (v.x - x[0]), x[1] = beta * (v.y - x[1]), x[2] = beta * (v.z - x[2]), x[3] = beta * (v.w - x[3]);
+#pragma unroll
+  for (int s = 0; s < TB; ++s)
+    if (s < cnt) {
+      const float kk = -beta * op.kk[nn][s], qk = op.qk[nn][s];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float u = __shfl_sync(0xffffffffu, x[i], s * 4 + m);
+        if (nn > s) x[i] = fmaf(kk, u, x[i]);
+        if (nn >= s) y[i] = fmaf(qk, u, y[i]);
       }
     }
+  if (want && valid) {
+    OT *const to = o + nn * v_stride + c;
+    if constexpr (sizeof(OT) == 2) {
+      __nv_bfloat162 p[2] = {__floats2bfloat162_rn(y[0], y[1]), __floats2bfloat162_rn(y[2], y[3])};
+      *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(p);
+    } else {
+      *reinterpret_cast<float4 *>(to) = make_float4(y[0], y[1], y[2], y[3]);
+    }
+  }
+  if (!update) return;
+  *reinterpret_cast<float4 *>(&op.u[nn][c]) = valid ? make_float4(x[0], x[1], x[2], x[3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+  __syncwarp();
+  const float2 ua = *reinterpret_cast<const float2 *>(&op.u[m][c0 + 2 * nn]), ub = *reinterpret_cast<const float2 *>(&op.u[m + 4][c0 + 2 * nn]);
+  const float4 hi = make_float4(to_tf32(ua.x), to_tf32(ua.y), to_tf32(ub.x), to_tf32(ub.y));
+  const float4 lo = make_float4(ua.x - hi.x, ua.y - hi.y, ub.x - hi.z, ub.y - hi.w);
+#pragma unroll
+  for (int b = 0; b < DK / 8; ++b) {
+    const float4 k = op.last[b][lane];
+    float d[4] = {}, e[4] = {};
+    mma_tf32(e, hi, k.z, k.w);
+    mma_tf32(e, lo, k.x, k.y);
+    mma_tf32(d, hi, k.x, k.y);
+    const float2 ph = *reinterpret_cast<const float2 *>(&op.hi[8 * b + 2 * m]), pl = *reinterpret_cast<const float2 *>(&op.lo[8 * b + 2 * m]);
+    float2 s0, s1;
+    state(b, s0, s1);
+    // (the tensor cores' own sums start from zero: they would cut the state's last bit off)
+    store(b, make_float2(fmaf(s0.x, ph.x, fmaf(s0.x, pl.x, e[0] + d[0])), fmaf(s0.y, ph.x, fmaf(s0.y, pl.x, e[2] + d[2]))),
+          make_float2(fmaf(s1.x, ph.y, fmaf(s1.x, pl.y, e[1] + d[1])), fmaf(s1.y, ph.y, fmaf(s1.y, pl.y, e[3] + d[3]))));
+  }
+}
 
-    if (!holds) continue;
-    // S^T (P_t k_t) and S^T (P_t q_t) of token t = nn, columns 4 m .. 4 m + 3
-    float big[2][4] = {}, one[2][4] = {}, two[2][4] = {};
+// A thread block goes from state to state; a group's rows are on their way, and the next state in L2, while the ones before are worked on.
+template <int DK, int NCOL, bool KDA, typename IO, typename OT>
+__global__ void __launch_bounds__((DraftShape<DK, NCOL>::NT), (512 / DraftShape<DK, NCOL>::NT)) delta_draft_kernel(const __grid_constant__ DascDeltaArgs a) {
+  using Sh = DraftShape<DK, NCOL>;
+  using Sm = DraftSmem<DK, NCOL, KDA, IO>;
+  constexpr int NT = Sh::NT, BLOCKS = Sh::BLOCKS;
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
+  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, m = lane % 4, nn = lane / 4;
+  const JobWalk<DK, NCOL> walk(a);
+  const int dv = walk.dv, v_stride = a.H_v * dv;
+  const bool write = !a.score, holds = warp < Sh::WARPS;
+  auto stage = [&](const Job &x, int t0) { copy_rows<DK, NCOL, KDA, IO, NT>(sm.raw, a, x, min(TB, x.n - t0), t0); };
+  stream_order_wait();
+
+  Job now = walk.first();
+  stage(now, 0);
+  while (now.r < a.n_req) {
+    const Job next = walk.after(now);
+    const int n = now.n;
+    float *const st = walk.state_of(now) + 2 * m * dv + warp * 16 + 2 * nn;
+    OT *const go = static_cast<OT *>(a.o) + ((static_cast<int64_t>(now.lc) * a.total_tokens + now.begin) * a.H_v + now.h) * dv + now.part * NCOL;
+    float2 S[BLOCKS][2];  // row 8 b + 2 m and the one behind it, columns 2 nn and 2 nn + 1; not looked at before the products
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) {
-      const float4 hi = sm.key_query[0][b][lane], lo = sm.key_query[1][b][lane];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float2 x = dunpack2(S[b][j]);
-        const float x0 = to_tf32(x.x), x1 = to_tf32(x.y);
-        mma_tf32(big[j], hi, x0, x1);
-        mma_tf32(one[j], lo, x0, x1);
-        mma_tf32(two[j], hi, x.x - x0, x.y - x1);
+      S[b][0] = S[b][1] = make_float2(0.f, 0.f);
+      if (holds && !now.zero && n > 0) {
+        S[b][0] = *reinterpret_cast<const float2 *>(st + 8 * b * dv);
+        S[b][1] = *reinterpret_cast<const float2 *>(st + (8 * b + 1) * dv);
       }
     }
-    float x[4], y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int j = i % 2, at = i / 2;
-      x[i] = (one[j][at] + two[j][at]) + big[j][at];
-      y[i] = (one[j][at + 2] + two[j][at + 2]) + big[j][at + 2];
-    }
-    // u_t, one token after the other, and outputs as the u_s come by
-    const int c = warp * 16 + 4 * m;
-    const bool valid = nn < cnt;
-    const float beta = valid ? sm.beta[nn] : 0.f;
-    const float4 v = valid ? *reinterpret_cast<const float4 *>(&sm.v[nn][c]) : make_float4(0.f, 0.f, 0.f, 0.f);
-    x[0] = beta * (v.x - x[0]), x[1] = beta * (v.y - x[1]), x[2] = beta * (v.z - x[2]), x[3] = beta * (v.w - x[3]);
-    float kk[TB], qk[TB];
-    *reinterpret_cast<float4 *>(kk) = *reinterpret_cast<const float4 *>(&sm.kk[nn][0]);
-    *reinterpret_cast<float4 *>(kk + 4) = *reinterpret_cast<const float4 *>(&sm.kk[nn][4]);
-    *reinterpret_cast<float4 *>(qk) = *reinterpret_cast<const float4 *>(&sm.qk[nn][0]);
-    *reinterpret_cast<float4 *>(qk + 4) = *reinterpret_cast<const float4 *>(&sm.qk[nn][4]);
-#pragma unroll
-    for (int s = 0; s < TB; ++s)
-      if (s < cnt) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float u = __shfl_sync(0xffffffffu, x[i], s * 4 + m);
-          if (nn > s) x[i] = fmaf(-beta * kk[s], u, x[i]);
-          if (nn >= s) y[i] = fmaf(qk[s], u, y[i]);
+    for (int t0 = 0; t0 < n; t0 += TB) {
+      const int cnt = min(TB, n - t0);
+      const bool update = write || t0 + TB < n;
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncthreads();
+      prepare<DK, NCOL, KDA, IO, NT>(sm.op, sm.raw, cnt, update, a.o != nullptr, a.q_scale);
+      __syncthreads();
+      if (t0 + TB < n) {
+        stage(now, t0 + TB);
+      } else {
+        stage(next, 0);
+        if (next.n > 0 && !next.zero) {
+          if (NCOL == 128) {
+            if (tid == 0) bulk_prefetch(walk.state_of(next), DK * NCOL * 4);
+          } else {
+            for (int i = tid; i < DK; i += NT) asm volatile("prefetch.global.L2 [%0];" ::"l"(walk.state_of(next) + i * dv));
+          }
         }
       }
-    if (a.o && valid) {
-      OT *const to = go + (t0 + nn) * v_stride + c;
-      if constexpr (sizeof(OT) == 2) {
-        __nv_bfloat162 p[2] = {__floats2bfloat162_rn(y[0], y[1]), __floats2bfloat162_rn(y[2], y[3])};
-        *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(p);
-      } else {
-        *reinterpret_cast<float4 *>(to) = make_float4(y[0], y[1], y[2], y[3]);
-      }
+      if (holds)
+        run_group<DK, NCOL>(
+            sm.op, cnt, warp * 16, update, a.o != nullptr, go + static_cast<int64_t>(t0) * v_stride, v_stride,
+            [&](int b, float2 &x, float2 &y) { x = S[b][0], y = S[b][1]; }, [&](int b, float2 x, float2 y) { S[b][0] = x, S[b][1] = y; });
     }
-    if (update) {
-      *reinterpret_cast<float4 *>(&sm.u[nn][c]) = valid ? make_float4(x[0], x[1], x[2], x[3]) : make_float4(0.f, 0.f, 0.f, 0.f);
-      __syncwarp();
-      const float2 ua = *reinterpret_cast<const float2 *>(&sm.u[m][warp * 16 + 2 * nn]), ub = *reinterpret_cast<const float2 *>(&sm.u[m + 4][warp * 16 + 2 * nn]);
-      const float4 hi = make_float4(to_tf32(ua.x), to_tf32(ua.y), to_tf32(ub.x), to_tf32(ub.y));
-      const float4 lo = make_float4(ua.x - hi.x, ua.y - hi.y, ub.x - hi.z, ub.y - hi.w);
+    if (n == 0) stage(next, 0);
+    if (holds && write && (n > 0 || (now.zero && now.req >= 0))) {
 #pragma unroll
       for (int b = 0; b < BLOCKS; ++b) {
-        const float4 k = sm.last[b][lane];
-        float d[4] = {}, e[4] = {};
-        mma_tf32(e, hi, k.z, k.w);
-        mma_tf32(e, lo, k.x, k.y);
-        mma_tf32(d, hi, k.x, k.y);
-        const float2 ph = *reinterpret_cast<const float2 *>(&sm.hi[8 * b + 2 * m]), pl = *reinterpret_cast<const float2 *>(&sm.lo[8 * b + 2 * m]);
-        const uint64_t h2 = dpack2(ph.x, ph.y), l2 = dpack2(pl.x, pl.y);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)  // (the tensor cores' own sums start from zero: they would cut the state's last bit off)
-          S[b][j] = dfma2(S[b][j], h2, dfma2(S[b][j], l2, dpack2(e[2 * j] + d[2 * j], e[2 * j + 1] + d[2 * j + 1])));
+        *reinterpret_cast<float2 *>(st + 8 * b * dv) = S[b][0];
+        *reinterpret_cast<float2 *>(st + (8 * b + 1) * dv) = S[b][1];
       }
     }
-  }
-  if (n == 0) stage(next, 0);
-  if (holds && write && (n > 0 || (now.zero && now.req >= 0))) {
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) {
-      const float2 x = dunpack2(S[b][0]), y = dunpack2(S[b][1]);
-      *reinterpret_cast<float2 *>(st + static_cast<int64_t>(8 * b) * a.d_v) = make_float2(x.x, y.x);
-      *reinterpret_cast<float2 *>(st + static_cast<int64_t>(8 * b + 1) * a.d_v) = make_float2(x.y, y.y);
-    }
-  }
-  now = next;
+    now = next;
   }
 }
 
 template <int DK, int NCOL, bool KDA, typename IO, typename OT>
 int launch(const DascDeltaArgs &a, void *stream) {
   const int64_t blocks = static_cast<int64_t>(a.n_req) * a.n_layers_in_call * a.H_v * (a.d_v / NCOL);
-  if (blocks > 2147483647LL) return static_cast<int>(cudaErrorInvalidConfiguration);
+  if (blocks > 2147483647LL || static_cast<int64_t>(a.H_v) * (a.d_k > a.d_v ? a.d_k : a.d_v) > 2147483647LL / 16) return static_cast<int>(cudaErrorInvalidConfiguration);
   const dim3 grid(static_cast<unsigned>(blocks));
   if constexpr (NCOL < 128)
     if (!a.cu_seqlens) return static_cast<int>(launch_blocks(delta_step_kernel<DK, NCOL, KDA, IO, OT>, grid, dim3(kThreads<DK, NCOL>), 0, stream, a));
@@ -516,7 +567,7 @@ int launch(const DascDeltaArgs &a, void *stream) {
 template <int DK, bool KDA, typename IO, typename OT>
 int launch_cols(const DascDeltaArgs &a, void *stream) {
   const int64_t units = static_cast<int64_t>(a.n_req) * a.n_layers_in_call * a.H_v;
-  if (a.cu_seqlens && a.d_v % 128 == 0 && units * (a.d_v / 128) >= 2 * 148) return launch<DK, 128, KDA, IO, OT>(a, stream);
+  if (a.cu_seqlens && a.d_v == 128 && units >= 2 * 148) return launch<DK, 128, KDA, IO, OT>(a, stream);
   if (a.d_v % 64 == 0 && units * (a.d_v / 64) >= 2 * 148) return launch<DK, 64, KDA, IO, OT>(a, stream);
   return launch<DK, 32, KDA, IO, OT>(a, stream);
 }
