@@ -79,10 +79,11 @@ struct SelectSmem {
   double lse[MAXW];
   float score[MAXW];
   int ended[MAXW];
+  int counts[MAXW];  // the beams whose rows count
   float warp_top[MAXW][NW], warp_sum[MAXW][NW];  // the warps' shares of each of this block's segments
   uint32_t best_of[NT], bound;  // 16 or 32 bits of order of each thread's largest value
   int n_hits[MAXW], odd[MAXW];  // of each of this block's segments
-  int n_above, n_entries, n_left;
+  int n_above, n_entries, n_left, n_rows;
   unsigned long long any_bit, all_bits;
   uint16_t chunk[CHUNKS][NT];   // the largest entry of each thread's chunks, 16 bits of order32
 };
@@ -377,23 +378,29 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
   const int W = a.width, N = a.n_out;
   stream_order_begin();
 
-  if (tid < W) {
-    const float score = a.scores[static_cast<int64_t>(r) * W + tid];
-    sm.score[tid] = score;
+  if (tid < 32) {
+    const float score = tid < W ? a.scores[static_cast<int64_t>(r) * W + tid] : kNone;
     // 0: its row counts, 1: it has ended, 2: it has no continuation
-    sm.ended[tid] = !finite(score) ? 2 : a.ended && a.ended[static_cast<int64_t>(r) * W + tid] != 0 ? 1 : 0;
+    const int ended = !finite(score) ? 2 : a.ended && a.ended[static_cast<int64_t>(r) * W + tid] != 0 ? 1 : 0;
+    const uint32_t rows = __ballot_sync(0xffffffffu, ended == 0);
+    const int place = __popc(rows & ((1u << tid) - 1u));
+    sm.score[tid] = score;
+    sm.ended[tid] = ended;
+    if (ended == 0) sm.counts[place] = tid;
+    if (tid == 0) sm.n_rows = __popc(rows);
   }
   if (tid < MAXW) sm.n_hits[tid] = sm.odd[tid] = 0;
   if (tid == 0) sm.n_entries = sm.n_left = 0;
   __syncthreads();
 
-  const int first = min(rank * a.per_block, W * a.segments), last = min(first + a.per_block, W * a.segments);
+  // the segments of the rows that count, shared out over the cluster's blocks
+  const int items = sm.n_rows * a.segments, per_block = max((items + CL - 1) / CL, 1);
+  const int first = min(rank * per_block, items), last = min(first + per_block, items);
   const int each = (a.segment_len + Rd::SIZE * CHUNKS - 1) / (Rd::SIZE * CHUNKS);  // rounds per chunk
   auto row_of = [&](int item) {
-    return static_cast<const T *>(a.logits) + (static_cast<int64_t>(r) * W + item / a.segments) * a.stride + item % a.segments * a.segment_len;
+    return static_cast<const T *>(a.logits) + (static_cast<int64_t>(r) * W + sm.counts[item / a.segments]) * a.stride + item % a.segments * a.segment_len;
   };
   for (int item = first; item < last; ++item) {
-    if (sm.ended[item / a.segments]) continue;  // (the same for the whole block)
     const int from = item % a.segments * a.segment_len, len = min(a.segment_len, a.vocab - from);
     const T *const row = row_of(item);
     // One pass over the segment: this thread's largest logit and its sum of exponentials, and the largest of each chunk of its entries.
@@ -454,8 +461,7 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
     }
     __syncthreads();
   }
-  for (int item = first + warp; item < last; item += NW)
-    if (!sm.ended[item / a.segments]) join_sums(sm, item - first, item, sm.odd[item - first]);
+  for (int item = first + warp; item < last; item += NW) join_sums(sm, item - first, item, sm.odd[item - first]);
 
   // The first block takes the hits and sums of all of them.
   cg::cluster_group cluster = cg::this_cluster();
@@ -463,20 +469,19 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
   Entry *const entry = reinterpret_cast<Entry *>(hit + (a.per_block * a.budget + 1) / 2 * 2);
   uint64_t mine = 0;  // this thread's best total
   if (rank == 0) {
-    for (int b = warp; b < W; b += NW)
-      if (sm.ended[b] == 0) {
-        const int item = b * a.segments + lane, c = item / a.per_block;
-        double ref = -INFINITY, x = 0.0, top;
-        if (lane < a.segments) {
-          ref = cluster.map_shared_rank(sm.reference, c)[item];
-          x = cluster.map_shared_rank(sm.sum, c)[item];
-        }
-        x = add_up(ref, x, top);
-        if (lane == 0) sm.lse[b] = top + log(x);
+    for (int row = warp; row < sm.n_rows; row += NW) {
+      const int item = row * a.segments + lane, c = item / per_block;
+      double ref = -INFINITY, x = 0.0, top;
+      if (lane < a.segments) {
+        ref = cluster.map_shared_rank(sm.reference, c)[item];
+        x = cluster.map_shared_rank(sm.sum, c)[item];
       }
+      x = add_up(ref, x, top);
+      if (lane == 0) sm.lse[sm.counts[row]] = top + log(x);
+    }
     __syncthreads();
-    for (int item = warp; item < W * a.segments; item += NW) {
-      const int c = item / a.per_block, local = item % a.per_block, b = item / a.segments, n = cluster.map_shared_rank(sm.n_hits, c)[local];
+    for (int item = warp; item < items; item += NW) {
+      const int c = item / per_block, local = item % per_block, b = sm.counts[item / a.segments], n = cluster.map_shared_rank(sm.n_hits, c)[local];
       int to = 0;
       if (lane == 0 && n > 0) to = atomicAdd(&sm.n_entries, n);
       to = __shfl_sync(0xffffffffu, to, 0);

@@ -20,7 +20,7 @@ def inputs(seed, R, W, V, dtype, spread=2.5):
 @TYPES
 @pytest.mark.parametrize("R, W, V, n", [(1, 1, 1, 1), (2, 3, 5, 4), (1, 4, 31, 8), (3, 2, 1000, 4), (1, 4, 32000, 4), (2, 5, 50257, 10), (1, 8, 131072, 16),
                                         (1, 32, 16385, 64), (1, 3, 300007, 33), (40, 4, 4099, 8), (80, 4, 20000, 4), (150, 2, 40001, 17), (300, 3, 2003, 6),
-                                        (1, 16, 70000, 32), (5, 7, 16384, 7), (2, 1, 40, 64)])
+                                        (1, 16, 70000, 32), (5, 7, 16384, 7), (2, 1, 40, 64), (150, 32, 501, 64), (3, 32, 40000, 64)])
 def test_select(dtype, R, W, V, n):
     x, s = inputs(R + W, R, W, V, dtype)
     bh.same(bh.call(x, s, n), bh.define(x, s, None, -1, n), x)
@@ -116,6 +116,33 @@ def test_scores_of_the_best_are_those_of_log_softmax():
     assert torch.equal(got[1].long() * 91234 + got[2].long(), at)
     # half a step of fp32, and a sum of exponentials: arguments of up to 16 rounded twice (2^-19), ex2 2^-22, 13 additions in fp32 (2^-20)
     assert float((got[0].double() - value).abs().max()) <= 2.0 ** -18 + float(value.abs().max()) * 2.0 ** -24
+
+
+@TYPES
+@pytest.mark.parametrize("V", [40000, 70001])
+def test_good_tokens_side_by_side(dtype, V):
+    """A grammar that leaves neighbours only, as -inf and as low values; logits that rise with the token; plateaus higher than what is wanted."""
+    x, s = inputs(11, 6, 3, V, dtype)
+    low = -1e30
+    x[0, :, :9000] = -float("inf")
+    x[0, :, 9150:] = -float("inf")
+    x[1, :, :9000] = low
+    x[1, :, 9150:] = low
+    x[2] = torch.arange(V, device="cuda").mul(1e-3).to(dtype)
+    x[3] = torch.arange(V, 0, -1, device="cuda").mul(1e-3).to(dtype)
+    x[4] = x[4].clamp(min=0.5)
+    x[5] = x[5].clamp(max=0.5)
+    for n in (4, 64):
+        got, want = bh.call(x, s, n), bh.define(x, s, None, -1, n)
+        bh.same(got, want, x)
+
+
+def test_beams_that_have_ended_in_every_place():
+    """What is shared out over a request's thread blocks are the rows that count."""
+    x, s = inputs(12, 32, 5, 9000, torch.float32)
+    ended = [[r >> b & 1 for b in range(5)] for r in range(32)]
+    for n in (5, 12):
+        bh.same(bh.call(x, s, n, ended, 7), bh.define(x, s, ended, 7, n), x)
 
 
 def test_equal_calls_give_equal_bits():
