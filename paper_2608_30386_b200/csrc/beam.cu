@@ -581,8 +581,10 @@ int select_type(const DascBeamSelectArgs &a, void *stream) {
     constexpr int CL = decltype(cl)::value;
     return vec ? select<T, true, CL>(a, stream) : select<T, false, CL>(a, stream);
   };
-  constexpr int kPlaces = 2 * 148;
-  constexpr int kClustered = kPlaces * 7 / 8;  // (not every GPC holds a whole number of clusters of 4 or 8)
+  // As many blocks per request as still fit the GPU at once, two per SM (not every GPC holds a whole number of clusters of 4 or 8).  4 beams over 65,536 entries
+  // in bf16, us with 8 / 4 / 2 / 1 blocks: 1 request 9.4 / 10.1 / 14.3 / 22.7, 37 requests 17.5 / 14.4 / 15.0 / 23.4, 64 requests 22.8 / 14.6 / 21.2 / 30.1, 148 requests
+  // 45.6 / 31.1 / 22.5 / 25.6, 296 requests 90 / 58 / 45 / 42.
+  constexpr int kPlaces = 2 * 148, kClustered = kPlaces * 7 / 8;
   if (a.n_req * int64_t{8} <= kClustered) return with(std::integral_constant<int, 8>{});
   if (a.n_req * int64_t{4} <= kClustered) return with(std::integral_constant<int, 4>{});
   if (a.n_req * int64_t{2} <= kPlaces) return with(std::integral_constant<int, 2>{});
@@ -591,24 +593,26 @@ int select_type(const DascBeamSelectArgs &a, void *stream) {
 
 // ---- reordering --------------------------------------------------------------------------------------------------------------
 
-constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyTile = kCopyThreads * kCopyUnroll;  // vectors of 16 bytes per round of a block
+// A thread block copies one tile of 16 KB of every fork of its request.  More of them per block are slower: two forks in each of 16 requests over 24 layers of 32 heads
+// (both from one beam) with 1 / 2 / 4 / 8 tiles 350 / 361 / 420 / 485 us, one request with one fork 13.9 / 13.4 / 14.2 / 14.6.
+constexpr int kCopyThreads = 256, kCopyUnroll = 4, kCopyTile = kCopyThreads * kCopyUnroll;  // vectors of 16 bytes
 
-__device__ __forceinline__ void copy_range(const uint4 *src, uint4 *dst, uint32_t begin, uint32_t end) {
-  for (uint32_t base = begin + threadIdx.x; base < end; base += kCopyTile) {
-    uint4 v[kCopyUnroll];
+// this block's vectors of a tile that ends at `end`
+__device__ __forceinline__ void copy_tile(const uint4 *src, uint4 *dst, uint32_t begin, uint32_t end) {
+  const uint32_t base = begin + threadIdx.x;
+  uint4 v[kCopyUnroll];
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u)
-      if (base + u * kCopyThreads < end)
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                     : "=r"(v[u].x), "=r"(v[u].y), "=r"(v[u].z), "=r"(v[u].w)
-                     : "l"(src + base + u * kCopyThreads));
+  for (int u = 0; u < kCopyUnroll; ++u)
+    if (base + u * kCopyThreads < end)
+      asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                   : "=r"(v[u].x), "=r"(v[u].y), "=r"(v[u].z), "=r"(v[u].w)
+                   : "l"(src + base + u * kCopyThreads));
 #pragma unroll
-    for (int u = 0; u < kCopyUnroll; ++u)
-      if (base + u * kCopyThreads < end)
-        asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(dst + base + u * kCopyThreads), "r"(v[u].x), "r"(v[u].y),
-                     "r"(v[u].z), "r"(v[u].w)
-                     : "memory");
-  }
+  for (int u = 0; u < kCopyUnroll; ++u)
+    if (base + u * kCopyThreads < end)
+      asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(dst + base + u * kCopyThreads), "r"(v[u].x), "r"(v[u].y),
+                   "r"(v[u].z), "r"(v[u].w)
+                   : "memory");
 }
 
 __global__ void __launch_bounds__(kCopyThreads) beam_reorder_kernel(const __grid_constant__ DascBeamReorderArgs a) {
@@ -645,13 +649,12 @@ __global__ void __launch_bounds__(kCopyThreads) beam_reorder_kernel(const __grid
     const int64_t s = __shfl_sync(0xffffffffu, src, i), d = __shfl_sync(0xffffffffu, dst, i);
     if (piece < state_pieces) {
       const int64_t layer = (a.layer_begin + static_cast<int64_t>(piece / a.layer_pieces)) * a.layer_stride;
-      const uint32_t begin = piece % a.layer_pieces * a.piece_vecs;
-      copy_range(reinterpret_cast<const uint4 *>(a.state + s * a.req_stride + layer), reinterpret_cast<uint4 *>(a.state + d * a.req_stride + layer), begin,
-                 min(begin + a.piece_vecs, a.layer_vecs));
+      const uint32_t begin = piece % a.layer_pieces * kCopyTile;
+      copy_tile(reinterpret_cast<const uint4 *>(a.state + s * a.req_stride + layer), reinterpret_cast<uint4 *>(a.state + d * a.req_stride + layer), begin,
+                a.layer_vecs);
     } else if (a.conv_vecs) {
-      const uint32_t begin = (piece - state_pieces) * a.piece_vecs;
-      copy_range(reinterpret_cast<const uint4 *>(static_cast<const char *>(a.conv) + s * a.conv_stride),
-                 reinterpret_cast<uint4 *>(static_cast<char *>(a.conv) + d * a.conv_stride), begin, min(begin + a.piece_vecs, a.conv_vecs));
+      copy_tile(reinterpret_cast<const uint4 *>(static_cast<const char *>(a.conv) + s * a.conv_stride),
+                reinterpret_cast<uint4 *>(static_cast<char *>(a.conv) + d * a.conv_stride), (piece - state_pieces) * kCopyTile, a.conv_vecs);
     }
   }
 }
@@ -663,12 +666,8 @@ int dasc_launch_beam_select(const DascBeamSelectArgs &a, void *stream) {
 }
 
 int dasc_launch_beam_reorder(DascBeamReorderArgs a, void *stream) {
-  // Pieces of a request's states: small ones where there is little to copy, so that all SMs have some
-  const int64_t layer_vecs = a.state ? a.layer_vecs : 0, all = a.n_layers_in_call * layer_vecs + a.conv_vecs;
-  const int64_t rounds = std::max(int64_t{1}, std::min(int64_t{8}, a.n_req * all / (int64_t{kCopyTile} * 148 * 32)));
-  a.piece_vecs = static_cast<uint32_t>(rounds * kCopyTile);
-  a.layer_pieces = static_cast<uint32_t>((layer_vecs + a.piece_vecs - 1) / a.piece_vecs);
-  const int64_t conv_pieces = (a.conv_vecs + a.piece_vecs - 1) / a.piece_vecs;
+  const int64_t layer_vecs = a.state ? a.layer_vecs : 0, conv_pieces = (a.conv_vecs + kCopyTile - 1) / kCopyTile;
+  a.layer_pieces = static_cast<uint32_t>((layer_vecs + kCopyTile - 1) / kCopyTile);
   const int64_t pieces = std::max(int64_t{1}, static_cast<int64_t>(a.n_layers_in_call) * a.layer_pieces + conv_pieces);
   if (pieces * a.n_req > 2147483647LL) return static_cast<int>(cudaErrorInvalidConfiguration);
   a.pieces = static_cast<uint32_t>(pieces);

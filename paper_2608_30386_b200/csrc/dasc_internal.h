@@ -223,6 +223,6 @@ struct DascBeamReorderArgs {
   int32_t n_req, width, layer_begin, n_layers_in_call;
   int32_t *new_idx, *src_idx;
   uint32_t layer_vecs, conv_vecs;                   // vectors of 16 bytes
-  uint32_t piece_vecs, layer_pieces, pieces;        // set by the launcher: what a thread block copies of each state
+  uint32_t layer_pieces, pieces;                    // set by the launcher: tiles of a layer's state, and of all of a request's
 };
 int dasc_launch_beam_reorder(DascBeamReorderArgs a, void *stream);
