@@ -969,7 +969,8 @@ dasc_status_t delta_validate(const dasc_plan_t *plan, float *state_base, int64_t
   if (o && o_dtype != DASC_IO_BF16 && o_dtype != DASC_IO_FP32) return DASC_ERR_INVALID_ARG;
   if (!decay_shape_ok(plan)) return DASC_ERR_SHAPE;
   const int32_t layers = layer_end - layer_begin;
-  if (total_tokens > INT32_MAX || static_cast<double>(n_req) * layers * plan->info.n_v_heads * (plan->info.d_v / 32) > INT32_MAX)
+  if (total_tokens > INT32_MAX || static_cast<double>(n_req) * layers * plan->info.n_v_heads * (plan->info.d_v / 32) > INT32_MAX ||
+      static_cast<double>(plan->info.n_v_heads) * std::max(plan->info.d_k, plan->info.d_v) > INT32_MAX / 16)  // (32-bit offsets between eight tokens)
     return DASC_ERR_SHAPE;
   if (n_req == 0 || layers == 0) return DASC_OK;
   if (!state_base || !req_idx || !aligned16(state_base)) return DASC_ERR_INVALID_ARG;
@@ -1117,6 +1118,7 @@ dasc_status_t dasc_beam_reorder(const dasc_plan_t *plan, float *state_base, int6
     a.conv_stride = conv_stride_bytes;
     a.conv_vecs = static_cast<uint32_t>(conv_bytes / 16);
   }
+  if ((a.layer_vecs / 1024.0 + 1) * layers * n_req + (a.conv_vecs / 1024.0 + 1) * n_req > INT32_MAX) return DASC_ERR_SHAPE;  // (thread blocks)
   if (const dasc_status_t ds = check_device(plan); ds != DASC_OK) return ds;
   a.req_idx = req_idx;
   a.parent = parent;

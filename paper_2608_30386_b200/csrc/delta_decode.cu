@@ -1,18 +1,24 @@
-// The gated delta rule in serving, in fp32 on the CUDA cores: one token per request (decoding), and a few drafted tokens.
+// The gated delta rule in serving: one token per request (decoding), and a few drafted tokens.
 //     S <- Diag(a_t) S,   u_t = beta_t (v_t - S^T k_t),   S <- S + k_t u_t^T,   o_t = q_scale S^T q_t
 // a_t is a vector over the key channels (KDA) or one number (GDN).
 //
-// One token: with r = S^T (a k) and y = S^T (a q) in one pass over the state, u = beta (v - r), o = q_scale (y + (k . q) u),
+// One token, in fp32 on the CUDA cores: with r = S^T (a k) and y = S^T (a q) in one pass over the state, u = beta (v - r), o = q_scale (y + (k . q) u),
 // and the new state is a S + k u^T on its way to memory.  The old state stays in registers, so beams that continue the same state read it once.
+// Bound: bytes of the state (128 KB read and written per 128 x 128 head).  256 requests x 32 heads: 172 us, 98 % of the measured copy rate of 6462 GB/s; 32 x 8
+// beams, 5.25 of 8 states read on average: 158 us, 88 % (the blocks of beams that share a source have up to eight times the work of others); one request: 2.7 us.
 //
-// Several tokens go through the state together.  P_t is the product of a group's decays up to token t, D_ts of those behind s up to t:
+// Several tokens go through the state together, in groups of TB.  P_t is the product of a group's decays up to token t, D_ts of those behind s up to t:
 //     u_t = beta_t (v_t - S^T (P_t k_t) - sum_{s < t} (k_t . D_ts k_s) u_s)
 //     o_t = q_scale (S^T (P_t q_t) + sum_{s <= t} (q_t . D_ts k_s) u_s),      S <- P_n S + sum_s (D_ns k_s) u_s^T
 // so that the sums over the state's rows of all tokens are independent of one another, and only sums over at most TB values per column are a chain.
-// Decays multiply, they are not differences of sums: exp(-inf) is a zero like any other.
+// The sums over rows and the update are products on the tensor cores; the state is held in fp32.
+// Bound: 5 tokens of 64 requests x 32 heads take 54 us scored and 80 us advanced (their bytes 23 and 42).  A block's steps follow one another: without the
+// products it is 43 us, without the preparation of operands 43 us, without reading states 40 us, with the reading alone 31 us; two blocks per SM, each
+// with its state in 64 registers of 256 threads, overlap little of that.  Tried and slower: multiply-adds on the CUDA cores (60 / 73 us: more instructions), states in shared
+// memory ahead of their use (57 / 88), preparation and products in warps of their own with a block per SM (73 / 115: the preparation
+// is a chain of latencies), states read twice instead of held, with four blocks per SM (50 / 104).
 //
-// Split: columns of the state do not interact, so a thread block owns NCOL columns of one (request, layer, head) state, all of it in
-// registers: a thread holds ROWS rows of four columns; sums over rows meet in shared memory in a fixed order.
+// Split: columns of the state do not interact, so a thread block owns NCOL columns of one (request, layer, head) state.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -53,9 +59,7 @@ __device__ __forceinline__ void decay_factor(float g, float &hi, float &lo) {
   lo = slow ? d - (a1 - 1.f) : 0.f;
 }
 
-// 128 x 128 values are held by 256 threads, all else by 128: at most 64 registers of state per thread
-template <int DK, int NCOL>
-constexpr int kThreads = DK * NCOL > 128 * 64 ? 256 : 128;
+constexpr int kStepThreads = 128;  // of a block for single tokens: at most 64 registers of state per thread
 
 struct Unit {
   int part, h, hk, lc, r;
@@ -73,7 +77,7 @@ __device__ __forceinline__ Unit unit_of(const DascDeltaArgs &a, int ncol) {
 
 template <int DK, int NCOL>
 struct StepSmem {
-  static constexpr int RG = kThreads<DK, NCOL> / (NCOL / 4);
+  static constexpr int RG = kStepThreads / (NCOL / 4);
   // each value twice: operands of the packed instructions
   alignas(16) uint64_t ak[DK], aq[DK], k[DK], hi[DK], lo[DK];
   alignas(16) float part[2][RG][NCOL];
@@ -82,8 +86,8 @@ struct StepSmem {
 };
 
 template <int DK, int NCOL, bool KDA, typename IO, typename OT>
-__global__ void __launch_bounds__((kThreads<DK, NCOL>)) delta_step_kernel(const __grid_constant__ DascDeltaArgs a) {
-  constexpr int NT = kThreads<DK, NCOL>, LPR = NCOL / 4, RG = NT / LPR, ROWS = DK / RG;
+__global__ void __launch_bounds__(kStepThreads) delta_step_kernel(const __grid_constant__ DascDeltaArgs a) {
+  constexpr int NT = kStepThreads, LPR = NCOL / 4, RG = NT / LPR, ROWS = DK / RG;
   __shared__ StepSmem<DK, NCOL> sm;
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, cg = tid % LPR, rg = tid / LPR;
   const Unit un = unit_of(a, NCOL);
@@ -274,12 +278,12 @@ struct JobWalk {
     return y;
   }
   __device__ __forceinline__ float *state_of(const Job &x) const {
-    return a.state + x.req * a.req_stride + (a.layer_begin + x.lc) * a.layer_stride + (x.h * DK * dv + x.part * NCOL);
+    return a.state + x.req * a.req_stride + (a.layer_begin + x.lc) * a.layer_stride + (static_cast<int64_t>(x.h) * DK * dv + x.part * NCOL);
   }
 };
 
 // The rows of `cnt` tokens of a job from token t0 on, as they are, 16 bytes per copy, by NT threads (the first ones of the block; offsets between eight
-// tokens are below 2^31: launch).
+// tokens are below 2^31: the caller has looked).
 template <int DK, int NCOL, bool KDA, typename IO, int NT>
 __device__ __forceinline__ void copy_rows(RawRows<DK, NCOL, KDA, IO> &raw, const DascDeltaArgs &a, const Job &x, int cnt, int t0) {
   const int tid = threadIdx.x, dv = NCOL == 128 ? 128 : a.d_v, group = a.H_v / a.H_k, v_stride = a.H_v * dv;
@@ -549,10 +553,10 @@ __global__ void __launch_bounds__((DraftShape<DK, NCOL>::NT), (512 / DraftShape<
 template <int DK, int NCOL, bool KDA, typename IO, typename OT>
 int launch(const DascDeltaArgs &a, void *stream) {
   const int64_t blocks = static_cast<int64_t>(a.n_req) * a.n_layers_in_call * a.H_v * (a.d_v / NCOL);
-  if (blocks > 2147483647LL || static_cast<int64_t>(a.H_v) * (a.d_k > a.d_v ? a.d_k : a.d_v) > 2147483647LL / 16) return static_cast<int>(cudaErrorInvalidConfiguration);
+  if (blocks > 2147483647LL) return static_cast<int>(cudaErrorInvalidConfiguration);
   const dim3 grid(static_cast<unsigned>(blocks));
   if constexpr (NCOL < 128)
-    if (!a.cu_seqlens) return static_cast<int>(launch_blocks(delta_step_kernel<DK, NCOL, KDA, IO, OT>, grid, dim3(kThreads<DK, NCOL>), 0, stream, a));
+    if (!a.cu_seqlens) return static_cast<int>(launch_blocks(delta_step_kernel<DK, NCOL, KDA, IO, OT>, grid, dim3(kStepThreads), 0, stream, a));
   constexpr size_t smem = sizeof(DraftSmem<DK, NCOL, KDA, IO>);
   auto kernel = delta_draft_kernel<DK, NCOL, KDA, IO, OT>;
   if (smem > 48 * 1024) {

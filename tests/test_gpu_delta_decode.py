@@ -22,6 +22,14 @@ def test_step(kind, d_k, d_v, H_v, H_k, n, dtype, o_dtype):
 
 
 @KINDS
+@pytest.mark.parametrize("d_k, d_v, H_v, H_k, n", [(128, 128, 16, 8, 80), (64, 256, 8, 8, 80), (32, 64, 32, 32, 76), (64, 64, 32, 16, 75)])
+def test_step_of_many_states(kind, d_k, d_v, H_v, H_k, n):
+    """Enough states for the wider parts."""
+    case = dh.make_case(n, [1] * n, kind=kind, H_v=H_v, H_k=H_k, d_k=d_k, d_v=d_v)
+    dh.check(case, dh.step(case, o_dtype=torch.bfloat16), dh.expected(case), torch.bfloat16)
+
+
+@KINDS
 @pytest.mark.parametrize("lens", [[1], [5] * 3, [8, 9], [0, 1, 2, 3, 4, 5, 6, 7], [17, 0, 30], [2] * 80, [9] * 40])
 @pytest.mark.parametrize("score", [False, True], ids=["advance", "score"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
@@ -36,7 +44,7 @@ def test_draft(kind, lens, score, dtype):
 
 
 @KINDS
-@pytest.mark.parametrize("d_k, d_v", [(64, 64), (32, 32), (32, 160), (64, 32), (128, 64), (128, 256)])
+@pytest.mark.parametrize("d_k, d_v", [(64, 64), (32, 32), (32, 160), (64, 32), (128, 64), (128, 256), (64, 128), (32, 128)])
 @pytest.mark.parametrize("H_v, R", [(2, 3), (6, 60)])
 def test_draft_shapes(kind, d_k, d_v, H_v, R):
     lens = [(3 * i) % 11 for i in range(R)]
@@ -67,6 +75,22 @@ def test_zero_starts_and_padding(kind):
     for i, x in enumerate(want):
         assert not bool(torch.isnan(x).any()), i
     dh.check(case, dh.run(case, zero=zero, req=req), want)
+
+
+@KINDS
+def test_requests_without_any_token(kind):
+    """Nothing is read but who starts from zero; nobody does, or states are set to zero."""
+    case = dh.make_case(19, [0, 0, 0], kind=kind, L=2)
+    req, cu = case.req, torch.zeros(4, dtype=torch.int32, device="cuda")
+    for zero in (None, [0, 1, 0]):
+        state = case.state.clone()
+        dasc.dasc_delta_draft(case.plan, state, *case.strides, req, None, case.k, case.v, case.g, case.beta, cu, 0, 0, from_zero=dh.i32(zero))
+        want = case.state.clone()
+        if zero:
+            want[int(req[1])] = 0
+        assert torch.equal(state, want)
+    empty = torch.empty(0, dtype=torch.int32, device="cuda")
+    dasc.dasc_delta_step(case.plan, state, *case.strides, empty, case.q, case.k, case.v, case.g, case.beta, torch.empty(2, 0, 2, 128, device="cuda"))
 
 
 @KINDS
