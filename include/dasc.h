@@ -634,13 +634,13 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
                                 int64_t out_stride, int32_t *n_kept, void *cuda_stream);
 
 /*
- * The gated delta rule (Eq. 1) in decoding: the recurrence and layouts of dasc_refresh, for plans of either kind.  States, q, k, v,
+ * The gated delta rule (Eq. 1) in decoding: the recurrence and layouts of dasc_refresh, for plans of either kind, in fp32.  States, q, k, v,
  * g (any g <= 0, -infinity: everything before the token is forgotten), beta, o, req_idx and strides as for dasc_refresh and
  * dasc_decay_attn: a negative req_idx is padding (state and rows of o stay as they were), and neither stride may be below a layer's
  * dense size where it reaches states that are written.  d_k of 32, 64 or 128 and any d_v that is a multiple of 32 (DASC_ERR_SHAPE
  * otherwise).  No workspace.  Sums run in a fixed order: equal calls give equal bits.
  *
- * dasc_delta_step, in fp32: one token per request; token r of the streams ([Lc][n_req][heads][d]) belongs to request r; o is required.
+ * dasc_delta_step: one token per request; token r of the streams ([Lc][n_req][heads][d]) belongs to request r; o is required.
  *   src_idx    DEVICE int32[n_req] or NULL: beams.  Request r then starts from the state of slot src_idx[r] and writes slot req_idx[r]
  *              (dasc_beam_reorder gives both).  Requests come in groups of beam_width (1 .. 32, divides n_req); beams of one group that
  *              continue the same state read it once.  A slot that is written by a beam may be read only by beams
@@ -648,8 +648,7 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
  *              is not looked at where src_idx is NULL.
  *
  * dasc_delta_draft: each request's token range, made for a few tokens (drafts; for prompts and suffixes dasc_refresh is the faster call); any
- *   number of tokens is right.  Eight at a time; products with the state on the tensor cores in three products of tf32 parts, good to 2^-21 of each
- *   term, sums and states in fp32.  cu_seqlens, seq_used, from_zero as for dasc_decay_attn.  max_seqlen is an upper bound on any
+ *   number of tokens is right.  cu_seqlens, seq_used, from_zero as for dasc_decay_attn.  max_seqlen is an upper bound on any
  *   request's token count; it limits nothing.
  *   mode DASC_DRAFT_ADVANCE  every state is advanced and written back; o may be NULL, and then q
  *   mode DASC_DRAFT_SCORE    outputs only, no state is written.  A recurrent state cannot be rewound the way a KV cache can,
@@ -657,7 +656,7 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
  *                            by a second call (ADVANCE, seq_used = n_kept, o = NULL).
  *   A request without tokens still has its state set to zero by ADVANCE where from_zero says so.  A token with a NaN or an infinity in v, or a state with one, reaches
  *   its own column of the state and of later outputs only (where exact arithmetic may keep an infinity, it may be a NaN); one in k, g or beta reaches everything
- *   behind it, and in a draft the tokens of its group of eight.
+ *   behind it.
  * Errors: as for dasc_decay_attn, before any launch (g of a KDA plan has to be 16-byte aligned).
  */
 typedef enum { DASC_DRAFT_ADVANCE = 0, DASC_DRAFT_SCORE = 1 } dasc_draft_mode_t;

@@ -11,12 +11,12 @@
 //     u_t = beta_t (v_t - S^T (P_t k_t) - sum_{s < t} (k_t . D_ts k_s) u_s)
 //     o_t = q_scale (S^T (P_t q_t) + sum_{s <= t} (q_t . D_ts k_s) u_s),      S <- P_n S + sum_s (D_ns k_s) u_s^T
 // so that the sums over the state's rows of all tokens are independent of one another, and only sums over at most TB values per column are a chain.
-// The sums over rows and the update are products on the tensor cores; the state is held in fp32.
-// Bound: 5 tokens of 64 requests x 32 heads take 54 us scored and 80 us advanced (their bytes 23 and 42).  A block's steps follow one another: without the
-// products it is 43 us, without the preparation of operands 43 us, without reading states 40 us, with the reading alone 31 us; two blocks per SM, each
-// with its state in 64 registers of 256 threads, overlap little of that.  Tried and slower: multiply-adds on the CUDA cores (60 / 73 us: more instructions), states in shared
-// memory ahead of their use (57 / 88), preparation and products in warps of their own with a block per SM (73 / 115: the preparation
-// is a chain of latencies), states read twice instead of held, with four blocks per SM (50 / 104).
+// All in fp32 on the CUDA cores: per token and value of the state three multiply-adds (key, query, update), 9 us of them where five tokens of 64 requests x 32 heads are
+// scored.  Bound: those take 51 us scored and 66 us advanced (their bytes 23 and 42).  Instructions of two blocks of 256 threads per SM, each with its state in 64 registers
+// of a thread, which issue in half of the cycles and overlap little of a block's steps: without the sums over rows it is 34 us, without the preparation of operands
+// 40, without reading states 43, with reading alone 25.  Tried and slower: the products on the tensor cores in three tf32 parts (53 and 83: splitting values costs what
+// the products gain, and eight tokens cost what one does), states in shared memory ahead of their use (57 / 88), preparation and products in warps of their
+// own with a block per SM (73 / 115: the preparation is a chain of latencies), states read twice instead of held, with four blocks per SM (50 / 104).
 //
 // Split: columns of the state do not interact, so a thread block owns NCOL columns of one (request, layer, head) state.
 #include <cuda_runtime.h>
@@ -189,25 +189,23 @@ __global__ void __launch_bounds__(kStepThreads) delta_step_kernel(const __grid_c
   }
 }
 
-// Several tokens: the products with the state are 16 x DK x NCOL (eight keys, eight queries) and DK x 8 x NCOL, on the tensor cores in three products of tf32 parts
-// (a value is its rounding to 11 bits and what that is short of, good to 2^-22 together): sums over rows end in one thread's registers, and eight tokens
-// cost what one does.  A warp has 16 columns of the state and all of its rows.  Row k of a block of eight rows is operand row k / 2, or k / 2 + 4 where k is odd, and column
-// n of the 16 is column n / 2 of the first tile or, where n is odd, of the second, so that what a thread holds of the state as an operand of the first
-// product is what it gets from the second: rows 2 m and 2 m + 1 of every block and columns 2 n and 2 n + 1, m = lane % 4, n = lane / 4.
+// Several tokens: a warp has 16 columns of the state and all of its rows, a lane four columns of rows 4 g .. 4 g + 3 of every 32, g = lane / 4.  They are held in
+// pairs of rows: a 16-byte load brings four rows of a key to eight packed multiply-adds.  In pairs of columns it would be two rows, each value twice, to four of
+// them, and these loads the bound (60 / 73 us).
 template <int DK, int NCOL>
 struct DraftShape {
-  static constexpr int WARPS = NCOL / 16, NT = NCOL > 32 ? WARPS * 32 : 128, BLOCKS = DK / 8;  // (a narrow part has two warps that only prepare)
+  static constexpr int WARPS = NCOL / 16, NT = NCOL > 32 ? WARPS * 32 : 128, STEPS = DK / 32;  // (a narrow part has two warps that only prepare)
 };
 
 // What a group of tokens brings to a state's NCOL columns, and the rows it is made from.
 template <int DK, int NCOL>
 struct Operands {
-  // as the lanes take them, the rounded parts and what they are short of; a block's 32 lanes and 64 bytes that spread the writes over the banks
-  alignas(16) float4 key_query[2][DK / 8][36];  // P_t k_t and q_scale P_t q_t of token t = lane / 4: rows 2 m (key, query), 2 m + 1 (key, query)
-  alignas(16) float4 last[DK / 8][36];          // D_ns k_s: row lane / 4, tokens m and m + 4 rounded, and what they are short of
-  alignas(16) float hi[DK], lo[DK];             // the group's decay
+  alignas(16) float k[TB][DK], q[TB][DK];    // P_t k_t, q_scale P_t q_t
+  alignas(16) float last[TB][DK];            // D_ns k_s
+  alignas(16) float hi[DK], lo[DK];          // the group's decay
   alignas(16) float v[TB][NCOL], u[TB][NCOL];
-  alignas(16) float kk[TB][TB], qk[TB][TB];     // k_t . D_ts k_s for s < t, q_scale q_t . D_ts k_s for s <= t, 0 for later s
+  // of s, then of t, first the even ones: -beta_t k_t . D_ts k_s where s < t, q_scale q_t . D_ts k_s where s <= t, else 0
+  alignas(16) float kk[TB][TB], qk[TB][TB];
   float beta[TB];
 };
 template <int DK, int NCOL, bool KDA, typename IO>
@@ -220,14 +218,6 @@ struct DraftSmem {
   Operands<DK, NCOL> op;
   RawRows<DK, NCOL, KDA, IO> raw;
 };
-
-__device__ __forceinline__ float to_tf32(float x) { return __uint_as_float((__float_as_uint(x) + 0x1000u) & 0xFFFFE000u); }  // (an infinity stays one)
-__device__ __forceinline__ void mma_tf32(float (&d)[4], const float4 &a, float b0, float b1) {
-  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(__float_as_uint(a.x)), "r"(__float_as_uint(a.y)), "r"(__float_as_uint(a.z)), "r"(__float_as_uint(a.w)), "r"(__float_as_uint(b0)),
-        "r"(__float_as_uint(b1)));
-}
 
 // A block takes every gridDim.x-th part of a state; what the next one needs is on its way while one is worked on.
 struct Job {
@@ -282,7 +272,7 @@ struct JobWalk {
   }
 };
 
-// The rows of `cnt` tokens of a job from token t0 on, as they are, 16 bytes per copy, by NT threads (the first ones of the block; offsets between eight
+// The rows of `cnt` tokens of a job from token t0 on, as they are, 16 bytes per copy, by the block's NT threads (offsets between eight
 // tokens are below 2^31: the caller has looked).
 template <int DK, int NCOL, bool KDA, typename IO, int NT>
 __device__ __forceinline__ void copy_rows(RawRows<DK, NCOL, KDA, IO> &raw, const DascDeltaArgs &a, const Job &x, int cnt, int t0) {
@@ -316,170 +306,171 @@ __device__ __forceinline__ void copy_rows(RawRows<DK, NCOL, KDA, IO> &raw, const
   asm volatile("cp.async.commit_group;" ::: "memory");
 }
 
-// The group's `cnt` tokens as operands, by NT threads (the first ones of the block).
+// The group's `cnt` tokens as operands, by the block's NT threads.
 template <int DK, int NCOL, bool KDA, typename IO, int NT>
 __device__ __forceinline__ void prepare(Operands<DK, NCOL> &op, const RawRows<DK, NCOL, KDA, IO> &raw, int cnt, bool update, bool want, float q_scale) {
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
-  // Half of the warps: keys and queries behind the group's start, and keys decayed to its end, a thread per channel and kind.  Decays of several tokens
-  // are exponentials of sums of their logarithms, always over the tokens between two points (-infinity is like any other number there); a factor e^G is off
-  // by 2^-24 |G| or so of itself, 2^-25 at most.
-  if (tid < NT / 2) {
-    const int kinds = update ? 3 : 2;
-    for (int i = tid; i < kinds * DK; i += NT / 2) {
-      const int c = i % DK, what = i / DK, b = c / 8;
-      if (what < 2) {
-        const IO(*const rows)[DK] = what ? raw.q : raw.k;
-        const float scale = what ? q_scale : 1.f;
-        float G = 0.f;
-        float *const to = reinterpret_cast<float *>(&op.key_query[0][b][c % 8 / 2]) + c % 2 * 2 + what, *const short_of = to + (DK / 8) * 36 * 4;
+  // Products between tokens.  A warp has one token t or more; its lanes' parts of the 16 sums fold into one another.
+  constexpr int PER = DK / 32;
+  for (int i = tid; i < cnt * NCOL; i += NT) op.v[i / NCOL][i % NCOL] = to_float<IO>(raw.v[i / NCOL][i % NCOL]);
+  if (tid < cnt) op.beta[tid] = raw.beta[tid];
+  for (int t = warp; t < TB; t += NT / 32) {
+    if (t >= cnt) {
+      if (lane < 2 * TB) (lane < TB ? op.kk : op.qk)[lane % TB][t % 2 * 4 + t / 2] = 0.f;
+      continue;
+    }
+    float x[2 * TB], k[PER], q[PER], G[PER];
 #pragma unroll
-        for (int t = 0; t < TB; ++t) {
-          float x = 0.f;
-          if (t < cnt && (what == 0 || want)) {
-            G += raw.g[t][KDA ? c : 0];
-            x = __expf(G) * (to_float<IO>(rows[t][c]) * scale);
-          }
-          const float hi = to_tf32(x);
-          to[t * 16] = hi;
-          short_of[t * 16] = x - hi;
-        }
-      } else {
-        float G = 0.f, hi, lo;
-        float *const to = reinterpret_cast<float *>(&op.last[b][c % 8 * 4]);
+    for (int j = 0; j < PER; ++j) {
+      k[j] = to_float<IO>(raw.k[t][lane * PER + j]);
+      q[j] = want ? to_float<IO>(raw.q[t][lane * PER + j]) * q_scale : 0.f;
+      G[j] = 0.f;
+    }
 #pragma unroll
-        for (int t = TB - 1; t >= 0; --t) {
-          float x = 0.f;
-          if (t < cnt) {
-            x = __expf(G) * to_float<IO>(raw.k[t][c]);
-            G += raw.g[t][KDA ? c : 0];
-          }
-          hi = to_tf32(x);
-          to[t % 4 * 4 + t / 4] = hi;
-          to[t % 4 * 4 + t / 4 + 2] = x - hi;
+    for (int s = TB - 1; s >= 0; --s) {
+      x[s] = x[TB + s] = 0.f;
+      if (s <= t) {
+        float d = __expf(G[0]);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+          const float e = (KDA ? __expf(G[j]) : d) * to_float<IO>(raw.k[s][lane * PER + j]);
+          x[s] = fmaf(k[j], e, x[s]);
+          x[TB + s] = fmaf(q[j], e, x[TB + s]);
+          G[j] += raw.g[s][KDA ? lane * PER + j : 0];
         }
-        decay_factor(G, hi, lo);
-        op.hi[c] = hi;
-        op.lo[c] = lo;
       }
     }
-  } else {
-    // The others: products between tokens.  A warp has one token t or more; its lanes' parts of the 16 sums fold into one another.
-    constexpr int PER = DK / 32, HALF = NT / 64;
-    for (int i = tid - NT / 2; i < cnt * NCOL; i += NT / 2) op.v[i / NCOL][i % NCOL] = to_float<IO>(raw.v[i / NCOL][i % NCOL]);
-    if (tid - NT / 2 < cnt) op.beta[tid - NT / 2] = raw.beta[tid - NT / 2];
-    for (int t = warp - HALF; t < TB; t += HALF) {
-      if (t >= cnt) {
-        if (lane < 2 * TB) (lane < TB ? op.kk : op.qk)[t][lane % TB] = 0.f;
-        continue;
+#pragma unroll
+    for (int w = TB; w > 0; w >>= 1) {
+      const bool up = lane & w;
+#pragma unroll
+      for (int j = 0; j < w; ++j) {
+        const float mine = up ? x[j + w] : x[j];
+        x[j] = mine + __shfl_xor_sync(0xffffffffu, up ? x[j] : x[j + w], w);
       }
-      float x[2 * TB], k[PER], q[PER], G[PER];
+    }
+    x[0] += __shfl_xor_sync(0xffffffffu, x[0], 16);
+    if (lane < 2 * TB) (lane < TB ? op.kk : op.qk)[lane % TB][t % 2 * 4 + t / 2] = lane >= TB ? x[0] : lane == t ? 0.f : -raw.beta[t] * x[0];
+  }
+  // Keys and queries behind the group's start, and keys decayed to its end, a thread per channel and kind.  Decays of several tokens
+  // are exponentials of sums of their logarithms, always over the tokens between two points (-infinity is like any other number there); a factor e^G is off
+  // by 2^-24 |G| or so of itself, 2^-25 at most.
+  const int kinds = (want ? 2 : 1) + update;
+  for (int i = tid; i < kinds * DK; i += NT) {
+    const int c = i % DK, what = i / DK;
+    float G = 0.f;
+    if (what < kinds - update) {
+      const IO(*const rows)[DK] = what ? raw.q : raw.k;
+      float(*const to)[DK] = what ? op.q : op.k;
+      const float scale = what ? q_scale : 1.f;
 #pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        k[j] = to_float<IO>(raw.k[t][lane * PER + j]);
-        q[j] = want ? to_float<IO>(raw.q[t][lane * PER + j]) * q_scale : 0.f;
-        G[j] = 0.f;
-      }
-#pragma unroll
-      for (int s = TB - 1; s >= 0; --s) {
-        x[s] = x[TB + s] = 0.f;
-        if (s <= t) {
-          float d = __expf(G[0]);
-#pragma unroll
-          for (int j = 0; j < PER; ++j) {
-            const float e = (KDA ? __expf(G[j]) : d) * to_float<IO>(raw.k[s][lane * PER + j]);
-            x[s] = fmaf(k[j], e, x[s]);
-            x[TB + s] = fmaf(q[j], e, x[TB + s]);
-            G[j] += raw.g[s][KDA ? lane * PER + j : 0];
-          }
+      for (int t = 0; t < TB; ++t)
+        if (t < cnt) {
+          G += raw.g[t][KDA ? c : 0];
+          to[t][c] = __expf(G) * (to_float<IO>(rows[t][c]) * scale);
         }
-      }
+    } else {
 #pragma unroll
-      for (int w = TB; w > 0; w >>= 1) {
-        const bool up = lane & w;
-#pragma unroll
-        for (int j = 0; j < w; ++j) {
-          const float mine = up ? x[j + w] : x[j];
-          x[j] = mine + __shfl_xor_sync(0xffffffffu, up ? x[j] : x[j + w], w);
+      for (int t = TB - 1; t >= 0; --t)
+        if (t < cnt) {
+          op.last[t][c] = __expf(G) * to_float<IO>(raw.k[t][c]);
+          G += raw.g[t][KDA ? c : 0];
         }
-      }
-      x[0] += __shfl_xor_sync(0xffffffffu, x[0], 16);
-      if (lane < 2 * TB) (lane < TB ? op.kk : op.qk)[t][lane % TB] = lane == t ? 0.f : x[0];
+      decay_factor(G, op.hi[c], op.lo[c]);
     }
   }
 }
 
-// A warp's 16 columns of a group, the first of which is `c0` of the block's.  `state(b)` gives its lanes' part of block b, row 2 m in x and row 2 m + 1 in y;
-// `store(b, x, y)` takes what it becomes, where `update`.  Outputs go to `o`, v_stride apart, where `want`.
-template <int DK, int NCOL, typename OT, typename State, typename Store>
-__device__ __forceinline__ void run_group(Operands<DK, NCOL> &op, int cnt, int c0, bool update, bool want, OT *o, int64_t v_stride, State state, Store store) {
-  const int lane = threadIdx.x % 32, m = lane % 4, nn = lane / 4;
-  // S^T (P_t k_t) and S^T (P_t q_t) of token t = nn, columns 4 m .. 4 m + 3
-  float big[2][4] = {}, one[2][4] = {}, two[2][4] = {};
+// A warp's 16 columns of a group, the lane's first of them `col` of the block's.  Outputs go to `o`, v_stride apart, where `want`.
+template <int DK, int NCOL, typename OT>
+__device__ __forceinline__ void run_group(Operands<DK, NCOL> &op, uint64_t (&S)[DK / 32][2][4], int cnt, int col, bool update, bool want, OT *o, int64_t v_stride) {
+  const int lane = threadIdx.x % 32, g = lane / 4;
+  // S^T (P_t k_t) and S^T (P_t q_t), two tokens at a time: a lane's sums over its rows, four columns each, then folded into one another, so that lane g
+  // ends with column col + g % 4 of the first token (g < 4) or the second
+  const int odd = g / 4, c = col + g % 4;
+  auto products = [&](const float *row, const float *other) {
+    uint64_t x[2][4] = {};
 #pragma unroll
-  for (int b = 0; b < DK / 8; ++b) {
-    const float4 hi = op.key_query[0][b][lane], lo = op.key_query[1][b][lane];
-    float2 row[2];
-    state(b, row[0], row[1]);
+    for (int i = 0; i < DK / 32; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float x0 = j ? row[0].y : row[0].x, x1 = j ? row[1].y : row[1].x, r0 = to_tf32(x0), r1 = to_tf32(x1);
-      mma_tf32(big[j], hi, r0, r1);
-      mma_tf32(one[j], lo, r0, r1);
-      mma_tf32(two[j], hi, x0 - r0, x1 - r1);
+      for (int j = 0; j < 2; ++j) {
+        const ulonglong2 k = *reinterpret_cast<const ulonglong2 *>((j ? other : row) + 32 * i + 4 * g);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[j][c] = dfma2(S[i][1][c], k.y, dfma2(S[i][0][c], k.x, x[j][c]));
+      }
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float2 a = dunpack2(x[j / 4][j % 4]);
+      f[j] = a.x + a.y;
     }
-  }
-  float x[4], y[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int j = i % 2, at = i / 2;
-    x[i] = (one[j][at] + two[j][at]) + big[j][at];
-    y[i] = (one[j][at + 2] + two[j][at + 2]) + big[j][at + 2];
-  }
-  // u_t, one token after the other, and outputs as the u_s come by
-  const int c = c0 + 4 * m;
-  const bool valid = nn < cnt;
-  const float beta = valid ? op.beta[nn] : 0.f;
-  const float4 v = valid ? *reinterpret_cast<const float4 *>(&op.v[nn][c]) : make_float4(0.f, 0.f, 0.f, 0.f);
-  x[0] = beta * (v.x - x[0]), x[1] = beta * (v.y - x[1]), x[2] = beta * (v.z - x[2]), x[3] = beta * (v.w - x[3]);
+    for (int w = 4; w > 0; w >>= 1) {
+      const bool up = g & w;
 #pragma unroll
-  for (int s = 0; s < TB; ++s)
-    if (s < cnt) {
-      const float kk = -beta * op.kk[nn][s], qk = op.qk[nn][s];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float u = __shfl_sync(0xffffffffu, x[i], s * 4 + m);
-        if (nn > s) x[i] = fmaf(kk, u, x[i]);
-        if (nn >= s) y[i] = fmaf(qk, u, y[i]);
+      for (int j = 0; j < w; ++j) {
+        const float mine = up ? f[j + w] : f[j];
+        f[j] = mine + __shfl_xor_sync(0xffffffffu, up ? f[j] : f[j + w], w * 4);
       }
     }
-  if (want && valid) {
-    OT *const to = o + nn * v_stride + c;
-    if constexpr (sizeof(OT) == 2) {
-      __nv_bfloat162 p[2] = {__floats2bfloat162_rn(y[0], y[1]), __floats2bfloat162_rn(y[2], y[3])};
-      *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(p);
-    } else {
-      *reinterpret_cast<float4 *>(to) = make_float4(y[0], y[1], y[2], y[3]);
+    return f[0];
+  };
+  float x[TB / 2], y[TB / 2];
+#pragma unroll
+  for (int p = 0; p < TB / 2; ++p)
+    if (2 * p < cnt) {  // (of a token behind the last one there is anything, and nothing reads it)
+      const bool alone = want && 2 * p + 1 == cnt;  // the last token's key and query at once
+      const float z = products(op.k[2 * p], alone ? op.q[2 * p] : op.k[2 * p + 1]);
+      x[p] = op.beta[2 * p + odd] * (op.v[2 * p + odd][c] - z);
+      if (alone)
+        y[p] = __shfl_down_sync(0xffffffffu, z, 16);
+      else if (want)
+        y[p] = products(op.q[2 * p], op.q[2 * p + 1]);
     }
+  // u_t, one token after the other, and what it brings to the later ones
+#pragma unroll
+  for (int t = 0; t < TB; ++t)
+    if (t < cnt) {
+      const float u = __shfl_sync(0xffffffffu, x[t / 2], lane % 16 + t % 2 * 16);
+      if (odd == t % 2) op.u[t][c] = u;
+      const float4 k4 = *reinterpret_cast<const float4 *>(&op.kk[t][4 * odd]), q4 = *reinterpret_cast<const float4 *>(&op.qk[t][4 * odd]);
+      const float kk[4] = {k4.x, k4.y, k4.z, k4.w}, qk[4] = {q4.x, q4.y, q4.z, q4.w};
+#pragma unroll
+      for (int p = t / 2; p < TB / 2; ++p)
+        if (p > t / 2 || odd >= t % 2) {
+          if (p > t / 2 || t % 2 == 0) x[p] = fmaf(kk[p], u, x[p]);
+          y[p] = fmaf(qk[p], u, y[p]);
+        }
+    }
+  if (want) {
+#pragma unroll
+    for (int p = 0; p < TB / 2; ++p)
+      if (2 * p + odd < cnt) o[(2 * p + odd) * v_stride + c] = from_float<OT>(y[p]);
   }
   if (!update) return;
-  *reinterpret_cast<float4 *>(&op.u[nn][c]) = valid ? make_float4(x[0], x[1], x[2], x[3]) : make_float4(0.f, 0.f, 0.f, 0.f);
   __syncwarp();
-  const float2 ua = *reinterpret_cast<const float2 *>(&op.u[m][c0 + 2 * nn]), ub = *reinterpret_cast<const float2 *>(&op.u[m + 4][c0 + 2 * nn]);
-  const float4 hi = make_float4(to_tf32(ua.x), to_tf32(ua.y), to_tf32(ub.x), to_tf32(ub.y));
-  const float4 lo = make_float4(ua.x - hi.x, ua.y - hi.y, ub.x - hi.z, ub.y - hi.w);
 #pragma unroll
-  for (int b = 0; b < DK / 8; ++b) {
-    const float4 k = op.last[b][lane];
-    float d[4] = {}, e[4] = {};
-    mma_tf32(e, hi, k.z, k.w);
-    mma_tf32(e, lo, k.x, k.y);
-    mma_tf32(d, hi, k.x, k.y);
-    const float2 ph = *reinterpret_cast<const float2 *>(&op.hi[8 * b + 2 * m]), pl = *reinterpret_cast<const float2 *>(&op.lo[8 * b + 2 * m]);
-    float2 s0, s1;
-    state(b, s0, s1);
-    // (the tensor cores' own sums start from zero: they would cut the state's last bit off)
-    store(b, make_float2(fmaf(s0.x, ph.x, fmaf(s0.x, pl.x, e[0] + d[0])), fmaf(s0.y, ph.x, fmaf(s0.y, pl.x, e[2] + d[2]))),
-          make_float2(fmaf(s1.x, ph.y, fmaf(s1.x, pl.y, e[1] + d[1])), fmaf(s1.y, ph.y, fmaf(s1.y, pl.y, e[3] + d[3]))));
+  for (int i = 0; i < DK / 32; ++i) {
+    const ulonglong2 hi = *reinterpret_cast<const ulonglong2 *>(&op.hi[32 * i + 4 * g]), lo = *reinterpret_cast<const ulonglong2 *>(&op.lo[32 * i + 4 * g]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      S[i][0][c] = dfma2(S[i][0][c], hi.x, dmul2(S[i][0][c], lo.x));
+      S[i][1][c] = dfma2(S[i][1][c], hi.y, dmul2(S[i][1][c], lo.y));
+    }
+  }
+#pragma unroll 2
+  for (int t = 0; t < cnt; ++t) {
+    const float4 w = *reinterpret_cast<const float4 *>(&op.u[t][col]);
+    const uint64_t ww[4] = {dpack2(w.x, w.x), dpack2(w.y, w.y), dpack2(w.z, w.z), dpack2(w.w, w.w)};
+#pragma unroll
+    for (int i = 0; i < DK / 32; ++i) {
+      const ulonglong2 k = *reinterpret_cast<const ulonglong2 *>(&op.last[t][32 * i + 4 * g]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        S[i][0][c] = dfma2(k.x, ww[c], S[i][0][c]);
+        S[i][1][c] = dfma2(k.y, ww[c], S[i][1][c]);
+      }
+    }
   }
 }
 
@@ -488,10 +479,10 @@ template <int DK, int NCOL, bool KDA, typename IO, typename OT>
 __global__ void __launch_bounds__((DraftShape<DK, NCOL>::NT), (512 / DraftShape<DK, NCOL>::NT)) delta_draft_kernel(const __grid_constant__ DascDeltaArgs a) {
   using Sh = DraftShape<DK, NCOL>;
   using Sm = DraftSmem<DK, NCOL, KDA, IO>;
-  constexpr int NT = Sh::NT, BLOCKS = Sh::BLOCKS;
+  constexpr int NT = Sh::NT, STEPS = Sh::STEPS;
   extern __shared__ __align__(16) unsigned char smem_raw[];
   Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
-  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, m = lane % 4, nn = lane / 4;
+  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, col = warp * 16 + lane % 4 * 4, row = lane / 4 * 4;
   const JobWalk<DK, NCOL> walk(a);
   const int dv = walk.dv, v_stride = a.H_v * dv;
   const bool write = !a.score, holds = warp < Sh::WARPS;
@@ -503,17 +494,23 @@ __global__ void __launch_bounds__((DraftShape<DK, NCOL>::NT), (512 / DraftShape<
   while (now.r < a.n_req) {
     const Job next = walk.after(now);
     const int n = now.n;
-    float *const st = walk.state_of(now) + 2 * m * dv + warp * 16 + 2 * nn;
+    float *const st = walk.state_of(now) + row * dv + col;
     OT *const go = static_cast<OT *>(a.o) + ((static_cast<int64_t>(now.lc) * a.total_tokens + now.begin) * a.H_v + now.h) * dv + now.part * NCOL;
-    float2 S[BLOCKS][2];  // row 8 b + 2 m and the one behind it, columns 2 nn and 2 nn + 1; not looked at before the products
+    uint64_t S[STEPS][2][4];  // rows row + 32 i + 2 j and the one behind it
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) {
-      S[b][0] = S[b][1] = make_float2(0.f, 0.f);
-      if (holds && !now.zero && n > 0) {
-        S[b][0] = *reinterpret_cast<const float2 *>(st + 8 * b * dv);
-        S[b][1] = *reinterpret_cast<const float2 *>(st + (8 * b + 1) * dv);
+    for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+        if (holds && !now.zero && n > 0) {
+          x = *reinterpret_cast<const float4 *>(st + (32 * i + 2 * j) * dv);
+          y = *reinterpret_cast<const float4 *>(st + (32 * i + 2 * j + 1) * dv);
+        }
+        S[i][j][0] = dpack2(x.x, y.x);
+        S[i][j][1] = dpack2(x.y, y.y);
+        S[i][j][2] = dpack2(x.z, y.z);
+        S[i][j][3] = dpack2(x.w, y.w);
       }
-    }
     for (int t0 = 0; t0 < n; t0 += TB) {
       const int cnt = min(TB, n - t0);
       const bool update = write || t0 + TB < n;
@@ -533,18 +530,18 @@ __global__ void __launch_bounds__((DraftShape<DK, NCOL>::NT), (512 / DraftShape<
           }
         }
       }
-      if (holds)
-        run_group<DK, NCOL>(
-            sm.op, cnt, warp * 16, update, a.o != nullptr, go + static_cast<int64_t>(t0) * v_stride, v_stride,
-            [&](int b, float2 &x, float2 &y) { x = S[b][0], y = S[b][1]; }, [&](int b, float2 x, float2 y) { S[b][0] = x, S[b][1] = y; });
+      if (holds) run_group<DK, NCOL>(sm.op, S, cnt, col, update, a.o != nullptr, go + static_cast<int64_t>(t0) * v_stride, v_stride);
     }
     if (n == 0) stage(next, 0);
     if (holds && write && (n > 0 || (now.zero && now.req >= 0))) {
 #pragma unroll
-      for (int b = 0; b < BLOCKS; ++b) {
-        *reinterpret_cast<float2 *>(st + 8 * b * dv) = S[b][0];
-        *reinterpret_cast<float2 *>(st + (8 * b + 1) * dv) = S[b][1];
-      }
+      for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float2 x = dunpack2(S[i][j][0]), y = dunpack2(S[i][j][1]), z = dunpack2(S[i][j][2]), w = dunpack2(S[i][j][3]);
+          *reinterpret_cast<float4 *>(st + (32 * i + 2 * j) * dv) = make_float4(x.x, y.x, z.x, w.x);
+          *reinterpret_cast<float4 *>(st + (32 * i + 2 * j + 1) * dv) = make_float4(x.y, y.y, z.y, w.y);
+        }
     }
     now = next;
   }
@@ -571,7 +568,7 @@ int launch(const DascDeltaArgs &a, void *stream) {
 template <int DK, bool KDA, typename IO, typename OT>
 int launch_cols(const DascDeltaArgs &a, void *stream) {
   // Drafts: the widest part, since what is prepared for a group serves all of its columns.  5 tokens of 1 / 8 / 32 requests of 32 heads, scored, in us with parts of
-  // 32 / 64 / 128 columns: 7.5 / 7.5 / 6.8, 17.6 / 11.9 / 9.7, 60.7 / 36.9 / 30.6; advanced, 16 requests: 43 / 30 / 25.
+  // 32 / 64 / 128 columns: 9.1 / 8.3 / 6.2, 21.1 / 11.8 / 8.2, 73.6 / 37.9 / 27.7; advanced, 16 requests: 43.5 / 24.4 / 19.0.
   if (a.cu_seqlens) {
     if (a.d_v == 128) return launch<DK, 128, KDA, IO, OT>(a, stream);
     return a.d_v % 64 == 0 ? launch<DK, 64, KDA, IO, OT>(a, stream) : launch<DK, 32, KDA, IO, OT>(a, stream);

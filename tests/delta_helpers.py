@@ -146,9 +146,7 @@ def roundoff(case):
     """How far a computed sum may be off, relative to the sum of its terms' absolute values.  Along a token, a term passes an exponential and products of up to
     eight of them (good to 2^-22 and 2^-24 each: under 48 roundings of 2^-24 in all), and sums of d_k products, each of whose additions rounds once;
     sums over at most eight earlier tokens and the update of the state are among the 48.  An error made at a token passes the later ones as a
-    term of theirs does, so they add up: (T + 1)(d_k + 48) 2^-24.
-    Products in tf32 parts stay below that: the parts of a term are good to 2^-21 together (8 of the 2^-24), and a sum of d_k of them is d_k / 8 additions of
-    sums of eight on the tensor cores, cut off at 2^-23 each: d_k / 4 of the 2^-24, and as much for the two small products, of 2^-11."""
+    term of theirs does, so they add up: (T + 1)(d_k + 48) 2^-24."""
     return (max(case.lens, default=0) + 1) * (case.d_k + 48) * 2.0 ** -24
 
 

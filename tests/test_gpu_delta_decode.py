@@ -182,6 +182,25 @@ def test_a_value_that_is_none_stays_in_its_column(kind):
     assert torch.equal(o, plain[1]) and torch.equal(state, plain[0])
 
 
+@KINDS
+@pytest.mark.parametrize("what", ["k", "g", "beta", "q"])
+def test_nothing_runs_backwards(kind, what):
+    """Tokens before one that is no number, in their group as well, and other requests keep their bits."""
+    case = dh.make_case(20, [7, 2, 11], kind=kind, dtype=torch.float32)
+    plain = dh.run(case)
+    for t in (4, 9 + 8):  # of the first and the third request
+        getattr(case, what)[0, t] = float("nan")
+    state, o = dh.run(case)
+    kept = [0, 1, 2, 3, 7, 8, *range(9, 17)]
+    assert torch.equal(o[0, kept], plain[1][0, kept])
+    if what == "q":
+        kept = [t for t in range(20) if t not in (4, 17)]
+        assert torch.equal(o[0, kept], plain[1][0, kept]) and torch.equal(state, plain[0])
+        assert bool(torch.isnan(o[0, [4, 17]]).all())
+    else:
+        assert bool(torch.isnan(o[0, [5, 6, 18, 19]]).all()) and torch.equal(state[int(case.req[1])], plain[0][int(case.req[1])])
+
+
 def test_states_that_hardly_decay_keep_their_precision():
     """A constant decay of 1 - 1e-5 rounded to fp32 would be off by 6e-8 in every one of 20,000 tokens, 1.2e-3 of a state in the end."""
     case = dh.make_case(15, [1], kind=dasc.GDN, H_v=2, dtype=torch.float32)
