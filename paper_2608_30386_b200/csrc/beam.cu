@@ -3,15 +3,21 @@
 // Selection.  A continuation of beam b by token v weighs s = score_b + (x_bv - log sum exp x_b), in 64 bits; the best n_out of a
 // request's width x vocab continuations are wanted.  Inside a beam they are ordered like the logits themselves, so each part of a row gives its best n_out
 // by 64-bit keys (logit, then lower token) while it sums exponentials, all from one pass over the row, and the few that are left meet with their beams' sums.
-// Split: a request is a cluster of CL thread blocks; the rows of its beams are cut into segments, alike for all rows, which the blocks take in
-// order.  A block goes through a segment in rounds of 64 bytes per thread, the next round's loads in flight.  Sums are kept by segment and added up in
-// their order, so that equal rows have equal sums whichever blocks they fell to.  A lower bound on the segment's n_out-th best entry comes from the
-// maxima of groups of threads (there are at least n_out groups); the entries above it, a few dozen as a rule, go to shared memory and are ranked
-// there by counting at the segment's end.  Where too many tie or the bound is poor, a round's n_out-th key is found by bisection.  The first block
-// ranks what all of them have left.  Nothing depends on the order of arrival.
+// Split: a request is a cluster of CL thread blocks; the rows of its beams that count (not ended, with a finite score) are cut into segments, alike for all rows, which
+// the blocks take in order.  A block goes once through a segment, two rounds of 64 bytes per thread loaded at a time, for nothing but each thread's largest
+// logit and sum of exponentials and the largest of each of its chunks of entries.  Sums are kept by segment and added up in their order, so that equal rows have equal sums
+// whichever blocks they fell to.  A lower bound on the segment's n_out-th best entry comes from the maxima of groups of threads (there are at least
+// n_out groups); the few chunks that reach it are read again, from L2 as a rule, an entry per lane, and entries from the bound on, a few dozen, go to shared
+// memory.  Where too many tie, or an entry is no number, the segment is gone through once more and its n_out best keys are found bit by bit.  The first
+// block ranks what all of them have left.  Nothing depends on the order of arrival.
+// Bound: reading, and an exponential per entry on 16 lanes of special functions per SM, alike: 64 requests x 8 beams x 131,072 entries in bf16 take 38 us (bytes 21,
+// exponentials 15; of a block's 57,000 cycles the stream takes 30,000, the ends of its two segments 14,000, ranking 11,000); one request of 4 x 32,000 7.4 us, a chain of latencies.  Tried and slower: lists of the best
+// kept while reading, ranked per segment (92), entries above a running bound written out by warps on their own (53).  Logits that fool the bound: all
+// equal 228 us, rising with the token 1020 us (64 x 8 x 131,072).
 //
 // Reordering.  The lowest new beam of each continued one keeps its slot; the others get the slots of beams that nobody continues, and only these are copied: sources
-// stay as they are and every destination is a slot that nobody reads, so nothing has to wait for anything and there is no second buffer.
+// stay as they are and every destination is a slot that nobody reads, so nothing has to wait for anything and there is no second buffer.  Bound: bytes.  16 requests
+// x 4 beams, two forks each of 48 MB: 409 us, 7.9 TB/s where every byte is read and written once per fork (two forks of one beam read it from L2).
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -29,6 +35,7 @@ constexpr int WORDS = 16;            // 32-bit words of a row that a thread hold
 constexpr int MAXW = kBeamMaxWidth, MAXN = kBeamMaxOut;  // beams per request, continuations wanted
 constexpr int MAXS = 16;             // segments of a row
 constexpr int CHUNKS = 16;           // parts of a thread's entries of a segment
+constexpr int kMostHits = 4 * MAXN + 128;  // of a segment
 constexpr float kNone = -__builtin_huge_valf(), kLog2e = 1.44269504f;
 template <typename T>
 constexpr float kLowest = sizeof(T) == 2 ? -3.38953139e38f : -3.40282347e38f;  // the type's lowest finite value
@@ -82,10 +89,11 @@ struct SelectSmem {
   int counts[MAXW];  // the beams whose rows count
   float warp_top[MAXW][NW], warp_sum[MAXW][NW];  // the warps' shares of each of this block's segments
   uint32_t best_of[NT], bound;  // 16 or 32 bits of order of each thread's largest value
-  int n_hits[MAXW], odd[MAXW];  // of each of this block's segments
+  int n_chosen[MAXW], n_hits[MAXW], odd[MAXW];  // of each of this block's segments
   int n_above, n_entries, n_left, n_rows;
   unsigned long long any_bit, all_bits;
   uint16_t chunk[CHUNKS][NT];   // the largest entry of each thread's chunks, 16 bits of order32
+  uint16_t chosen[kMostHits];   // chunks that are read again: number * NT + thread
 };
 // behind it: uint64_t hit[segments of this block][a.budget], then in the first block Entry entry[all of them]
 
@@ -187,7 +195,7 @@ struct Round {
   }
 };
 
-// Sums of exponentials are relative to 2^c with c = round(m log2 e), m the largest logit of what they are over.
+// Sums of exponentials are relative to 2^c, c the product of m and log2 e in fp32, m the largest logit of what they are over.
 __device__ __forceinline__ float reference(float m) { return m == kNone ? 0.f : __fmul_rn(m, kLog2e); }  // (not part of a multiply-add)
 // one more round's part of a thread's sum
 template <typename Rd>
@@ -217,19 +225,15 @@ __device__ __forceinline__ double warp_sum(double x) {
   for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
   return x;
 }
-// Sums x relative to e^ref, one per lane, as one: `top` is what it is relative to (-infinity: no lane has any).
-__device__ __forceinline__ double add_up(double ref, double x, double &top) {
-  top = warp_max(ref);
-  return warp_sum(ref > -INFINITY ? x * exp(ref - top) : 0.0);
-}
+// (factors between sums are good to 2^-22, as the exponentials themselves)
 __device__ __forceinline__ void join_sums(SelectSmem &sm, int local, int item, bool plain) {
   const int lane = threadIdx.x % 32;
-  const float m = lane < NW ? sm.warp_top[local][lane] : kNone;
-  double top;
-  const double x = add_up(m == kNone ? -INFINITY : plain ? m : reference(m) * (1.0 / static_cast<double>(kLog2e)),
-                          lane < NW ? sm.warp_sum[local][lane] : 0.0, top);
+  const float m = lane < NW ? sm.warp_top[local][lane] : kNone, top = warp_max(m);
+  float x = lane < NW && m > kNone ? sm.warp_sum[local][lane] * ex2(plain ? (m - top) * kLog2e : reference(m) - reference(top)) : 0.f;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
   if (lane == 0) {
-    sm.reference[item] = top;
+    sm.reference[item] = top == kNone ? -INFINITY : plain ? top : reference(top) * (1.0 / static_cast<double>(kLog2e));
     sm.sum[item] = x;
   }
 }
@@ -389,7 +393,7 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
     if (ended == 0) sm.counts[place] = tid;
     if (tid == 0) sm.n_rows = __popc(rows);
   }
-  if (tid < MAXW) sm.n_hits[tid] = sm.odd[tid] = 0;
+  if (tid < MAXW) sm.n_chosen[tid] = sm.n_hits[tid] = sm.odd[tid] = 0;
   if (tid == 0) sm.n_entries = sm.n_left = 0;
   __syncthreads();
 
@@ -432,36 +436,45 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
     __syncthreads();
     const uint32_t t = max(sm.bound, order32(kLowest<T>) >> 16);
     if (odd) continue;
-    // The few chunks that may hold one of the best are read again, an entry per lane.
+    // The few chunks that may hold one of the best (each has an entry from the bound on) are shared out over the warps and read again, an entry per lane, while the last
+    // warp adds up the sums.  Each warp with those of its own threads, us: 64 requests x 4 beams x 131,072 fp32 entries 32.4 instead of 30.3, one of 4 x 32,000 with many
+    // good neighbours 8.2 instead of 7.3, 64 x 32 x 32,768 (eight short segments per block) 59 instead of 63.  All segments' at the end: 31.4, 8.0, 67.
+#pragma unroll 4
+    for (int c = 0; c < chunks; ++c) {
+      const bool chosen = sm.chunk[c][tid] >= t;
+      const uint32_t who = __ballot_sync(0xffffffffu, chosen);
+      if (!who) continue;
+      int to = lane == 0 ? atomicAdd(&sm.n_chosen[item - first], __popc(who)) : 0;
+      to = __shfl_sync(0xffffffffu, to, 0) + __popc(who & ((1u << lane) - 1u));
+      if (chosen && to < a.budget) sm.chosen[to] = static_cast<uint16_t>(c * NT + tid);
+    }
+    __syncthreads();
+    const int n = sm.n_chosen[item - first];
+    if (n > a.budget) continue;  // (all of it once more, see rescan)
+    if (warp == NW - 1) join_sums(sm, item - first, item, false);
     const float bound = value32(t << 16);
-    volatile int *const hits = &sm.n_hits[item - first];
-    for (int c = 0; c < chunks && *hits <= a.budget; ++c) {  // (too many: all of it once more, see rescan)
-      for (uint32_t who = __ballot_sync(0xffffffffu, sm.chunk[c][tid] >= t); who; who &= who - 1) {
-        const int thread = warp * 32 + __ffs(who) - 1;
-        for (int i = lane; i < each * Rd::EPT; i += 32) {
-          const int at = (c * each + i / Rd::EPT) * Rd::SIZE + Rd::index(i % Rd::EPT, thread);
-          const float x = at < len ? __uint_as_float(Rd::bits(row[at])) : kNone;
-          if (x >= bound) {
-            const int to = atomicAdd(const_cast<int *>(hits), 1);
-            if (to < a.budget) hit[(item - first) * a.budget + to] = key_of(x, from + at);
-          }
+    for (int j = warp == NW - 1 ? n : warp; j < n; j += NW - 1) {
+      const int c = sm.chosen[j] / NT, thread = sm.chosen[j] % NT;
+      for (int i = lane; i < each * Rd::EPT; i += 32) {
+        const int at = (c * each + i / Rd::EPT) * Rd::SIZE + Rd::index(i % Rd::EPT, thread);
+        const float x = at < len ? __uint_as_float(Rd::bits(row[at])) : kNone;
+        if (x >= bound) {
+          const int to = atomicAdd(&sm.n_hits[item - first], 1);
+          if (to < a.budget) hit[(item - first) * a.budget + to] = key_of(x, from + at);
         }
       }
     }
   }
   __syncthreads();
   for (int item = first; item < last; ++item) {
-    const bool again = sm.odd[item - first] || sm.n_hits[item - first] > a.budget;  // (the same for the whole block)
+    const bool again = sm.odd[item - first] || sm.n_chosen[item - first] > a.budget || sm.n_hits[item - first] > a.budget;  // (the same for the whole block)
     if (!again) continue;
     const int from = item % a.segments * a.segment_len;
     const int n = rescan<Rd>(sm, row_of(item), min(a.segment_len, a.vocab - from), from, item - first, hit + (item - first) * a.budget, N);
-    if (tid == 0) {
-      sm.n_hits[item - first] = n;
-      sm.odd[item - first] = 1;
-    }
+    if (warp == 0) join_sums(sm, item - first, item, true);
     __syncthreads();
+    if (tid == 0) sm.n_hits[item - first] = n;
   }
-  for (int item = first + warp; item < last; item += NW) join_sums(sm, item - first, item, sm.odd[item - first]);
 
   // The first block takes the hits and sums of all of them.
   cg::cluster_group cluster = cg::this_cluster();
@@ -471,12 +484,13 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
   if (rank == 0) {
     for (int row = warp; row < sm.n_rows; row += NW) {
       const int item = row * a.segments + lane, c = item / per_block;
-      double ref = -INFINITY, x = 0.0, top;
+      double ref = -INFINITY, x = 0.0;
       if (lane < a.segments) {
         ref = cluster.map_shared_rank(sm.reference, c)[item];
         x = cluster.map_shared_rank(sm.sum, c)[item];
       }
-      x = add_up(ref, x, top);
+      const double top = warp_max(ref);
+      x = warp_sum(ref > -INFINITY ? x * ex2(static_cast<float>(ref - top) * kLog2e) : 0.0);
       if (lane == 0) sm.lse[sm.counts[row]] = top + log(x);
     }
     __syncthreads();
