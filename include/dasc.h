@@ -647,7 +647,7 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
  *              that start from this beam's own source, and beams of different groups share no source; a negative src_idx is padding.  beam_width
  *              is not looked at where src_idx is NULL.
  *
- * dasc_delta_draft: each request's token range, made for a few tokens (drafts; for prompts and suffixes dasc_refresh is the faster call); any
+ * dasc_delta_draft: each request's token range, made for a few tokens (drafts; for prompts and suffixes of more than eight dasc_refresh is the faster call); any
  *   number of tokens is right.  cu_seqlens, seq_used, from_zero as for dasc_decay_attn.  max_seqlen is an upper bound on any
  *   request's token count; it limits nothing.
  *   mode DASC_DRAFT_ADVANCE  every state is advanced and written back; o may be NULL, and then q
