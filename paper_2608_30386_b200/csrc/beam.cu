@@ -23,6 +23,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "decay_common.cuh"
 
@@ -226,15 +227,15 @@ __device__ __forceinline__ double warp_sum(double x) {
   return x;
 }
 // (factors between sums are good to 2^-22, as the exponentials themselves)
-__device__ __forceinline__ void join_sums(SelectSmem &sm, int local, int item, bool plain) {
+__device__ __forceinline__ void join_sums(const SelectSmem &sm, int local, bool plain, double *to_reference, double *to_sum) {
   const int lane = threadIdx.x % 32;
   const float m = lane < NW ? sm.warp_top[local][lane] : kNone, top = warp_max(m);
   float x = lane < NW && m > kNone ? sm.warp_sum[local][lane] * ex2(plain ? (m - top) * kLog2e : reference(m) - reference(top)) : 0.f;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
   if (lane == 0) {
-    sm.reference[item] = top == kNone ? -INFINITY : plain ? top : reference(top) * (1.0 / static_cast<double>(kLog2e));
-    sm.sum[item] = x;
+    *to_reference = top == kNone ? -INFINITY : plain ? top : reference(top) * (1.0 / static_cast<double>(kLog2e));
+    *to_sum = x;
   }
 }
 
@@ -377,6 +378,7 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
   extern __shared__ __align__(16) unsigned char smem_raw[];
   SelectSmem &sm = *reinterpret_cast<SelectSmem *>(smem_raw);
   uint64_t *const hit = reinterpret_cast<uint64_t *>(smem_raw + sizeof(SelectSmem));
+  Entry *const entry = reinterpret_cast<Entry *>(hit + (a.per_block * a.budget + 1) / 2 * 2);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r = blockIdx.x / CL, rank = blockIdx.x % CL;
   const int W = a.width, N = a.n_out;
@@ -396,6 +398,8 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
   if (tid < MAXW) sm.n_chosen[tid] = sm.n_hits[tid] = sm.odd[tid] = 0;
   if (tid == 0) sm.n_entries = sm.n_left = 0;
   __syncthreads();
+  cg::cluster_group cluster = cg::this_cluster();
+  auto there = cluster.barrier_arrive();  // (the first block is: waited for before anything is written to it)
 
   // the segments of the rows that count, shared out over the cluster's blocks
   const int items = sm.n_rows * a.segments, per_block = max((items + CL - 1) / CL, 1);
@@ -436,8 +440,8 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
     __syncthreads();
     const uint32_t t = max(sm.bound, order32(kLowest<T>) >> 16);
     if (odd) continue;
-    // The few chunks that may hold one of the best (each has an entry from the bound on) are shared out over the warps and read again, an entry per lane, while the last
-    // warp adds up the sums.  Each warp with those of its own threads, us: 64 requests x 4 beams x 131,072 fp32 entries 32.4 instead of 30.3, one of 4 x 32,000 with many
+    // The few chunks that may hold one of the best (each has an entry from the bound on) are shared out over the warps and read again, an entry
+    // per lane.  Each warp with those of its own threads, us: 64 requests x 4 beams x 131,072 fp32 entries 32.4 instead of 30.3, one of 4 x 32,000 with many
     // good neighbours 8.2 instead of 7.3, 64 x 32 x 32,768 (eight short segments per block) 59 instead of 63.  All segments' at the end: 31.4, 8.0, 67.
 #pragma unroll 4
     for (int c = 0; c < chunks; ++c) {
@@ -451,9 +455,8 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
     __syncthreads();
     const int n = sm.n_chosen[item - first];
     if (n > a.budget) continue;  // (all of it once more, see rescan)
-    if (warp == NW - 1) join_sums(sm, item - first, item, false);
     const float bound = value32(t << 16);
-    for (int j = warp == NW - 1 ? n : warp; j < n; j += NW - 1) {
+    for (int j = warp; j < n; j += NW) {
       const int c = sm.chosen[j] / NT, thread = sm.chosen[j] % NT;
       for (int i = lane; i < each * Rd::EPT; i += 32) {
         const int at = (c * each + i / Rd::EPT) * Rd::SIZE + Rd::index(i % Rd::EPT, thread);
@@ -471,56 +474,54 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
     if (!again) continue;
     const int from = item % a.segments * a.segment_len;
     const int n = rescan<Rd>(sm, row_of(item), min(a.segment_len, a.vocab - from), from, item - first, hit + (item - first) * a.budget, N);
-    if (warp == 0) join_sums(sm, item - first, item, true);
+    if (tid == 0) {
+      sm.n_hits[item - first] = n;
+      sm.odd[item - first] = 1;
+    }
     __syncthreads();
-    if (tid == 0) sm.n_hits[item - first] = n;
   }
 
   // The first block takes the hits and sums of all of them.
-  cg::cluster_group cluster = cg::this_cluster();
-  cluster.sync();
-  Entry *const entry = reinterpret_cast<Entry *>(hit + (a.per_block * a.budget + 1) / 2 * 2);
-  uint64_t mine = 0;  // this thread's best total
-  if (rank == 0) {
-    for (int row = warp; row < sm.n_rows; row += NW) {
-      const int item = row * a.segments + lane, c = item / per_block;
-      double ref = -INFINITY, x = 0.0;
-      if (lane < a.segments) {
-        ref = cluster.map_shared_rank(sm.reference, c)[item];
-        x = cluster.map_shared_rank(sm.sum, c)[item];
-      }
-      const double top = warp_max(ref);
-      x = warp_sum(ref > -INFINITY ? x * ex2(static_cast<float>(ref - top) * kLog2e) : 0.0);
-      if (lane == 0) sm.lse[sm.counts[row]] = top + log(x);
-    }
-    __syncthreads();
-    for (int item = warp; item < items; item += NW) {
-      const int c = item / per_block, local = item % per_block, b = sm.counts[item / a.segments], n = cluster.map_shared_rank(sm.n_hits, c)[local];
-      int to = 0;
-      if (lane == 0 && n > 0) to = atomicAdd(&sm.n_entries, n);
-      to = __shfl_sync(0xffffffffu, to, 0);
+  cluster.barrier_wait(std::move(there));
+  {
+    SelectSmem &to = *cluster.map_shared_rank(&sm, 0);
+    Entry *const entries = cluster.map_shared_rank(entry, 0);
+    for (int item = first + warp; item < last; item += NW) {
+      const int local = item - first, n = sm.n_hits[local];
+      int at = 0;
+      if (lane == 0 && n > 0) at = atomicAdd(&to.n_entries, n);
+      join_sums(sm, local, sm.odd[local], &to.reference[item], &to.sum[item]);
+      at = __shfl_sync(0xffffffffu, at, 0);
       for (int i = lane; i < n; i += 32) {
-        Entry e;
-        e.key = cluster.map_shared_rank(hit, c)[local * a.budget + i];
-        e.total = order64(static_cast<double>(sm.score[b]) + (static_cast<double>(logit_of(e.key)) - sm.lse[b]));
-        e.beam = b;
-        entry[to + i] = e;
-        mine = max(mine, e.total);
+        entries[at + i].key = hit[local * a.budget + i];
+        entries[at + i].beam = sm.counts[item / a.segments];
       }
     }
-    if (tid < W && sm.ended[tid] == 1) {
-      Entry e;
-      e.key = key_of(0.f, a.end_token);
-      e.total = order64(sm.score[tid]);
-      e.beam = tid;
-      entry[atomicAdd(&sm.n_entries, 1)] = e;
-      mine = max(mine, e.total);
+    if (rank == 0 && tid < W && sm.ended[tid] == 1) {
+      const int at = atomicAdd(&sm.n_entries, 1);
+      entry[at].key = key_of(0.f, a.end_token);
+      entry[at].beam = tid;
     }
   }
-  cluster.sync();  // (no block ends while the first one still reads it)
+  cluster.sync();
   if (rank != 0) return;
-  // Those that may be among the N best by 32 bits of their totals; where there are few, all.
+  for (int row = warp; row < sm.n_rows; row += NW) {
+    const int item = row * a.segments + lane;
+    const double ref = lane < a.segments ? sm.reference[item] : -INFINITY, top = warp_max(ref);
+    const double x = warp_sum(ref > -INFINITY ? sm.sum[item] * ex2(static_cast<float>(ref - top) * kLog2e) : 0.0);
+    if (lane == 0) sm.lse[sm.counts[row]] = top + log(x);
+  }
+  __syncthreads();
   int total = sm.n_entries;
+  uint64_t mine = 0;  // this thread's best total
+  for (int i = tid; i < total; i += NT) {
+    const int b = entry[i].beam;
+    const double score = sm.score[b];
+    entry[i].total = order64(sm.ended[b] ? score : score + (static_cast<double>(logit_of(entry[i].key)) - sm.lse[b]));
+    mine = max(mine, entry[i].total);
+  }
+  __syncthreads();
+  // Those that may be among the N best by 32 bits of their totals; where there are few, all.
   uint16_t *const kept = sm.chunk[0];  // (indexes of at most MAXW * budget of them)
   if (total > NT / 8) {
     sm.best_of[tid] = static_cast<uint32_t>(mine >> 32);
