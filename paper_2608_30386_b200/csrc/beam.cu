@@ -10,8 +10,9 @@
 // n_out groups); the few chunks that reach it are read again, from L2 as a rule, an entry per lane, and entries from the bound on, a few dozen, go to shared
 // memory.  Where too many tie, or an entry is no number, the segment is gone through once more and its n_out best keys are found bit by bit.  The first
 // block ranks what all of them have left.  Nothing depends on the order of arrival.
-// Bound: reading, and an exponential per entry on 16 lanes of special functions per SM, alike: 64 requests x 8 beams x 131,072 entries in bf16 take 38 us (bytes 21,
-// exponentials 15; of a block's 57,000 cycles the stream takes 30,000, the ends of its two segments 14,000, ranking 11,000); one request of 4 x 32,000 7.4 us, a chain of latencies.  Tried and slower: lists of the best
+// Bound: reading, and an exponential per entry on 16 lanes of special functions per SM, alike: 64 requests x 8 beams x 131,072 entries in bf16 take 37.4 us (bytes 21,
+// exponentials 15; of a block's 57,000 cycles the stream takes 31,000, the ends of its two segments 11,500, joining and ranking 11,500); one request of 4 x 32,000 7.0 us, a chain of
+// latencies.  Tried and slower: lists of the best
 // kept while reading, ranked per segment (92), entries above a running bound written out by warps on their own (53).  Logits that fool the bound: all
 // equal 228 us, rising with the token 1020 us (64 x 8 x 131,072).
 //
