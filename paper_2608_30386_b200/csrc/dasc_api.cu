@@ -1044,7 +1044,6 @@ dasc_status_t dasc_delta_draft(const dasc_plan_t *plan, float *state_base, int64
   a.cu_seqlens = cu_seqlens;
   a.seq_used = seq_used;
   a.from_zero = from_zero;
-  a.max_seqlen = max_seqlen;
   return dasc_launch_delta(a, cuda_stream) == 0 ? DASC_OK : DASC_ERR_CUDA;
 }
 

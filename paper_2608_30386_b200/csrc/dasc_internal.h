@@ -191,7 +191,6 @@ struct DascDeltaArgs {
   const int32_t *from_zero;   // device, [n_req], or null: != 0 starts from a zero state
   int32_t n_req;
   int64_t total_tokens;
-  int32_t max_seqlen;         // drafts: no request's tokens behind that many are run
   int32_t layer_begin, n_layers_in_call;
   float q_scale;
   void *o;
