@@ -4,8 +4,8 @@
 //
 // One token, in fp32 on the CUDA cores: with r = S^T (a k) and y = S^T (a q) in one pass over the state, u = beta (v - r), o = q_scale (y + (k . q) u),
 // and the new state is a S + k u^T on its way to memory.  The old state stays in registers, so beams that continue the same state read it once.
-// Bound: bytes of the state (128 KB read and written per 128 x 128 head).  256 requests x 32 heads: 172 us, 98 % of the measured copy rate of 6462 GB/s; 32 x 8
-// beams, 5.25 of 8 states read on average: 158 us, 88 % (the blocks of beams that share a source have up to eight times the work of others); one request: 2.7 us.
+// Bound: bytes of the state (128 KB read and written per 128 x 128 head).  256 requests x 32 heads: 165 us, the measured copy rate of 6462 GB/s; 32 x 8
+// beams, 5.25 of 8 states read on average: 148 us, 94 % (the blocks of beams that share a source have up to eight times the work of others); one request: 2.7 us.
 //
 // Several tokens go through the state together, in groups of TB.  P_t is the product of a group's decays up to token t, D_ts of those behind s up to t:
 //     u_t = beta_t (v_t - S^T (P_t k_t) - sum_{s < t} (k_t . D_ts k_s) u_s)
@@ -59,7 +59,9 @@ __device__ __forceinline__ void decay_factor(float g, float &hi, float &lo) {
   lo = slow ? d - (a1 - 1.f) : 0.f;
 }
 
-constexpr int kStepThreads = 128;  // of a block for single tokens: at most 64 registers of state per thread
+// Of a block for single tokens: at most 64 registers of state per thread.  Four blocks per SM: with the 140 registers that the compiler would take where decays go by channel it
+// is three, and 256 requests x 32 heads take 167 us instead of 159, 128 pairs of beams of one state 143 instead of 128 (five blocks, 96 registers: 160 and 125).
+constexpr int kStepThreads = 128;
 
 struct Unit {
   int part, h, hk, lc, r;
@@ -86,7 +88,7 @@ struct StepSmem {
 };
 
 template <int DK, int NCOL, bool KDA, typename IO, typename OT>
-__global__ void __launch_bounds__(kStepThreads) delta_step_kernel(const __grid_constant__ DascDeltaArgs a) {
+__global__ void __launch_bounds__(kStepThreads, 4) delta_step_kernel(const __grid_constant__ DascDeltaArgs a) {
   constexpr int NT = kStepThreads, LPR = NCOL / 4, RG = NT / LPR, ROWS = DK / RG;
   __shared__ StepSmem<DK, NCOL> sm;
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, cg = tid % LPR, rg = tid / LPR;
