@@ -59,8 +59,9 @@ __device__ __forceinline__ void decay_factor(float g, float &hi, float &lo) {
   lo = slow ? d - (a1 - 1.f) : 0.f;
 }
 
-// Of a block for single tokens: at most 64 registers of state per thread.  Four blocks per SM: with the 140 registers that the compiler would take where decays go by channel it
-// is three, and 256 requests x 32 heads take 167 us instead of 159, 128 pairs of beams of one state 143 instead of 128 (five blocks, 96 registers: 160 and 125).
+// Of a block for single tokens: at most 64 registers of state per thread.  Four blocks per SM where there are as many (with the 140 registers that the compiler would take where
+// decays go by channel it is three, and 256 requests x 32 heads take 167 us instead of 159, 128 pairs of beams of one state 143 instead of 128; five blocks
+// of 96 registers 160 and 125), five where there are 32 (four: 36 requests 24 us instead of 21, six 20 but ten requests 7.1 instead of 6.9).
 constexpr int kStepThreads = 128;
 
 struct Unit {
@@ -88,7 +89,7 @@ struct StepSmem {
 };
 
 template <int DK, int NCOL, bool KDA, typename IO, typename OT>
-__global__ void __launch_bounds__(kStepThreads, 4) delta_step_kernel(const __grid_constant__ DascDeltaArgs a) {
+__global__ void __launch_bounds__(kStepThreads, NCOL == 64 ? 4 : 5) delta_step_kernel(const __grid_constant__ DascDeltaArgs a) {
   constexpr int NT = kStepThreads, LPR = NCOL / 4, RG = NT / LPR, ROWS = DK / RG;
   __shared__ StepSmem<DK, NCOL> sm;
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, cg = tid % LPR, rg = tid / LPR;
@@ -575,10 +576,10 @@ int launch_cols(const DascDeltaArgs &a, void *stream) {
     if (a.d_v == 128) return launch<DK, 128, KDA, IO, OT>(a, stream);
     return a.d_v % 64 == 0 ? launch<DK, 64, KDA, IO, OT>(a, stream) : launch<DK, 32, KDA, IO, OT>(a, stream);
   }
-  // Single tokens: narrow parts until they fill the GPU a few times over.  Requests of 32 heads, in us with parts of 32 / 64 columns: 1 2.7 / 3.1, 10 6.8 / 7.3,
-  // 16 9.6 / 9.9, 64 47.0 / 45.7.
+  // Single tokens: narrow parts until wide ones fill the GPU's places once.  KDA requests of 32 heads, in us with parts of 32 / 64 columns: 4 4.3 / 4.8,
+  // 6 5.3 / 5.4, 10 6.9 / 7.1, 16 9.6 / 9.2, 36 21.2 / 18.1, 64 47.1 / 43.3.
   const int64_t units = static_cast<int64_t>(a.n_req) * a.n_layers_in_call * a.H_v;
-  if (a.d_v % 64 == 0 && units * (a.d_v / 64) >= 16 * 148) return launch<DK, 64, KDA, IO, OT>(a, stream);
+  if (a.d_v % 64 == 0 && units * (a.d_v / 64) >= 4 * 148) return launch<DK, 64, KDA, IO, OT>(a, stream);
   return launch<DK, 32, KDA, IO, OT>(a, stream);
 }
 
