@@ -10,11 +10,12 @@
 // n_out groups); the few chunks that reach it are read again, from L2 as a rule, an entry per lane, and entries from the bound on, a few dozen, go to shared
 // memory.  Where too many tie, or an entry is no number, the segment is gone through once more and its n_out best keys are found bit by bit.  The first
 // block ranks what all of them have left.  Nothing depends on the order of arrival.
-// Bound: reading, and an exponential per entry on 16 lanes of special functions per SM, alike: 64 requests x 8 beams x 131,072 entries in bf16 take 37.4 us (bytes 21,
+// Bound: reading, and an exponential per entry on 16 lanes of special functions per SM, alike: 64 requests x 8 beams x 131,072 entries in bf16 take 37.6 us (bytes 21,
 // exponentials 15; of a block's 57,000 cycles the stream takes 31,000, the ends of its two segments 11,500, joining and ranking 11,500); one request of 4 x 32,000 7.0 us, a chain of
 // latencies.  Tried and slower: lists of the best
 // kept while reading, ranked per segment (92), entries above a running bound written out by warps on their own (53).  Logits that fool the bound: all
-// equal 228 us, rising with the token 1020 us (64 x 8 x 131,072).
+// equal 228 us, rising with the token 1010 us (64 x 8 x 131,072); nine tenths masked with -1e10 or less, behind the others or among them, 37.4 us as with -infinity, but
+// 38 us where one request of 4 x 32,000 has its good tokens side by side.
 //
 // Reordering.  The lowest new beam of each continued one keeps its slot; the others get the slots of beams that nobody continues, and only these are copied: sources
 // stay as they are and every destination is a slot that nobody reads, so nothing has to wait for anything and there is no second buffer.  Bound: bytes.  16 requests
@@ -182,14 +183,14 @@ struct Round {
       }
     }
   }
-  // sum of 2^(x log2 e - c).  With log2 e rounded to l this is the sum of e^((x - c / l)(1 + d)), d = 1.3e-8: all that d touches are differences from
-  // the reference c / l, so it is as good as one that subtracts first, for half of the instructions.
-  static __device__ __forceinline__ float sum(const uint32_t (&w)[WORDS], float c) {
-    const uint64_t r = dpack2(-c, -c), l = dpack2(kLog2e, kLog2e);
+  // Sum of e^(x - m).  The difference comes first, so that m's own term is 1 and no other one is larger however large m is: one multiply-add, x log2 e - c with c
+  // a rounded m log2 e, is off by half a step of c, which from |m| of 2e9 on is more than an exponent has room for.
+  static __device__ __forceinline__ float sum(const uint32_t (&w)[WORDS], float m) {
+    const uint64_t r = dpack2(m, m), l = dpack2(kLog2e, kLog2e);
     uint64_t s[2] = {0, 0};
 #pragma unroll
     for (int e = 0; e < EPT; e += 2) {
-      const float2 y = dunpack2(dfma2(dpack2(get(w, e), get(w, e + 1)), l, r));
+      const float2 y = dunpack2(dmul2(dsub2(dpack2(get(w, e), get(w, e + 1)), r), l));
       s[e / 2 % 2] = dadd2(s[e / 2 % 2], dpack2(ex2(y.x), ex2(y.y)));
     }
     const float2 t = dunpack2(dadd2(s[0], s[1]));
@@ -197,18 +198,16 @@ struct Round {
   }
 };
 
-// Sums of exponentials are relative to 2^c, c the product of m and log2 e in fp32, m the largest logit of what they are over.
-__device__ __forceinline__ float reference(float m) { return m == kNone ? 0.f : __fmul_rn(m, kLog2e); }  // (not part of a multiply-add)
-// one more round's part of a thread's sum
+// One more round's part of a thread's sum.  Sums of exponentials are relative to e^m, m the largest logit of what they are over.
 template <typename Rd>
 __device__ __forceinline__ float add_sum(const uint32_t (&w)[WORDS], float &m, float &s) {
-  const float mr = Rd::max(w), mn = fmaxf(m, mr), c = reference(mn);
-  const float part = Rd::sum(w, c), more = fmaf(s, ex2(reference(m) - c), part);
+  const float mr = Rd::max(w), mn = fmaxf(m, mr);
+  const float part = Rd::sum(w, mn == kNone ? 0.f : mn), more = fmaf(s, ex2((m - mn) * kLog2e), part);
   s = m == kNone ? part : more;
   m = mn;
   return mr;
 }
-// A segment's sum of the threads': each warp leaves its share, and a warp adds them up at the end.  `plain`: they are relative to e^m itself.
+// A segment's sum of the threads': each warp leaves its share, and a warp adds them up at the end.
 __device__ __forceinline__ void share_sum(SelectSmem &sm, int local, float m, float x) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
@@ -228,20 +227,20 @@ __device__ __forceinline__ double warp_sum(double x) {
   return x;
 }
 // (factors between sums are good to 2^-22, as the exponentials themselves)
-__device__ __forceinline__ void join_sums(const SelectSmem &sm, int local, bool plain, double *to_reference, double *to_sum) {
+__device__ __forceinline__ void join_sums(const SelectSmem &sm, int local, double *to_reference, double *to_sum) {
   const int lane = threadIdx.x % 32;
   const float m = lane < NW ? sm.warp_top[local][lane] : kNone, top = warp_max(m);
-  float x = lane < NW && m > kNone ? sm.warp_sum[local][lane] * ex2(plain ? (m - top) * kLog2e : reference(m) - reference(top)) : 0.f;
+  float x = lane < NW && m > kNone ? sm.warp_sum[local][lane] * ex2((m - top) * kLog2e) : 0.f;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
   if (lane == 0) {
-    *to_reference = top == kNone ? -INFINITY : plain ? top : reference(top) * (1.0 / static_cast<double>(kLog2e));
+    *to_reference = top;
     *to_sum = x;
   }
 }
 
-// A segment with a NaN, an infinity or a logit that is too large to be a power of two, or in which more entries were above the bound than there is room for (many that
-// tie): once more, with differences from the largest logit, and its N best keys bit by bit from the top.  Called by the whole block; returns how many there are.
+// A segment with a NaN or an infinity, or in which more entries were above the bound than there is room for (many that tie): once more, without what is no
+// number, and its N best keys bit by bit from the top.  Called by the whole block; returns how many there are.
 template <typename Rd, typename T>
 __device__ __noinline__ int rescan(SelectSmem &sm, const T *row, int len, int from, int local, uint64_t *hit, int N) {
   const int tid = threadIdx.x;
@@ -433,7 +432,7 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
     if (left != each) sm.chunk[chunks++][tid] = static_cast<uint16_t>(order32(top) >> 16);
     sm.best_of[tid] = order32(m) >> 16;
     const float high = warp_max(m);
-    share_sum(sm, item - first, high, m == kNone ? 0.f : s * ex2(reference(m) - reference(high)));
+    share_sum(sm, item - first, high, m == kNone ? 0.f : s * ex2((m - high) * kLog2e));
     // a NaN or an infinity, looked at as bits: a sum of ex2 is taken to be at least 0 by the assembler, and `!(s >= 0)` for never true
     const bool odd = __syncthreads_or(__float_as_uint(s) >= 0x7F800000u);
     find_bound(sm, N);
@@ -475,10 +474,7 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
     if (!again) continue;
     const int from = item % a.segments * a.segment_len;
     const int n = rescan<Rd>(sm, row_of(item), min(a.segment_len, a.vocab - from), from, item - first, hit + (item - first) * a.budget, N);
-    if (tid == 0) {
-      sm.n_hits[item - first] = n;
-      sm.odd[item - first] = 1;
-    }
+    if (tid == 0) sm.n_hits[item - first] = n;
     __syncthreads();
   }
 
@@ -491,7 +487,7 @@ __global__ void __launch_bounds__(NT, 2) beam_select_kernel(const __grid_constan
       const int local = item - first, n = sm.n_hits[local];
       int at = 0;
       if (lane == 0 && n > 0) at = atomicAdd(&to.n_entries, n);
-      join_sums(sm, local, sm.odd[local], &to.reference[item], &to.sum[item]);
+      join_sums(sm, local, &to.reference[item], &to.sum[item]);
       at = __shfl_sync(0xffffffffu, at, 0);
       for (int i = lane; i < n; i += 32) {
         entries[at + i].key = hit[local * a.budget + i];
