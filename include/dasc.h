@@ -637,7 +637,7 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
  * The gated delta rule (Eq. 1) in decoding: the recurrence and layouts of dasc_refresh, for plans of either kind, in fp32.  States, q, k, v,
  * g (any g <= 0, -infinity: everything before the token is forgotten), beta, o, req_idx and strides as for dasc_refresh and
  * dasc_decay_attn: a negative req_idx is padding (state and rows of o stay as they were), and neither stride may be below a layer's
- * dense size where it reaches states that are written.  d_k of 32, 64 or 128 and any d_v that is a multiple of 32 (DASC_ERR_SHAPE
+ * dense size where it reaches states that are written (req_stride always does where src_idx is given).  d_k of 32, 64 or 128 and any d_v that is a multiple of 32 (DASC_ERR_SHAPE
  * otherwise).  No workspace.  Sums run in a fixed order: equal calls give equal bits.
  *
  * dasc_delta_step: one token per request; token r of the streams ([Lc][n_req][heads][d]) belongs to request r; o is required.

@@ -957,11 +957,12 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
 
 namespace {
 
-// Every argument check of dasc_delta_step and dasc_delta_draft (cu_seqlens given there), before anything is launched.
+// Every argument check of dasc_delta_step and dasc_delta_draft (cu_seqlens given there), before anything is launched.  `sources`: a request may start from another slot
+// than its own.
 dasc_status_t delta_validate(const dasc_plan_t *plan, float *state_base, int64_t layer_stride, int64_t req_stride, const int32_t *req_idx,
                              const void *q, const void *k, const void *v, int32_t io_dtype, const float *g, const float *beta, int32_t n_req,
                              int64_t total_tokens, int32_t layer_begin, int32_t layer_end, float q_scale, void *o, int32_t o_dtype, bool score,
-                             DascDeltaArgs *a) {
+                             bool sources, DascDeltaArgs *a) {
   if (!plan || plan->info.device < 0) return DASC_ERR_INVALID_ARG;
   if (n_req < 0 || total_tokens < 0) return DASC_ERR_INVALID_ARG;
   if (layer_begin < 0 || layer_end < layer_begin || layer_end > plan->info.n_layers) return DASC_ERR_INVALID_ARG;
@@ -980,8 +981,8 @@ dasc_status_t delta_validate(const dasc_plan_t *plan, float *state_base, int64_t
   if ((reinterpret_cast<uintptr_t>(g) & (kda ? 15u : 3u)) || (reinterpret_cast<uintptr_t>(beta) & 3u)) return DASC_ERR_INVALID_ARG;
   if (layer_stride < 0 || req_stride < 0 || layer_stride % 4 || req_stride % 4) return DASC_ERR_INVALID_ARG;
   const int64_t dense = plan->info.dense_floats_per_layer;
-  if (!score && ((layers > 1 && layer_stride < dense) || (n_req > 1 && req_stride < dense)))
-    return DASC_ERR_INVALID_ARG;  // layers of one request, or requests in one layer, would overlap and be written from several blocks
+  if (!score && ((layers > 1 && layer_stride < dense) || ((n_req > 1 || sources) && req_stride < dense)))
+    return DASC_ERR_INVALID_ARG;  // layers of one request, or requests in one layer, would overlap and be written while other blocks read or write them
   if (const dasc_status_t ds = check_device(plan); ds != DASC_OK) return ds;
   a->H_v = plan->info.n_v_heads;
   a->H_k = plan->info.n_k_heads;
@@ -1019,7 +1020,7 @@ dasc_status_t dasc_delta_step(const dasc_plan_t *plan, float *state_base, int64_
   DascDeltaArgs a{};
   if (src_idx && (beam_width < 1 || beam_width > kBeamMaxWidth || (n_req > 0 && n_req % beam_width))) return DASC_ERR_INVALID_ARG;
   const dasc_status_t st = delta_validate(plan, state_base, layer_stride, req_stride, req_idx, q, k, v, io_dtype, g, beta, n_req, n_req,
-                                          layer_begin, layer_end, q_scale, o, o_dtype, false, &a);
+                                          layer_begin, layer_end, q_scale, o, o_dtype, false, src_idx != nullptr, &a);
   if (st != DASC_OK || n_req == 0 || layer_end == layer_begin) return st;
   if (!o) return DASC_ERR_INVALID_ARG;
   a.src_idx = src_idx;
@@ -1038,7 +1039,7 @@ dasc_status_t dasc_delta_draft(const dasc_plan_t *plan, float *state_base, int64
   if (mode != DASC_DRAFT_ADVANCE && mode != DASC_DRAFT_SCORE) return DASC_ERR_INVALID_ARG;
   if (max_seqlen < 0 || (mode == DASC_DRAFT_SCORE && !o)) return DASC_ERR_INVALID_ARG;
   const dasc_status_t st = delta_validate(plan, state_base, layer_stride, req_stride, req_idx, q, k, v, io_dtype, g, beta, n_req, total_tokens,
-                                          layer_begin, layer_end, q_scale, o, o_dtype, mode == DASC_DRAFT_SCORE, &a);
+                                          layer_begin, layer_end, q_scale, o, o_dtype, mode == DASC_DRAFT_SCORE, false, &a);
   if (st != DASC_OK || n_req == 0 || layer_end == layer_begin) return st;
   if (!cu_seqlens) return DASC_ERR_INVALID_ARG;
   a.cu_seqlens = cu_seqlens;
