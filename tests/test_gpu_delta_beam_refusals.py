@@ -47,3 +47,12 @@ def test_a_beam_with_a_source_reaches_two_states(kind):
     assert torch.equal(s.case.state, before)
     assert call("dasc_delta_step", s.step, **one) == binding.OK
     assert call("dasc_delta_step", s.step, n=1, rs=0) == binding.OK  # (one state, whichever the stride)
+
+
+def test_sizes_whose_offsets_pass_32_bits():
+    """Between the rows of eight tokens (both calls), and inside a head's state (drafts)."""
+    s = States(dasc.KDA)
+    rows, state = dh.make_plan(dasc.KDA, 2, 1, 1, 32, 2 ** 27 + 32), dh.make_plan(dasc.KDA, 2, 1, 1, 128, 2 ** 24)
+    assert call("dasc_delta_step", s.step, plan=rows.handle) == binding.ERR_SHAPE
+    for plan in (rows, state):
+        assert call("dasc_delta_draft", s.draft, plan=plan.handle) == binding.ERR_SHAPE
