@@ -651,7 +651,7 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
  *   number of tokens is right.  cu_seqlens, seq_used, from_zero as for dasc_decay_attn.  max_seqlen is an upper bound on any
  *   request's token count; it limits nothing.
  *   mode DASC_DRAFT_ADVANCE  every state is advanced and written back; o may be NULL, and then q
- *   mode DASC_DRAFT_SCORE    outputs only, no state is written.  A recurrent state cannot be rewound the way a KV cache can,
+ *   mode DASC_DRAFT_SCORE    outputs only, no state is written; o is required where there are tokens.  A recurrent state cannot be rewound the way a KV cache can,
  *                            so drafts are scored first, then verified (dasc_verify_draft), and the state is advanced over those that stand
  *                            by a second call (ADVANCE, seq_used = n_kept, o = NULL).
  *   A request without tokens still has its state set to zero by ADVANCE where from_zero says so.  A token with a NaN or an infinity in v, or a state with one, reaches

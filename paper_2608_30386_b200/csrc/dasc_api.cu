@@ -1037,7 +1037,7 @@ dasc_status_t dasc_delta_draft(const dasc_plan_t *plan, float *state_base, int64
   TraceRange trace("dasc_delta_draft");
   DascDeltaArgs a{};
   if (mode != DASC_DRAFT_ADVANCE && mode != DASC_DRAFT_SCORE) return DASC_ERR_INVALID_ARG;
-  if (max_seqlen < 0 || (mode == DASC_DRAFT_SCORE && !o)) return DASC_ERR_INVALID_ARG;
+  if (max_seqlen < 0 || (mode == DASC_DRAFT_SCORE && !o && n_req > 0 && total_tokens > 0)) return DASC_ERR_INVALID_ARG;
   if (plan && static_cast<double>(plan->info.d_k) * plan->info.d_v > INT32_MAX) return DASC_ERR_SHAPE;  // (32-bit offsets inside a head's state)
   const dasc_status_t st = delta_validate(plan, state_base, layer_stride, req_stride, req_idx, q, k, v, io_dtype, g, beta, n_req, total_tokens,
                                           layer_begin, layer_end, q_scale, o, o_dtype, mode == DASC_DRAFT_SCORE, false, &a);

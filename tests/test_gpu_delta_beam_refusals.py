@@ -56,3 +56,16 @@ def test_sizes_whose_offsets_pass_32_bits():
     assert call("dasc_delta_step", s.step, plan=rows.handle) == binding.ERR_SHAPE
     for plan in (rows, state):
         assert call("dasc_delta_draft", s.draft, plan=plan.handle) == binding.ERR_SHAPE
+
+
+@KINDS
+def test_scoring_nothing(kind):
+    """No requests, or requests without a token: tensors without values have no address, and nothing is refused for it."""
+    case = dh.make_case(82, [0, 0], kind=kind)
+    before = case.state.clone()
+    empty = lambda *shape: torch.empty(*shape, device="cuda")  # noqa: E731
+    streams = [empty(1, 0, 2, 128), empty(1, 0, 2, 128), empty(1, 0, 2, 128), empty(1, 0, 2, 128) if kind == dasc.KDA else empty(1, 0, 2), empty(1, 0, 2)]
+    for n in (0, 2):
+        cu = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+        dasc.dasc_delta_draft(case.plan, case.state, *case.strides, case.req[:n], *streams, cu, 0, 0, o=empty(1, 0, 2, 128), mode=dasc.DRAFT_SCORE)
+    assert torch.equal(case.state, before)
