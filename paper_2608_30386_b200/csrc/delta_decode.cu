@@ -558,11 +558,8 @@ int launch(const DascDeltaArgs &a, void *stream) {
   if constexpr (NCOL < 128)
     if (!a.cu_seqlens) return static_cast<int>(launch_blocks(delta_step_kernel<DK, NCOL, KDA, IO, OT>, grid, dim3(kStepThreads), 0, stream, a));
   constexpr size_t smem = sizeof(DraftSmem<DK, NCOL, KDA, IO>);
+  static_assert(smem <= 48 * 1024, "what a kernel has without asking for more");
   auto kernel = delta_draft_kernel<DK, NCOL, KDA, IO, OT>;
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-    if (e != cudaSuccess) return static_cast<int>(e);
-  }
   constexpr int NT = DraftShape<DK, NCOL>::NT;
   const dim3 some(static_cast<unsigned>(std::min<int64_t>(blocks, 148 * (512 / NT))));  // as many as fit the GPU at once
   return static_cast<int>(launch_blocks(kernel, some, dim3(NT), smem, stream, a));
