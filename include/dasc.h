@@ -637,8 +637,9 @@ dasc_status_t dasc_verify_draft(const void *target, int64_t target_stride, const
  * The gated delta rule (Eq. 1) in decoding: the recurrence and layouts of dasc_refresh, for plans of either kind, in fp32.  States, q, k, v,
  * g (any g <= 0, -infinity: everything before the token is forgotten), beta, o, req_idx and strides as for dasc_refresh and
  * dasc_decay_attn: a negative req_idx is padding (state and rows of o stay as they were), and neither stride may be below a layer's
- * dense size where it reaches states that are written (req_stride always does where src_idx is given).  d_k of 32, 64 or 128 and any d_v that is a multiple of 32 (DASC_ERR_SHAPE
- * otherwise).  No workspace.  Sums run in a fixed order: equal calls give equal bits.
+ * dense size where it reaches states that are written (req_stride always does where src_idx is given).  d_k of 32, 64 or 128 and any
+ * d_v that is a multiple of 32 (DASC_ERR_SHAPE otherwise, and where eight tokens' values or, for drafts, those of a head's state pass
+ * 2^30 or 2^31).  No workspace.  Sums run in a fixed order: equal calls give equal bits.
  *
  * dasc_delta_step: one token per request; token r of the streams ([Lc][n_req][heads][d]) belongs to request r; o is required.
  *   src_idx    DEVICE int32[n_req] or NULL: beams.  Request r then starts from the state of slot src_idx[r] and writes slot req_idx[r]
@@ -687,6 +688,9 @@ dasc_status_t dasc_delta_draft(const dasc_plan_t *plan, float *state_base, int64
  *   out_ended  DEVICE int32[n_req][n_out] or NULL: 1 where the beam had ended, the token is end_token, or there is no continuation
  * width <= 32, n_out <= 64 (DASC_ERR_SHAPE otherwise).  With n_out == width, out_scores may be scores and out_ended may be ended.
  * The current device must be the one that holds the buffers.  One launch, no workspace; equal calls give equal bits.
+ * The time goes by the logits too: parts of a row in which more than a few dozen entries may be among the best (all equal, or rising with the token), or that hold a
+ * NaN or +infinity, are read several times, and a call of nothing else takes up to 27 times as long.  Masks, by -infinity or by finite values, cost nothing by themselves, but
+ * where what they leave lies side by side in a short row (4 x 32,000: 38 us instead of 7).
  */
 dasc_status_t dasc_beam_select(const void *logits, int64_t logits_stride, int32_t dtype, int32_t vocab, const float *scores,
                                const int32_t *ended, int32_t end_token, int32_t n_req, int32_t width, int32_t n_out,

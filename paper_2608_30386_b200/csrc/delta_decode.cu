@@ -4,8 +4,9 @@
 //
 // One token, in fp32 on the CUDA cores: with r = S^T (a k) and y = S^T (a q) in one pass over the state, u = beta (v - r), o = q_scale (y + (k . q) u),
 // and the new state is a S + k u^T on its way to memory.  The old state stays in registers, so beams that continue the same state read it once.
-// Bound: bytes of the state (128 KB read and written per 128 x 128 head).  256 requests x 32 heads: 165 us, the measured copy rate of 6462 GB/s; 32 x 8
-// beams, 5.25 of 8 states read on average: 148 us, 94 % (the blocks of beams that share a source have up to eight times the work of others); one request: 2.7 us.
+// Bound: bytes of the state (128 KB read and written per 128 x 128 head).  256 requests x 32 heads: 165 us over inputs that change from call to call (161 back to back over
+// the same ones), the measured copy rate of 6462 GB/s; 32 x 8 beams, 5.25 of 8 states read on average: 148 us, 94 % (the blocks of beams that share a source have up to eight
+// times the work of others); one request: 2.4 to 3.2 us.
 //
 // Several tokens go through the state together, in groups of TB.  P_t is the product of a group's decays up to token t, D_ts of those behind s up to t:
 //     u_t = beta_t (v_t - S^T (P_t k_t) - sum_{s < t} (k_t . D_ts k_s) u_s)
@@ -59,9 +60,11 @@ __device__ __forceinline__ void decay_factor(float g, float &hi, float &lo) {
   lo = slow ? d - (a1 - 1.f) : 0.f;
 }
 
-// Of a block for single tokens: at most 64 registers of state per thread.  Four blocks per SM where there are as many (with the 140 registers that the compiler would take where
-// decays go by channel it is three, and 256 requests x 32 heads take 167 us instead of 159, 128 pairs of beams of one state 143 instead of 128; five blocks
-// of 96 registers 160 and 125), five where there are 32 (four: 36 requests 24 us instead of 21, six 20 but ten requests 7.1 instead of 6.9).
+// Of a block for single tokens: at most 64 registers of state per thread.  Where parts are 64 columns wide four blocks per SM: with the registers that the compiler
+// would take where decays go by channel it is three, and 256 requests x 32 heads take 174 us instead of 161, 128 pairs of beams of one state 147 instead of 133; five
+// blocks take 162 and 128, and 256 requests of d_k = d_v = 64 58 instead of 67.  Where they are 32 wide (few states, or a d_v that is no multiple of 64) five blocks
+// instead of four: 5 requests x 32 heads 5.7 us instead of 6.7, 9 requests 9.1 instead of 9.5, 256 of d_v = 32 48 instead of 52, of d_v = 96 141 instead of 161; six
+// 5.9, 8.9, 46 and 132.  (All back to back, layer after layer from memory.)
 constexpr int kStepThreads = 128;
 
 struct Unit {
@@ -356,8 +359,9 @@ __device__ __forceinline__ void prepare(Operands<DK, NCOL> &op, const RawRows<DK
     if (lane < 2 * TB) (lane < TB ? op.kk : op.qk)[lane % TB][t % 2 * 4 + t / 2] = lane >= TB ? x[0] : lane == t ? 0.f : -raw.beta[t] * x[0];
   }
   // Keys and queries behind the group's start, and keys decayed to its end, a thread per channel and kind.  Decays of several tokens
-  // are exponentials of sums of their logarithms, always over the tokens between two points (-infinity is like any other number there); a factor e^G is off
-  // by 2^-24 |G| or so of itself, 2^-25 at most.
+  // are exponentials of sums of their logarithms, always over the tokens between two points (-infinity is like any other number there).  A factor e^G is good to
+  // (2 + 1.2 |G|) 2^-23 of itself, the documented bound of __expf, and the sum's rounding, 2^-24 |G|: together never worse than 2^-22 of an undecayed one.  Only the decay
+  // of the state itself, the same token after token, is better than that (decay_factor).
   const int kinds = (want ? 2 : 1) + update;
   for (int i = tid; i < kinds * DK; i += NT) {
     const int c = i % DK, what = i / DK;
@@ -567,14 +571,17 @@ int launch(const DascDeltaArgs &a, void *stream) {
 
 template <int DK, bool KDA, typename IO, typename OT>
 int launch_cols(const DascDeltaArgs &a, void *stream) {
-  // Drafts: the widest part, since what is prepared for a group serves all of its columns.  5 tokens of 1 / 8 / 32 requests of 32 heads, scored, in us with parts of
-  // 32 / 64 / 128 columns: 9.1 / 8.3 / 6.2, 21.1 / 11.8 / 8.2, 73.6 / 37.9 / 27.7; advanced, 16 requests: 43.5 / 24.4 / 19.0.
+  // Drafts: wide parts, since what is prepared for a group serves all of its columns.  5 tokens of 1 / 8 / 32 requests of 32 heads with d_v = 128, scored, in us with parts
+  // of 32 / 64 / 128 columns: 9.1 / 8.3 / 6.2, 21.1 / 11.8 / 8.2, 73.6 / 37.9 / 27.7; advanced, 16 requests: 43.5 / 24.4 / 19.0.  Parts of 128 columns have d_v as a
+  // constant; larger multiples of 128 go in parts of 64, and what is no multiple of 64 in parts of 32, which do not hold all of their values in registers (up to 232
+  // bytes are spilled): 64 requests of d_v = 32 / 64 / 96 / 128 / 256 take 40 / 39 / 110 / 50 / 140 us scored and 45 / 47 / 121 / 66 / 171 advanced.
   if (a.cu_seqlens) {
     if (a.d_v == 128) return launch<DK, 128, KDA, IO, OT>(a, stream);
     return a.d_v % 64 == 0 ? launch<DK, 64, KDA, IO, OT>(a, stream) : launch<DK, 32, KDA, IO, OT>(a, stream);
   }
-  // Single tokens: narrow parts until wide ones fill the GPU's places once.  KDA requests of 32 heads, in us with parts of 32 / 64 columns: 4 4.3 / 4.8,
-  // 6 5.3 / 5.4, 10 6.9 / 7.1, 16 9.6 / 9.2, 36 21.2 / 18.1, 64 47.1 / 43.3.
+  // Single tokens: narrow parts until wide ones fill the GPU's places once.  KDA requests of 32 heads, layer after layer from memory, in us with parts of 32 / 64 columns:
+  // 2 4.4 / 4.6, 4 5.4 / 6.1, 6 6.6 / 6.9, 8 8.4 / 7.7, 9 9.0 / 8.1, 10 9.7 / 9.6, 16 14.0 / 13.6, 36 28.1 / 26.4, 64 47.9 / 44.1; one layer that stays in L2: 4 4.2 / 5.0,
+  // 8 5.9 / 5.8, 10 6.5 / 6.8, 12 7.7 / 7.5, 16 9.1 / 8.8, 36 21.8 / 18.7.  (The crossing is between 7 and 11 requests, the rule's between 9 and 10.)
   const int64_t units = static_cast<int64_t>(a.n_req) * a.n_layers_in_call * a.H_v;
   if (a.d_v % 64 == 0 && units * (a.d_v / 64) >= 4 * 148) return launch<DK, 64, KDA, IO, OT>(a, stream);
   return launch<DK, 32, KDA, IO, OT>(a, stream);
